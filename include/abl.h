@@ -73,8 +73,10 @@ enum {
                               convolution consumes the ReLU of the DEQUANTIZED copy (Eq. 10) instead
                               of the exact A3, so the approximation error enters the forward pass and
                               compounds from layer to layer; for error studies, not for speed */
-  ABL_XIN_PACKED = 1u << 4 /* abl_postact_backward: xin / xin_stats are the previous layer's
+  ABL_XIN_PACKED = 1u << 4, /* abl_postact_backward: xin / xin_stats are the previous layer's
                               packed store and stats (its ReLU output is rebuilt on the fly)   */
+  ABL_NORM_CENTER = 1u << 6, /* abl_resnorm_*: the norms subtract the row's mean                */
+  ABL_ACCUM_DW = 1u << 7   /* abl_ckpt_wgrad: dW += result (gradients of several batches)       */
 };
 
 #define ABL_BN_EPS 1e-5f
@@ -326,6 +328,83 @@ int abl_stack_forward_traced(void* stream, const abl_layer* layers, int32_t L, i
 int abl_stack_backward_traced(void* stream, const abl_layer* layers, int32_t L, int K, uint32_t flags,
                               int32_t skip_every, float* buf_s, float* buf_t,
                               void* scratch, size_t scratch_bytes, float* const* trace);
+
+/* ---- blocks of language models: rows of channels kept in block stores ------------------------
+ * The method carried over to blocks that normalize each row (token) by itself: the forward pass is exact, what is
+ * kept of an activation for the backward pass is a K-bit copy, and the gradients are computed from that copy.  Without batch statistics
+ * the scale of a code cannot come from the channel's constants (Eq. 9), so each copy carries its own:
+ *
+ * Block store of a tensor [M, C] (K = 4 or 8; opaque to callers, specified because parity is on bytes): every row is cut into
+ * B = ceil(C / 32) blocks of 32 channels, the last one filled up with zeros.  A block has the scale 2^e, e the smallest integer
+ * >= -119 for which no code overflows: max|x| 2^-e < 127.5 (K = 8), < 7 (K = 4).  Its codes are x 2^-e rounded to the nearest
+ * value of their type, ties to even: 8-bit two's complement integers (K = 8), or 4-bit floats
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} = sign in bit 3, index in bits 0-2 (K = 4).  Every value that a store stands for
+ * is exact in bf16.  A block that holds an infinity or a NaN has zero codes and the scale byte 255, and every value of it reads
+ * as NaN: it does not come back as a finite gradient.
+ * Bytes: codes [M][B][32 K / 8] (K = 4: element 2j of a block in bits 0-3 of its byte j, 2j + 1 in bits 4-7), then the scale bytes
+ * e + 127 [M][B], then zeros up to a multiple of 128.  abl_ckpt_bytes gives the size (0 on invalid arguments).
+ *
+ * Common to the calls below: dtype is that of the activations and of their gradients (arithmetic is in fp32, each
+ * output rounded once; gradients of parameters are fp32).  M = 0 is allowed: the calls do nothing but write gradients of
+ * parameters as zeros.  M ceil(C / 32) < 2^29, or ABL_ERR_SHAPE.  Stores and workspaces are
+ * 16-byte aligned, other tensors aligned to their elements.  `ld`: elements from one row to the next, >= C; tensors without one are contiguous. */
+enum { ABL_F32 = 0, ABL_BF16 = 1 };               /* dtype */
+enum { ABL_ACT_SILU = 0, ABL_ACT_GELU = 1 };      /* act(g) = g sigmoid(g); the tanh form of GELU */
+
+size_t abl_ckpt_bytes(int64_t M, int32_t C, int K);
+/* x [M][ldx] -> store; store -> x (which may have another dtype than what was packed). */
+int abl_ckpt_pack(void* stream, int dtype, const void* x, int64_t ldx, int64_t M, int32_t C, int K, void* ckpt);
+int abl_ckpt_unpack(void* stream, int dtype, const void* ckpt, int64_t M, int32_t C, int K, void* x, int64_t ldx);
+
+/* The step between two blocks of a residual network: norm of the block's output, gate, residual sum, norm before the next block.
+ *     p = gate * (w_post * N(b)),   r' = alpha r + beta p,   n = w_pre * N(r')
+ * N(x) = x / sqrt(mean x^2 + eps) over the row; with ABL_NORM_CENTER (x - mean) / sqrt(var + eps).  n is computed from the
+ * unrounded r'.  w_post = NULL: p = gate * b; gate = NULL: no gate; b = NULL: r' = alpha r (then w_post and gate
+ * are NULL too).  Row m takes row m / gate_rows of the gate: gate_rows = M: one gate for all rows, the rows of a
+ * sample: one per sample, 1: one per token.  C <= 16384, M <= 2^25.
+ * K = 4 or 8 keeps for the backward pass: ckpt_n, the store of N(r'), with rstd_n [M]; ckpt_b, the store of N(b) with rstd_b
+ * [M] (w_post given), or of b itself (only gate given), or nothing (neither).  K = 0 keeps nothing (serving). */
+typedef struct abl_resnorm {
+  int64_t M, gate_rows;   /* rows; rows that share a row of the gate (ignored without one) */
+  int32_t C, dtype, K;
+  uint32_t flags;         /* ABL_NORM_CENTER */
+  float alpha, beta, eps; /* eps > 0; not looked at by the backward (rstd holds it)         */
+} abl_resnorm;
+/*   r, b, r_out, n [M][C]; gate [ceil(M / gate_rows)][C]; w_post, w_pre [C], all of dtype; rstd_b, rstd_n [M] fp32
+ *   r_out may alias r or b, or be NULL (not wanted); n may alias b or r. */
+int abl_resnorm_forward(void* stream, const abl_resnorm* step, const void* r, const void* b, const void* gate,
+                        const void* w_post, const void* w_pre, void* r_out, void* n, void* ckpt_b, float* rstd_b,
+                        void* ckpt_n, float* rstd_n);
+/* Its gradients, from the stores alone (gate, w_post, w_pre as given to the forward):
+ *   dn [M][C], dr_out [M][C] (NULL: zero) in; dr, db [M][C] out (NULL: not wanted); dgate [G][C], dw_post [C], dw_pre [C]
+ *   out in fp32 (dgate, dw_post: NULL exactly where gate, w_post are).  dr may alias dr_out or dn, db may alias dn or dr_out.
+ *   has_b = 0: the forward had b = NULL (db is NULL then).  Sums over rows are taken in a fixed order.
+ *   scratch: abl_resnorm_scratch_bytes(M, C). */
+size_t abl_resnorm_scratch_bytes(int64_t M, int32_t C);
+int abl_resnorm_backward(void* stream, const abl_resnorm* step, int has_b, const void* dn, const void* dr_out, const void* gate,
+                         const void* w_post, const void* w_pre, const void* ckpt_b, const float* rstd_b,
+                         const void* ckpt_n, const float* rstd_n, void* scratch, size_t scratch_bytes,
+                         void* dr, void* db, float* dgate, float* dw_post, float* dw_pre);
+
+/* Gated unit: h = act(g) * u, elementwise.  K = 4 or 8 keeps the stores of g and u; K = 0 keeps nothing (serving).
+ * g, u, h may be slices (own ld each); h may alias g or u (same ld). */
+int abl_glu_forward(void* stream, int dtype, int act, const void* g, int64_t ldg, const void* u, int64_t ldu, int64_t M,
+                    int32_t C, int K, void* h, int64_t ldh, void* ckpt_g, void* ckpt_u);
+/* dg = dh * u * act'(g), du = dh * act(g), from the stores.  ckpt_h (NULL: not wanted) receives the K = 8 store of act(g) * u as
+ * rebuilt from them: the input of the following product, for its weight gradient.  dg or du may alias dh (same ld). */
+int abl_glu_backward(void* stream, int dtype, int act, const void* dh, int64_t lddh, const void* ckpt_g,
+                     const void* ckpt_u, int64_t M, int32_t C, int K, void* dg, int64_t lddg, void* du, int64_t lddu,
+                     void* ckpt_h);
+
+/* Weight gradient of a product y = (scale * x) W from the block store of x [M][Cin]: dW [Cin][Cout] = (scale * x~)^T dy in
+ * fp32.  scale [Cin] of dtype (NULL: ones): the weight of the norm that made x, whose store is that of the normalized rows.
+ * The stored values go into the matrix cores as they are; bf16 dy too, fp32 dy in three bf16 parts (24 bits), or rounded to
+ * bf16 with ABL_MATH_BF16.  Sums are in fp32 and in a fixed order.
+ * Cin, Cout <= 2^20, Cin Cout < 2^31.  flags: ABL_MATH_BF16, ABL_ACCUM_DW.  scratch: abl_ckpt_wgrad_scratch_bytes (0 on invalid arguments, never 0 otherwise). */
+size_t abl_ckpt_wgrad_scratch_bytes(int64_t M, int32_t Cin, int32_t Cout, int dtype);
+int abl_ckpt_wgrad(void* stream, int dtype, uint32_t flags, const void* ckpt, int64_t M, int32_t Cin, int K,
+                   const void* scale, const void* dy, int64_t lddy, int32_t Cout, void* scratch,
+                   size_t scratch_bytes, float* dW);
 
 /* ---- parameter update -----------------------------------------------------------
  * SGD with momentum and weight decay, the update rule of the paper's experiments

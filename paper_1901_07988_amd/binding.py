@@ -18,6 +18,10 @@ ABL_MATH_BF16 = 2
 ABL_XIN_F32 = 8
 ABL_NAIVE_FWD = 32
 ABL_XIN_PACKED = 16
+ABL_NORM_CENTER = 64
+ABL_ACCUM_DW = 128
+ABL_F32, ABL_BF16 = 0, 1
+ABL_ACT_SILU, ABL_ACT_GELU = 0, 1
 STATS_PLANES = 8
 
 
@@ -35,6 +39,12 @@ class abl_layer(ctypes.Structure):
     _fields_ = [("shape", abl_shape), ("W", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
                 ("beta", ctypes.c_void_p), ("packed", ctypes.c_void_p), ("stats", ctypes.c_void_p),
                 ("dW", ctypes.c_void_p), ("dgamma", ctypes.c_void_p), ("dbeta", ctypes.c_void_p)]
+
+
+class abl_resnorm(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("gate_rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("K", ctypes.c_int32), ("flags", ctypes.c_uint32), ("alpha", ctypes.c_float), ("beta", ctypes.c_float),
+                ("eps", ctypes.c_float)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -89,6 +99,19 @@ _SIGS = {
                                                 ctypes.POINTER(_vp)]),
     "abl_stack_backward_traced": (ctypes.c_int, [_vp, _lay, _i32, ctypes.c_int, _u32, _i32, _vp, _vp, _vp, _sz,
                                                  ctypes.POINTER(_vp)]),
+    "abl_ckpt_bytes": (_sz, [_i64, _i32, ctypes.c_int]),
+    "abl_ckpt_pack": (ctypes.c_int, [_vp, ctypes.c_int, _vp, _i64, _i64, _i32, ctypes.c_int, _vp]),
+    "abl_ckpt_unpack": (ctypes.c_int, [_vp, ctypes.c_int, _vp, _i64, _i32, ctypes.c_int, _vp, _i64]),
+    "abl_resnorm_forward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_resnorm)] + [_vp] * 11),
+    "abl_resnorm_scratch_bytes": (_sz, [_i64, _i32]),
+    "abl_resnorm_backward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_resnorm), ctypes.c_int] + [_vp] * 10 + [_sz] + [_vp] * 5),
+    "abl_glu_forward": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _i64, _i64, _i32, ctypes.c_int,
+                                       _vp, _i64, _vp, _vp]),
+    "abl_glu_backward": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _vp, _i64, _i32, ctypes.c_int,
+                                        _vp, _i64, _vp, _i64, _vp]),
+    "abl_ckpt_wgrad_scratch_bytes": (_sz, [_i64, _i32, _i32, ctypes.c_int]),
+    "abl_ckpt_wgrad": (ctypes.c_int, [_vp, ctypes.c_int, _u32, _vp, _i64, _i32, ctypes.c_int, _vp, _vp, _i64, _i32, _vp,
+                                      _sz, _vp]),
     "abl_sgd_momentum": (ctypes.c_int, [_vp, _i64, ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp]),
     "abl_hbm_probe": (ctypes.c_int, [_vp, ctypes.c_int, _vp, _vp, _sz]),
     "abl_mfma_probe_out_bytes": (_sz, []),
@@ -352,6 +375,152 @@ def abl_stack_backward_traced(layers, K, skip_every, buf_s, buf_t, scratch, trac
     _check(lib.abl_stack_backward_traced(_stream(), layers, len(layers), K, flags, skip_every, _ptr(buf_s),
                                          _ptr(buf_t), _ptr(scratch), scratch.numel() * scratch.element_size(),
                                          _trace_array(trace, len(layers))), "abl_stack_backward_traced")
+
+
+# ---- blocks of language models ---------------------------------------------------------------
+_DTYPES = {torch.float32: ABL_F32, torch.bfloat16: ABL_BF16}
+
+
+def _dtype(t):
+    """The ABL_* dtype of a tensor (or torch dtype); ABL_ERR_ARG for others."""
+    return _DTYPES.get(t if isinstance(t, torch.dtype) else t.dtype, -1)
+
+
+def _rows(t, M, C):
+    """(pointer, elements from one row to the next) of a tensor [M, C] whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2 and t.shape[0] == M and t.shape[1] == C, "device tensors [%d, %d] only" % (M, C)
+    ld, one = t.stride()
+    assert one == 1 or C == 1, "rows have to be contiguous"
+    return t.data_ptr(), (ld if M > 1 else C)
+
+
+def _same(dtype, *tensors):
+    """The tensors' common dtype: the C ABI sees addresses only."""
+    for t in tensors:
+        assert t is None or t.dtype == dtype, "all of these tensors have one dtype"
+
+
+def _holds(t, n, what):
+    """A contiguous tensor of at least n elements (None passes: the C ABI says where that is an error)."""
+    assert t is None or t.numel() >= n, "%s: %d elements, %d are needed" % (what, t.numel(), n)
+
+
+def _store(t, M, C, K, what="store"):
+    _holds(t, lib.abl_ckpt_bytes(M, C, K), what)
+    assert t is None or t.element_size() == 1, "stores are tensors of bytes"
+
+
+def abl_ckpt_bytes(M, C, K):
+    return lib.abl_ckpt_bytes(M, C, K)
+
+
+def abl_ckpt_pack(x, K, ckpt):
+    """x [M, C] (rows contiguous, any distance between them) -> its block store."""
+    M, C = x.shape
+    p, ld = _rows(x, M, C)
+    _store(ckpt, M, C, K)
+    _check(lib.abl_ckpt_pack(_stream(), _dtype(x), p, ld, M, C, K, _ptr(ckpt)), "abl_ckpt_pack")
+
+
+def abl_ckpt_unpack(ckpt, K, x):
+    """The values that the block store stands for -> x [M, C]."""
+    M, C = x.shape
+    p, ld = _rows(x, M, C)
+    _store(ckpt, M, C, K)
+    _check(lib.abl_ckpt_unpack(_stream(), _dtype(x), _ptr(ckpt), M, C, K, p, ld), "abl_ckpt_unpack")
+
+
+def _check_step(M, C, K, gate, gate_rows, w_post, w_pre, ckpt_b, rstd_b, ckpt_n, rstd_n, dtype):
+    _same(dtype, gate, w_post, w_pre)
+    _same(torch.float32, rstd_b, rstd_n)
+    _holds(w_post, C, "w_post")
+    _holds(w_pre, C, "w_pre")
+    if gate is not None and gate_rows > 0:
+        _holds(gate, -(-M // gate_rows) * C, "gate")
+    if K:
+        _store(ckpt_n, M, C, K, "ckpt_n")
+        _store(ckpt_b, M, C, K, "ckpt_b")
+        _holds(rstd_n, M, "rstd_n")
+        _holds(rstd_b, M, "rstd_b")
+
+
+def abl_resnorm_forward(r, b, gate, gate_rows, w_post, w_pre, r_out, n, K=0, ckpt_b=None, rstd_b=None, ckpt_n=None,
+                        rstd_n=None, alpha=1.0, beta=1.0, eps=1e-5, flags=0):
+    """r, b, r_out, n [M, C]; gate [ceil(M / gate_rows), C]; w_post, w_pre [C]; b, gate, w_post, r_out may be None."""
+    M, C = r.shape
+    _same(r.dtype, b, r_out, n)
+    for t, name in ((b, "b"), (r_out, "r_out"), (n, "n")):
+        _holds(t, M * C, name)
+    _check_step(M, C, K, gate, gate_rows, w_post, w_pre, ckpt_b, rstd_b, ckpt_n, rstd_n, r.dtype)
+    s = abl_resnorm(M, gate_rows, C, _dtype(r), K, flags, alpha, beta, eps)
+    _check(lib.abl_resnorm_forward(_stream(), ctypes.byref(s), _ptr(r), _ptr(b), _ptr(gate), _ptr(w_post), _ptr(w_pre),
+                                   _ptr(r_out), _ptr(n), _ptr(ckpt_b), _ptr(rstd_b), _ptr(ckpt_n), _ptr(rstd_n)),
+           "abl_resnorm_forward")
+
+
+def abl_resnorm_scratch_bytes(M, C):
+    return lib.abl_resnorm_scratch_bytes(M, C)
+
+
+def abl_resnorm_backward(dn, dr_out, gate, gate_rows, w_post, w_pre, K, ckpt_b, rstd_b, ckpt_n, rstd_n, scratch, dr, db,
+                         dgate, dw_post, dw_pre, alpha=1.0, beta=1.0, flags=0, has_b=True):
+    """dn, dr_out, dr, db [M, C]; dgate [ceil(M / gate_rows), C], dw_post, dw_pre [C] in fp32."""
+    M, C = dn.shape
+    _same(dn.dtype, dr_out, dr, db)
+    _same(torch.float32, dgate, dw_post, dw_pre)
+    for t, name in ((dr_out, "dr_out"), (dr, "dr"), (db, "db")):
+        _holds(t, M * C, name)
+    for t, name in ((dw_post, "dw_post"), (dw_pre, "dw_pre")):
+        _holds(t, C, name)
+    if dgate is not None and gate_rows > 0:
+        _holds(dgate, -(-M // gate_rows) * C, "dgate")
+    _check_step(M, C, K, gate, gate_rows, w_post, w_pre, ckpt_b, rstd_b, ckpt_n, rstd_n, dn.dtype)
+    s = abl_resnorm(M, gate_rows, C, _dtype(dn), K, flags, alpha, beta, 0.0)
+    _check(lib.abl_resnorm_backward(_stream(), ctypes.byref(s), int(has_b), _ptr(dn), _ptr(dr_out), _ptr(gate), _ptr(w_post),
+                                    _ptr(w_pre), _ptr(ckpt_b), _ptr(rstd_b), _ptr(ckpt_n), _ptr(rstd_n), _ptr(scratch),
+                                    scratch.numel() * scratch.element_size(), _ptr(dr), _ptr(db), _ptr(dgate),
+                                    _ptr(dw_post), _ptr(dw_pre)), "abl_resnorm_backward")
+
+
+def abl_glu_forward(g, u, h, act, K=0, ckpt_g=None, ckpt_u=None):
+    """h = act(g) * u; g, u, h [M, C], rows contiguous (column slices of wider tensors are fine)."""
+    M, C = g.shape
+    _same(g.dtype, u, h)
+    (pg, lg), (pu, lu), (ph, lh) = _rows(g, M, C), _rows(u, M, C), _rows(h, M, C)
+    if K:
+        _store(ckpt_g, M, C, K, "ckpt_g")
+        _store(ckpt_u, M, C, K, "ckpt_u")
+    _check(lib.abl_glu_forward(_stream(), _dtype(g), act, pg, lg, pu, lu, M, C, K, ph, lh, _ptr(ckpt_g), _ptr(ckpt_u)),
+           "abl_glu_forward")
+
+
+def abl_glu_backward(dh, ckpt_g, ckpt_u, K, dg, du, act, ckpt_h=None):
+    M, C = dh.shape
+    _same(dh.dtype, dg, du)
+    (ph, lh), (pg, lg), (pu, lu) = _rows(dh, M, C), _rows(dg, M, C), _rows(du, M, C)
+    _store(ckpt_g, M, C, K, "ckpt_g")
+    _store(ckpt_u, M, C, K, "ckpt_u")
+    _store(ckpt_h, M, C, 8, "ckpt_h")
+    _check(lib.abl_glu_backward(_stream(), _dtype(dh), act, ph, lh, _ptr(ckpt_g), _ptr(ckpt_u), M, C, K, pg, lg, pu, lu,
+                                _ptr(ckpt_h)), "abl_glu_backward")
+
+
+def abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype):
+    """dtype: the torch dtype of dy."""
+    return lib.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, _dtype(dtype))
+
+
+def abl_ckpt_wgrad(ckpt, K, scale, dy, scratch, dW, flags=0):
+    """dW [Cin, Cout] fp32 = (scale * x~)^T dy from the store of x [M, Cin]; dy [M, Cout], rows contiguous."""
+    Cin, Cout = dW.shape
+    M = dy.shape[0]
+    p, ld = _rows(dy, M, Cout)
+    _same(dy.dtype, scale)
+    _same(torch.float32, dW)
+    _store(ckpt, M, Cin, K)
+    _holds(scale, Cin, "scale")
+    _check(lib.abl_ckpt_wgrad(_stream(), _dtype(dy), flags, _ptr(ckpt), M, Cin, K, _ptr(scale), p, ld, Cout, _ptr(scratch),
+                              scratch.numel() * scratch.element_size(), _ptr(dW)), "abl_ckpt_wgrad")
 
 
 def abl_sgd_momentum(w, grad, v, lr, momentum, weight_decay):

@@ -30,6 +30,10 @@ UNITS = {
     "conv_narrow.hip": ["-ffp-contract=off"],
     "conv_split.hip": ["-ffp-contract=off"],
     "wgrad_split.hip": ["-ffp-contract=off"],
+    "block_store.hip": [],
+    "resnorm.hip": [],
+    "store_wgrad.hip": [],
+    "rows_api.hip": [],
     "abl_api.hip": [],
     "abl_noalloc.hip": [],
     "probe_kernels.hip": [],

@@ -1,0 +1,200 @@
+// Block stores (abl_ckpt_pack / abl_ckpt_unpack) and the gated unit that makes and reads them (abl_glu_*): passes in which every
+// thread takes one piece of eight channels (block_store.h).
+//
+//   pack        codes and scales of x                 reads t bytes an element (2 in bf16), writes K / 8 + 1 / 32
+//   unpack      x~ = 2^e code                         the other way round
+//   glu_fwd     h = g s(g) u, codes of g and u        reads 2 t, writes t and two stores
+//   glu_bwd     dg = dh u a'(g), du = dh a(g), codes of a(g) u      reads t and two stores, writes 2 t and an 8-bit store
+//
+// with s(g) = 1 / (1 + exp(-q(g))), a = g s and a' = s + g s (1 - s) q': q = g for SiLU, and for the tanh form of GELU
+// q = 2 sqrt(2 / pi) (g + 0.044715 g^3), since (1 + tanh z) / 2 = 1 / (1 + exp(-2 z)).  All are bound by memory.
+
+#include "block_store.h"
+
+namespace abl {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Where the pieces of a pass lie: 4 B pieces per row, the blocks of threads one after the other.
+struct Pieces {
+  int64_t total, per_row;
+  int C;
+  Divisor by_row;   // (of numbers below 4 B + the threads of a block)
+  Pieces(int64_t M, int c) : total(M * store_blocks(c) * 4), per_row(store_blocks(c) * 4), C(c), by_row((int)(store_blocks(c) * 4)) {}
+  int64_t grid() const { return (total + kThreads - 1) / kThreads; }
+};
+
+struct Place {
+  int64_t piece, row;
+  int c, n;   // first channel, channels that exist (may be negative)
+};
+__device__ inline Place place_of(const Pieces& g) {
+  const int64_t first = (int64_t)blockIdx.x * kThreads;
+  const int64_t row = first / g.per_row;
+  const int rel = (int)(first - row * g.per_row) + (int)threadIdx.x;
+  const int more = g.by_row.of(rel);
+  Place p;
+  p.piece = first + threadIdx.x;
+  p.row = row + more;
+  p.c = (rel - more * (int)g.per_row) * 8;
+  p.n = g.C - p.c;
+  return p;
+}
+
+// The zeros behind the scales, up to a multiple of 128 bytes.
+__device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
+  if (blockIdx.x != 0) return;
+  const int64_t used = pieces * K + (pieces >> 2);
+  const int64_t all = (used + 127) / 128 * 128;
+  if (used + threadIdx.x < all) store[used + threadIdx.x] = 0;
+}
+
+template <typename T, int K>
+__global__ __launch_bounds__(kThreads) void pack_kernel(Pieces g, const T* __restrict__ x, int64_t ldx, unsigned char* __restrict__ store) {
+  zero_tail(store, g.total, K);
+  const Place p = place_of(g);
+  if (p.piece >= g.total) return;
+  float v[8];
+  load_piece(x + p.row * ldx + p.c, p.n, v);
+  keep_piece<K>(store, store + g.total * K, p.piece, v);
+}
+
+template <typename T, int K>
+__global__ __launch_bounds__(kThreads) void unpack_kernel(Pieces g, const unsigned char* __restrict__ store, T* __restrict__ x, int64_t ldx) {
+  const Place p = place_of(g);
+  if (p.piece >= g.total) return;
+  float v[8];
+  decode<K>(load_codes<K>(store, p.piece), store[g.total * K + (p.piece >> 2)], v);
+  store_piece(x + p.row * ldx + p.c, p.n, v);
+}
+
+template <int ACT>
+__device__ inline void gate(float g, float& s, float& dq) {
+  float q = g;
+  dq = 1.0f;
+  if constexpr (ACT == ABL_ACT_GELU) {
+    const float k = 1.5957691216057308f, k3 = 0.071354816272600f;   // 2 sqrt(2 / pi), 0.044715 of it
+    const float g2 = fminf(g * g, 1e30f);   // (beyond it s is 0 or 1, and dq only has to stay finite)
+    q = g * __builtin_fmaf(k3, g2, k);
+    dq = __builtin_fmaf(3.0f * k3, g2, k);
+  }
+  s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * q));
+}
+
+template <typename T, int ACT, int K>
+__global__ __launch_bounds__(kThreads) void glu_fwd_kernel(Pieces pc, const T* g, int64_t ldg, const T* u, int64_t ldu, T* h, int64_t ldh,
+                                                           unsigned char* __restrict__ store_g, unsigned char* __restrict__ store_u) {
+  if constexpr (K != 0) {
+    zero_tail(store_g, pc.total, K);
+    zero_tail(store_u, pc.total, K);
+  }
+  const Place p = place_of(pc);
+  if (p.piece >= pc.total) return;
+  float a[8], b[8], o[8];
+  load_piece(g + p.row * ldg + p.c, p.n, a);
+  load_piece(u + p.row * ldu + p.c, p.n, b);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float s, dq;
+    gate<ACT>(a[i], s, dq);
+    o[i] = a[i] * s * b[i];
+  }
+  store_piece(h + p.row * ldh + p.c, p.n, o);
+  if constexpr (K != 0) {
+    keep_piece<K>(store_g, store_g + pc.total * K, p.piece, a);
+    keep_piece<K>(store_u, store_u + pc.total * K, p.piece, b);
+  }
+}
+
+template <typename T, int ACT, int K>
+__global__ __launch_bounds__(kThreads) void glu_bwd_kernel(Pieces pc, const T* dh, int64_t lddh, const unsigned char* __restrict__ store_g,
+                                                           const unsigned char* __restrict__ store_u, T* dg, int64_t lddg, T* du, int64_t lddu,
+                                                           unsigned char* __restrict__ store_h) {
+  if (store_h != nullptr) zero_tail(store_h, pc.total, 8);
+  const Place p = place_of(pc);
+  if (p.piece >= pc.total) return;
+  float d[8], a[8], b[8], o[8];
+  load_piece(dh + p.row * lddh + p.c, p.n, d);
+  decode<K>(load_codes<K>(store_g, p.piece), store_g[pc.total * K + (p.piece >> 2)], a);
+  decode<K>(load_codes<K>(store_u, p.piece), store_u[pc.total * K + (p.piece >> 2)], b);
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float s, dq;
+    gate<ACT>(a[i], s, dq);
+    const float act = a[i] * s;
+    x[i] = d[i] * b[i] * __builtin_fmaf(act * (1.0f - s), dq, s);
+    y[i] = d[i] * act;
+    o[i] = act * b[i];
+  }
+  store_piece(dg + p.row * lddg + p.c, p.n, x);
+  store_piece(du + p.row * lddu + p.c, p.n, y);
+  if (store_h != nullptr) keep_piece<8>(store_h, store_h + pc.total * 8, p.piece, o);
+}
+
+// f(type, K) with the dtype and K as types of their own.
+template <typename F>
+void by_dtype(int dtype, F&& f) {
+  if (dtype == ABL_F32)
+    f(float{});
+  else
+    f(bf16_t{});
+}
+
+}  // namespace
+
+int launch_ckpt_pack(hipStream_t st, int dtype, Rows x, int64_t M, int C, int K, void* ckpt) {
+  const Pieces g(M, C);
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto kern = K == 8 ? pack_kernel<T, 8> : pack_kernel<T, 4>;
+    kern<<<dim3((unsigned)g.grid()), kThreads, 0, st>>>(g, (const T*)x.p, x.ld, (unsigned char*)ckpt);
+  });
+  return hip_status();
+}
+
+int launch_ckpt_unpack(hipStream_t st, int dtype, const void* ckpt, int64_t M, int C, int K, RowsOut x) {
+  const Pieces g(M, C);
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto kern = K == 8 ? unpack_kernel<T, 8> : unpack_kernel<T, 4>;
+    kern<<<dim3((unsigned)g.grid()), kThreads, 0, st>>>(g, (const unsigned char*)ckpt, (T*)x.p, x.ld);
+  });
+  return hip_status();
+}
+
+int launch_glu_forward(hipStream_t st, int dtype, int act, Rows g, Rows u, int64_t M, int C, int K, RowsOut h, void* ckpt_g,
+                       void* ckpt_u) {
+  const Pieces pc(M, C);
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto pick = [&](auto a) {
+      constexpr int A = decltype(a)::value;
+      return K == 0 ? glu_fwd_kernel<T, A, 0> : K == 8 ? glu_fwd_kernel<T, A, 8> : glu_fwd_kernel<T, A, 4>;
+    };
+    auto kern = act == ABL_ACT_SILU ? pick(std::integral_constant<int, ABL_ACT_SILU>{}) : pick(std::integral_constant<int, ABL_ACT_GELU>{});
+    kern<<<dim3((unsigned)pc.grid()), kThreads, 0, st>>>(pc, (const T*)g.p, g.ld, (const T*)u.p, u.ld, (T*)h.p, h.ld,
+                                                         (unsigned char*)ckpt_g, (unsigned char*)ckpt_u);
+  });
+  return hip_status();
+}
+
+int launch_glu_backward(hipStream_t st, int dtype, int act, Rows dh, const void* ckpt_g, const void* ckpt_u, int64_t M, int C, int K,
+                        RowsOut dg, RowsOut du, void* ckpt_h) {
+  const Pieces pc(M, C);
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto pick = [&](auto a) {
+      constexpr int A = decltype(a)::value;
+      return K == 8 ? glu_bwd_kernel<T, A, 8> : glu_bwd_kernel<T, A, 4>;
+    };
+    auto kern = act == ABL_ACT_SILU ? pick(std::integral_constant<int, ABL_ACT_SILU>{}) : pick(std::integral_constant<int, ABL_ACT_GELU>{});
+    kern<<<dim3((unsigned)pc.grid()), kThreads, 0, st>>>(pc, (const T*)dh.p, dh.ld, (const unsigned char*)ckpt_g,
+                                                         (const unsigned char*)ckpt_u, (T*)dg.p, dg.ld, (T*)du.p, du.ld,
+                                                         (unsigned char*)ckpt_h);
+  });
+  return hip_status();
+}
+
+}  // namespace abl
