@@ -170,17 +170,17 @@ __device__ inline Codes<K> encode(const float (&v)[8], uint32_t byte) {
   return c;
 }
 
-// K = 8: codes offset to 0..255, converted, and s (c + 128) - 128 s in one rounding (nothing is lost).
+// K = 8: codes offset to 0..255, which convert from any byte of a register; the offset is taken off before the scale (128 times
+// the largest scales is infinite).
 template <int K>
 __device__ inline void decode(const Codes<K>& c, uint32_t byte, float (&v)[8]) {
   const float s = scale_of(byte);
   if constexpr (K == 8) {
-    const float m = -128.0f * s;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t u = c.w[h] ^ 0x80808080u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[4 * h + i] = __builtin_fmaf((float)((u >> (8 * i)) & 0xFFu), s, m);
+      for (int i = 0; i < 4; ++i) v[4 * h + i] = ((float)((u >> (8 * i)) & 0xFFu) - 128.0f) * s;
     }
   } else {
     typedef float f32x2 __attribute__((ext_vector_type(2)));

@@ -67,8 +67,8 @@ int abl_resnorm_forward(void* stream, const abl_resnorm* step, const void* r, co
                         void* ckpt_n, float* rstd_n) {
   if (int e = check_step(step, true)) return e;
   if (!(step->eps > 0.0f) || (gate != nullptr && step->gate_rows < 1)) return ABL_ERR_ARG;
-  if (b == nullptr && (gate != nullptr || w_post != nullptr)) return ABL_ERR_ARG;
   if (step->M == 0) return ABL_OK;
+  if (b == nullptr && (gate != nullptr || w_post != nullptr)) return ABL_ERR_ARG;
   const size_t t = size_of(step->dtype);
   if (bad(r, t) || off(b, t) || off(gate, t) || off(w_post, t) || bad(w_pre, t) || off(r_out, t) || bad(n, t)) return ABL_ERR_ARG;
   if (step->K != 0) {
@@ -93,7 +93,7 @@ int abl_resnorm_backward(void* stream, const abl_resnorm* step, int has_b, const
   if (int e = check_step(step, false)) return e;
   if (gate != nullptr && step->gate_rows < 1) return ABL_ERR_ARG;
   if (!has_b && (gate != nullptr || w_post != nullptr || db != nullptr)) return ABL_ERR_ARG;
-  if ((gate != nullptr) != (dgate != nullptr) || (w_post != nullptr) != (dw_post != nullptr)) return ABL_ERR_ARG;
+  if ((step->M > 0 && (gate != nullptr) != (dgate != nullptr)) || (w_post != nullptr) != (dw_post != nullptr)) return ABL_ERR_ARG;
   if (bad(dw_pre, 4) || off(dw_post, 4) || off(dgate, 4)) return ABL_ERR_ARG;
   const size_t t = size_of(step->dtype);
   if (step->M > 0) {
