@@ -18,6 +18,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_any2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any2 __attribute__((aligned(2)));
 
 __host__ __device__ inline int64_t store_blocks(int C) { return (C + 31) / 32; }
 __host__ __device__ inline int64_t store_code_bytes(int64_t M, int C, int K) { return M * store_blocks(C) * 4 * K; }
@@ -41,18 +43,22 @@ struct Raw<bf16_t> {
   u32x4 a;
 };
 
-// n: channels that exist (a piece at the end of a row may have fewer than eight, down to none); the others read as zero.
+// n: channels that exist (a piece at the end of a row may have fewer than eight, down to none); the others read as zero.  A short
+// piece is taken as four, two and one of them, all on their way together and in few registers.
 __device__ inline Raw<float> load_raw(const float* p, int n) {
   Raw<float> r{};
   if (n >= 8) {
     r.a = *reinterpret_cast<const f32x4_any4*>(p);
     r.b = *reinterpret_cast<const f32x4_any4*>(p + 4);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i < n) r.a[i] = p[i];
-      if (i + 4 < n) r.b[i] = p[i + 4];
-    }
+  } else if (n > 0) {
+    f32x4_any4 four{};
+    float x = 0.0f, y = 0.0f, z = 0.0f;
+    if (n & 4) four = *reinterpret_cast<const f32x4_any4*>(p);
+    if (n & 2) x = p[n & 4], y = p[(n & 4) + 1];
+    if (n & 1) z = p[n & 6];
+    const f32x4_any4 rest = n & 2 ? f32x4_any4{x, y, z, 0.0f} : f32x4_any4{z, 0.0f, 0.0f, 0.0f};
+    r.a = n & 4 ? four : rest;
+    if (n & 4) r.b = rest;
   }
   return r;
 }
@@ -60,15 +66,15 @@ __device__ inline Raw<bf16_t> load_raw(const bf16_t* p, int n) {
   Raw<bf16_t> r{};
   if (n >= 8) {
     r.a = *reinterpret_cast<const u32x4_any2*>(p);
-  } else {
+  } else if (n > 0) {
     const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t w = 0;
-      if (2 * i < n) w = h[2 * i];
-      if (2 * i + 1 < n) w |= (uint32_t)h[2 * i + 1] << 16;
-      r.a[i] = w;
-    }
+    u32x2_any2 four{};
+    uint32_t two = 0, one = 0;
+    if (n & 4) four = *reinterpret_cast<const u32x2_any2*>(h);
+    if (n & 2) two = *reinterpret_cast<const u32_any2*>(h + (n & 4));
+    if (n & 1) one = h[n & 6];
+    const u32x2 rest = n & 2 ? u32x2{two, one} : u32x2{one, 0u};
+    r.a = n & 4 ? u32x4{four[0], four[1], rest[0], rest[1]} : u32x4{rest[0], rest[1], 0u, 0u};
   }
   return r;
 }
@@ -88,21 +94,22 @@ __device__ inline void store_piece(float* p, int n, const float (&v)[8]) {
   if (n >= 8) {
     *reinterpret_cast<f32x4_any4*>(p) = f32x4_any4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4_any4*>(p + 4) = f32x4_any4{v[4], v[5], v[6], v[7]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = v[i];
+  } else if (n > 0) {
+    if (n & 4) *reinterpret_cast<f32x4_any4*>(p) = f32x4_any4{v[0], v[1], v[2], v[3]};
+    const float a = v[0], b = v[1], c = v[2], d = v[4], e = v[5], f = v[6];   // (not chosen by address: v stays in registers)
+    if (n & 2) p[n & 4] = n & 4 ? d : a, p[(n & 4) + 1] = n & 4 ? e : b;
+    if (n & 1) p[n & 6] = n & 4 ? (n & 2 ? f : d) : (n & 2 ? c : a);
   }
 }
 __device__ inline void store_piece(bf16_t* p, int n, const float (&v)[8]) {
   const u32x4 w{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
   if (n >= 8) {
     *reinterpret_cast<u32x4_any2*>(p) = w;
-  } else {
+  } else if (n > 0) {
     uint16_t* h = reinterpret_cast<uint16_t*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) h[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    if (n & 4) *reinterpret_cast<u32x2_any2*>(h) = u32x2_any2{w[0], w[1]};
+    if (n & 2) *reinterpret_cast<u32_any2*>(h + (n & 4)) = n & 4 ? w[2] : w[0];
+    if (n & 1) h[n & 6] = (uint16_t)(n & 4 ? (n & 2 ? w[3] : w[2]) : (n & 2 ? w[1] : w[0]));
   }
 }
 
@@ -191,13 +198,13 @@ __device__ inline void decode(const Codes<K>& c, uint32_t byte, float (&v)[8]) {
   }
 }
 
-template <int K>
-__device__ inline Codes<K> load_codes(const unsigned char* codes, int64_t piece) {
+template <int K, typename I>
+__device__ inline Codes<K> load_codes(const unsigned char* codes, I piece) {
   return *reinterpret_cast<const Codes<K>*>(codes + piece * K);
 }
 // Writes the codes of a piece and, from the quad's first lane, the block's scale.
-template <int K>
-__device__ inline void keep_piece(unsigned char* codes, unsigned char* scales, int64_t piece, const float (&v)[8]) {
+template <int K, typename I>
+__device__ inline void keep_piece(unsigned char* codes, unsigned char* scales, I piece, const float (&v)[8]) {
   const uint32_t byte = scale_byte<K>(v);
   *reinterpret_cast<Codes<K>*>(codes + piece * K) = encode<K>(v, byte);
   if ((threadIdx.x & 3u) == 0) scales[piece >> 2] = (unsigned char)byte;
