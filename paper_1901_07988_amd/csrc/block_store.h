@@ -31,6 +31,12 @@ __device__ inline uint32_t two_bf16(float a, float b) {   // rounded to nearest 
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
+// ---- accesses through buffer descriptors: an offset beyond the descriptor's bytes reads zero and stores nothing ----
+constexpr uint32_t kNowhere = 0x80000000u;   // (stays beyond with a row's offset added: descriptors hold less than 2^31 bytes)
+__device__ inline __amdgpu_buffer_rsrc_t descriptor(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p != nullptr ? (int)bytes : 0, 0x00027000);
+}
+
 // ---- a piece as it lies in memory ----
 template <typename T>
 struct Raw;
@@ -113,6 +119,11 @@ __device__ inline void store_piece(bf16_t* p, int n, const float (&v)[8]) {
   }
 }
 
+// Here the loads of a value have to have come: what is loaded in a branch or before a loop is waited for there, and not, together with
+// all that was asked for since, where it is used.
+__device__ inline void settle(Raw<bf16_t>& r) { asm volatile("" : "+v"(r.a)); }
+__device__ inline void settle(Raw<float>& r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
+
 // ---- scale of a block ----
 template <int CTRL>
 __device__ inline uint32_t dpp_u32(uint32_t v) {
@@ -177,18 +188,12 @@ __device__ inline Codes<K> encode(const float (&v)[8], uint32_t byte) {
   return c;
 }
 
-// K = 8: codes offset to 0..255, which convert from any byte of a register; the offset is taken off before the scale (128 times
-// the largest scales is infinite).
 template <int K>
 __device__ inline void decode(const Codes<K>& c, uint32_t byte, float (&v)[8]) {
   const float s = scale_of(byte);
   if constexpr (K == 8) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t u = c.w[h] ^ 0x80808080u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[4 * h + i] = ((float)((u >> (8 * i)) & 0xFFu) - 128.0f) * s;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(c.w[i / 4] >> (8 * (i % 4))) * s;
   } else {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c.w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c.w, 1.0f, 1);

@@ -26,12 +26,6 @@ __device__ inline int left(int C, uint32_t c) { return C - (int)c; }
 // this row's stores, and from row to row only three scalar offsets change.  (A store takes the sum of its offsets in a vector register:
 // with the row's in the instruction's scalar operand the compiler lets the next instruction overwrite the store's data, and wrong
 // words have been written here.)
-constexpr uint32_t kNowhere = 0x80000000u;   // (stays beyond with a row's offset added: descriptors hold less than 2^31 bytes)
-
-__device__ inline auto descriptor(const void* p, int64_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p != nullptr ? (int)bytes : 0, 0x00027000);
-}
-
 // Rows of T from `first` on; WHOLE: of a multiple of eight channels.  Others take their last piece in parts (load_raw, store_piece).
 // Piece q of the k-th row; `at`: this lane's byte offset of it in a row (kNowhere beyond the end).
 template <typename T, bool WHOLE>
@@ -115,11 +109,6 @@ __device__ inline Raw<T> load_weights(const void* w, int64_t row, int C, uint32_
     r.a = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
   return r;
 }
-
-// Here the loads of a value have to have come: what is loaded in a branch or before a loop is waited for there, and not, together with
-// all that was asked for since, where it is used.
-__device__ inline void settle(Raw<bf16_t>& r) { asm volatile("" : "+v"(r.a)); }
-__device__ inline void settle(Raw<float>& r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
 
 // ---- a team's sums over a row ----
 template <int TEAM>

@@ -33,10 +33,45 @@ __device__ inline float row_scale(const void* s, int i) {
   return s == nullptr ? 1.0f : (float)((const T*)s)[i];
 }
 
-// NP: bf16 parts of an element of dy.
-template <typename T, int K, int NP, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * 64) void store_wgrad_kernel(WgArgs a) {
-  constexpr int BK = 32, kThreads = WI * WJ * 64;
+template <int K>
+__device__ inline float stored_value(const WgArgs& a, int64_t row, int c) {
+  const int64_t block = row * a.blocks + c / 32;
+  const float s = scale_of(a.scales[block]);
+  if constexpr (K == 8) {
+    return (float)(int8_t)a.codes[block * 32 + c % 32] * s;
+  } else {
+    float v[8];
+    decode<4>(Codes<4>{(uint32_t)(a.codes[block * 16 + c % 32 / 2] >> (4 * (c & 1))) & 15u}, a.scales[block], v);
+    return v[0];
+  }
+}
+
+// fp32 as three bf16 parts whose sum it is: the upper 16 bits of what is left, twice (nothing is rounded); a value that is not finite is its first part.
+__device__ inline void parts_of(const float (&v)[8], u32x4 (&part)[3]) {
+  uint32_t h[8], m[8], l[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t b = __float_as_uint(v[e]);
+    const bool fine = finite(v[e]), nan = (b & 0x7FFFFFFFu) > 0x7F800000u;
+    h[e] = nan ? 0x7FC00000u : b & 0xFFFF0000u;
+    const float r = fine ? v[e] - __uint_as_float(h[e]) : 0.0f;
+    m[e] = __float_as_uint(r);
+    l[e] = __float_as_uint(r - __uint_as_float(m[e] & 0xFFFF0000u));
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {   // the upper halves of two words
+    part[0][e] = __builtin_amdgcn_perm(h[2 * e + 1], h[2 * e], 0x07060302u);
+    part[1][e] = __builtin_amdgcn_perm(m[2 * e + 1], m[2 * e], 0x07060302u);
+    part[2][e] = __builtin_amdgcn_perm(l[2 * e + 1], l[2 * e], 0x07060302u);
+  }
+}
+
+// ---- rows far apart ----
+// The plain form of the kernel below, with 64-bit addresses: for a dy whose rows lie so far apart that a step of 32 of them does not fit a buffer
+// descriptor.  NP: bf16 parts of an element of dy.
+template <typename T, int K, int NP>
+__global__ __launch_bounds__(256) void store_wgrad_far_kernel(WgArgs a) {
+  constexpr int BI = 128, BJ = 128, WI = 2, WJ = 2, BK = 32, kThreads = WI * WJ * 64;
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;   // 16 x 16 tiles of a wave
   constexpr int PX = BK * BI / 8 / kThreads, PY = BK * BJ / 8 / kThreads;   // pieces of a thread
   constexpr int kXBytes = BK * BI * 2, kYBytes = BK * BJ * 2, kStage = kXBytes + NP * kYBytes;
@@ -89,12 +124,13 @@ __global__ __launch_bounds__(WI * WJ * 64) void store_wgrad_kernel(WgArgs a) {
       } else {
         float v[8];
         expand(ry[p], v);
+        if constexpr (NP == 1) {
+          put(y, to_bf16x8(v));
+        } else {
+          u32x4 part[3];
+          parts_of(v, part);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          const bf16x8_t h = to_bf16x8(v);
-          put(y + n * kYBytes, h);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = finite(v[e]) ? v[e] - (float)h[e] : 0.0f;
+          for (int n = 0; n < 3; ++n) *reinterpret_cast<u32x4*>(y + n * kYBytes) = part[n];
         }
       }
     }
@@ -160,50 +196,378 @@ __global__ __launch_bounds__(WI * WJ * 64) void store_wgrad_kernel(WgArgs a) {
   }
 }
 
-// The shares' copies, added in turn.
+// ---- the product ----
+// A block of eight waves has a tile of 256 channels of x and BJ of dy, a wave 64 x BJ / 2 of it.  Waves w and w + 4 share a SIMD and take turns:
+// while one issues the matrix instructions of a step of 32 rows, the other reads its next fragments from LDS and writes its share of the next
+// tile there; a barrier changes the roles, and waves 4 to 7 are one barrier behind.  A wave issues an instruction about every four cycles, so what
+// needs registers only - codes to bf16, the loads of later tiles - goes between its matrix instructions, which leave three such places each.
+//   phase 2 s      waves 0-3 read step s and write their share of tile s + 1       waves 4-7 multiply step s - 1
+//   phase 2 s + 1  waves 0-3 multiply step s                                       waves 4-7 read step s, write tile s + 1
+// Two tiles in LDS are enough: tile s + 1 replaces tile s - 1, which waves 4-7 read in phase 2 s - 1.
+template <typename T, int K, int NP, int BI, int BJ, bool RAGGED>
+__global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_wgrad_kernel(WgArgs a) {
+  constexpr int BK = 32, WI = 4, WJ = 2;
+  constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;
+  constexpr int XP = BI / 128;                       // pieces of x of a thread
+  constexpr int PY = BK * BJ / 8 / 512;              // pieces of dy of a thread
+  constexpr int kXBytes = BK * BI * 2, kYBytes = BK * BJ * 2, kStage = kXBytes + NP * kYBytes;
+  extern __shared__ __align__(16) char lds[];        // [2][kStage]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool late = wave >= 4;
+
+  // Blocks 8 apart share an XCD and its L2.  Each XCD takes consecutive items, in the order of columns of four tiles of x: what runs there at one
+  // time shares four tiles of x and a few of dy.
+  const int tiles = a.tiles_i * a.tiles_j, items = gridDim.x;
+  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = items >> 3, more = items & 7;
+  const int item = xcd * per + (xcd < more ? xcd : more) + slot;
+  const int share = item / tiles, tile = item - share * tiles;
+  const int band = tile / (4 * a.tiles_j), rest = tile - band * 4 * a.tiles_j;
+  const int high = a.tiles_i - band * 4 < 4 ? a.tiles_i - band * 4 : 4;
+  const int i0 = (band * 4 + rest % high) * BI, j0 = rest / high * BJ;
+  const int64_t m0 = share * a.rows, m1 = m0 + a.rows < a.M ? m0 + a.rows : a.M;
+  const int steps = (int)((m1 - m0 + BK - 1) / BK);
+
+  // This thread's share of a tile: XP pieces of x next to each other in a row, PY pieces of dy.  Loads go through descriptors of the share's rows; rows beyond them
+  // and channels that do not exist read zero.
+  const int xr = tid >> 4, xq = (tid & 15) * XP;
+  const int block = i0 / 32 + (xq >> 2);
+  const int rows = (int)(m1 - m0);
+  const auto codes = descriptor(a.codes + m0 * a.blocks * 4 * K, (int64_t)rows * a.blocks * 4 * K);
+  const auto scales = descriptor(a.scales + m0 * a.blocks, (int64_t)rows * a.blocks);
+  // (RAGGED, where another share follows: a piece may reach beyond the channels, which adds to columns that are not written)
+  const bool ends = m1 == a.M;
+  const int64_t last = rows == 0 ? 0 : ends ? (rows - 1) * a.ldy + a.Cout : rows * a.ldy + (RAGGED ? 8 : 0);
+  const auto dy = descriptor((const T*)a.dy + m0 * a.ldy, last * (int64_t)sizeof(T));
+  const uint32_t s_at = block < a.blocks ? (uint32_t)xr * (uint32_t)a.blocks + (uint32_t)block : kNowhere;
+  const uint32_t c_at = block < a.blocks ? s_at * (4u * K) + (uint32_t)(xq & 3) * K : kNowhere;
+  uint32_t y_at[PY];
+  int y_row[PY];   // RAGGED: its row in a tile; the piece of the last row that is not whole is left out here and added at the end
+  bool y_part[PY];
+#pragma unroll
+  for (int p = 0; p < PY; ++p) {
+    const int c = j0 + (p * 512 + tid) % (BJ / 8) * 8;
+    y_row[p] = (p * 512 + tid) / (BJ / 8);
+    y_part[p] = c < a.Cout && c + 8 > a.Cout;
+    y_at[p] = c < a.Cout ? ((uint32_t)y_row[p] * (uint32_t)a.ldy + (uint32_t)c) * (uint32_t)sizeof(T) : kNowhere;
+  }
+  const uint32_t c_step = (uint32_t)a.blocks * (4u * K * BK), s_step = (uint32_t)a.blocks * BK, y_step = (uint32_t)a.ldy * (uint32_t)(sizeof(T) * BK);
+
+  struct XCodes {
+    Codes<K> c[XP];
+    uint32_t s;
+  };
+  struct YPieces {
+    Raw<T> r[PY];
+  };
+  auto fetch_x = [&](int step, XCodes& t) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)step * c_step;
+    if constexpr (K * XP == 16) {
+      const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, c_at, at, 0));
+      t.c[0].w = u32x2{w[0], w[1]}, t.c[1].w = u32x2{w[2], w[3]};
+    } else if constexpr (K * XP == 8) {
+      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, c_at, at, 0));
+      if constexpr (K == 8)
+        t.c[0].w = w;
+      else
+        t.c[0].w = w[0], t.c[1].w = w[1];
+    } else {
+      t.c[0].w = __builtin_amdgcn_raw_buffer_load_b32(codes, c_at, at, 0);
+    }
+    t.s = __builtin_amdgcn_raw_buffer_load_b8(scales, s_at, (uint32_t)step * s_step, 0);
+  };
+  auto fetch_y = [&](int step, YPieces& t) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)step * y_step;
+    const int left = rows - step * BK;
+#pragma unroll
+    for (int p = 0; p < PY; ++p) {
+      uint32_t of = y_at[p];
+      if constexpr (RAGGED) of = y_row[p] < left - (ends && y_part[p] ? 1 : 0) ? of : kNowhere;
+      if constexpr (std::is_same_v<T, float>) {
+        t.r[p].a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at, 0));
+        t.r[p].b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at + 16, 0));
+      } else {
+        t.r[p].a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at, 0));
+      }
+    }
+  };
+  u32x4 xw[XP];   // of the next tile, in bf16
+  auto decode_x = [&](const XCodes& t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < XP; ++p) {
+      float v[8];
+      decode<K>(t.c[p], t.s, v);
+#pragma unroll   // (the upper halves: nothing is below them)
+      for (int e = 0; e < 4; ++e) xw[p][e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]), 0x07060302u);
+    }
+  };
+  constexpr bool kSplit = NP == 3;   // dy's parts, too, are made between the matrix instructions
+  u32x4 yw[PY][NP];
+  auto split_y = [&](const YPieces& t) __attribute__((always_inline)) {
+    if constexpr (kSplit) {
+#pragma unroll
+      for (int p = 0; p < PY; ++p) {
+        float v[8];
+        expand(t.r[p], v);
+        parts_of(v, yw[p]);
+      }
+    }
+  };
+  auto stage = [&](const YPieces& t, char* to) __attribute__((always_inline)) {
+    char* x = to + xr * (BI * 2) + (((xq >> 1) ^ (xr & 7)) * 32) + (xq & 1) * 16;
+#pragma unroll
+    for (int p = 0; p < XP; ++p) *reinterpret_cast<u32x4*>(x + 16 * p) = xw[p];
+#pragma unroll
+    for (int p = 0; p < PY; ++p) {
+      const int at = p * 512 + tid, r = at / (BJ / 8), q = at % (BJ / 8);
+      char* y = to + kXBytes + r * (BJ * 2) + (((q >> 1) ^ (r & 7)) * 32) + (q & 1) * 16;
+      if constexpr (kSplit) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) *reinterpret_cast<u32x4*>(y + n * kYBytes) = yw[p][n];
+      } else if constexpr (std::is_same_v<T, bf16_t>) {
+        *reinterpret_cast<u32x4*>(y) = t.r[p].a;
+      } else {
+        float v[8];
+        expand(t.r[p], v);
+        put(y, to_bf16x8(v));
+      }
+    }
+  };
+
+  floatx4 acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int wi = wave / WJ * (FI * 16), wj = wave % WJ * (FJ * 16);
+  const int fr = (lane >> 4) * 4 + ((lane & 15) >> 2);
+  auto fragment = [&](const char* plane, int pitch, int c) __attribute__((always_inline)) {
+    const char* p = plane + fr * pitch + (((c >> 4) ^ (fr & 7)) * 32) + (lane & 3) * 8;
+    return transposed(p, p + 16 * pitch);
+  };
+  auto phase_end = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // tile t waits in registers of set t % 2
+  XCodes xs[2];
+  YPieces ys[2];
+  fetch_x(0, xs[0]);
+  fetch_x(1, xs[1]);
+  fetch_y(0, ys[0]);
+  fetch_y(1, ys[1]);
+  decode_x(xs[0]);
+  split_y(ys[0]);
+  stage(ys[0], lds);
+  fetch_x(2, xs[0]);
+  fetch_y(2, ys[0]);
+  decode_x(xs[1]);
+  fetch_x(3, xs[1]);
+  if constexpr (kSplit) {
+    split_y(ys[1]);
+    fetch_y(3, ys[1]);
+  }
+  phase_end();
+  if (late) phase_end();
+  bf16x8_t x[FI], y[NP][FJ];
+  auto step = [&](int s, XCodes& xset, YPieces& ynow, YPieces& ynext, char* now, char* then) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FI; ++i) x[i] = fragment(now, BI * 2, wi + 16 * i);
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) y[n][j] = fragment(now + kXBytes + n * kYBytes, BJ * 2, wj + 16 * j);
+    stage(ynext, then);                      // tile s + 1
+    phase_end();
+    decode_x(xset);                          // tile s + 2
+    fetch_x(s + 4, xset);
+    if constexpr (kSplit) {
+      split_y(ynow);                         // tile s + 2
+      fetch_y(s + 4, ynow);
+    } else {
+      fetch_y(s + 3, ynext);
+    }
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[i][j] = mfma32(y[n][j], x[i], acc[i][j]);
+#pragma unroll
+    for (int k = 0; k < NP * FI * FJ; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
+      __builtin_amdgcn_sched_group_barrier(0x002, kSplit ? 3 : 2, 0);   // two or three vector ones
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // a load
+    }
+    phase_end();
+  };
+  for (int s = 0; s < steps; s += 2) {
+    step(s, xs[0], ys[0], ys[1], lds, lds + kStage);
+    step(s + 1, xs[1], ys[1], ys[0], lds + kStage, lds);   // (beyond the last step of an odd number: of zeros)
+  }
+  if (!late) phase_end();
+
+  const bool whole = a.copy == 0;
+  float* out = a.out + share * a.copy;
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {
+    const int ci = i0 + wi + 16 * i + (lane & 15);
+    if (ci >= a.Cin) continue;
+    const float s = whole ? row_scale<T>(a.scale, ci) : 1.0f;
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) {
+      const int cj = j0 + wj + 16 * j + (lane >> 4) * 4;
+      float* to = out + (int64_t)ci * a.Cout + cj;
+      f32x4_any4 v = acc[i][j];
+      if (RAGGED && ends && a.M > 0 && cj + 4 > a.Cout / 8 * 8 && cj < a.Cout) {
+        const float xv = stored_value<K>(a, a.M - 1, ci);
+        const T* row = (const T*)a.dy + (a.M - 1) * a.ldy;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (cj + e < a.Cout / 8 * 8 || cj + e >= a.Cout) continue;
+          const float yv = (float)row[cj + e];
+          v[e] = __builtin_fmaf(xv, NP == 1 ? (float)(__bf16)yv : yv, v[e]);
+        }
+      }
+      v *= s;
+      if (cj + 4 <= a.Cout) {
+        if (whole && a.accum) v += *reinterpret_cast<const f32x4_any4*>(to);
+        *reinterpret_cast<f32x4_any4*>(to) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (cj + e < a.Cout) to[e] = whole && a.accum ? to[e] + v[e] : v[e];
+      }
+    }
+  }
+}
+
+// The shares' copies, added in turn: four neighbouring elements a thread, the copies' loads on their way together.
 template <typename T>
 __global__ __launch_bounds__(256) void wgrad_sum_kernel(const float* copies, int n, int64_t size, const void* scale, Divisor by_cout, int accum,
                                                         float* dW) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (e >= size) return;
-  float s = 0.0f;
-  for (int i = 0; i < n; ++i) s += copies[i * size + e];
-  s *= row_scale<T>(scale, by_cout.of((int)e));
-  dW[e] = accum ? dW[e] + s : s;
+  const bool whole = e + 4 <= size;
+  f32x4_any4 s{};
+  for (int i = 0; i < n; i += 8) {
+    f32x4_any4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* from = copies + (int64_t)(i + k) * size + e;
+      v[k] = f32x4_any4{};
+      if (i + k < n) {
+        if (whole) {
+          v[k] = *reinterpret_cast<const f32x4_any4*>(from);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (e + j < size) v[k][j] = from[j];
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += v[k];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (e + j >= size) continue;
+    const float v = s[j] * row_scale<T>(scale, by_cout.of((int)(e + j)));
+    s[j] = accum ? dW[e + j] + v : v;
+  }
+  if (whole) {
+    *reinterpret_cast<f32x4_any4*>(dW + e) = s;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (e + j < size) dW[e + j] = s[j];
+  }
 }
 
-template <int TILE>
+// How a product is cut: tiles of bi x bj channels, and the rows into shares whose sums go to copies of dW that a second launch adds.
 struct Plan {
-  int tiles_i, tiles_j, shares;
-  int64_t rows;
-  Plan(int64_t M, int Cin, int Cout) {
-    tiles_i = (Cin + TILE - 1) / TILE, tiles_j = (Cout + TILE - 1) / TILE;
-    const int64_t tiles = (int64_t)tiles_i * tiles_j;
-    int64_t n = tiles >= 256 ? 1 : 512 / tiles;
-    const int64_t most = (M + 255) / 256;
-    if (n > most) n = most;
-    if (n < 1) n = 1;
-    rows = ((M + n - 1) / n + 31) / 32 * 32;
-    shares = M > 0 ? (int)((M + rows - 1) / rows) : 1;
-  }
+  int bi = 128, bj = 128, tiles_i = 0, tiles_j = 0, shares = 1;
+  int64_t rows = 0;
 };
 
-template <typename T>
-void sum_copies(hipStream_t st, const float* copies, int n, int Cin, int Cout, const void* scale, bool accum, float* dW) {
-  const int64_t size = (int64_t)Cin * Cout;
-  wgrad_sum_kernel<T><<<(unsigned)((size + 255) / 256), 256, 0, st>>>(copies, n, size, scale, Divisor(Cout), accum, dW);
+// The choice with the least time by these estimates, in us as measured on products of 128 to 16384 rows and 256 to 4096 channels (a step is 32 rows):
+//   256 x 256, bf16      one block a compute unit: 7 and 0.65 a step, 0.85 where all units have one
+//   128 x 128, bf16      4 and 0.34 a step, or 0.56 with two blocks on a unit
+//   256 x 128, fp32      7 and 1.0 a step, 1.25 where all units have a block (three products)
+//   128 x 128, fp32      4 and 0.68 a step, 0.85 where all units have one (its registers leave room for one)
+//   copies               4 for the second launch, 0.6 for each eight of them, their bytes written and read at 8.5 TB/s
+Plan plan_of(int64_t M, int Cin, int Cout, int dtype, bool parts) {
+  const int64_t size = dtype == ABL_F32 ? 4 : 2;
+  Plan best;
+  best.tiles_i = (Cin + 127) / 128, best.tiles_j = (Cout + 127) / 128, best.rows = M;
+  const int64_t room = (int64_t)1 << 30;   // bytes that a share's rows may span
+  const int64_t wide = Cout * size > (int64_t)Cin * 2 ? Cout * size : (int64_t)Cin * 2;
+  const int64_t least = (M * wide + room - 1) / room;   // shares that the descriptors ask for
+  double time = 1e30;
+  for (int large = 0; large < 2; ++large) {
+    const int bi = large ? 256 : 128, bj = large && !parts ? 256 : 128;
+    const int64_t ti = (Cin + bi - 1) / bi, tj = (Cout + bj - 1) / bj, tiles = ti * tj;
+    for (int64_t n = 1; n <= 64 || n < 2 * least; n *= 2) {
+      const int64_t want = n > least ? n : least;
+      const int64_t rows = ((M + want - 1) / want + 63) / 64 * 64;
+      const int64_t shares = M > 0 ? (M + rows - 1) / rows : 1, items = tiles * shares;
+      if (n > 1 && n > least && shares * Cin * Cout > (int64_t)24 << 20) break;   // (96 MB of copies)
+      const double steps = (double)(rows < M ? rows : M) / 32, load = items < 256 ? (double)items / 256 : 1.0;
+      const int64_t rounds = (items + 255) / 256;
+      double t;
+      if (large) {
+        t = (double)rounds * (steps * (parts ? 1.0 + 0.25 * load : 0.65 + 0.2 * load) + 7);
+      } else if (parts) {
+        t = (double)rounds * (steps * (0.68 + 0.17 * load) + 4);
+      } else {
+        t = (double)(rounds / 2) * (steps * 0.56 + 4) + (double)(rounds % 2) * (steps * 0.34 + 4);
+      }
+      if (shares > 1) t += 4 + 0.6 * (double)((shares + 7) / 8) + (double)shares * Cin * Cout * 8 / 8.5e6;
+      if (t < time) {
+        time = t;
+        best.bi = bi, best.bj = bj, best.tiles_i = (int)ti, best.tiles_j = (int)tj, best.shares = (int)shares, best.rows = rows;
+      }
+    }
+  }
+  return best;
+}
+
+template <typename T, int NP, int BI, int BJ>
+int launch_tiles(hipStream_t st, int K, bool ragged, unsigned grid, const WgArgs& a) {
+  auto kern = K == 8 ? (ragged ? store_wgrad_kernel<T, 8, NP, BI, BJ, true> : store_wgrad_kernel<T, 8, NP, BI, BJ, false>)
+                     : (ragged ? store_wgrad_kernel<T, 4, NP, BI, BJ, true> : store_wgrad_kernel<T, 4, NP, BI, BJ, false>);
+  constexpr int kBytes = 2 * 32 * 2 * (BI + NP * BJ);
+  if (kBytes > 64 * 1024)
+    if (int e = allow_full_lds((const void*)kern)) return e;
+  kern<<<grid, 512, kBytes, st>>>(a);
+  return hip_status();
 }
 
 }  // namespace
 
+// (For any distance of dy's rows and either way of fp32: the copies are limited alike, so the most that a choice may take is asked for.)
 size_t store_wgrad_scratch_bytes(int64_t M, int Cin, int Cout, int dtype) {
-  const Plan<128> p(M, Cin, Cout);
-  return p.shares > 1 ? (size_t)p.shares * Cin * Cout * sizeof(float) : 16;
+  size_t most = 16;
+  for (int parts = 0; parts < (dtype == ABL_F32 ? 2 : 1); ++parts) {
+    const Plan p = plan_of(M, Cin, Cout, dtype, parts != 0);
+    const size_t need = p.shares > 1 ? (size_t)p.shares * Cin * Cout * sizeof(float) : 16;
+    if (need > most) most = need;
+  }
+  return most;
 }
 
 int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ckpt, int64_t M, int Cin, int K, const void* scale,
                        Rows dy, int Cout, void* scratch, float* dW) {
-  const Plan<128> p(M, Cin, Cout);
+  const bool parts = dtype == ABL_F32 && !(flags & ABL_MATH_BF16), f32 = dtype == ABL_F32;
+  Plan p = plan_of(M, Cin, Cout, dtype, parts);
+  // (planned as if dy were contiguous, which the workspace is asked for without knowing.)  A share whose offsets, some steps beyond its end
+  // included, do not fit 31 bits takes the far kernel, and so do fewer than eight channels, where several rows' pieces would reach beyond
+  // the tensor's end.
+  const bool far = (p.rows + 256) * dy.ld * (f32 ? 4 : 2) >= (int64_t)0x7FFFFF00 || Cout < 8;
+  if (far) p.bi = p.bj = 128, p.tiles_i = (Cin + 127) / 128, p.tiles_j = (Cout + 127) / 128;
   WgArgs a;
   a.codes = (const unsigned char*)ckpt, a.scales = a.codes + store_code_bytes(M, Cin, K);
   a.dy = dy.p, a.ldy = dy.ld, a.scale = scale, a.M = M, a.rows = p.rows, a.Cin = Cin, a.Cout = Cout, a.blocks = (int)store_blocks(Cin);
@@ -211,25 +575,26 @@ int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ck
   a.copy = p.shares > 1 ? (int64_t)Cin * Cout : 0;
   a.out = p.shares > 1 ? (float*)scratch : dW;
   const unsigned grid = (unsigned)(p.tiles_i * p.tiles_j * p.shares);
-  if (dtype == ABL_BF16) {
-    auto kern = K == 8 ? store_wgrad_kernel<bf16_t, 8, 1, 128, 128, 2, 2> : store_wgrad_kernel<bf16_t, 4, 1, 128, 128, 2, 2>;
+  const bool ragged = Cout % 8 != 0;
+  int e;
+  if (far) {
+    auto kern = f32 ? (parts ? (K == 8 ? store_wgrad_far_kernel<float, 8, 3> : store_wgrad_far_kernel<float, 4, 3>)
+                             : (K == 8 ? store_wgrad_far_kernel<float, 8, 1> : store_wgrad_far_kernel<float, 4, 1>))
+                    : (K == 8 ? store_wgrad_far_kernel<bf16_t, 8, 1> : store_wgrad_far_kernel<bf16_t, 4, 1>);
     kern<<<grid, 256, 0, st>>>(a);
-  } else if (flags & ABL_MATH_BF16) {
-    auto kern = K == 8 ? store_wgrad_kernel<float, 8, 1, 128, 128, 2, 2> : store_wgrad_kernel<float, 4, 1, 128, 128, 2, 2>;
-    kern<<<grid, 256, 0, st>>>(a);
+    e = hip_status();
+  } else if (!f32) {
+    e = p.bi == 256 ? launch_tiles<bf16_t, 1, 256, 256>(st, K, ragged, grid, a) : launch_tiles<bf16_t, 1, 128, 128>(st, K, ragged, grid, a);
+  } else if (!parts) {
+    e = p.bi == 256 ? launch_tiles<float, 1, 256, 256>(st, K, ragged, grid, a) : launch_tiles<float, 1, 128, 128>(st, K, ragged, grid, a);
   } else {
-    auto kern = K == 8 ? store_wgrad_kernel<float, 8, 3, 128, 128, 2, 2> : store_wgrad_kernel<float, 4, 3, 128, 128, 2, 2>;
-    kern<<<grid, 256, 0, st>>>(a);
+    e = p.bi == 256 ? launch_tiles<float, 3, 256, 128>(st, K, ragged, grid, a) : launch_tiles<float, 3, 128, 128>(st, K, ragged, grid, a);
   }
-  if (int e = hip_status()) return e;
-  if (p.shares > 1) {
-    if (dtype == ABL_BF16)
-      sum_copies<bf16_t>(st, (const float*)scratch, p.shares, Cin, Cout, scale, a.accum, dW);
-    else
-      sum_copies<float>(st, (const float*)scratch, p.shares, Cin, Cout, scale, a.accum, dW);
-    return hip_status();
-  }
-  return ABL_OK;
+  if (e != ABL_OK || p.shares == 1) return e;
+  const int64_t size = (int64_t)Cin * Cout;
+  auto sum = f32 ? wgrad_sum_kernel<float> : wgrad_sum_kernel<bf16_t>;
+  sum<<<(unsigned)((size + 1023) / 1024), 256, 0, st>>>((const float*)scratch, p.shares, size, scale, Divisor(Cout), a.accum, dW);
+  return hip_status();
 }
 
 }  // namespace abl
