@@ -49,13 +49,29 @@ struct Raw<bf16_t> {
   u32x4 a;
 };
 
+// (T is one of the types above: a type that only differs in its alignment cannot be a template's argument)
+#define ABL_FETCH(T, p) (STREAM ? __builtin_nontemporal_load(reinterpret_cast<const T*>(p)) : *reinterpret_cast<const T*>(p))
+#define ABL_WRITE(T, p, v)                                             \
+  do {                                                                 \
+    if constexpr (STREAM)                                              \
+      __builtin_nontemporal_store(v, reinterpret_cast<T*>(p));         \
+    else                                                               \
+      *reinterpret_cast<T*>(p) = v;                                    \
+  } while (0)
+
+// STREAM: past the caches, for passes that move more than the last-level cache holds (256 MB): nothing of them would stay there for the
+// next pass, and what else lies there does.  Measured on 16384 x 8192 bf16, K = 4: unpack 65 -> 47 us, pack 63 -> 61; 8192 x 12288 gated unit
+// without stores 103 -> 95, its backward 158 -> 150; on tensors that fit the cache the next pass would lose.
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
+
 // n: channels that exist (a piece at the end of a row may have fewer than eight, down to none); the others read as zero.  A short
 // piece is taken as four, two and one of them, all on their way together and in few registers.
+template <bool STREAM = false>
 __device__ inline Raw<float> load_raw(const float* p, int n) {
   Raw<float> r{};
   if (n >= 8) {
-    r.a = *reinterpret_cast<const f32x4_any4*>(p);
-    r.b = *reinterpret_cast<const f32x4_any4*>(p + 4);
+    r.a = ABL_FETCH(f32x4_any4, p);
+    r.b = ABL_FETCH(f32x4_any4, p + 4);
   } else if (n > 0) {
     f32x4_any4 four{};
     float x = 0.0f, y = 0.0f, z = 0.0f;
@@ -68,10 +84,11 @@ __device__ inline Raw<float> load_raw(const float* p, int n) {
   }
   return r;
 }
+template <bool STREAM = false>
 __device__ inline Raw<bf16_t> load_raw(const bf16_t* p, int n) {
   Raw<bf16_t> r{};
   if (n >= 8) {
-    r.a = *reinterpret_cast<const u32x4_any2*>(p);
+    r.a = ABL_FETCH(u32x4_any2, p);
   } else if (n > 0) {
     const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
     u32x2_any2 four{};
@@ -92,14 +109,15 @@ __device__ inline void expand(const Raw<bf16_t>& r, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[2 * i] = low_bf16(r.a[i]), v[2 * i + 1] = high_bf16(r.a[i]);
 }
-template <typename T>
+template <bool STREAM = false, typename T>
 __device__ inline void load_piece(const T* p, int n, float (&v)[8]) {
-  expand(load_raw(p, n), v);
+  expand(load_raw<STREAM>(p, n), v);
 }
+template <bool STREAM = false>
 __device__ inline void store_piece(float* p, int n, const float (&v)[8]) {
   if (n >= 8) {
-    *reinterpret_cast<f32x4_any4*>(p) = f32x4_any4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_any4*>(p + 4) = f32x4_any4{v[4], v[5], v[6], v[7]};
+    ABL_WRITE(f32x4_any4, p, (f32x4_any4{v[0], v[1], v[2], v[3]}));
+    ABL_WRITE(f32x4_any4, p + 4, (f32x4_any4{v[4], v[5], v[6], v[7]}));
   } else if (n > 0) {
     if (n & 4) *reinterpret_cast<f32x4_any4*>(p) = f32x4_any4{v[0], v[1], v[2], v[3]};
     const float a = v[0], b = v[1], c = v[2], d = v[4], e = v[5], f = v[6];   // (not chosen by address: v stays in registers)
@@ -107,10 +125,11 @@ __device__ inline void store_piece(float* p, int n, const float (&v)[8]) {
     if (n & 1) p[n & 6] = n & 4 ? (n & 2 ? f : d) : (n & 2 ? c : a);
   }
 }
+template <bool STREAM = false>
 __device__ inline void store_piece(bf16_t* p, int n, const float (&v)[8]) {
   const u32x4 w{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
   if (n >= 8) {
-    *reinterpret_cast<u32x4_any2*>(p) = w;
+    ABL_WRITE(u32x4_any2, p, (u32x4_any2)w);
   } else if (n > 0) {
     uint16_t* h = reinterpret_cast<uint16_t*>(p);
     if (n & 4) *reinterpret_cast<u32x2_any2*>(h) = u32x2_any2{w[0], w[1]};
@@ -216,18 +235,20 @@ __device__ inline void keep_piece(unsigned char* codes, unsigned char* scales, I
 }
 
 // ---- sums ----
-// Sum over the 64 lanes, the same for all of them.
-__device__ inline float wave_sum(float v) {
+// Sum over the 64 lanes, the same for all of them; of the four rows of 16 in S.
+template <typename S = float>
+__device__ inline S wave_sum(float v) {
   v += __uint_as_float(dpp_u32<0xB1>(__float_as_uint(v)));    // quad_perm [1,0,3,2]
   v += __uint_as_float(dpp_u32<0x4E>(__float_as_uint(v)));    // quad_perm [2,3,0,1]
   v += __uint_as_float(dpp_u32<0x141>(__float_as_uint(v)));   // row_half_mirror
   v += __uint_as_float(dpp_u32<0x140>(__float_as_uint(v)));   // row_mirror
   const int u = __float_as_int(v);
-  return (__int_as_float(__builtin_amdgcn_readlane(u, 0)) + __int_as_float(__builtin_amdgcn_readlane(u, 16))) +
-         (__int_as_float(__builtin_amdgcn_readlane(u, 32)) + __int_as_float(__builtin_amdgcn_readlane(u, 48)));
+  return ((S)__int_as_float(__builtin_amdgcn_readlane(u, 0)) + (S)__int_as_float(__builtin_amdgcn_readlane(u, 16))) +
+         ((S)__int_as_float(__builtin_amdgcn_readlane(u, 32)) + (S)__int_as_float(__builtin_amdgcn_readlane(u, 48)));
 }
 
 // ---- launchers ----
+inline int64_t size_of(int dtype) { return dtype == ABL_F32 ? 4 : 2; }
 struct Rows {   // a matrix of rows: elements from one row to the next
   const void* p;
   int64_t ld;

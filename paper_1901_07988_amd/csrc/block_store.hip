@@ -50,23 +50,23 @@ __device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
   if (used + threadIdx.x < all) store[used + threadIdx.x] = 0;
 }
 
-template <typename T, int K>
+template <typename T, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void pack_kernel(Pieces g, const T* __restrict__ x, int64_t ldx, unsigned char* __restrict__ store) {
   zero_tail(store, g.total, K);
   const Place p = place_of(g);
   if (p.piece >= g.total) return;
   float v[8];
-  load_piece(x + p.row * ldx + p.c, p.n, v);
+  load_piece<STREAM>(x + p.row * ldx + p.c, p.n, v);
   keep_piece<K>(store, store + g.total * K, p.piece, v);
 }
 
-template <typename T, int K>
+template <typename T, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(Pieces g, const unsigned char* __restrict__ store, T* __restrict__ x, int64_t ldx) {
   const Place p = place_of(g);
   if (p.piece >= g.total) return;
   float v[8];
   decode<K>(load_codes<K>(store, p.piece), store[g.total * K + (p.piece >> 2)], v);
-  store_piece(x + p.row * ldx + p.c, p.n, v);
+  store_piece<STREAM>(x + p.row * ldx + p.c, p.n, v);
 }
 
 template <int ACT>
@@ -82,7 +82,7 @@ __device__ inline void gate(float g, float& s, float& dq) {
   s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * q));
 }
 
-template <typename T, int ACT, int K>
+template <typename T, int ACT, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void glu_fwd_kernel(Pieces pc, const T* g, int64_t ldg, const T* u, int64_t ldu, T* h, int64_t ldh,
                                                            unsigned char* __restrict__ store_g, unsigned char* __restrict__ store_u) {
   if constexpr (K != 0) {
@@ -92,22 +92,22 @@ __global__ __launch_bounds__(kThreads) void glu_fwd_kernel(Pieces pc, const T* g
   const Place p = place_of(pc);
   if (p.piece >= pc.total) return;
   float a[8], b[8], o[8];
-  load_piece(g + p.row * ldg + p.c, p.n, a);
-  load_piece(u + p.row * ldu + p.c, p.n, b);
+  load_piece<STREAM>(g + p.row * ldg + p.c, p.n, a);
+  load_piece<STREAM>(u + p.row * ldu + p.c, p.n, b);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float s, dq;
     gate<ACT>(a[i], s, dq);
     o[i] = a[i] * s * b[i];
   }
-  store_piece(h + p.row * ldh + p.c, p.n, o);
+  store_piece<STREAM>(h + p.row * ldh + p.c, p.n, o);
   if constexpr (K != 0) {
     keep_piece<K>(store_g, store_g + pc.total * K, p.piece, a);
     keep_piece<K>(store_u, store_u + pc.total * K, p.piece, b);
   }
 }
 
-template <typename T, int ACT, int K>
+template <typename T, int ACT, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void glu_bwd_kernel(Pieces pc, const T* dh, int64_t lddh, const unsigned char* __restrict__ store_g,
                                                            const unsigned char* __restrict__ store_u, T* dg, int64_t lddg, T* du, int64_t lddu,
                                                            unsigned char* __restrict__ store_h) {
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void glu_bwd_kernel(Pieces pc, const T* d
   const Place p = place_of(pc);
   if (p.piece >= pc.total) return;
   float d[8], a[8], b[8], o[8];
-  load_piece(dh + p.row * lddh + p.c, p.n, d);
+  load_piece<STREAM>(dh + p.row * lddh + p.c, p.n, d);
   decode<K>(load_codes<K>(store_g, p.piece), store_g[pc.total * K + (p.piece >> 2)], a);
   decode<K>(load_codes<K>(store_u, p.piece), store_u[pc.total * K + (p.piece >> 2)], b);
   float x[8], y[8];
@@ -128,27 +128,34 @@ __global__ __launch_bounds__(kThreads) void glu_bwd_kernel(Pieces pc, const T* d
     y[i] = d[i] * act;
     o[i] = act * b[i];
   }
-  store_piece(dg + p.row * lddg + p.c, p.n, x);
-  store_piece(du + p.row * lddu + p.c, p.n, y);
+  store_piece<STREAM>(dg + p.row * lddg + p.c, p.n, x);
+  store_piece<STREAM>(du + p.row * lddu + p.c, p.n, y);
   if (store_h != nullptr) keep_piece<8>(store_h, store_h + pc.total * 8, p.piece, o);
 }
 
-// f(type, K) with the dtype and K as types of their own.
+// f(type, STREAM): with the dtype as a type, and whether the pass goes by the caches.
 template <typename F>
-void by_dtype(int dtype, F&& f) {
+void by_dtype(int dtype, int64_t bytes, F&& f) {
+  auto stream = [&](auto t) {
+    if (bytes > kStreamBytes)
+      f(t, std::true_type{});
+    else
+      f(t, std::false_type{});
+  };
   if (dtype == ABL_F32)
-    f(float{});
+    stream(float{});
   else
-    f(bf16_t{});
+    stream(bf16_t{});
 }
 
 }  // namespace
 
 int launch_ckpt_pack(hipStream_t st, int dtype, Rows x, int64_t M, int C, int K, void* ckpt) {
   const Pieces g(M, C);
-  by_dtype(dtype, [&](auto t) {
+  by_dtype(dtype, g.total * (8 * size_of(dtype) + K), [&](auto t, auto s) {
     using T = decltype(t);
-    auto kern = K == 8 ? pack_kernel<T, 8> : pack_kernel<T, 4>;
+    constexpr bool S = decltype(s)::value;
+    auto kern = K == 8 ? pack_kernel<T, 8, S> : pack_kernel<T, 4, S>;
     kern<<<dim3((unsigned)g.grid()), kThreads, 0, st>>>(g, (const T*)x.p, x.ld, (unsigned char*)ckpt);
   });
   return hip_status();
@@ -156,9 +163,10 @@ int launch_ckpt_pack(hipStream_t st, int dtype, Rows x, int64_t M, int C, int K,
 
 int launch_ckpt_unpack(hipStream_t st, int dtype, const void* ckpt, int64_t M, int C, int K, RowsOut x) {
   const Pieces g(M, C);
-  by_dtype(dtype, [&](auto t) {
+  by_dtype(dtype, g.total * (8 * size_of(dtype) + K), [&](auto t, auto s) {
     using T = decltype(t);
-    auto kern = K == 8 ? unpack_kernel<T, 8> : unpack_kernel<T, 4>;
+    constexpr bool S = decltype(s)::value;
+    auto kern = K == 8 ? unpack_kernel<T, 8, S> : unpack_kernel<T, 4, S>;
     kern<<<dim3((unsigned)g.grid()), kThreads, 0, st>>>(g, (const unsigned char*)ckpt, (T*)x.p, x.ld);
   });
   return hip_status();
@@ -167,11 +175,12 @@ int launch_ckpt_unpack(hipStream_t st, int dtype, const void* ckpt, int64_t M, i
 int launch_glu_forward(hipStream_t st, int dtype, int act, Rows g, Rows u, int64_t M, int C, int K, RowsOut h, void* ckpt_g,
                        void* ckpt_u) {
   const Pieces pc(M, C);
-  by_dtype(dtype, [&](auto t) {
+  by_dtype(dtype, pc.total * (3 * 8 * size_of(dtype) + 2 * K), [&](auto t, auto s) {
     using T = decltype(t);
+    constexpr bool S = decltype(s)::value;
     auto pick = [&](auto a) {
       constexpr int A = decltype(a)::value;
-      return K == 0 ? glu_fwd_kernel<T, A, 0> : K == 8 ? glu_fwd_kernel<T, A, 8> : glu_fwd_kernel<T, A, 4>;
+      return K == 0 ? glu_fwd_kernel<T, A, 0, S> : K == 8 ? glu_fwd_kernel<T, A, 8, S> : glu_fwd_kernel<T, A, 4, S>;
     };
     auto kern = act == ABL_ACT_SILU ? pick(std::integral_constant<int, ABL_ACT_SILU>{}) : pick(std::integral_constant<int, ABL_ACT_GELU>{});
     kern<<<dim3((unsigned)pc.grid()), kThreads, 0, st>>>(pc, (const T*)g.p, g.ld, (const T*)u.p, u.ld, (T*)h.p, h.ld,
@@ -183,11 +192,12 @@ int launch_glu_forward(hipStream_t st, int dtype, int act, Rows g, Rows u, int64
 int launch_glu_backward(hipStream_t st, int dtype, int act, Rows dh, const void* ckpt_g, const void* ckpt_u, int64_t M, int C, int K,
                         RowsOut dg, RowsOut du, void* ckpt_h) {
   const Pieces pc(M, C);
-  by_dtype(dtype, [&](auto t) {
+  by_dtype(dtype, pc.total * (3 * 8 * size_of(dtype) + 2 * K), [&](auto t, auto s) {
     using T = decltype(t);
+    constexpr bool S = decltype(s)::value;
     auto pick = [&](auto a) {
       constexpr int A = decltype(a)::value;
-      return K == 8 ? glu_bwd_kernel<T, A, 8> : glu_bwd_kernel<T, A, 4>;
+      return K == 8 ? glu_bwd_kernel<T, A, 8, S> : glu_bwd_kernel<T, A, 4, S>;
     };
     auto kern = act == ABL_ACT_SILU ? pick(std::integral_constant<int, ABL_ACT_SILU>{}) : pick(std::integral_constant<int, ABL_ACT_GELU>{});
     kern<<<dim3((unsigned)pc.grid()), kThreads, 0, st>>>(pc, (const T*)dh.p, dh.ld, (const unsigned char*)ckpt_g,

@@ -11,6 +11,8 @@
 // backward a team takes consecutive rows and keeps its share of the sums over rows in registers as well; the teams' sums are added
 // in a fixed order by a second launch.
 
+#include <utility>
+
 #include "block_store.h"
 
 namespace abl {
@@ -26,50 +28,129 @@ __device__ inline int left(int C, uint32_t c) { return C - (int)c; }
 // this row's stores, and from row to row only three scalar offsets change.  (A store takes the sum of its offsets in a vector register:
 // with the row's in the instruction's scalar operand the compiler lets the next instruction overwrite the store's data, and wrong
 // words have been written here.)
-// Rows of T from `first` on; WHOLE: of a multiple of eight channels.  Others take their last piece in parts (load_raw, store_piece).
-// Piece q of the k-th row; `at`: this lane's byte offset of it in a row (kNowhere beyond the end).
-template <typename T, bool WHOLE>
-struct TeamRows {
-  const T* p;
-  int C;
-  __amdgpu_buffer_rsrc_t d;
-  __device__ inline TeamRows(const void* base, int64_t first, int64_t rows, int c)
-      : p(base != nullptr ? (const T*)base + first * c : nullptr), C(c), d(descriptor(p, rows * c * (int64_t)sizeof(T))) {}
-  static __device__ inline uint32_t offset(uint32_t q, int c) {
-    return q * 8 < (uint32_t)c ? q * 8 * (uint32_t)sizeof(T) : kNowhere;
-  }
-  __device__ inline Raw<T> load(uint32_t k, uint32_t q, uint32_t at) const {
-    if constexpr (!WHOLE) {
-      return p != nullptr ? load_raw(p + (int64_t)k * C + q * 8, left(C, q * 8)) : Raw<T>{};
-    } else {
-      const uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
-      if constexpr (std::is_same_v<T, float>) {
-        Raw<float> r;
-        r.a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, at, row, 0));
-        r.b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, at, row + 16, 0));
-        return r;
-      } else {
-        return Raw<bf16_t>{__builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(d, at, row, 0))};
-      }
-    }
-  }
-  __device__ inline void store(uint32_t k, uint32_t q, uint32_t at, const float (&v)[8]) const {
-    if constexpr (!WHOLE) {
-      if (p != nullptr) store_piece(const_cast<T*>(p) + (int64_t)k * C + q * 8, left(C, q * 8), v);
-    } else {
-      const uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
-      if constexpr (std::is_same_v<T, float>) {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4_any4{v[0], v[1], v[2], v[3]}), d, at + row, 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4_any4{v[4], v[5], v[6], v[7]}), d, at + row + 16, 0, 0);
-      } else {
-        __builtin_amdgcn_raw_buffer_store_b128(u32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])}, d,
-                                               at + row, 0, 0);
+//
+// A row of a multiple of eight channels is whole pieces (kWhole).  Where it is not (kRagged), the lane of the last piece loads the row's last eight
+// channels and shifts them down, so that nothing beyond the row is read, and stores four, two and one of them, as many as there are.
+// Rows of fewer than eight channels (kShort) are taken in parts (load_raw, store_piece).
+// kStream: whole pieces past the caches (kStreamBytes).  8192 x 4096 bf16, K = 8, which moves 338 MB: forward 70 -> 57 us, backward 79 -> 66.
+enum Form { kWhole, kRagged, kShort, kStream };
+
+// Where a lane's piece of a row lies: byte offsets in the row, kNowhere where there is nothing of the kind.
+template <typename T, Form FORM>
+struct Lane {
+  uint32_t q, at;               // piece; whole pieces, and the loads of the last one
+  uint32_t four, two, one, n;   // kRagged: stores of the last piece, its channels (8 for others)
+  __device__ inline Lane(uint32_t piece, int C) : q(piece) {
+    const uint32_t size = sizeof(T), c = piece * 8;
+    const int left = C - (int)c;
+    at = left > 0 ? c * size : kNowhere;
+    four = two = one = kNowhere, n = 8;
+    if constexpr (FORM == kRagged) {
+      if (left > 0 && left < 8) {
+        n = (uint32_t)left;
+        at = (uint32_t)(C - 8) * size;
+        if (n & 4) four = c * size;
+        if (n & 2) two = (c + (n & 4)) * size;
+        if (n & 1) one = (c + (n & 6)) * size;
       }
     }
   }
 };
 
+__device__ inline void shift_down(Raw<bf16_t>& r, uint32_t by) {   // by so many channels, zeros from above
+  u32x4 w = r.a;
+  const uint32_t bits = (by & 1) * 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbit(i < 3 ? w[i + 1] : 0u, w[i], bits);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = by & 2 ? (i < 3 ? w[i + 1] : 0u) : w[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = by & 4 ? (i < 2 ? w[i + 2] : 0u) : w[i];
+  r.a = w;
+}
+__device__ inline void shift_down(Raw<float>& r, uint32_t by) {
+  float w[8];
+  expand(r, w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = by & 4 ? (i < 4 ? w[i + 4] : 0.0f) : w[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = by & 2 ? (i < 6 ? w[i + 2] : 0.0f) : w[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = by & 1 ? (i < 7 ? w[i + 1] : 0.0f) : w[i];
+  r.a = f32x4_any4{w[0], w[1], w[2], w[3]}, r.b = f32x4_any4{w[4], w[5], w[6], w[7]};
+}
+
+// Rows of T from `first` on.
+template <typename T, Form FORM>
+struct TeamRows {
+  const T* p;
+  int C;
+  __amdgpu_buffer_rsrc_t d;
+  static constexpr int kAux = FORM == kStream ? 2 : 0;   // (non-temporal)
+  __device__ inline TeamRows(const void* base, int64_t first, int64_t rows, int c)
+      : p(base != nullptr ? (const T*)base + first * c : nullptr), C(c), d(descriptor(p, rows * c * (int64_t)sizeof(T))) {}
+  // What lies in memory; `unpack` makes the channels of it.
+  template <typename L>
+  __device__ inline Raw<T> load(uint32_t k, const L& l) const {
+    if constexpr (FORM == kShort) {
+      return p != nullptr ? load_raw(p + (int64_t)k * C + l.q * 8, left(C, l.q * 8)) : Raw<T>{};
+    } else {
+      const uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
+      if constexpr (std::is_same_v<T, float>) {
+        Raw<float> r;
+        r.a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row, kAux));
+        r.b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row + 16, kAux));
+        return r;
+      } else {
+        return Raw<bf16_t>{__builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row, kAux))};
+      }
+    }
+  }
+  __device__ inline void store(uint32_t k, const Lane<T, FORM>& l, const float (&v)[8]) const {
+    if constexpr (FORM == kShort) {
+      if (p != nullptr) store_piece(const_cast<T*>(p) + (int64_t)k * C + l.q * 8, left(C, l.q * 8), v);
+    } else {
+      const uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
+      const uint32_t at = (FORM == kRagged && l.n < 8 ? kNowhere : l.at) + row;
+      const bool n4 = l.n & 4, n2 = l.n & 2;
+      if constexpr (std::is_same_v<T, float>) {
+        const u32x4 lo = __builtin_bit_cast(u32x4, f32x4_any4{v[0], v[1], v[2], v[3]});
+        const u32x4 hi = __builtin_bit_cast(u32x4, f32x4_any4{v[4], v[5], v[6], v[7]});
+        __builtin_amdgcn_raw_buffer_store_b128(lo, d, at, 0, kAux);
+        __builtin_amdgcn_raw_buffer_store_b128(hi, d, at + 16, 0, kAux);
+        if constexpr (FORM == kRagged) {
+          __builtin_amdgcn_raw_buffer_store_b128(lo, d, l.four + row, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{n4 ? hi[0] : lo[0], n4 ? hi[1] : lo[1]}, d, l.two + row, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(n4 ? (n2 ? hi[2] : hi[0]) : (n2 ? lo[2] : lo[0]), d, l.one + row, 0, 0);
+        }
+      } else {
+        const u32x4 w{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
+        __builtin_amdgcn_raw_buffer_store_b128(w, d, at, 0, kAux);
+        if constexpr (FORM == kRagged) {
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[0], w[1]}, d, l.four + row, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(n4 ? w[2] : w[0], d, l.two + row, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(n4 ? (n2 ? w[3] : w[2]) : (n2 ? w[1] : w[0])), d, l.one + row, 0, 0);
+        }
+      }
+    }
+  }
+};
+template <typename T, Form FORM>
+__device__ inline void unpack(Raw<T> r, const Lane<T, FORM>& l, float (&v)[8]) {
+  if constexpr (FORM == kRagged) shift_down(r, 8 - l.n);
+  expand(r, v);
+}
+
 // The rows of a store: `pieces` = 4 B of each.
+struct StoreLane {   // byte offsets in a row of a lane's codes (over K) and scale, and of the scale that it writes
+  uint32_t q, scale, own;
+  __device__ inline StoreLane(uint32_t piece, int pieces) {
+    const bool in = piece < (uint32_t)pieces;
+    q = in ? piece : kNowhere / 8;
+    scale = in ? piece >> 2 : kNowhere;
+    own = in && (piece & 3u) == 0 ? piece >> 2 : kNowhere;
+  }
+};
 template <int K>
 struct StoreRows {
   __amdgpu_buffer_rsrc_t codes, scales;
@@ -78,52 +159,65 @@ struct StoreRows {
       : codes(descriptor(store != nullptr ? store + first * n * K : nullptr, rows * n * K)),
         scales(descriptor(store != nullptr ? store + M * n * K + (first * n >> 2) : nullptr, rows * n >> 2)),
         pieces((uint32_t)n) {}
-  __device__ inline void load(uint32_t k, uint32_t q, Codes<K>& c, uint32_t& byte) const {
-    const bool in = q < pieces;
+  static __device__ inline uint32_t at(const StoreLane& l) { return l.q < kNowhere / 8 ? l.q * K : kNowhere; }
+  __device__ inline void load(uint32_t k, const StoreLane& l, Codes<K>& c, uint32_t& byte) const {
     if constexpr (K == 8)
-      c.w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, in ? q * 8 : kNowhere, k * pieces * 8, 0));
+      c.w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at(l), k * pieces * 8, 0));
     else
-      c.w = __builtin_amdgcn_raw_buffer_load_b32(codes, in ? q * 4 : kNowhere, k * pieces * 4, 0);
-    byte = __builtin_amdgcn_raw_buffer_load_b8(scales, in ? q >> 2 : kNowhere, k * (pieces >> 2), 0);
+      c.w = __builtin_amdgcn_raw_buffer_load_b32(codes, at(l), k * pieces * 4, 0);
+    byte = __builtin_amdgcn_raw_buffer_load_b8(scales, l.scale, k * (pieces >> 2), 0);
   }
-  __device__ inline void keep(uint32_t k, uint32_t q, const float (&v)[8]) const {
-    const bool in = q < pieces;
+  __device__ inline void keep(uint32_t k, const StoreLane& l, const float (&v)[8]) const {
     const uint32_t byte = scale_byte<K>(v);
     const Codes<K> c = encode<K>(v, byte);
     if constexpr (K == 8)
-      __builtin_amdgcn_raw_buffer_store_b64(c.w, codes, (in ? q * 8 : kNowhere) + k * pieces * 8, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b64(c.w, codes, at(l) + k * pieces * 8, 0, 0);
     else
-      __builtin_amdgcn_raw_buffer_store_b32(c.w, codes, (in ? q * 4 : kNowhere) + k * pieces * 4, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b8((unsigned char)byte, scales, (in && (q & 3u) == 0 ? q >> 2 : kNowhere) + k * (pieces >> 2), 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(c.w, codes, at(l) + k * pieces * 4, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b8((unsigned char)byte, scales, l.own + k * (pieces >> 2), 0, 0);
   }
 };
 
-// A vector over the channels, for all rows: ones where there is none.
-template <typename T, bool WHOLE>
-__device__ inline Raw<T> load_weights(const void* w, int64_t row, int C, uint32_t q) {
-  if (w != nullptr) return TeamRows<T, WHOLE>(w, row, 1, C).load(0, q, TeamRows<T, WHOLE>::offset(q, C));
+// A vector over the channels (a row of the gate): ones where there is none, zeros beyond the channels.  Shifted already where that is needed.
+template <typename T, Form FORM>
+__device__ inline Raw<T> load_weights(const void* w, int64_t row, int C, const Lane<T, FORM>& l) {
   Raw<T> r;
-  if constexpr (std::is_same_v<T, float>)
+  if (w != nullptr) {
+    r = TeamRows<T, FORM == kStream ? kWhole : FORM>(w, row, 1, C).load(0, l);   // (all rows read it: through the caches)
+    if constexpr (FORM == kRagged) shift_down(r, 8 - l.n);
+  } else if constexpr (std::is_same_v<T, float>) {
     r.a = r.b = f32x4_any4{1.0f, 1.0f, 1.0f, 1.0f};
-  else
+  } else {
     r.a = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+  }
   return r;
 }
 
+template <typename T, Form FORM, int NV>
+struct Lanes {
+  Lane<T, FORM> l[NV];
+  StoreLane s[NV];
+};
+template <typename T, Form FORM, int TEAM, int... I>
+__device__ inline Lanes<T, FORM, sizeof...(I)> lanes(uint32_t t, int C, int pieces, std::integer_sequence<int, I...>) {
+  return {{Lane<T, FORM>(t + TEAM * I, C)...}, {StoreLane(t + TEAM * I, pieces)...}};
+}
+
 // ---- a team's sums over a row ----
-template <int TEAM>
+// S: of the sums over the waves; a lane's and a row of 16 lanes' are in fp32.
+template <int TEAM, typename S>
 struct TeamSum {
-  float* slots;   // [2][TEAM / 64], used in turn: the barrier of one sum keeps the next from overwriting what is still read
+  S* slots;   // [2][TEAM / 64], used in turn: the barrier of one sum keeps the next from overwriting what is still read
   int turn = 0;
-  __device__ explicit TeamSum(float* s) : slots(s) {}
-  __device__ inline float operator()(float v) {
-    v = wave_sum(v);
+  __device__ explicit TeamSum(S* s) : slots(s) {}
+  __device__ inline S operator()(float w) {
+    S v = wave_sum<S>(w);
     if constexpr (TEAM > 64) {
-      float* s = slots + turn * (TEAM / 64);
+      S* s = slots + turn * (TEAM / 64);
       turn ^= 1;
       if ((threadIdx.x & 63u) == 0) s[threadIdx.x >> 6] = v;
       __syncthreads();
-      v = 0.0f;
+      v = 0;
 #pragma unroll
       for (int i = 0; i < TEAM / 64; ++i) v += s[i];
     }
@@ -140,7 +234,8 @@ struct FwdArgs {
   int64_t rows;    // of a team
   int C, pieces;   // pieces of a row
   int center;
-  float alpha, beta, eps, inv_c;
+  float alpha, beta, eps;
+  double inv_c;
 };
 
 __device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
@@ -150,15 +245,18 @@ __device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
 }
 
 // v <- N(v); returns 1 / sqrt(mean square + eps).  Channels that do not exist hold zeros and stay zero.
+// A normalized value should be off by its own rounding only: the rounding of the factor, common to a row, would shift all values that lie near the
+// middle of two codes to one side.  So the sums over waves, the mean and a Newton step on the instruction's root are in 64 bits, and the
+// factor is applied as a float and what it lacks.
 template <int TEAM, int NV>
-__device__ inline float normalize(float (&v)[NV][8], const FwdArgs& a, TeamSum<TEAM>& sum, uint32_t t) {
+__device__ inline float normalize(float (&v)[NV][8], const FwdArgs& a, TeamSum<TEAM, double>& sum, uint32_t t) {
   if (a.center) {
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) m += v[i][j];
-    m = sum(m) * a.inv_c;
+    m = (float)(sum(m) * a.inv_c);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -170,12 +268,15 @@ __device__ inline float normalize(float (&v)[NV][8], const FwdArgs& a, TeamSum<T
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = __builtin_fmaf(v[i][j], v[i][j], s);
-  const float rstd = 1.0f / sqrtf(__builtin_fmaf(sum(s), a.inv_c, a.eps));
+  const double x = __builtin_fma(sum(s), a.inv_c, (double)a.eps);
+  const float root = __builtin_amdgcn_rsqf((float)x);
+  const double e = __builtin_fma(-x * root, root, 1.0);
+  const float more = finite((float)x) ? (float)(0.5 * root * e) : 0.0f;   // (an infinite or NaN sum: zero or NaN)
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] *= rstd;
-  return rstd;
+    for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(v[i][j], root, v[i][j] * more);
+  return root + more;
 }
 
 // Blocks of teams of 64 hold four of them.
@@ -188,10 +289,10 @@ __device__ inline int64_t team_index() {
 
 // A team takes consecutive rows and asks for the next one's elements before it works on this one's: the sums over a row are two
 // waits for all waves of the team, during which nothing else would be on its way.
-template <typename T, int K, bool WHOLE, int TEAM, int NV>
-__global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
-  __shared__ float slots[2 * (TEAM / 64)];
-  TeamSum<TEAM> sum(slots);
+template <typename T, int K, Form FORM, int TEAM, int NV>
+__global__ __launch_bounds__(kBlock<TEAM>, NV >= 2 ? 2 : 4) void resnorm_fwd_kernel(FwdArgs a) {
+  __shared__ double slots[2 * (TEAM / 64)];
+  TeamSum<TEAM, double> sum(slots);
   const uint32_t t = threadIdx.x % TEAM;
   if (K != 0 && blockIdx.x == 0) {
     zero_tail(a.ckpt_n, a.M * a.pieces, K);
@@ -200,29 +301,27 @@ __global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
   const int64_t first = team_index<TEAM>() * a.rows;
   if (first >= a.M) return;   // (a whole wave; blocks of larger teams are as many as teams)
   const uint32_t rows = (uint32_t)(first + a.rows < a.M ? a.rows : a.M - first);
-  using In = TeamRows<T, WHOLE>;
+  using In = TeamRows<T, FORM>;
   const In from_r(a.r, first, rows, a.C), from_b(a.b, first, rows, a.C), to_r(a.r_out, first, rows, a.C), to_n(a.n, first, rows, a.C);
   const StoreRows<K == 0 ? 8 : K> keep_b(K != 0 ? a.ckpt_b : nullptr, a.M, a.pieces, first, rows);
   const StoreRows<K == 0 ? 8 : K> keep_n(K != 0 ? a.ckpt_n : nullptr, a.M, a.pieces, first, rows);
-  uint32_t at[NV];
+  const auto lane = lanes<T, FORM, TEAM>(t, a.C, a.pieces, std::make_integer_sequence<int, NV>{});
   Raw<T> r[NV], b[NV], w_post[NV], w_pre[NV], gate[NV];
   auto fetch = [&](uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      r[i] = from_r.load(k, t + TEAM * i, at[i]);
-      b[i] = from_b.load(k, t + TEAM * i, at[i]);
+      r[i] = from_r.load(k, lane.l[i]);
+      b[i] = from_b.load(k, lane.l[i]);
     }
   };
   int64_t group = a.gate != nullptr ? first / a.gate_rows : 0;
   int64_t group_end = a.gate != nullptr ? (group + 1) * a.gate_rows : a.M;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) at[i] = In::offset(t + TEAM * i, a.C);
   fetch(0);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    w_pre[i] = load_weights<T, WHOLE>(a.w_pre, 0, a.C, t + TEAM * i);
-    w_post[i] = load_weights<T, WHOLE>(a.w_post, 0, a.C, t + TEAM * i);
-    gate[i] = load_weights<T, WHOLE>(a.gate, group, a.C, t + TEAM * i);
+    w_pre[i] = load_weights<T, FORM>(a.w_pre, 0, a.C, lane.l[i]);
+    w_post[i] = load_weights<T, FORM>(a.w_post, 0, a.C, lane.l[i]);
+    gate[i] = load_weights<T, FORM>(a.gate, group, a.C, lane.l[i]);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) settle(w_pre[i]), settle(w_post[i]), settle(gate[i]);
@@ -230,8 +329,8 @@ __global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
     float v[NV][8], x[NV][8], w[8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      expand(r[i], x[i]);
-      expand(b[i], v[i]);
+      unpack(r[i], lane.l[i], x[i]);
+      unpack(b[i], lane.l[i], v[i]);
     }
     if (k + 1 < rows) fetch(k + 1);
     if (a.w_post != nullptr) {
@@ -240,7 +339,7 @@ __global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
     }
     if constexpr (K != 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) keep_b.keep(k, t + TEAM * i, v[i]);
+      for (int i = 0; i < NV; ++i) keep_b.keep(k, lane.s[i], v[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -250,13 +349,13 @@ __global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
       expand(gate[i], w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = a.alpha * x[i][j] + a.beta * (v[i][j] * w[j]);   // (v is zero where there is no b)
-      to_r.store(k, t + TEAM * i, at[i], v[i]);
+      to_r.store(k, lane.l[i], v[i]);
     }
     if (first + k + 1 == group_end && k + 1 < rows) {   // the next row has the next gate
       ++group;
       group_end += a.gate_rows;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) gate[i] = load_weights<T, WHOLE>(a.gate, group, a.C, t + TEAM * i);
+      for (int i = 0; i < NV; ++i) gate[i] = load_weights<T, FORM>(a.gate, group, a.C, lane.l[i]);
 #pragma unroll
       for (int i = 0; i < NV; ++i) settle(gate[i]);
     }
@@ -264,14 +363,14 @@ __global__ __launch_bounds__(kBlock<TEAM>) void resnorm_fwd_kernel(FwdArgs a) {
     if constexpr (K != 0) {
       if (t == 0) a.rstd_n[first + k] = rstd;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) keep_n.keep(k, t + TEAM * i, v[i]);
+      for (int i = 0; i < NV; ++i) keep_n.keep(k, lane.s[i], v[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       expand(w_pre[i], w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] *= v[i][j];
-      to_n.store(k, t + TEAM * i, at[i], w);
+      to_n.store(k, lane.l[i], w);
     }
   }
 }
@@ -288,17 +387,17 @@ struct Shares {
 constexpr int64_t kFwdThreads = 256 * 1024, kBwdThreads = 256 * 1024;   // of a launch at most (256 compute units)
 Shares shares_of(int64_t M, int64_t gate_rows, int team, bool gate) {
   const int64_t most = kBwdThreads / team;   // up to twice as many where groups are cut
+  const int64_t block = team == 64 ? 4 : 1;   // teams of a block: of one group, where a group is cut
   Shares s;
   s.rows = (M + most - 1) / most;
   if (gate && gate_rows <= s.rows) {
     s.rows = (s.rows + gate_rows - 1) / gate_rows * gate_rows;
-  } else if (gate && gate_rows < M) {
-    s.per_group = (gate_rows + s.rows - 1) / s.rows;
-    s.rows = (gate_rows + s.per_group - 1) / s.per_group;
-    s.teams = (M + gate_rows - 1) / gate_rows * s.per_group;
+  } else if (gate) {
+    const int64_t group = gate_rows < M ? gate_rows : M;
+    s.per_group = ((group + s.rows - 1) / s.rows + block - 1) / block * block;
+    s.rows = (group + s.per_group - 1) / s.per_group;
+    s.teams = (M + group - 1) / group * s.per_group;
     return s;
-  } else if (gate) {   // one group
-    s.per_group = (M + s.rows - 1) / s.rows;
   }
   s.teams = (M + s.rows - 1) / s.rows;
   return s;
@@ -317,9 +416,9 @@ struct BwdArgs {
   float alpha, beta, inv_c;
 };
 
-// v <- rstd (v - y mean(v y)) (less the mean of v where the norm took the mean out)
-template <int TEAM, int NV>
-__device__ inline void norm_gradient(float (&v)[NV][8], const float (&y)[NV][8], float rstd, const BwdArgs& a, TeamSum<TEAM>& sum) {
+// v <- rstd (v - y mean(v y)) + more (less rstd times the mean of v where the norm took the mean out)
+template <int TEAM, int NV, typename More>
+__device__ inline void norm_gradient(float (&v)[NV][8], const float (&y)[NV][8], float rstd, const BwdArgs& a, TeamSum<TEAM, float>& sum, More&& more) {
   float s = 0.0f, m = 0.0f;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -333,10 +432,20 @@ __device__ inline void norm_gradient(float (&v)[NV][8], const float (&y)[NV][8],
       for (int j = 0; j < 8; ++j) m += v[i][j];
     m = sum(m) * a.inv_c;
   }
+  const float rs = -rstd * s;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    float t[8];
+    more(i, t);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = rstd * (v[i][j] - m - y[i][j] * s);
+    for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(rstd, v[i][j], __builtin_fmaf(rs, y[i][j], t[j]));
+  }
+  if (a.center) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(-rstd, m, v[i][j]);
+  }
 }
 
 // What a thread reads of a row.
@@ -349,13 +458,14 @@ struct RowIn {
 };
 
 // As in the forward, the next row's elements are asked for before this one's are worked on.
-template <typename T, int K, bool WHOLE, int TEAM, int NV>
-__global__ __launch_bounds__(kBlock<TEAM>, 4) void resnorm_bwd_kernel(BwdArgs a) {
+template <typename T, int K, Form FORM, int TEAM, int NV>
+__global__ __launch_bounds__(kBlock<TEAM>, NV == 1 ? 4 : 2) void resnorm_bwd_kernel(BwdArgs a) {
+  constexpr bool kHold = NV < 4;   // registers for the weights and for the next row; rows of four pieces a thread read the weights again
   __shared__ float slots[2 * (TEAM / 64)];
-  TeamSum<TEAM> sum(slots);
+  TeamSum<TEAM, float> sum(slots);
   const uint32_t t = threadIdx.x % TEAM;
   const int64_t team = team_index<TEAM>();
-  if (team >= a.share.teams) return;
+  if (TEAM > 64 && team >= a.share.teams) return;   // (teams of a wave meet at the end)
   int64_t row, end;
   if (a.share.per_group > 0) {
     const int64_t group = team / a.share.per_group, last = (group + 1) * a.gate_rows;
@@ -366,123 +476,176 @@ __global__ __launch_bounds__(kBlock<TEAM>, 4) void resnorm_bwd_kernel(BwdArgs a)
     end = row + a.share.rows;
   }
   end = end < a.M ? end : a.M;
+  if (team >= a.share.teams) end = row;
 
   const int64_t first = row;
   const uint32_t rows = row < end ? (uint32_t)(end - row) : 0;
-  using In = TeamRows<T, WHOLE>;
+  using In = TeamRows<T, FORM>;
   const In from_dn(a.dn, first, rows, a.C), from_dr(a.dr_out, first, rows, a.C), to_r(a.dr, first, rows, a.C), to_b(a.db, first, rows, a.C);
   const StoreRows<K> kept_n(a.ckpt_n, a.M, a.pieces, first, rows), kept_b(a.ckpt_b, a.M, a.pieces, first, rows);
-  uint32_t at[NV];
+  const auto lane = lanes<T, FORM, TEAM>(t, a.C, a.pieces, std::make_integer_sequence<int, NV>{});
   RowIn<T, K, NV> in;
   auto fetch = [&](uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const uint32_t q = t + TEAM * i;
-      in.dn[i] = from_dn.load(k, q, at[i]);
-      in.dr[i] = from_dr.load(k, q, at[i]);
-      kept_n.load(k, q, in.z[i], in.sz[i]);
-      kept_b.load(k, q, in.y[i], in.sy[i]);
+      in.dn[i] = from_dn.load(k, lane.l[i]);
+      in.dr[i] = from_dr.load(k, lane.l[i]);
+      kept_n.load(k, lane.s[i], in.z[i], in.sz[i]);
+      kept_b.load(k, lane.s[i], in.y[i], in.sy[i]);
     }
     in.rstd_n = a.rstd_n[first + k];
     in.rstd_b = a.w_post != nullptr ? a.rstd_b[first + k] : 0.0f;
   };
-  float pre[NV][8] = {}, post[NV][8] = {}, gsum[NV][8] = {};
-  Raw<T> w_pre[NV], w_post[NV], gate[NV];
+  float pre[NV][8] = {}, post[NV][8] = {}, both[NV][8] = {};   // sums of dn z; of e gate y; of D y over the rows of a group
+  Raw<T> w_pre[kHold ? NV : 1], w_post[kHold ? NV : 1], gate[kHold ? NV : 1];
+  auto weights = [&](const Raw<T>* held, const void* from, int64_t row, int i, float (&w)[8]) __attribute__((always_inline)) {
+    if constexpr (kHold)
+      expand(held[i], w);
+    else
+      expand(load_weights<T, FORM>(from, row, a.C, lane.l[i]), w);
+  };
   const bool flush = a.gate != nullptr && a.share.per_group == 0;
   int64_t group = a.gate != nullptr ? row / a.gate_rows : 0;
   int64_t group_end = flush ? (group + 1) * a.gate_rows : a.M;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) at[i] = In::offset(t + TEAM * i, a.C);
-  if (rows > 0) {
+  if (kHold && rows > 0) {
     fetch(0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      w_pre[i] = load_weights<T, WHOLE>(a.w_pre, 0, a.C, t + TEAM * i);
-      w_post[i] = load_weights<T, WHOLE>(a.w_post, 0, a.C, t + TEAM * i);
-      gate[i] = load_weights<T, WHOLE>(a.gate, group, a.C, t + TEAM * i);
+    for (int i = 0; i < (kHold ? NV : 0); ++i) {
+      w_pre[i] = load_weights<T, FORM>(a.w_pre, 0, a.C, lane.l[i]);
+      w_post[i] = load_weights<T, FORM>(a.w_post, 0, a.C, lane.l[i]);
+      gate[i] = load_weights<T, FORM>(a.gate, group, a.C, lane.l[i]);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) settle(w_pre[i]), settle(w_post[i]), settle(gate[i]);
+    for (int i = 0; i < (kHold ? NV : 0); ++i) settle(w_pre[i]), settle(w_post[i]), settle(gate[i]);
   }
   for (uint32_t k = 0; k < rows; ++k) {
     float v[NV][8], y[NV][8], w[8], g[8];
+    if (!kHold) fetch(k);
     const RowIn<T, K, NV> now = in;
-    if (k + 1 < rows) fetch(k + 1);
+    if (kHold && k + 1 < rows) fetch(k + 1);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       decode<K>(now.z[i], now.sz[i], y[i]);
-      expand(now.dn[i], v[i]);
-      expand(w_pre[i], w);
+      unpack(now.dn[i], lane.l[i], v[i]);
+      weights(w_pre, a.w_pre, 0, i, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         pre[i][j] = __builtin_fmaf(v[i][j], y[i][j], pre[i][j]);
         v[i][j] *= w[j];
       }
     }
-    norm_gradient<TEAM, NV>(v, y, now.rstd_n, a, sum);
+    norm_gradient<TEAM, NV>(v, y, now.rstd_n, a, sum, [&](int i, float (&t)[8]) __attribute__((always_inline)) { unpack(now.dr[i], lane.l[i], t); });
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      expand(now.dr[i], w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] += w[j];
+    for (int i = 0; i < NV; ++i) {   // v is D
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = a.alpha * v[i][j];
-      to_r.store(k, t + TEAM * i, at[i], w);
+      to_r.store(k, lane.l[i], w);
       decode<K>(now.y[i], now.sy[i], y[i]);   // (zeros where nothing is kept of b)
-      expand(w_post[i], w);
-      expand(gate[i], g);
+      weights(w_post, a.w_post, 0, i, w);
+      weights(gate, a.gate, group, i, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float e = a.beta * v[i][j], ey = e * y[i][j];
-        gsum[i][j] = __builtin_fmaf(ey, w[j], gsum[i][j]);
-        post[i][j] = __builtin_fmaf(ey, g[j], post[i][j]);
-        v[i][j] = e * g[j] * w[j];
+        both[i][j] = __builtin_fmaf(v[i][j], y[i][j], both[i][j]);
+        v[i][j] *= g[j] * w[j];
       }
     }
-    if (a.w_post != nullptr) norm_gradient<TEAM, NV>(v, y, now.rstd_b, a, sum);
+    if (a.w_post != nullptr) {
+      norm_gradient<TEAM, NV>(v, y, a.beta * now.rstd_b, a, sum, [&](int, float (&t)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) to_b.store(k, t + TEAM * i, at[i], v[i]);
+        for (int j = 0; j < 8; ++j) t[j] = 0.0f;
+      });
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= a.beta;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) to_b.store(k, lane.l[i], v[i]);
     if (flush && (first + k + 1 == group_end || k + 1 == rows)) {   // (a team's last row ends a group)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const uint32_t c = (t + TEAM * i) * 8;
-        store_piece(a.dgate + group * a.C + c, left(a.C, c), gsum[i]);
+        weights(w_post, a.w_post, 0, i, w);
+        weights(gate, a.gate, group, i, g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gsum[i][j] = 0.0f;
+        for (int j = 0; j < 8; ++j) {
+          const float e = a.beta * both[i][j];
+          post[i][j] = __builtin_fmaf(e, g[j], post[i][j]);
+          w[j] *= e;
+          both[i][j] = 0.0f;
+        }
+        store_piece(a.dgate + group * a.C + c, left(a.C, c), w);
       }
       ++group;
       group_end += a.gate_rows;
-      if (k + 1 < rows) {
+      if (kHold && k + 1 < rows) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) gate[i] = load_weights<T, WHOLE>(a.gate, group, a.C, t + TEAM * i);
+        for (int i = 0; i < (kHold ? NV : 0); ++i) gate[i] = load_weights<T, FORM>(a.gate, group, a.C, lane.l[i]);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) settle(gate[i]);
+        for (int i = 0; i < (kHold ? NV : 0); ++i) settle(gate[i]);
       }
     }
   }
-  const int64_t width = (int64_t)a.pieces * 8, plane = a.share.teams * width;
+  if (!flush) {   // one row of the gate, or none: both sums are multiples of one
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const uint32_t q = t + TEAM * i;
-    if (q >= (uint32_t)a.pieces) continue;
-    float* to = a.part + team * width + q * 8;
-    store_piece(to, 8, pre[i]);
-    if (a.w_post != nullptr) store_piece(to + plane, 8, post[i]);
-    if (a.share.per_group > 0) store_piece(to + 2 * plane, 8, gsum[i]);
+    for (int i = 0; i < NV; ++i) {
+      float w[8] = {}, g[8] = {};
+      if (rows > 0) {
+        weights(w_post, a.w_post, 0, i, w);
+        weights(gate, a.gate, group, i, g);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e = a.beta * both[i][j];
+        post[i][j] = e * g[j];
+        both[i][j] = e * w[j];
+      }
+    }
+  }
+  // The shares' sums, one for a block: the four teams of a wave each are added in LDS, one plane after the other.
+  const int64_t width = (int64_t)a.pieces * 8, plane = (int64_t)gridDim.x * width;
+  if constexpr (TEAM == 64) {
+    static_assert(NV == 1, "teams of a wave have a piece a lane");
+    __shared__ float parts[3][64][8];
+    const int wave = threadIdx.x / 64;
+    auto add = [&](float (&v)[8], int which) __attribute__((always_inline)) {
+      if (wave > 0) store_piece(parts[wave - 1][t], 8, v);
+      __syncthreads();
+      if (wave == 0 && t < (uint32_t)a.pieces) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (v[j] + parts[0][t][j]) + (parts[1][t][j] + parts[2][t][j]);
+        store_piece(a.part + which * plane + (int64_t)blockIdx.x * width + t * 8, 8, v);
+      }
+      __syncthreads();
+    };
+    add(pre[0], 0);
+    if (a.w_post != nullptr) add(post[0], 1);
+    if (a.share.per_group > 0) add(both[0], 2);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t q = t + TEAM * i;
+      if (q >= (uint32_t)a.pieces) continue;
+      float* to = a.part + team * width + q * 8;
+      store_piece(to, 8, pre[i]);
+      if (a.w_post != nullptr) store_piece(to + plane, 8, post[i]);
+      if (a.share.per_group > 0) store_piece(to + 2 * plane, 8, both[i]);
+    }
   }
 }
 
 // The teams' sums: blockIdx.y = 0 dw_pre, 1 dw_post, 2 + g row g of dgate.  32 channels a block; thread (s, l) adds every 64th share
 // of four channels, eight of them on their way at a time, then the 64 sums are added in turn.
 constexpr int kSumRows = 64;
-__global__ __launch_bounds__(8 * kSumRows) void resnorm_sum_kernel(const float* part, Shares share, int pieces, int C, float* dw_pre,
+__global__ __launch_bounds__(8 * kSumRows) void resnorm_sum_kernel(const float* part, int64_t shares, int64_t per_group, int pieces, int C, float* dw_pre,
                                                                    float* dw_post, float* dgate) {
   __shared__ float4 sums[kSumRows][8];
   const int job = blockIdx.y, l = threadIdx.x & 7, s = threadIdx.x >> 3;
   float* out = job == 0 ? dw_pre : job == 1 ? dw_post : dgate + (int64_t)(job - 2) * C;
   if (out == nullptr) return;
-  const int64_t width = (int64_t)pieces * 8, plane = share.teams * width;
-  const int64_t first = job < 2 ? 0 : (job - 2) * share.per_group, last = job < 2 ? share.teams : first + share.per_group;
+  const int64_t width = (int64_t)pieces * 8, plane = shares * width;
+  const int64_t first = job < 2 ? 0 : (job - 2) * per_group, last = job < 2 ? shares : first + per_group;
   const float* from = part + (job < 2 ? job : 2) * plane + (int64_t)blockIdx.x * 32 + l * 4;
   float4 a{0.0f, 0.0f, 0.0f, 0.0f};
   for (int64_t i = first + s; i < last; i += 8 * kSumRows) {
@@ -510,25 +673,37 @@ __global__ __launch_bounds__(256) void zero_kernel(float* p, int64_t n) {
   if (i < n) p[i] = 0.0f;
 }
 
-// Threads of a team for rows of so many pieces: a piece for each; above 1024 two.
+// Threads of a team for rows of so many pieces: a piece for each up to 512 threads, then two and four (a block of 1024 threads has too few
+// registers for the backward: 4096 x 8192 bf16 took 162 us).
 int team_of(int pieces) {
   int t = 64;
-  while (t < pieces && t < 1024) t *= 2;
+  while (t < pieces && t < 512) t *= 2;
   return t;
 }
 
-// f(TEAM, NV) as constants.
+// f(TEAM, NV, FORM) as constants.
 template <typename F>
-void by_team(int pieces, F&& f) {
+void by_team(int C, int64_t bytes, F&& f) {
+  const int pieces = (int)store_blocks(C) * 4;
+  auto form = [&](auto team, auto nv) {
+    if constexpr (decltype(team)::value >= 256) {
+      if (C % 8 == 0 && bytes > kStreamBytes) return f(team, nv, std::integral_constant<Form, kStream>{});
+    }
+    if (C % 8 == 0) return f(team, nv, std::integral_constant<Form, kWhole>{});
+    return f(team, nv, std::integral_constant<Form, kRagged>{});
+  };
   const std::integral_constant<int, 1> one;
+  if (C < 8) return f(std::integral_constant<int, 64>{}, one, std::integral_constant<Form, kShort>{});
   switch (team_of(pieces)) {
-    case 64: return f(std::integral_constant<int, 64>{}, one);
-    case 128: return f(std::integral_constant<int, 128>{}, one);
-    case 256: return f(std::integral_constant<int, 256>{}, one);
-    case 512: return f(std::integral_constant<int, 512>{}, one);
-    default:
-      if (pieces <= 1024) return f(std::integral_constant<int, 1024>{}, one);
-      return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+    case 64: return form(std::integral_constant<int, 64>{}, one);
+    case 128: return form(std::integral_constant<int, 128>{}, one);
+    case 256: return form(std::integral_constant<int, 256>{}, one);
+    default: {
+      const std::integral_constant<int, 512> team;
+      if (pieces <= 512) return form(team, one);
+      if (pieces <= 1024) return form(team, std::integral_constant<int, 2>{});
+      return form(team, std::integral_constant<int, 4>{});
+    }
   }
 }
 
@@ -540,22 +715,20 @@ int launch_resnorm_forward(hipStream_t st, const abl_resnorm& s, const void* r, 
   a.M = s.M, a.gate_rows = s.gate_rows, a.r = r, a.b = b, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
   a.r_out = r_out, a.n = n, a.ckpt_b = (unsigned char*)ckpt_b, a.ckpt_n = (unsigned char*)ckpt_n;
   a.rstd_b = rstd_b, a.rstd_n = rstd_n, a.C = s.C, a.pieces = (int)store_blocks(s.C) * 4;
-  a.center = (s.flags & ABL_NORM_CENTER) != 0, a.alpha = s.alpha, a.beta = s.beta, a.eps = s.eps, a.inv_c = 1.0f / (float)s.C;
-  by_team(a.pieces, [&](auto t, auto nv) {
+  a.center = (s.flags & ABL_NORM_CENTER) != 0, a.alpha = s.alpha, a.beta = s.beta, a.eps = s.eps, a.inv_c = 1.0 / s.C;
+  const int64_t bytes = s.M * s.C * (4 * size_of(s.dtype) + 2 * s.K / 8);
+  by_team(s.C, bytes, [&](auto t, auto nv, auto form) {
     constexpr int TEAM = decltype(t)::value, NV = decltype(nv)::value;
+    constexpr Form FORM = decltype(form)::value;
     const int64_t most = kFwdThreads / TEAM;
     a.rows = (s.M + most - 1) / most;
     const int64_t teams = (s.M + a.rows - 1) / a.rows;
     const unsigned grid = (unsigned)(TEAM == 64 ? (teams + 3) / 4 : teams);
     auto pick = [&](auto e) {
       using T = decltype(e);
-      if (s.C % 8 == 0)
-        return s.K == 0   ? resnorm_fwd_kernel<T, 0, true, TEAM, NV>
-               : s.K == 8 ? resnorm_fwd_kernel<T, 8, true, TEAM, NV>
-                          : resnorm_fwd_kernel<T, 4, true, TEAM, NV>;
-      return s.K == 0   ? resnorm_fwd_kernel<T, 0, false, TEAM, NV>
-             : s.K == 8 ? resnorm_fwd_kernel<T, 8, false, TEAM, NV>
-                        : resnorm_fwd_kernel<T, 4, false, TEAM, NV>;
+      return s.K == 0   ? resnorm_fwd_kernel<T, 0, FORM, TEAM, NV>
+             : s.K == 8 ? resnorm_fwd_kernel<T, 8, FORM, TEAM, NV>
+                        : resnorm_fwd_kernel<T, 4, FORM, TEAM, NV>;
     };
     auto kern = s.dtype == ABL_F32 ? pick(float{}) : pick(bf16_t{});
     kern<<<grid, kBlock<TEAM>, 0, st>>>(a);
@@ -565,9 +738,12 @@ int launch_resnorm_forward(hipStream_t st, const abl_resnorm& s, const void* r, 
 
 size_t resnorm_scratch_bytes(int64_t M, int C) {
   const int pieces = (int)store_blocks(C) * 4;
-  // the shares of the smallest rows, and twice as many where groups of the gate are cut
-  const Shares s = shares_of(M, 0, team_of(pieces), false);
-  return (size_t)(2 * s.teams + 1) * 3 * pieces * 8 * sizeof(float);
+  // The blocks without a gate, and where groups of rows are cut: a group of g rows takes at most g / rows + 1 teams, or a block more where a block
+  // has four, and there are M / g + 1 groups of more than `rows` rows, so at most M / rows + M / g + g / rows + ... <= 2 M / rows + 2 blocks' worth.
+  const int team = team_of(pieces);
+  const Shares s = shares_of(M, 0, team, false);
+  const int64_t blocks = 2 * s.teams + 2;
+  return (size_t)blocks * 3 * pieces * 8 * sizeof(float);
 }
 
 int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, bool has_b, const void* dn, const void* dr_out, const void* gate,
@@ -586,20 +762,22 @@ int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, bool has_b, co
   a.C = s.C, a.pieces = (int)store_blocks(s.C) * 4, a.center = (s.flags & ABL_NORM_CENTER) != 0;
   a.alpha = s.alpha, a.beta = s.beta, a.inv_c = 1.0f / (float)s.C;
   a.share = shares_of(s.M, s.gate_rows, team_of(a.pieces), gate != nullptr);
-  by_team(a.pieces, [&](auto t, auto nv) {
+  const int64_t bytes = s.M * s.C * (4 * size_of(s.dtype) + 2 * s.K / 8);
+  by_team(s.C, bytes, [&](auto t, auto nv, auto form) {
     constexpr int TEAM = decltype(t)::value, NV = decltype(nv)::value;
+    constexpr Form FORM = decltype(form)::value;
     const unsigned grid = (unsigned)(TEAM == 64 ? (a.share.teams + 3) / 4 : a.share.teams);
     auto pick = [&](auto e) {
       using T = decltype(e);
-      if (s.C % 8 == 0) return s.K == 8 ? resnorm_bwd_kernel<T, 8, true, TEAM, NV> : resnorm_bwd_kernel<T, 4, true, TEAM, NV>;
-      return s.K == 8 ? resnorm_bwd_kernel<T, 8, false, TEAM, NV> : resnorm_bwd_kernel<T, 4, false, TEAM, NV>;
+      return s.K == 8 ? resnorm_bwd_kernel<T, 8, FORM, TEAM, NV> : resnorm_bwd_kernel<T, 4, FORM, TEAM, NV>;
     };
     auto kern = s.dtype == ABL_F32 ? pick(float{}) : pick(bf16_t{});
     kern<<<grid, kBlock<TEAM>, 0, st>>>(a);
   });
   if (int e = hip_status()) return e;
+  const int64_t a_block = team_of(a.pieces) == 64 ? 4 : 1, blocks = (a.share.teams + a_block - 1) / a_block;   // teams of a block
   const unsigned jobs = 2 + (gate != nullptr && a.share.per_group > 0 ? (unsigned)groups : 0);
-  resnorm_sum_kernel<<<dim3((unsigned)((s.C + 31) / 32), jobs), 8 * kSumRows, 0, st>>>(a.part, a.share, a.pieces, s.C, dw_pre, dw_post, dgate);
+  resnorm_sum_kernel<<<dim3((unsigned)((s.C + 31) / 32), jobs), 8 * kSumRows, 0, st>>>(a.part, blocks, a.share.per_group / a_block, a.pieces, s.C, dw_pre, dw_post, dgate);
   return hip_status();
 }
 

@@ -11,7 +11,6 @@ constexpr int64_t kBlocks = (int64_t)1 << 29;   // of a store (four pieces each:
 constexpr int64_t kNormRows = (int64_t)1 << 25;
 
 inline bool bad_store(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-inline size_t size_of(int dtype) { return dtype == ABL_F32 ? 4 : 2; }
 // elements of `size` bytes
 inline bool off(const void* p, size_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
 inline bool bad(const void* p, size_t size) { return p == nullptr || off(p, size); }
@@ -51,14 +50,14 @@ size_t abl_ckpt_bytes(int64_t M, int32_t C, int K) {
 int abl_ckpt_pack(void* stream, int dtype, const void* x, int64_t ldx, int64_t M, int32_t C, int K, void* ckpt) {
   if (int e = check(dtype, K, false, M, C)) return e;
   if (M == 0) return ABL_OK;
-  if (bad_rows(x, size_of(dtype), ldx, C) || bad_store(ckpt)) return ABL_ERR_ARG;
+  if (bad_rows(x, (size_t)size_of(dtype), ldx, C) || bad_store(ckpt)) return ABL_ERR_ARG;
   return launch_ckpt_pack((hipStream_t)stream, dtype, {x, ldx}, M, C, K, ckpt);
 }
 
 int abl_ckpt_unpack(void* stream, int dtype, const void* ckpt, int64_t M, int32_t C, int K, void* x, int64_t ldx) {
   if (int e = check(dtype, K, false, M, C)) return e;
   if (M == 0) return ABL_OK;
-  if (bad_rows(x, size_of(dtype), ldx, C) || bad_store(ckpt)) return ABL_ERR_ARG;
+  if (bad_rows(x, (size_t)size_of(dtype), ldx, C) || bad_store(ckpt)) return ABL_ERR_ARG;
   return launch_ckpt_unpack((hipStream_t)stream, dtype, ckpt, M, C, K, {x, ldx});
 }
 
@@ -69,7 +68,7 @@ int abl_resnorm_forward(void* stream, const abl_resnorm* step, const void* r, co
   if (!(step->eps > 0.0f) || (gate != nullptr && step->gate_rows < 1)) return ABL_ERR_ARG;
   if (step->M == 0) return ABL_OK;
   if (b == nullptr && (gate != nullptr || w_post != nullptr)) return ABL_ERR_ARG;
-  const size_t t = size_of(step->dtype);
+  const size_t t = (size_t)size_of(step->dtype);
   if (bad(r, t) || off(b, t) || off(gate, t) || off(w_post, t) || bad(w_pre, t) || off(r_out, t) || bad(n, t)) return ABL_ERR_ARG;
   if (step->K != 0) {
     if (bad_store(ckpt_n) || bad(rstd_n, 4)) return ABL_ERR_ARG;
@@ -95,7 +94,7 @@ int abl_resnorm_backward(void* stream, const abl_resnorm* step, int has_b, const
   if (!has_b && (gate != nullptr || w_post != nullptr || db != nullptr)) return ABL_ERR_ARG;
   if ((step->M > 0 && (gate != nullptr) != (dgate != nullptr)) || (w_post != nullptr) != (dw_post != nullptr)) return ABL_ERR_ARG;
   if (bad(dw_pre, 4) || off(dw_post, 4) || off(dgate, 4)) return ABL_ERR_ARG;
-  const size_t t = size_of(step->dtype);
+  const size_t t = (size_t)size_of(step->dtype);
   if (step->M > 0) {
     if (bad(dn, t) || off(dr_out, t) || off(gate, t) || off(w_post, t) || bad(w_pre, t) || off(dr, t) || off(db, t)) return ABL_ERR_ARG;
     if (bad_store(ckpt_n) || bad(rstd_n, 4) || bad_store(scratch)) return ABL_ERR_ARG;
@@ -113,7 +112,7 @@ int abl_glu_forward(void* stream, int dtype, int act, const void* g, int64_t ldg
   if (int e = check(dtype, K, true, M, C)) return e;
   if (act != ABL_ACT_SILU && act != ABL_ACT_GELU) return ABL_ERR_ARG;
   if (M == 0) return ABL_OK;
-  const size_t t = size_of(dtype);
+  const size_t t = (size_t)size_of(dtype);
   if (bad_rows(g, t, ldg, C) || bad_rows(u, t, ldu, C) || bad_rows(h, t, ldh, C)) return ABL_ERR_ARG;
   if (K != 0 && (bad_store(ckpt_g) || bad_store(ckpt_u))) return ABL_ERR_ARG;
   return launch_glu_forward((hipStream_t)stream, dtype, act, {g, ldg}, {u, ldu}, M, C, K, {h, ldh}, ckpt_g, ckpt_u);
@@ -125,7 +124,7 @@ int abl_glu_backward(void* stream, int dtype, int act, const void* dh, int64_t l
   if (int e = check(dtype, K, false, M, C)) return e;
   if (act != ABL_ACT_SILU && act != ABL_ACT_GELU) return ABL_ERR_ARG;
   if (M == 0) return ABL_OK;
-  const size_t t = size_of(dtype);
+  const size_t t = (size_t)size_of(dtype);
   if (bad_rows(dh, t, lddh, C) || bad_rows(dg, t, lddg, C) || bad_rows(du, t, lddu, C)) return ABL_ERR_ARG;
   if (bad_store(ckpt_g) || bad_store(ckpt_u) || (ckpt_h != nullptr && bad_store(ckpt_h))) return ABL_ERR_ARG;
   return launch_glu_backward((hipStream_t)stream, dtype, act, {dh, lddh}, ckpt_g, ckpt_u, M, C, K, {dg, lddg}, {du, lddu}, ckpt_h);
@@ -148,7 +147,7 @@ int abl_ckpt_wgrad(void* stream, int dtype, uint32_t flags, const void* ckpt, in
   if (int e = check_wgrad(dtype, M, Cin, Cout)) return e;
   if (int e = check_k(K)) return e;
   if ((flags & ~(uint32_t)(ABL_MATH_BF16 | ABL_ACCUM_DW)) != 0) return ABL_ERR_ARG;
-  const size_t t = size_of(dtype);
+  const size_t t = (size_t)size_of(dtype);
   if (off(scale, t) || bad(dW, 4)) return ABL_ERR_ARG;
   if (M > 0) {
     if (bad_store(ckpt) || bad_rows(dy, t, lddy, Cout) || bad_store(scratch)) return ABL_ERR_ARG;
