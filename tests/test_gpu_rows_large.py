@@ -1,0 +1,231 @@
+"""Operators on rows of channels at the sizes where other kernels are chosen (large tiles, shares of the rows, passes that go by the
+caches, rows of several pieces a thread), and the network that uses them together.  References in 64 bits with torch on the GPU from
+the stores' values; tolerances as in test_gpu_rows.py: a sum of M products is off by at most M u of the sum of their magnitudes, u = 2^-24,
+element-wise results by 2^-16 of their terms and half a unit of their type."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1901_07988_amd import binding as B
+from paper_1901_07988_amd import token_blocks as T
+from tests import rows_reference as R
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def normal(gen, *shape, std=1.0, dtype=torch.float32):
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def generator(seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return gen
+
+
+def stored(x, K):
+    """The store of x and its values in 64 bits."""
+    s = torch.full((B.abl_ckpt_bytes(*x.shape, K),), 0xEE, dtype=torch.uint8, device="cuda")
+    B.abl_ckpt_pack(x, K, s)
+    v = torch.empty(x.shape, dtype=torch.float32, device="cuda")
+    B.abl_ckpt_unpack(s, K, v)
+    return s, v.double()
+
+
+def within(got, want, bound, what):
+    off = (got.double() - want).abs() - bound
+    assert not bool((off > 0).any()), (what, float((off / bound).max()))
+    assert bool(torch.isfinite(got).all()), what
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype,flags", [(torch.bfloat16, 0), (torch.float32, 0), (torch.float32, B.ABL_MATH_BF16)])
+@pytest.mark.parametrize("M,Cin,Cout", [
+    (2048, 4096, 4096),     # large tiles, every unit with one
+    (300, 4000, 4099),      # large tiles, ragged, few rows
+    (8192, 1024, 1000),     # shares of the rows
+    (8191, 2050, 1023),     # shares of large tiles, ragged
+    (16384, 256, 264),      # many shares
+    (16383, 250, 257),
+    (33, 5000, 70),
+])
+def test_weight_gradient_of_large_products(M, Cin, Cout, dtype, flags, K):
+    gen = generator(M + Cin)
+    s, x = stored(normal(gen, M, Cin), K)
+    dy = normal(gen, M, Cout, std=0.02, dtype=dtype)
+    scale = normal(gen, Cin, std=0.2, dtype=dtype) + 1
+    y = (dy.bfloat16() if flags else dy).double()
+    w = scale.double()[:, None]
+    want = w * torch.mm(x.t().contiguous(), y)
+    size = w.abs() * torch.mm(x.abs().t().contiguous(), y.abs())
+    ws = torch.full((B.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
+    dW = torch.full((Cin, Cout), 7.0, device="cuda")
+    B.abl_ckpt_wgrad(s, K, scale, dy, ws, dW, flags)
+    within(dW, want, U * (M + 8) * size, "dW")
+    again = torch.full((Cin, Cout), 7.0, device="cuda")
+    B.abl_ckpt_wgrad(s, K, scale, dy, ws, again, flags)
+    assert torch.equal(dW, again)
+    B.abl_ckpt_wgrad(s, K, scale, dy, ws, again, flags | B.ABL_ACCUM_DW)
+    within(again, want + dW.double(), U * (M + 10) * (size + dW.double().abs()), "dW accumulated")
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weight_gradient_takes_a_slice_of_a_wide_tensor_and_leaves_nan_where_it_is(dtype, K):
+    """Columns next to the slice hold NaN: a piece that reaches beyond the slice must not bring them into its sums."""
+    gen = generator(3)
+    M, Cin, Cout, first, wide = 515, 300, 203, 5, 230
+    x = normal(gen, M, Cin)
+    x[7, 100] = float("nan")
+    s = torch.zeros(B.abl_ckpt_bytes(M, Cin, K), dtype=torch.uint8, device="cuda")
+    B.abl_ckpt_pack(x, K, s)
+    v = torch.empty(M, Cin, device="cuda")
+    B.abl_ckpt_unpack(s, K, v)
+    big = torch.full((M, wide), float("nan"), dtype=dtype, device="cuda")
+    dy = big[:, first: first + Cout]
+    dy.copy_(normal(gen, M, Cout, dtype=dtype))
+    ws = torch.empty(B.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype), dtype=torch.uint8, device="cuda")
+    dW = torch.full((Cin, Cout), 7.0, device="cuda")
+    B.abl_ckpt_wgrad(s, K, None, dy, ws, dW)
+    bad = torch.isnan(dW).cpu().numpy()
+    want = np.zeros((Cin, Cout), bool)
+    want[96:128] = True                                  # the block with the NaN
+    np.testing.assert_array_equal(bad, want)
+    ok = torch.ones(Cin, dtype=torch.bool, device="cuda")
+    ok[96:128] = False
+    a, y = v[:, ok].double(), dy.double()
+    within(dW[ok], torch.mm(a.t().contiguous(), y), U * (M + 8) * torch.mm(a.abs().t().contiguous(), y.abs()), "dW")
+
+
+@pytest.mark.parametrize("M,C,K,gate_rows", [(8192, 4096, 8, 2048), (4096, 8192, 4, 1), (70000, 1500, 8, 0), (9000, 4104, 8, 9000)])
+def test_step_on_tensors_beyond_the_caches(M, C, K, gate_rows):
+    gen = generator(C)
+    bf = torch.bfloat16
+    r, b = normal(gen, M, C, dtype=bf), normal(gen, M, C, dtype=bf)
+    gate = normal(gen, -(-M // gate_rows), C, std=0.3, dtype=bf) if gate_rows else None
+    w_post, w_pre = normal(gen, C, std=0.2, dtype=bf) + 1, normal(gen, C, std=0.2, dtype=bf) + 1
+    r_out, n = torch.empty_like(r), torch.empty_like(r)
+    sb, sn = (torch.empty(B.abl_ckpt_bytes(M, C, K), dtype=torch.uint8, device="cuda") for _ in range(2))
+    rb, rn = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    B.abl_resnorm_forward(r, b, gate, gate_rows, w_post, w_pre, r_out, n, K, sb, rb, sn, rn)
+    y, z = torch.empty(M, C, device="cuda"), torch.empty(M, C, device="cuda")
+    B.abl_ckpt_unpack(sb, K, y)
+    B.abl_ckpt_unpack(sn, K, z)
+    at = torch.cat([torch.arange(0, M, max(1, M // 50), device="cuda"), torch.tensor([M - 1], device="cuda")])
+    f = {k: t[at].double().cpu().numpy() for k, t in dict(r=r, b=b, r_out=r_out, n=n, y=y, z=z, rb=rb, rn=rn).items()}
+    g = None if gate is None else gate.double().cpu().numpy()[at.cpu().numpy() // gate_rows]
+    wp, wq = w_post.double().cpu().numpy(), w_pre.double().cpu().numpy()
+    want = R.step_forward(f["r"], f["b"], g, 1, wp, wq, 1.0, 1.0, 1e-5, False)
+    for k, ref in (("r_out", want["r"]), ("n", want["n"])):
+        assert (np.abs(f[k] - ref) <= 2.0 ** -8 * 1.01 * np.abs(ref) + 2.0 ** -14).all(), k
+    for k, ref in (("rb", want["rstd_b"]), ("rn", want["rstd_n"])):
+        np.testing.assert_allclose(f[k], ref, rtol=2.0 ** -16)
+    for k, ref in (("y", want["y"]), ("z", want["z"])):   # the next code at most: a quarter of the value in 4 bits, the step of the block in 8
+        step = np.repeat(np.abs(R.blocked(ref)).max(-1), 32, axis=1)[:, :C] / (63 if K == 8 else 3)
+        assert (np.abs(f[k] - ref) <= step).all(), k
+        assert (R.unpack(R.pack(ref, K), len(at), C, K) != f[k]).mean() < 1e-3, k
+    # backward, from the stores' values
+    dn, dr_out = normal(gen, M, C, std=0.02, dtype=bf), normal(gen, M, C, std=0.02, dtype=bf)
+    dr, db = torch.empty_like(r), torch.empty_like(r)
+    dgate = torch.empty(gate.shape, device="cuda") if gate_rows else None
+    dwp, dwq = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    ws = torch.full((B.abl_resnorm_scratch_bytes(M, C),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.abl_resnorm_backward(dn, dr_out, gate, gate_rows, w_post, w_pre, K, sb, rb, sn, rn, ws, dr, db, dgate, dwp, dwq)
+    h = {k: t[at].double().cpu().numpy() for k, t in dict(dn=dn, dr_out=dr_out, dr=dr, db=db).items()}
+    ref = R.step_backward(h["dn"], h["dr_out"], f["y"], f["rb"], f["z"], f["rn"], g, 1, wp, wq, 1.0, 1.0, False)
+    for k in ("dr", "db"):
+        terms = 2.0 ** -16 * (np.abs(ref[k]) + np.abs(ref[k]).max(1, keepdims=True))
+        assert (np.abs(h[k] - ref[k]) <= 2.0 ** -8 * 1.01 * np.abs(ref[k]) + 4 * terms).all(), k
+    # sums over all rows, in parts of them
+    sums = [torch.zeros(C, dtype=torch.float64, device="cuda") for _ in range(4)]
+    gsum = torch.zeros(gate.shape, dtype=torch.float64, device="cuda") if gate_rows else None
+    for i in range(0, M, 2048):
+        p = slice(i, min(i + 2048, M))
+        d, zz, yy = dn[p].double(), z[p].double(), y[p].double()
+        v = d * w_pre.double()
+        D = dr_out[p].double() + rn[p].double()[:, None] * (v - zz * (v * zz).mean(1, keepdim=True))
+        sums[0] += (d * zz).sum(0)
+        sums[1] += (d * zz).abs().sum(0)
+        group = torch.arange(p.start, p.stop, device="cuda") // gate_rows if gate_rows else None
+        e = D * gate.double()[group] if gate_rows else D
+        sums[2] += (e * yy).sum(0)
+        sums[3] += (e * yy).abs().sum(0)
+        if gate_rows:
+            gsum.index_add_(0, group, D * yy * w_post.double())
+    terms = 2.0 ** -16 + U * M
+    within(dwq, sums[0], terms * sums[1], "dw_pre")
+    within(dwp, sums[2], terms * sums[3], "dw_post")
+    if gate_rows:
+        size = sums[3].max() if gate_rows > 1 else gsum.abs().max()
+        within(dgate, gsum, terms * size.expand_as(gsum), "dgate")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_step_of_the_widest_rows_that_are_not_whole_pieces(dtype):
+    M, C, K = 5, 16381, 8
+    gen = generator(1)
+    r, b = normal(gen, M, C, dtype=dtype), normal(gen, M, C, dtype=dtype)
+    w = normal(gen, C, std=0.2, dtype=dtype) + 1
+    guard = torch.full((M + 2, C), 7.0, dtype=dtype, device="cuda")
+    n = guard[1: M + 1]
+    sb, sn = (torch.empty(B.abl_ckpt_bytes(M, C, K), dtype=torch.uint8, device="cuda") for _ in range(2))
+    rb, rn = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    B.abl_resnorm_forward(r, b, None, 0, w, w, None, n, K, sb, rb, sn, rn)
+    want = R.step_forward(*(t.double().cpu().numpy() for t in (r, b)), None, 0, *(w.double().cpu().numpy(),) * 2, 1.0, 1.0, 1e-5, False)
+    got = n.double().cpu().numpy()
+    half = 2.0 ** -8 * 1.01 if dtype == torch.bfloat16 else 0.0
+    assert (np.abs(got - want["n"]) <= half * np.abs(want["n"]) + 2.0 ** -14).all()
+    assert bool((guard[0] == 7).all()) and bool((guard[M + 1] == 7).all())
+    dn = normal(gen, M, C, std=0.02, dtype=dtype)
+    dr = torch.full((M + 2, C), 7.0, dtype=dtype, device="cuda")
+    dwp, dwq = torch.full((C + 8,), 7.0, device="cuda"), torch.full((C + 8,), 7.0, device="cuda")
+    db = torch.empty_like(r)
+    ws = torch.empty(B.abl_resnorm_scratch_bytes(M, C), dtype=torch.uint8, device="cuda")
+    B.abl_resnorm_backward(dn, None, None, 0, w, w, K, sb, rb, sn, rn, ws, dr[1: M + 1], db, None, dwp[:C], dwq[:C])
+    y, z = (R.unpack(t.cpu().numpy(), M, C, K) for t in (sb, sn))
+    ref = R.step_backward(dn.double().cpu().numpy(), None, y, rb.double().cpu().numpy(), z, rn.double().cpu().numpy(), None, 0,
+                          *(w.double().cpu().numpy(),) * 2, 1.0, 1.0, False)
+    for k, t in (("dr", dr[1: M + 1]), ("db", db)):
+        terms = 2.0 ** -14 * np.abs(ref[k]).max(1, keepdims=True)
+        assert (np.abs(t.double().cpu().numpy() - ref[k]) <= half * np.abs(ref[k]) + terms).all(), k
+    for t, k in ((dwp, "dw_post"), (dwq, "dw_pre")):
+        assert (np.abs(t[:C].double().cpu().numpy() - ref[k]) <= 2.0 ** -14 * np.abs(ref[k]).max()).all(), k
+        assert bool((t[C:] == 7).all())
+    assert bool((dr[0] == 7).all()) and bool((dr[M + 1] == 7).all())
+
+
+# ---- the network --------------------------------------------------------------------------------------
+def test_network_gradients_are_those_of_the_exact_one_up_to_the_stores():
+    """What a store leaves out: 8 bits 0.7 %, 4 bits 10 % of a block's standard deviation, and bf16 0.2 % at each of some twenty tensors on a
+    path of two blocks; relative errors of gradients are held to three times the root of the sum of squares."""
+    tokens, C, F, layers = 1000, 256, 352, 2
+    fresh = lambda: T.random_parameters(layers, C, F, 3, seed=5)  # noqa: E731
+    for act in (B.ABL_ACT_SILU, B.ABL_ACT_GELU):
+        exact = T.ExactNet(*fresh(), tokens, act=act, alpha=0.9, beta=0.8)
+        x, dn = T.batch(tokens, C, 1), T.batch(tokens, C, 2)
+        out = exact.forward(x)
+        exact.backward(dn)
+        for K, bound in ((8, 3 * (8 * 0.007 ** 2 + 20 * 0.002 ** 2) ** 0.5), (4, 3 * (8 * 0.1 ** 2) ** 0.5)):
+            net = T.TokenNet(*fresh(), tokens, K, act=act, alpha=0.9, beta=0.8)
+            got = net.forward(x)
+            assert T.relative(got, out.detach()) < 3 * (20 * 0.002 ** 2) ** 0.5      # the forward pass does not depend on K
+            net.backward(dn)
+            for name, e in T.gradient_errors(net, exact).items():
+                assert e < bound, (K, act, name, e)
+            assert T.relative(net.g_last, exact.g_last) < bound
+            first = [{k: v.clone() for k, v in g.items()} for g in net.grads]
+            net.backward(dn, accumulate=True)
+            for a, b in zip(net.grads, first):
+                for k in ("W1", "W2"):
+                    assert torch.equal(a[k], 2 * b[k]), k                            # twice the same sum
+                assert torch.equal(a["gate"], b["gate"])
+
+
+def test_network_trains_as_the_exact_one():
+    curves = T.main(["--layers", "2", "--tokens", "512", "--channels", "128", "--width", "192", "--steps", "25", "--samples", "2"])
+    exact = np.array(curves["exact"])
+    assert exact[-1] < 0.95 * exact[0]
+    np.testing.assert_allclose(curves["K=8"], exact, rtol=0.01)
+    np.testing.assert_allclose(curves["K=4"], exact, rtol=0.06)
