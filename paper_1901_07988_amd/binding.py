@@ -47,10 +47,11 @@ class abl_resnorm(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
-if not os.path.exists(LIB_PATH):
-    raise ImportError("libabl.so is not built: run `python -m paper_1901_07988_amd.build` "
+if not (os.path.exists(LIB_PATH) and os.path.exists(os.path.join(_HERE, "_rows.so"))):
+    raise ImportError("libabl.so (and _rows.so) is not built: run `python -m paper_1901_07988_amd.build` "
                       "(there is no CPU fallback)")
 lib = ctypes.CDLL(LIB_PATH)
+from . import _rows  # noqa: E402  (links libabl.so)
 
 _vp, _sz, _i32, _i64, _u32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
 _shp = ctypes.POINTER(abl_shape)
@@ -378,57 +379,9 @@ def abl_stack_backward_traced(layers, K, skip_every, buf_s, buf_t, scratch, trac
 
 
 # ---- blocks of language models ---------------------------------------------------------------
-# The C ABI sees addresses only, so dtypes and sizes are checked here.  A call's checks cost about as much as its launch does:
-# each argument is looked at once.
+# The C ABI sees addresses only: dtypes, sizes and layouts are checked in the compiled marshalling (csrc/rows_binding.cpp), which
+# raises AssertionError for wrong tensors and returns the library's code.
 _DTYPES = {torch.float32: ABL_F32, torch.bfloat16: ABL_BF16}
-_F32 = torch.float32
-
-
-def _dtype(dtype):
-    """The ABL_* dtype of a torch dtype (-1, an ABL_ERR_ARG, for others)."""
-    return _DTYPES.get(dtype, -1)
-
-
-try:
-    _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-
-    def _current():
-        """The current stream, as _stream() without the stream object (0.1 us for 2.8)."""
-        return _raw_stream(_device())
-except AttributeError:
-    _current = _stream
-
-
-def _arg(t, dtype, n, what):
-    """Address of a contiguous device tensor of that dtype with n elements at least (None passes: the library says where
-    that is an error)."""
-    if t is None:
-        return None
-    assert t.is_cuda and t.dtype is dtype and t.numel() >= n and t.is_contiguous(), \
-        "%s: a contiguous device tensor of %d elements of %s" % (what, n, dtype)
-    return t.data_ptr()
-
-
-def _rows(t, dtype, M, C, what):
-    """(address, elements from one row to the next) of a device tensor [M, C] whose rows are contiguous."""
-    assert t.is_cuda and t.dtype is dtype and t.shape == (M, C), "%s: a device tensor [%d, %d] of %s" % (what, M, C, dtype)
-    ld, one = t.stride()
-    assert one == 1 or C == 1 or M == 0, "%s: rows have to be contiguous" % what
-    return t.data_ptr(), (ld if M > 1 else C)
-
-
-def _store(t, M, C, K, what):
-    """Address of a tensor of bytes that holds the K-bit store of [M, C]."""
-    if t is None:
-        return None
-    n = -(-M * -(-C // 32) * (4 * K + 1) // 128) * 128
-    assert t.is_cuda and t.element_size() == 1 and t.numel() >= n and t.is_contiguous(), \
-        "%s: %d contiguous bytes on the device" % (what, n)
-    return t.data_ptr()
-
-
-def _workspace(t):
-    return (t.data_ptr() if t.is_cuda and t.is_contiguous() else None), t.numel() * t.element_size()
 
 
 def abl_ckpt_bytes(M, C, K):
@@ -437,30 +390,19 @@ def abl_ckpt_bytes(M, C, K):
 
 def abl_ckpt_pack(x, K, ckpt):
     """x [M, C] (rows contiguous, any distance between them) -> its block store."""
-    M, C = x.shape
-    p, ld = _rows(x, x.dtype, M, C, "x")
-    _check(lib.abl_ckpt_pack(_current(), _dtype(x.dtype), p, ld, M, C, K, _store(ckpt, M, C, K, "ckpt")), "abl_ckpt_pack")
+    _check(_rows.ckpt_pack(x, K, ckpt), "abl_ckpt_pack")
 
 
 def abl_ckpt_unpack(ckpt, K, x):
     """The values that the block store stands for -> x [M, C]."""
-    M, C = x.shape
-    p, ld = _rows(x, x.dtype, M, C, "x")
-    _check(lib.abl_ckpt_unpack(_current(), _dtype(x.dtype), _store(ckpt, M, C, K, "ckpt"), M, C, K, p, ld), "abl_ckpt_unpack")
+    _check(_rows.ckpt_unpack(ckpt, K, x), "abl_ckpt_unpack")
 
 
 def abl_resnorm_forward(r, b, gate, gate_rows, w_post, w_pre, r_out, n, K=0, ckpt_b=None, rstd_b=None, ckpt_n=None,
                         rstd_n=None, alpha=1.0, beta=1.0, eps=1e-5, flags=0):
     """r, b, r_out, n [M, C]; gate [ceil(M / gate_rows), C]; w_post, w_pre [C]; b, gate, w_post, r_out may be None."""
-    M, C = r.shape
-    t, E = r.dtype, M * C
-    groups = -(-M // gate_rows) if gate_rows > 0 else 0
-    s = abl_resnorm(M, gate_rows, C, _dtype(t), K, flags, alpha, beta, eps)
-    _check(lib.abl_resnorm_forward(
-        _current(), ctypes.byref(s), _arg(r, t, E, "r"), _arg(b, t, E, "b"), _arg(gate, t, groups * C, "gate"),
-        _arg(w_post, t, C, "w_post"), _arg(w_pre, t, C, "w_pre"), _arg(r_out, t, E, "r_out"), _arg(n, t, E, "n"),
-        _store(ckpt_b, M, C, K, "ckpt_b"), _arg(rstd_b, _F32, M, "rstd_b"), _store(ckpt_n, M, C, K, "ckpt_n"),
-        _arg(rstd_n, _F32, M, "rstd_n")), "abl_resnorm_forward")
+    _check(_rows.resnorm_forward(r, b, gate, gate_rows, w_post, w_pre, r_out, n, K, ckpt_b, rstd_b, ckpt_n, rstd_n, alpha,
+                                 beta, eps, flags), "abl_resnorm_forward")
 
 
 def abl_resnorm_scratch_bytes(M, C):
@@ -470,52 +412,28 @@ def abl_resnorm_scratch_bytes(M, C):
 def abl_resnorm_backward(dn, dr_out, gate, gate_rows, w_post, w_pre, K, ckpt_b, rstd_b, ckpt_n, rstd_n, scratch, dr, db,
                          dgate, dw_post, dw_pre, alpha=1.0, beta=1.0, flags=0, has_b=True):
     """dn, dr_out, dr, db [M, C]; dgate [ceil(M / gate_rows), C], dw_post, dw_pre [C] in fp32."""
-    M, C = dn.shape
-    t, E = dn.dtype, M * C
-    groups = -(-M // gate_rows) if gate_rows > 0 else 0
-    s = abl_resnorm(M, gate_rows, C, _dtype(t), K, flags, alpha, beta, 0.0)
-    ws, ws_bytes = _workspace(scratch)
-    _check(lib.abl_resnorm_backward(
-        _current(), ctypes.byref(s), has_b, _arg(dn, t, E, "dn"), _arg(dr_out, t, E, "dr_out"),
-        _arg(gate, t, groups * C, "gate"), _arg(w_post, t, C, "w_post"), _arg(w_pre, t, C, "w_pre"),
-        _store(ckpt_b, M, C, K, "ckpt_b"), _arg(rstd_b, _F32, M, "rstd_b"), _store(ckpt_n, M, C, K, "ckpt_n"),
-        _arg(rstd_n, _F32, M, "rstd_n"), ws, ws_bytes, _arg(dr, t, E, "dr"), _arg(db, t, E, "db"),
-        _arg(dgate, _F32, groups * C, "dgate"), _arg(dw_post, _F32, C, "dw_post"), _arg(dw_pre, _F32, C, "dw_pre")),
-        "abl_resnorm_backward")
+    _check(_rows.resnorm_backward(dn, dr_out, gate, gate_rows, w_post, w_pre, K, ckpt_b, rstd_b, ckpt_n, rstd_n, scratch,
+                                  dr, db, dgate, dw_post, dw_pre, alpha, beta, flags, has_b), "abl_resnorm_backward")
 
 
 def abl_glu_forward(g, u, h, act, K=0, ckpt_g=None, ckpt_u=None):
     """h = act(g) * u; g, u, h [M, C], rows contiguous (column slices of wider tensors are fine)."""
-    M, C = g.shape
-    t = g.dtype
-    (pg, lg), (pu, lu), (ph, lh) = _rows(g, t, M, C, "g"), _rows(u, t, M, C, "u"), _rows(h, t, M, C, "h")
-    _check(lib.abl_glu_forward(_current(), _dtype(t), act, pg, lg, pu, lu, M, C, K, ph, lh,
-                               _store(ckpt_g, M, C, K, "ckpt_g"), _store(ckpt_u, M, C, K, "ckpt_u")), "abl_glu_forward")
+    _check(_rows.glu_forward(g, u, h, act, K, ckpt_g, ckpt_u), "abl_glu_forward")
 
 
 def abl_glu_backward(dh, ckpt_g, ckpt_u, K, dg, du, act, ckpt_h=None):
-    M, C = dh.shape
-    t = dh.dtype
-    (ph, lh), (pg, lg), (pu, lu) = _rows(dh, t, M, C, "dh"), _rows(dg, t, M, C, "dg"), _rows(du, t, M, C, "du")
-    _check(lib.abl_glu_backward(_current(), _dtype(t), act, ph, lh, _store(ckpt_g, M, C, K, "ckpt_g"),
-                                _store(ckpt_u, M, C, K, "ckpt_u"), M, C, K, pg, lg, pu, lu,
-                                _store(ckpt_h, M, C, 8, "ckpt_h")), "abl_glu_backward")
+    """dh, dg, du [M, C], rows contiguous; ckpt_h: receives the 8-bit store of act(g) * u."""
+    _check(_rows.glu_backward(dh, ckpt_g, ckpt_u, K, dg, du, act, ckpt_h), "abl_glu_backward")
 
 
 def abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype):
     """dtype: the torch dtype of dy."""
-    return lib.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, _dtype(dtype))
+    return lib.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, _DTYPES.get(dtype, -1))
 
 
 def abl_ckpt_wgrad(ckpt, K, scale, dy, scratch, dW, flags=0):
     """dW [Cin, Cout] fp32 = (scale * x~)^T dy from the store of x [M, Cin]; dy [M, Cout], rows contiguous."""
-    Cin, Cout = dW.shape
-    M, t = dy.shape[0], dy.dtype
-    p, ld = _rows(dy, t, M, Cout, "dy")
-    ws, ws_bytes = _workspace(scratch)
-    _check(lib.abl_ckpt_wgrad(_current(), _dtype(t), flags, _store(ckpt, M, Cin, K, "ckpt"), M, Cin, K,
-                              _arg(scale, t, Cin, "scale"), p, ld, Cout, ws, ws_bytes, _arg(dW, _F32, Cin * Cout, "dW")),
-           "abl_ckpt_wgrad")
+    _check(_rows.ckpt_wgrad(ckpt, K, scale, dy, scratch, dW, flags), "abl_ckpt_wgrad")
 
 
 def abl_sgd_momentum(w, grad, v, lr, momentum, weight_decay):

@@ -9,6 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libabl.so")
+ROWS = os.path.join(HERE, "_rows.so")     # compiled marshalling of the operators on rows (a Python extension module)
 
 # every HIP translation unit: no packed-fp32 instructions (some forms have given wrong results on this hardware)
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-variable",
@@ -47,6 +48,20 @@ def hipcc():
     raise RuntimeError("hipcc not found")
 
 
+def rows_command():
+    """The host compiler's command for _rows.so: torch's headers and libraries, and libabl.so next to it."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = [sysconfig.get_paths()["include"], os.path.join(ROOT, "include"), *cpp_extension.include_paths(device_type="cuda")]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            *["-isystem" + d if "torch" in d or "rocm" in d else "-I" + d for d in include],
+            os.path.join(CSRC, "rows_binding.cpp"), "-o", ROWS, "-L" + lib, "-L" + HERE, "-labl", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python",
+            "-Wl,-rpath,$ORIGIN"]
+
+
 def build(verbose: bool = True, only=None) -> str:
     """Compile every translation unit (or, with `only`, just the named ones, reusing the other
     object files of an earlier build) and link libabl.so."""
@@ -74,6 +89,11 @@ def build(verbose: bool = True, only=None) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
+    if not only or "rows_binding" in only or not os.path.exists(ROWS):
+        cmd = rows_command()
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
     return LIB
 
 
