@@ -7,8 +7,11 @@
 //
 // Both operands lie with the contraction index outermost.  They are staged that way, [m][channels] in bf16, and the fragments
 // are read with ds_read_b64_tr_b16: 16 lanes fetch four rows' 16 channels and receive one channel's four rows each.  The order
-// of the rows within a step of 32 is 4 (lane / 16) + 0..3 and 16 more, for both operands alike.  A row's 32-byte chunks (16
-// channels) are stored at their number xor row % 8, which puts the 8 rows that half a wave reads at once on different banks.
+// of the rows within a step of 32 is 4 (lane / 16) + 0..3 and 16 more, for both operands alike.  In a staged row the even 16-byte pieces
+// come first and then the odd ones, the c-th of each at place c xor row % 8, the odd ones moved by four places more (and by half of the even
+// ones' range): half a wave's read, 16 pieces of eight rows, takes all 64 banks once, and eight lanes' writes, of neighbouring
+// pieces or of every other one, 128 different bytes modulo 128 (both counted: no conflicts; with 32-byte chunks at c xor row % 8 an
+// eighth of the LDS cycles were conflicts).
 
 #include "block_store.h"
 
@@ -32,6 +35,13 @@ template <typename T>
 __device__ inline float row_scale(const void* s, int i) {
   return s == nullptr ? 1.0f : (float)((const T*)s)[i];
 }
+
+// Byte of piece q of row r in a staged tile whose rows have `pitch` bytes (256 or 512), and of the eight bytes that a lane of a fragment's read asks for
+// (chunk c of 16 channels, rows from r on).
+__device__ inline int staged_at(int r, int q, int pitch) {
+  return r * pitch + (q & 1) * (pitch / 2) + (((q >> 1) ^ (r & 7) ^ ((q & 1) * (pitch / 32 - 4))) * 16);
+}
+__device__ inline int fragment_at(int r, int c, int lane, int pitch) { return staged_at(r, 2 * c + ((lane >> 1) & 1), pitch) + (lane & 1) * 8; }
 
 template <int K>
 __device__ inline float stored_value(const WgArgs& a, int64_t row, int c) {
@@ -113,12 +123,12 @@ __global__ __launch_bounds__(256) void store_wgrad_far_kernel(WgArgs a) {
       const int at = p * kThreads + tid, r = at / (BI / 8), q = at % (BI / 8);
       float v[8];
       decode<K>(cx[p], sx[p], v);
-      put(to + r * (BI * 2) + (((q >> 1) ^ (r & 7)) * 32) + (q & 1) * 16, to_bf16x8(v));
+      put(to + staged_at(r, q, BI * 2), to_bf16x8(v));
     }
 #pragma unroll
     for (int p = 0; p < PY; ++p) {
       const int at = p * kThreads + tid, r = at / (BJ / 8), q = at % (BJ / 8);
-      char* y = to + kXBytes + r * (BJ * 2) + (((q >> 1) ^ (r & 7)) * 32) + (q & 1) * 16;
+      char* y = to + kXBytes + staged_at(r, q, BJ * 2);
       if constexpr (std::is_same_v<T, bf16_t>) {
         put(y, __builtin_bit_cast(bf16x8_t, ry[p]));
       } else {
@@ -145,7 +155,7 @@ __global__ __launch_bounds__(256) void store_wgrad_far_kernel(WgArgs a) {
   const int wi = wave / WJ * (FI * 16), wj = wave % WJ * (FJ * 16);
   const int r = (lane >> 4) * 4 + ((lane & 15) >> 2);   // row of this lane's first address; 16 more for the second
   auto fragment = [&](const char* plane, int pitch, int c) __attribute__((always_inline)) {
-    const char* p = plane + r * pitch + (((c >> 4) ^ (r & 7)) * 32) + (lane & 3) * 8;
+    const char* p = plane + fragment_at(r, c >> 4, lane, pitch);
     return transposed(p, p + 16 * pitch);
   };
 
@@ -294,10 +304,19 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
   auto decode_x = [&](const XCodes& t) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < XP; ++p) {
-      float v[8];
-      decode<K>(t.c[p], t.s, v);
+      if constexpr (K == 4) {   // (the conversion makes pairs of bf16 with the scale applied)
+        const float scale = scale_of(t.s);
+        auto two = [&](auto b) { xw[p][b.value] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.c[p].w, scale, b.value)); };
+        two(std::integral_constant<int, 0>{}), two(std::integral_constant<int, 1>{});
+        two(std::integral_constant<int, 2>{}), two(std::integral_constant<int, 3>{});
+#pragma unroll
+        for (int e = 0; e < 4; ++e) xw[p][e] = t.s == 255u ? 0x7FC07FC0u : xw[p][e];
+      } else {
+        float v[8];
+        decode<K>(t.c[p], t.s, v);
 #pragma unroll   // (the upper halves: nothing is below them)
-      for (int e = 0; e < 4; ++e) xw[p][e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]), 0x07060302u);
+        for (int e = 0; e < 4; ++e) xw[p][e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]), 0x07060302u);
+      }
     }
   };
   constexpr bool kSplit = NP == 3;   // dy's parts, too, are made between the matrix instructions
@@ -313,13 +332,12 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
     }
   };
   auto stage = [&](const YPieces& t, char* to) __attribute__((always_inline)) {
-    char* x = to + xr * (BI * 2) + (((xq >> 1) ^ (xr & 7)) * 32) + (xq & 1) * 16;
 #pragma unroll
-    for (int p = 0; p < XP; ++p) *reinterpret_cast<u32x4*>(x + 16 * p) = xw[p];
+    for (int p = 0; p < XP; ++p) *reinterpret_cast<u32x4*>(to + staged_at(xr, xq + p, BI * 2)) = xw[p];
 #pragma unroll
     for (int p = 0; p < PY; ++p) {
       const int at = p * 512 + tid, r = at / (BJ / 8), q = at % (BJ / 8);
-      char* y = to + kXBytes + r * (BJ * 2) + (((q >> 1) ^ (r & 7)) * 32) + (q & 1) * 16;
+      char* y = to + kXBytes + staged_at(r, q, BJ * 2);
       if constexpr (kSplit) {
 #pragma unroll
         for (int n = 0; n < NP; ++n) *reinterpret_cast<u32x4*>(y + n * kYBytes) = yw[p][n];
@@ -341,7 +359,7 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
   const int wi = wave / WJ * (FI * 16), wj = wave % WJ * (FJ * 16);
   const int fr = (lane >> 4) * 4 + ((lane & 15) >> 2);
   auto fragment = [&](const char* plane, int pitch, int c) __attribute__((always_inline)) {
-    const char* p = plane + fr * pitch + (((c >> 4) ^ (fr & 7)) * 32) + (lane & 3) * 8;
+    const char* p = plane + fragment_at(fr, c >> 4, lane, pitch);
     return transposed(p, p + 16 * pitch);
   };
   auto phase_end = [&]() __attribute__((always_inline)) {
