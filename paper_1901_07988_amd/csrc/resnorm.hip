@@ -384,7 +384,13 @@ struct Shares {
   int64_t per_group = 0;  // teams of a group of rows (0: teams hold whole groups)
 };
 
-constexpr int64_t kFwdThreads = 256 * 1024, kBwdThreads = 256 * 1024;   // of a launch at most (256 compute units)
+// Threads of a launch at most (256 compute units).  The backward: what stays on the units at once where a thread has two pieces, and half as many sums for the
+// second launch where it has one: 1024 / 512 threads a unit take 108 / 92 us at 4096 x 8192 bf16 with a gate a row, 64.4 / 59.4 at
+// 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32; 19.8 / 21 at 16384 x 200.
+constexpr int64_t kBwdThreads = 128 * 1024;
+// The forward, 2048 / 1024 threads a unit: 53.5 / 55.2 us at 8192 x 4096 bf16 and 9.4 / 10.3 at 1500 x 1112 fp32; rows of more pieces than
+// threads take the smaller launch (48 / 40 us at 1024 x 16384 bf16).
+constexpr int64_t fwd_threads(int pieces_a_thread) { return (pieces_a_thread == 1 ? 512 : 256) * 1024; }
 Shares shares_of(int64_t M, int64_t gate_rows, int team, bool gate) {
   const int64_t most = kBwdThreads / team;   // up to twice as many where groups are cut
   const int64_t block = team == 64 ? 4 : 1;   // teams of a block: of one group, where a group is cut
@@ -720,7 +726,7 @@ int launch_resnorm_forward(hipStream_t st, const abl_resnorm& s, const void* r, 
   by_team(s.C, bytes, [&](auto t, auto nv, auto form) {
     constexpr int TEAM = decltype(t)::value, NV = decltype(nv)::value;
     constexpr Form FORM = decltype(form)::value;
-    const int64_t most = kFwdThreads / TEAM;
+    const int64_t most = fwd_threads(NV) / TEAM;
     a.rows = (s.M + most - 1) / most;
     const int64_t teams = (s.M + a.rows - 1) / a.rows;
     const unsigned grid = (unsigned)(TEAM == 64 ? (teams + 3) / 4 : teams);
