@@ -6,10 +6,11 @@
 //   dr = alpha D,   e = beta D,   dgate = sum e w_post y,   dw_post = sum e gate y,   dw_pre = sum dn z
 //   db = rstd_b (v - y mean(v y)),   v = e gate w_post
 //
-// Both are bound by memory: an element of bf16 costs 8 bytes and its two stores (10.1 at K = 8).  A team of threads holds a row in registers,
-// so that every tensor is read once; the sums over a row go through the waves' registers and, between waves, LDS.  In the
-// backward a team takes consecutive rows and keeps its share of the sums over rows in registers as well; the teams' sums are added
-// in a fixed order by a second launch.
+// Both are bound by memory: an element of bf16 costs 8 bytes and its two stores (10.1 at K = 8).  8192 x 4096 bf16 with a gate for
+// 2048 rows, K = 8 (338 MB): forward 54 us (6.2 TB/s, as a copy), backward 60 with the second launch (5.6); calls of a few rows
+// are the launch: 8 rows 3.9 us.  A team of threads holds a row in registers, so that every tensor is read once; the sums over a
+// row go through the waves' registers and, between waves, LDS.  In the backward a team takes consecutive rows and keeps its share
+// of the sums over rows in registers as well; the teams' sums are added in a fixed order by a second launch.
 
 #include <utility>
 
@@ -32,7 +33,8 @@ __device__ inline int left(int C, uint32_t c) { return C - (int)c; }
 // A row of a multiple of eight channels is whole pieces (kWhole).  Where it is not (kRagged), the lane of the last piece loads the row's last eight
 // channels and shifts them down, so that nothing beyond the row is read, and stores four, two and one of them, as many as there are.
 // Rows of fewer than eight channels (kShort) are taken in parts (load_raw, store_piece).
-// kStream: whole pieces past the caches (kStreamBytes).  8192 x 4096 bf16, K = 8, which moves 338 MB: forward 70 -> 57 us, backward 79 -> 66.
+// kStream: whole pieces past the caches (kStreamBytes).  8192 x 4096 bf16, K = 8, which moves 338 MB: forward 70 -> 57 us,
+// backward 79 -> 66 (both with 1024 threads a unit).
 enum Form { kWhole, kRagged, kShort, kStream };
 
 // Where a lane's piece of a row lies: byte offsets in the row, kNowhere where there is nothing of the kind.
@@ -384,12 +386,12 @@ struct Shares {
   int64_t per_group = 0;  // teams of a group of rows (0: teams hold whole groups)
 };
 
-// Threads of a launch at most (256 compute units).  The backward: what stays on the units at once where a thread has two pieces, and half as many sums for the
-// second launch where it has one: 1024 / 512 threads a unit take 108 / 92 us at 4096 x 8192 bf16 with a gate a row, 64.4 / 59.4 at
-// 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32; 19.8 / 21 at 16384 x 200.
+// Threads of a launch at most (256 compute units).  The backward: what stays on the units at once where a thread has two pieces,
+// and half as many sums for the second launch where it has one: 1024 / 512 threads a unit take 108 / 92 us at 4096 x 8192 bf16
+// with a gate a row, 64.4 / 59.4 at 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32; 19.8 / 21 at 16384 x 200.
 constexpr int64_t kBwdThreads = 128 * 1024;
-// The forward, 2048 / 1024 threads a unit: 53.5 / 55.2 us at 8192 x 4096 bf16 and 9.4 / 10.3 at 1500 x 1112 fp32; rows of more pieces than
-// threads take the smaller launch (48 / 40 us at 1024 x 16384 bf16).
+// The forward, 2048 / 1024 threads a unit: 53.5 / 55.2 us at 8192 x 4096 bf16 and 9.4 / 10.3 at 1500 x 1112 fp32; rows of more
+// pieces than threads take the smaller launch (48 / 40 us at 1024 x 16384 bf16).
 constexpr int64_t fwd_threads(int pieces_a_thread) { return (pieces_a_thread == 1 ? 512 : 256) * 1024; }
 Shares shares_of(int64_t M, int64_t gate_rows, int team, bool gate) {
   const int64_t most = kBwdThreads / team;   // up to twice as many where groups are cut
