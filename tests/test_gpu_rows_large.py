@@ -73,6 +73,29 @@ def test_weight_gradient_of_large_products(M, Cin, Cout, dtype, flags, K):
 
 @pytest.mark.parametrize("K", [4, 8])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,Cin", [(4096, 4096), (500, 1001), (70, 70)])   # large tiles; shares, ragged; few rows
+def test_weight_gradient_reads_every_code_and_scale(M, Cin, dtype, K):
+    """dy is the identity: dW is the transposed store, exactly.  (Scales up to 2^115: no value overflows.)"""
+    blocks = (Cin + 31) // 32
+    gen = generator(K + M)
+    s = torch.zeros(B.abl_ckpt_bytes(M, Cin, K), dtype=torch.uint8, device="cuda")
+    codes = torch.randint(0, 256, (M * blocks, 4 * K), generator=gen, device="cuda").to(torch.uint8)
+    if K == 8:
+        codes[codes == 128] = 127   # (not a code)
+    s[:codes.numel()] = codes.flatten()
+    s[codes.numel():codes.numel() + M * blocks] = torch.randint(8, 243, (M * blocks,), generator=gen, device="cuda").to(torch.uint8)
+    x = torch.empty((M, Cin), dtype=torch.float32, device="cuda")
+    B.abl_ckpt_unpack(s, K, x)
+    assert bool(torch.isfinite(x).all()) and int((x == 0).sum()) < x.numel() // 4
+    dy = torch.eye(M, device="cuda").to(dtype)
+    ws = torch.full((B.abl_ckpt_wgrad_scratch_bytes(M, Cin, M, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
+    dW = torch.full((Cin, M), 7.0, device="cuda")
+    B.abl_ckpt_wgrad(s, K, None, dy, ws, dW)
+    assert torch.equal(dW, x.t())
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_weight_gradient_takes_a_slice_of_a_wide_tensor_and_leaves_nan_where_it_is(dtype, K):
     """Columns next to the slice hold NaN: a piece that reaches beyond the slice must not bring them into its sums."""
     gen = generator(3)
