@@ -528,22 +528,18 @@ struct Plan {
 //   256 x 128, fp32      7 and 1.0 a step, 1.25 where all units have a block (three products)
 //   128 x 128, fp32      4 and 0.68 a step, 0.85 where all units have one (its registers leave room for one)
 //   copies               4 for the second launch, 0.6 for each eight of them, their bytes written and read at 8.5 TB/s
-Plan plan_of(int64_t M, int Cin, int Cout, int dtype, bool parts) {
-  const int64_t size = dtype == ABL_F32 ? 4 : 2;
+// most: shares at most.
+Plan plan_of(int64_t M, int Cin, int Cout, bool parts, int64_t most) {
   Plan best;
   best.tiles_i = (Cin + 127) / 128, best.tiles_j = (Cout + 127) / 128, best.rows = M;
-  const int64_t room = (int64_t)1 << 30;   // bytes that a share's rows may span
-  const int64_t wide = Cout * size > (int64_t)Cin * 2 ? Cout * size : (int64_t)Cin * 2;
-  const int64_t least = (M * wide + room - 1) / room;   // shares that the descriptors ask for
   double time = 1e30;
   for (int large = 0; large < 2; ++large) {
     const int bi = large ? 256 : 128, bj = large && !parts ? 256 : 128;
     const int64_t ti = (Cin + bi - 1) / bi, tj = (Cout + bj - 1) / bj, tiles = ti * tj;
-    for (int64_t n = 1; n <= 64 || n < 2 * least; n *= 2) {
-      const int64_t want = n > least ? n : least;
-      const int64_t rows = ((M + want - 1) / want + 63) / 64 * 64;
+    for (int64_t n = 1; n <= 64; n *= 2) {
+      const int64_t rows = ((M + n - 1) / n + 63) / 64 * 64;
       const int64_t shares = M > 0 ? (M + rows - 1) / rows : 1, items = tiles * shares;
-      if (n > 1 && n > least && shares * Cin * Cout > (int64_t)24 << 20) break;   // (96 MB of copies)
+      if (shares > most || (n > 1 && shares * Cin * Cout > (int64_t)24 << 20)) break;   // (96 MB of copies)
       const double steps = (double)(rows < M ? rows : M) / 32, load = items < 256 ? (double)items / 256 : 1.0;
       const int64_t rounds = (items + 255) / 256;
       double t;
@@ -564,6 +560,31 @@ Plan plan_of(int64_t M, int Cin, int Cout, int dtype, bool parts) {
   return best;
 }
 
+// How M rows are cut into products, one after the other, of which all but the first add to dW: into as few as there can be (a power of two, up to
+// the last) for the offsets of a share, some steps beyond its end included, to fit 31 bits.  Where not even kFewest rows fit, and for fewer
+// than eight channels, whose pieces would reach beyond the tensor's end, the far kernel takes all rows.  8192 rows 2 MB apart, 4096 x 4096:
+// products 510 us, far kernel 700.
+struct Cut {
+  Plan plan;
+  int64_t rows;   // of a product
+  bool far;
+};
+constexpr int64_t kFewest = 256;
+bool offsets_fit(const Plan& p, int64_t row_bytes, int Cin) {
+  const int64_t x_bytes = store_blocks(Cin) * 32, wide = row_bytes > x_bytes ? row_bytes : x_bytes;
+  return (p.rows + 256) * wide < (int64_t)0x7FFFFF00;
+}
+Cut cut_of(int64_t M, int64_t row_bytes, int Cin, int Cout, bool parts, int64_t most) {
+  Cut c{plan_of(M, Cin, Cout, parts, most), M, Cout < 8};
+  if (c.far || offsets_fit(c.plan, row_bytes, Cin)) return c;
+  for (int64_t n = 2; c.rows > kFewest; n *= 2) {
+    c.rows = ((M + n - 1) / n + 63) / 64 * 64;
+    c.plan = plan_of(c.rows, Cin, Cout, parts, most);
+    if (offsets_fit(c.plan, row_bytes, Cin)) return c;
+  }
+  return Cut{plan_of(M, Cin, Cout, parts, most), M, true};
+}
+
 template <typename T, int NP, int BI, int BJ>
 int launch_tiles(hipStream_t st, int K, bool ragged, unsigned grid, const WgArgs& a) {
   auto kern = K == 8 ? (ragged ? store_wgrad_kernel<T, 8, NP, BI, BJ, true> : store_wgrad_kernel<T, 8, NP, BI, BJ, false>)
@@ -577,34 +598,23 @@ int launch_tiles(hipStream_t st, int K, bool ragged, unsigned grid, const WgArgs
 
 }  // namespace
 
-// (For any distance of dy's rows and either way of fp32: the copies are limited alike, so the most that a choice may take is asked for.)
+// (For either way of fp32 and any distance of dy's rows: rows that are farther apart take no more shares.)
 size_t store_wgrad_scratch_bytes(int64_t M, int Cin, int Cout, int dtype) {
   size_t most = 16;
   for (int parts = 0; parts < (dtype == ABL_F32 ? 2 : 1); ++parts) {
-    const Plan p = plan_of(M, Cin, Cout, dtype, parts != 0);
-    const size_t need = p.shares > 1 ? (size_t)p.shares * Cin * Cout * sizeof(float) : 16;
+    const int shares = cut_of(M, (int64_t)Cout * size_of(dtype), Cin, Cout, parts != 0, 64).plan.shares;
+    const size_t need = shares > 1 ? (size_t)shares * Cin * Cout * sizeof(float) : 16;
     if (need > most) most = need;
   }
   return most;
 }
 
-int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ckpt, int64_t M, int Cin, int K, const void* scale,
-                       Rows dy, int Cout, void* scratch, float* dW) {
-  const bool parts = dtype == ABL_F32 && !(flags & ABL_MATH_BF16), f32 = dtype == ABL_F32;
-  Plan p = plan_of(M, Cin, Cout, dtype, parts);
-  // (planned as if dy were contiguous, which the workspace is asked for without knowing.)  A share whose offsets, some steps beyond its end
-  // included, do not fit 31 bits takes the far kernel, and so do fewer than eight channels, where several rows' pieces would reach beyond
-  // the tensor's end.
-  const bool far = (p.rows + 256) * dy.ld * (f32 ? 4 : 2) >= (int64_t)0x7FFFFF00 || Cout < 8;
-  if (far) p.bi = p.bj = 128, p.tiles_i = (Cin + 127) / 128, p.tiles_j = (Cout + 127) / 128;
-  WgArgs a;
-  a.codes = (const unsigned char*)ckpt, a.scales = a.codes + store_code_bytes(M, Cin, K);
-  a.dy = dy.p, a.ldy = dy.ld, a.scale = scale, a.M = M, a.rows = p.rows, a.Cin = Cin, a.Cout = Cout, a.blocks = (int)store_blocks(Cin);
-  a.tiles_i = p.tiles_i, a.tiles_j = p.tiles_j, a.accum = (flags & ABL_ACCUM_DW) != 0;
-  a.copy = p.shares > 1 ? (int64_t)Cin * Cout : 0;
-  a.out = p.shares > 1 ? (float*)scratch : dW;
+static int launch_product(hipStream_t st, const Plan& p, bool far, bool f32, bool parts, int K, WgArgs a, float* copies, float* dW) {
+  a.rows = p.rows, a.tiles_i = p.tiles_i, a.tiles_j = p.tiles_j;
+  a.copy = p.shares > 1 ? (int64_t)a.Cin * a.Cout : 0;
+  a.out = p.shares > 1 ? copies : dW;
   const unsigned grid = (unsigned)(p.tiles_i * p.tiles_j * p.shares);
-  const bool ragged = Cout % 8 != 0;
+  const bool ragged = a.Cout % 8 != 0;
   int e;
   if (far) {
     auto kern = f32 ? (parts ? (K == 8 ? store_wgrad_far_kernel<float, 8, 3> : store_wgrad_far_kernel<float, 4, 3>)
@@ -620,10 +630,35 @@ int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ck
     e = p.bi == 256 ? launch_tiles<float, 3, 256, 128>(st, K, ragged, grid, a) : launch_tiles<float, 3, 128, 128>(st, K, ragged, grid, a);
   }
   if (e != ABL_OK || p.shares == 1) return e;
-  const int64_t size = (int64_t)Cin * Cout;
+  const int64_t size = (int64_t)a.Cin * a.Cout;
   auto sum = f32 ? wgrad_sum_kernel<float> : wgrad_sum_kernel<bf16_t>;
-  sum<<<(unsigned)((size + 1023) / 1024), 256, 0, st>>>((const float*)scratch, p.shares, size, scale, Divisor(Cout), a.accum, dW);
+  sum<<<(unsigned)((size + 1023) / 1024), 256, 0, st>>>(copies, p.shares, size, a.scale, Divisor(a.Cout), a.accum, dW);
   return hip_status();
+}
+
+int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ckpt, int64_t M, int Cin, int K, const void* scale,
+                       Rows dy, int Cout, void* scratch, float* dW) {
+  const bool parts = dtype == ABL_F32 && !(flags & ABL_MATH_BF16), f32 = dtype == ABL_F32;
+  const int64_t size = size_of(dtype), blocks = store_blocks(Cin);
+  const int64_t ld = M > 1 ? dy.ld : Cout;
+  Cut c = cut_of(M, Cout * size, Cin, Cout, parts, 64);
+  if (!c.far && !offsets_fit(c.plan, ld * size, Cin)) c = cut_of(M, ld * size, Cin, Cout, parts, c.plan.shares);
+  if (c.far) c.plan.bi = c.plan.bj = 128, c.plan.tiles_i = (Cin + 127) / 128, c.plan.tiles_j = (Cout + 127) / 128;
+  WgArgs a{};
+  a.ldy = ld, a.scale = scale, a.Cin = Cin, a.Cout = Cout, a.blocks = (int)blocks, a.accum = (flags & ABL_ACCUM_DW) != 0;
+  int64_t m = 0;
+  do {
+    a.M = m + c.rows < M ? c.rows : M - m;
+    a.codes = (const unsigned char*)ckpt + m * blocks * 4 * K;
+    a.scales = (const unsigned char*)ckpt + store_code_bytes(M, Cin, K) + m * blocks;
+    a.dy = (const char*)dy.p + m * ld * size;
+    Plan p = c.plan;
+    if (a.M < c.rows) p.shares = (int)((a.M + p.rows - 1) / p.rows);
+    if (int e = launch_product(st, p, c.far, f32, parts, K, a, (float*)scratch, dW)) return e;
+    a.accum = 1;
+    m += c.rows;   // (a multiple of 64 where more follow: pieces stay aligned)
+  } while (m < M);
+  return ABL_OK;
 }
 
 }  // namespace abl

@@ -122,6 +122,34 @@ def test_weight_gradient_takes_a_slice_of_a_wide_tensor_and_leaves_nan_where_it_
     within(dW[ok], torch.mm(a.t().contiguous(), y), U * (M + 8) * torch.mm(a.abs().t().contiguous(), y.abs()), "dW")
 
 
+@pytest.mark.parametrize("M,Cin,Cout,pitch,dtype,K", [
+    (40000, 96, 64, 1 << 16, torch.bfloat16, 8),         # shares of the rows are near enough
+    (5000, 4096, 4096, 1 << 19, torch.bfloat16, 8),      # products of 1280 rows, one after the other
+    (5000, 4000, 4099, 1 << 19, torch.float32, 4),       # of 640 rows, ragged
+    (20001, 2050, 2007, 1 << 18, torch.bfloat16, 4),     # with shares of their own
+    (5000, 1 << 19, 16, 16, torch.bfloat16, 4),          # a wide input
+    (300, 70, 40, 1 << 23, torch.bfloat16, 8),           # farther apart than products reach
+])
+def test_weight_gradient_of_rows_whose_offsets_pass_31_bits(M, Cin, Cout, pitch, dtype, K):
+    gen = generator(M + Cin)
+    s, x = stored(normal(gen, M, Cin), K)
+    big = torch.full((M, pitch), float("nan"), dtype=dtype, device="cuda")
+    dy = big[:, :Cout]
+    dy.copy_(normal(gen, M, Cout, std=0.02))
+    scale = normal(gen, Cin, std=0.2, dtype=dtype) + 1
+    w, y = scale.double()[:, None], dy.double()
+    want = w * torch.mm(x.t().contiguous(), y)
+    size = w.abs() * torch.mm(x.abs().t().contiguous(), y.abs())
+    ws = torch.full((B.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert ws.numel() <= 256 << 20
+    dW = torch.full((Cin, Cout), 7.0, device="cuda")
+    B.abl_ckpt_wgrad(s, K, scale, dy, ws, dW)
+    within(dW, want, U * (M + 8) * size, "dW")
+    again = dW.clone()
+    B.abl_ckpt_wgrad(s, K, scale, dy, ws, again, B.ABL_ACCUM_DW)
+    within(again, want + dW.double(), U * (M + 10) * (size + dW.double().abs()), "dW accumulated")
+
+
 @pytest.mark.parametrize("M,C,K,gate_rows", [(8192, 4096, 8, 2048), (4096, 8192, 4, 1), (70000, 1500, 8, 0), (9000, 4104, 8, 9000)])
 def test_step_on_tensors_beyond_the_caches(M, C, K, gate_rows):
     gen = generator(C)

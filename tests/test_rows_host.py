@@ -204,3 +204,11 @@ def test_wgrad_refuses():
         assert 0 < need <= 256 << 20
         assert call(M=M, Cin=ci, Cout=co, lddy=co, bytes=need - 1) == B.ABL_ERR_SCRATCH
     assert B.abl_ckpt_wgrad_scratch_bytes(4, 64, 64, torch.float16) == 0
+
+
+def test_wgrad_workspace_stays_small_for_long_batches():
+    """Rows beyond what one product's offsets reach are further products: no copies of dW for them."""
+    import torch
+    for M, ci, co in ((1 << 18, 8192, 32768), (1 << 20, 4096, 8192), (1 << 13, 1 << 20, 2047), (1 << 13, 2047, 1 << 20), (1 << 22, 96, 64)):
+        for dtype in (torch.bfloat16, torch.float32):
+            assert 0 < B.abl_ckpt_wgrad_scratch_bytes(M, ci, co, dtype) <= 256 << 20
