@@ -720,7 +720,7 @@ void by_team(int C, int64_t bytes, F&& f) {
 int launch_resnorm_forward(hipStream_t st, const abl_resnorm& s, const void* r, const void* b, const void* gate, const void* w_post,
                            const void* w_pre, void* r_out, void* n, void* ckpt_b, float* rstd_b, void* ckpt_n, float* rstd_n) {
   FwdArgs a;
-  a.M = s.M, a.gate_rows = s.gate_rows, a.r = r, a.b = b, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
+  a.M = s.M, a.gate_rows = s.gate_rows < s.M ? s.gate_rows : s.M, a.r = r, a.b = b, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
   a.r_out = r_out, a.n = n, a.ckpt_b = (unsigned char*)ckpt_b, a.ckpt_n = (unsigned char*)ckpt_n;
   a.rstd_b = rstd_b, a.rstd_n = rstd_n, a.C = s.C, a.pieces = (int)store_blocks(s.C) * 4;
   a.center = (s.flags & ABL_NORM_CENTER) != 0, a.alpha = s.alpha, a.beta = s.beta, a.eps = s.eps, a.inv_c = 1.0 / s.C;
@@ -757,14 +757,14 @@ size_t resnorm_scratch_bytes(int64_t M, int C) {
 int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, bool has_b, const void* dn, const void* dr_out, const void* gate,
                             const void* w_post, const void* w_pre, const void* ckpt_b, const float* rstd_b, const void* ckpt_n,
                             const float* rstd_n, void* scratch, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre) {
-  const int64_t groups = gate != nullptr ? (s.M + s.gate_rows - 1) / s.gate_rows : 0;
+  const int64_t groups = gate != nullptr && s.M > 0 ? (s.M - 1) / s.gate_rows + 1 : 0;
   if (s.M == 0) {
     for (float* p : {dw_pre, dw_post})
       if (p != nullptr) zero_kernel<<<(unsigned)((s.C + 255) / 256), 256, 0, st>>>(p, s.C);
     return hip_status();
   }
   BwdArgs a;
-  a.M = s.M, a.gate_rows = s.gate_rows, a.dn = dn, a.dr_out = dr_out, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
+  a.M = s.M, a.gate_rows = s.gate_rows < s.M ? s.gate_rows : s.M, a.dn = dn, a.dr_out = dr_out, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
   a.ckpt_b = (const unsigned char*)ckpt_b, a.ckpt_n = (const unsigned char*)ckpt_n, a.rstd_b = rstd_b, a.rstd_n = rstd_n;
   a.dr = dr, a.db = db, a.dgate = dgate, a.part = (float*)scratch;
   a.C = s.C, a.pieces = (int)store_blocks(s.C) * 4, a.center = (s.flags & ABL_NORM_CENTER) != 0;

@@ -125,7 +125,7 @@ PyObject* ckpt_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return code(abl_ckpt_unpack(stream(), dtype_of(x.type), s, x.M, (int32_t)x.C, (int)K, x.p, x.ld));
 }
 
-int64_t groups_of(int64_t M, long rows) { return rows > 0 ? (M + rows - 1) / rows : 0; }
+int64_t groups_of(int64_t M, long rows) { return rows > 0 && M > 0 ? (M - 1) / rows + 1 : 0; }
 
 // (r, b, gate, gate_rows, w_post, w_pre, r_out, n, K, ckpt_b, rstd_b, ckpt_n, rstd_n, alpha, beta, eps, flags)
 PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {

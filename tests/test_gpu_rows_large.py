@@ -150,6 +150,27 @@ def test_weight_gradient_of_rows_whose_offsets_pass_31_bits(M, Cin, Cout, pitch,
     within(again, want + dW.double(), U * (M + 10) * (size + dW.double().abs()), "dW accumulated")
 
 
+@pytest.mark.parametrize("M,C", [(70, 200), (600, 1111)])
+def test_one_gate_row_for_any_number_of_rows(M, C):
+    """gate_rows far beyond the rows: as one group of them all."""
+    gen, K = generator(C), 8
+    r, b, dn, dr_out = (normal(gen, M, C) for _ in range(4))
+    gate, w = normal(gen, 1, C), normal(gen, C)
+    results = []
+    for rows in (M, 2 ** 62, 2 ** 63 - 1):
+        sb, sn = (torch.zeros(B.abl_ckpt_bytes(M, C, K), dtype=torch.uint8, device="cuda") for _ in range(2))
+        rb, rn = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+        r2, n, dr, db = (torch.empty_like(r) for _ in range(4))
+        dg, dp, dq = torch.empty(1, C, device="cuda"), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ws = torch.empty(B.abl_resnorm_scratch_bytes(M, C), dtype=torch.uint8, device="cuda")
+        B.abl_resnorm_forward(r, b, gate, rows, w, w, r2, n, K, sb, rb, sn, rn)
+        B.abl_resnorm_backward(dn, dr_out, gate, rows, w, w, K, sb, rb, sn, rn, ws, dr, db, dg, dp, dq)
+        results.append((r2, n, sb, sn, rb, rn, dr, db, dg, dp, dq))
+    for other in results[1:]:
+        for a, c in zip(results[0], other):
+            assert torch.equal(a, c)
+
+
 @pytest.mark.parametrize("M,C,K,gate_rows", [(8192, 4096, 8, 2048), (4096, 8192, 4, 1), (70000, 1500, 8, 0), (9000, 4104, 8, 9000)])
 def test_step_on_tensors_beyond_the_caches(M, C, K, gate_rows):
     gen = generator(C)
