@@ -301,3 +301,53 @@ def test_network_trains_as_the_exact_one():
     assert exact[-1] < 0.95 * exact[0]
     np.testing.assert_allclose(curves["K=8"], exact, rtol=0.01)
     np.testing.assert_allclose(curves["K=4"], exact, rtol=0.06)
+
+
+def empty_store(M, C, K):
+    return torch.empty(B.abl_ckpt_bytes(M, C, K), dtype=torch.uint8, device="cuda")
+
+
+def test_step_on_tensors_of_more_than_4_gb():
+    """The last rows, as a tensor of their own, give the same bits."""
+    M, C, K, tail = 300001, 8192, 8, 65
+    gen = generator(5)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    r, b, dn, dr_out = (torch.randn(M, C, generator=gen, **bf) for _ in range(4))
+    gate, w = normal(gen, 1, C, dtype=torch.bfloat16), normal(gen, C, dtype=torch.bfloat16)
+
+    def step(r, b, dn, dr_out):
+        M = len(r)
+        sb, sn, rb, rn = empty_store(M, C, K), empty_store(M, C, K), torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+        r2, n, dr, db = (torch.empty_like(r) for _ in range(4))
+        dg, dp, dq = torch.empty(1, C, device="cuda"), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ws = torch.empty(B.abl_resnorm_scratch_bytes(M, C), dtype=torch.uint8, device="cuda")
+        B.abl_resnorm_forward(r, b, gate, M, w, w, r2, n, K, sb, rb, sn, rn)
+        B.abl_resnorm_backward(dn, dr_out, gate, M, w, w, K, sb, rb, sn, rn, ws, dr, db, dg, dp, dq)
+        values = torch.empty_like(r)
+        B.abl_ckpt_unpack(sn, K, values)
+        return r2, n, rb, rn, dr, db, values
+
+    whole = [t[-tail:].clone() for t in step(r, b, dn, dr_out)]
+    part = step(*(t[-tail:].clone() for t in (r, b, dn, dr_out)))
+    for a, c in zip(whole, part):
+        assert torch.equal(a, c)
+
+
+def test_gated_unit_on_tensors_of_more_than_4_gb():
+    M, F, K, tail = 70001, 32768, 8, 33
+    gen = generator(6)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    gu, dh = torch.randn(M, 2 * F, generator=gen, **bf), torch.randn(M, F, generator=gen, **bf)
+
+    def unit(gu, dh):
+        M = len(gu)
+        sg, su, sh = (empty_store(M, F, K) for _ in range(3))
+        h, dgu, values = torch.empty_like(dh), torch.empty_like(gu), torch.empty_like(dh)
+        B.abl_glu_forward(gu[:, :F], gu[:, F:], h, B.ABL_ACT_SILU, K, sg, su)
+        B.abl_glu_backward(dh, sg, su, K, dgu[:, :F], dgu[:, F:], B.ABL_ACT_SILU, sh)
+        B.abl_ckpt_unpack(sh, K, values)
+        return h, dgu, values
+
+    whole = [t[-tail:].clone() for t in unit(gu, dh)]
+    for a, c in zip(whole, unit(gu[-tail:].clone(), dh[-tail:].clone())):
+        assert torch.equal(a, c)
