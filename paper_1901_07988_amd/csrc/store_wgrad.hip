@@ -6,7 +6,7 @@
 // reaches 2420 TFLOP/s on zeros and 2050 on normal data.  Without decoding it would take 374, without loads 368, without staging
 // 294, with a quarter of the matrix instructions 292: the two halves of a step overlap, not perfectly.  dy straight from memory to
 // LDS, past the registers, measured the same.  4096 x 4096 x 4096: 114 us (1210 TFLOP/s); fp32 at 8192 x 1024 x 4096, three
-// products: 181 us.
+// products: 178 us.
 //
 // A stored value is a code of at most eight bits times a power of two, so it is exact in bf16: the codes become the bf16 operand of the
 // matrix cores while a tile is staged and nothing is rounded.  dy in bf16 goes in as it is, dy in fp32 as
@@ -222,9 +222,12 @@ __global__ __launch_bounds__(256) void store_wgrad_far_kernel(WgArgs a) {
 //   phase 2 s      waves 0-3 read step s and write their share of tile s + 1       waves 4-7 multiply step s - 1
 //   phase 2 s + 1  waves 0-3 multiply step s                                       waves 4-7 read step s, write tile s + 1
 // Two tiles in LDS are enough: tile s + 1 replaces tile s - 1, which waves 4-7 read in phase 2 s - 1.
+// Blocks that a compute unit holds (ragged tiles of three parts lack a few registers; with them spilled they take 1 us more).
+template <int BI, int NP, bool RAGGED>
+constexpr int kPerUnit = BI > 128 || (NP == 3 && RAGGED) ? 1 : 2;
 template <typename T, int K, int NP, int BI, int BJ, bool RAGGED>
-__global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_wgrad_kernel(WgArgs a) {
-  constexpr int BK = 32, WI = 4, WJ = 2;
+__global__ __launch_bounds__(512, (kPerUnit<BI, NP, RAGGED> * 2)) void store_wgrad_kernel(WgArgs a) {
+  constexpr int BK = 32, WI = NP == 3 ? 2 : 4, WJ = 8 / WI;   // (three parts: fewer columns of dy a wave)
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;
   constexpr int XP = BI / 128;                       // pieces of x of a thread
   constexpr int PY = BK * BJ / 8 / 512;              // pieces of dy of a thread
@@ -259,14 +262,13 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
   const uint32_t s_at = block < a.blocks ? (uint32_t)xr * (uint32_t)a.blocks + (uint32_t)block : kNowhere;
   const uint32_t c_at = block < a.blocks ? s_at * (4u * K) + (uint32_t)(xq & 3) * K : kNowhere;
   uint32_t y_at[PY];
-  int y_row[PY];   // RAGGED: its row in a tile; the piece of the last row that is not whole is left out here and added at the end
-  bool y_part[PY];
+  int y_row[PY];   // RAGGED: its row in a tile, one more for a piece that is not whole: that of the last row is left out here and added at the end
 #pragma unroll
   for (int p = 0; p < PY; ++p) {
     const int c = j0 + (p * 512 + tid) % (BJ / 8) * 8;
     y_row[p] = (p * 512 + tid) / (BJ / 8);
-    y_part[p] = c < a.Cout && c + 8 > a.Cout;
     y_at[p] = c < a.Cout ? ((uint32_t)y_row[p] * (uint32_t)a.ldy + (uint32_t)c) * (uint32_t)sizeof(T) : kNowhere;
+    if (RAGGED && ends && c < a.Cout && c + 8 > a.Cout) ++y_row[p];
   }
   const uint32_t c_step = (uint32_t)a.blocks * (4u * K * BK), s_step = (uint32_t)a.blocks * BK, y_step = (uint32_t)a.ldy * (uint32_t)(sizeof(T) * BK);
 
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
 #pragma unroll
     for (int p = 0; p < PY; ++p) {
       uint32_t of = y_at[p];
-      if constexpr (RAGGED) of = y_row[p] < left - (ends && y_part[p] ? 1 : 0) ? of : kNowhere;
+      if constexpr (RAGGED) of = y_row[p] < left ? of : kNowhere;
       if constexpr (std::is_same_v<T, float>) {
         t.r[p].a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at, 0));
         t.r[p].b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at + 16, 0));
@@ -440,6 +442,27 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
 
   const bool whole = a.copy == 0;
   float* out = a.out + share * a.copy;
+  // The piece of the last row that was left out: its loads on their way together, from places that exist.
+  float last_x[FI] = {}, last_y[FJ][4] = {};
+  if constexpr (RAGGED) {
+    const int part = a.Cout / 8 * 8;   // its first column
+    if (ends && a.M > 0 && j0 + BJ > part && j0 < a.Cout) {
+      const T* row = (const T*)a.dy + (a.M - 1) * a.ldy;
+#pragma unroll
+      for (int i = 0; i < FI; ++i) {
+        const int ci = i0 + wi + 16 * i + (lane & 15);
+        last_x[i] = stored_value<K>(a, a.M - 1, ci < a.Cin ? ci : a.Cin - 1);
+      }
+#pragma unroll
+      for (int j = 0; j < FJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int cj = j0 + wj + 16 * j + (lane >> 4) * 4 + e;
+          const float yv = (float)row[cj < a.Cout ? cj : a.Cout - 1];
+          last_y[j][e] = NP == 1 ? (float)(__bf16)yv : yv;
+        }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
     const int ci = i0 + wi + 16 * i + (lane & 15);
@@ -450,15 +473,9 @@ __global__ __launch_bounds__(512, BI * BJ * NP > 128 * 128 ? 2 : 4) void store_w
       const int cj = j0 + wj + 16 * j + (lane >> 4) * 4;
       float* to = out + (int64_t)ci * a.Cout + cj;
       f32x4_any4 v = acc[i][j];
-      if (RAGGED && ends && a.M > 0 && cj + 4 > a.Cout / 8 * 8 && cj < a.Cout) {
-        const float xv = stored_value<K>(a, a.M - 1, ci);
-        const T* row = (const T*)a.dy + (a.M - 1) * a.ldy;
+      if (RAGGED && cj >= a.Cout / 8 * 8) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (cj + e < a.Cout / 8 * 8 || cj + e >= a.Cout) continue;
-          const float yv = (float)row[cj + e];
-          v[e] = __builtin_fmaf(xv, NP == 1 ? (float)(__bf16)yv : yv, v[e]);
-        }
+        for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(last_x[i], last_y[j][e], v[e]);
       }
       v *= s;
       if (cj + 4 <= a.Cout) {
@@ -521,36 +538,38 @@ struct Plan {
   int64_t rows = 0;
 };
 
-// The choice with the least time by these estimates, in us as measured on products of 128 to 16384 rows and 256 to 4096 channels (a
-// step is 32 rows).  With every tiling and cut timed on 15 such products of either type, the choice is within 9 % of the best.
-//   256 x 256, bf16      one block a compute unit: 7 and 0.65 a step, 0.85 where all units have one
-//   128 x 128, bf16      4 and 0.34 a step, or 0.56 with two blocks on a unit
-//   256 x 128, fp32      7 and 1.0 a step, 1.25 where all units have a block (three products)
-//   128 x 128, fp32      4 and 0.68 a step, 0.85 where all units have one (its registers leave room for one)
-//   copies               4 for the second launch, 0.6 for each eight of them, their bytes written and read at 8.5 TB/s
+// The choice with the least time by these estimates, in us, fitted to 20 products of either type (128 to 16384 rows, 256 to 4096 channels, K = 8),
+// each timed with both tilings and 1 to 64 shares.  On these and 12 others the choices are within 9 % of the fastest, most within 3 %.
+// A step of 32 rows: `one` with a block on a compute unit and `load` more where all units have one, `two` with two blocks on a unit.
+// `second`, `eight`: the launch that adds the shares' copies, and more for each eight; `bytes_per_us`: of the copies, written and read.
+struct Cost {
+  double one, load, two, start, second, eight, bytes_per_us;
+};
+constexpr Cost kCost[2][2] = {   // dy in one part: tiles of 128 x 128, 256 x 256; in three: 128 x 128, 256 x 128
+    {{0.28, 0.068, 0.579, 5.8, 3.3, 0.38, 8.5e6}, {0.542, 0.127, 0.0, 11.4, 3.3, 0.38, 8.5e6}},
+    {{0.551, 0.19, 1.23, 7.7, 3.4, 0.73, 11.3e6}, {0.837, 0.246, 0.0, 9.1, 3.4, 0.73, 11.3e6}}};
+constexpr int kShares[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 24, 32, 48, 64};
+constexpr int64_t kUnits = 256, kFewestRows = 192;   // of a share, if there are several
 // most: shares at most.
 Plan plan_of(int64_t M, int Cin, int Cout, bool parts, int64_t most) {
   Plan best;
   best.tiles_i = (Cin + 127) / 128, best.tiles_j = (Cout + 127) / 128, best.rows = M;
   double time = 1e30;
   for (int large = 0; large < 2; ++large) {
+    const Cost& c = kCost[parts][large];
     const int bi = large ? 256 : 128, bj = large && !parts ? 256 : 128;
     const int64_t ti = (Cin + bi - 1) / bi, tj = (Cout + bj - 1) / bj, tiles = ti * tj;
-    for (int64_t n = 1; n <= 64; n *= 2) {
+    const int64_t held = large || (parts && Cout % 8 != 0) ? kUnits : 2 * kUnits;    // blocks
+    for (int n : kShares) {
+      if (n > 1 && n * kFewestRows > M) break;
       const int64_t rows = ((M + n - 1) / n + 63) / 64 * 64;
       const int64_t shares = M > 0 ? (M + rows - 1) / rows : 1, items = tiles * shares;
       if (shares > most || (n > 1 && shares * Cin * Cout > (int64_t)24 << 20)) break;   // (96 MB of copies)
-      const double steps = (double)(rows < M ? rows : M) / 32, load = items < 256 ? (double)items / 256 : 1.0;
-      const int64_t rounds = (items + 255) / 256;
-      double t;
-      if (large) {
-        t = (double)rounds * (steps * (parts ? 1.0 + 0.25 * load : 0.65 + 0.2 * load) + 7);
-      } else if (parts) {
-        t = (double)rounds * (steps * (0.68 + 0.17 * load) + 4);
-      } else {
-        t = (double)(rounds / 2) * (steps * 0.56 + 4) + (double)(rounds % 2) * (steps * 0.34 + 4);
-      }
-      if (shares > 1) t += 4 + 0.6 * (double)((shares + 7) / 8) + (double)shares * Cin * Cout * 8 / 8.5e6;
+      const double steps = (double)(rows < M ? rows : M) / 32;
+      const int64_t rounds = items / held, rest = items % held;
+      double t = (double)rounds * (steps * (held == kUnits ? c.one + c.load : c.two) + c.start);
+      if (rest > 0) t += steps * (rest <= kUnits ? c.one + c.load * (double)rest / kUnits : c.two) + c.start;
+      if (shares > 1) t += c.second + c.eight * (double)((shares + 7) / 8) + (double)(shares * Cin * Cout * 8) / c.bytes_per_us;
       if (t < time) {
         time = t;
         best.bi = bi, best.bj = bj, best.tiles_i = (int)ti, best.tiles_j = (int)tj, best.shares = (int)shares, best.rows = rows;
