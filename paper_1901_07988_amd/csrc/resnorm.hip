@@ -7,10 +7,11 @@
 //   db = rstd_b (v - y mean(v y)),   v = e gate w_post
 //
 // Both are bound by memory: an element of bf16 costs 8 bytes and its two stores (10.1 at K = 8).  8192 x 4096 bf16 with a gate for
-// 2048 rows, K = 8 (338 MB): forward 54 us (6.2 TB/s, as a copy), backward 60 with the second launch (5.6); calls of a few rows
-// are the launch: 8 rows 3.9 us.  A team of threads holds a row in registers, so that every tensor is read once; the sums over a
-// row go through the waves' registers and, between waves, LDS.  In the backward a team takes consecutive rows and keeps its share
-// of the sums over rows in registers as well; the teams' sums are added in a fixed order by a second launch.
+// 2048 rows, K = 8 (338 MB): forward 54 us (6.2 TB/s, as a copy; 64 after passes whose output the caches still have to write),
+// backward 60 with the second launch (5.6); calls of a few rows are the launch: 8 rows 3.9 us.  A team of threads holds a row in
+// registers, so that every tensor is read once; the sums over a row go through the waves' registers and, between waves, LDS.  In
+// the backward a team takes consecutive rows and keeps its share of the sums over rows in registers as well; the teams' sums are
+// added in a fixed order by a second launch.
 
 #include <utility>
 
@@ -388,7 +389,8 @@ struct Shares {
 
 // Threads of a launch at most (256 compute units).  The backward: what stays on the units at once where a thread has two pieces,
 // and half as many sums for the second launch where it has one: 1024 / 512 threads a unit take 108 / 92 us at 4096 x 8192 bf16
-// with a gate a row, 64.4 / 59.4 at 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32; 19.8 / 21 at 16384 x 200.
+// with a gate a row, 64.4 / 59.4 at 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32 (with teams of 256);
+// 19.8 / 21 at 16384 x 200.
 constexpr int64_t kBwdThreads = 128 * 1024;
 // The forward, 2048 / 1024 threads a unit: 53.5 / 55.2 us at 8192 x 4096 bf16 and 9.4 / 10.3 at 1500 x 1112 fp32; rows of more
 // pieces than threads take the smaller launch (48 / 40 us at 1024 x 16384 bf16).
@@ -682,11 +684,13 @@ __global__ __launch_bounds__(256) void zero_kernel(float* p, int64_t n) {
 }
 
 // Threads of a team for rows of so many pieces: a piece for each up to 512 threads, then two and four (a block of 1024 threads has too few
-// registers for the backward: 4096 x 8192 bf16 took 162 us).
+// registers for the backward: 4096 x 8192 bf16 took 162 us).  Between 128 and 256 also 192: 1500 x 1111 fp32 11.0 us forward and 17.4 backward,
+// with 256 11.8 and 18.6.  384 and 768 lose to 512 threads with idle ones or two pieces: 8192 x 2560 bf16 50 and 60 us instead of 45 and 54,
+// 4096 x 5120 51 and 66 instead of 46 and 56.
 int team_of(int pieces) {
-  int t = 64;
-  while (t < pieces && t < 512) t *= 2;
-  return t;
+  for (int t : {64, 128, 192, 256})
+    if (pieces <= t) return t;
+  return 512;
 }
 
 // f(TEAM, NV, FORM) as constants.
@@ -705,6 +709,7 @@ void by_team(int C, int64_t bytes, F&& f) {
   switch (team_of(pieces)) {
     case 64: return form(std::integral_constant<int, 64>{}, one);
     case 128: return form(std::integral_constant<int, 128>{}, one);
+    case 192: return form(std::integral_constant<int, 192>{}, one);
     case 256: return form(std::integral_constant<int, 256>{}, one);
     default: {
       const std::integral_constant<int, 512> team;

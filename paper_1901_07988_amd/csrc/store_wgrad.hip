@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void store_wgrad_far_kernel(WgArgs a) {
 }
 
 // ---- the product ----
-// A block of eight waves has a tile of 256 channels of x and BJ of dy, a wave 64 x BJ / 2 of it.  Waves w and w + 4 share a SIMD and take turns:
+// A block of eight waves has a tile of BI channels of x and BJ of dy, a wave an eighth of it.  Waves w and w + 4 share a SIMD and take turns:
 // while one issues the matrix instructions of a step of 32 rows, the other reads its next fragments from LDS and writes its share of the next
 // tile there; a barrier changes the roles, and waves 4 to 7 are one barrier behind.  A wave issues an instruction about every four cycles, so what
 // needs registers only - codes to bf16, the loads of later tiles - goes between its matrix instructions, which leave three such places each.

@@ -351,3 +351,12 @@ def test_gated_unit_on_tensors_of_more_than_4_gb():
     whole = [t[-tail:].clone() for t in unit(gu, dh)]
     for a, c in zip(whole, unit(gu[-tail:].clone(), dh[-tail:].clone())):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("M,C,K,gate_rows", [
+    (3000, 1025, 8, 3000), (2500, 1280, 8, 500), (2000, 1529, 4, 1), (3000, 1536, 8, 0), (1500, 1537, 8, 300),   # teams of 192 threads, and of 256 beside them
+    (40000, 1280, 8, 2000),                                                                                      # beyond the caches
+    (1000, 500, 8, 250), (1000, 513, 8, 1), (1000, 1016, 4, 0),
+])
+def test_step_at_the_widths_where_teams_change(M, C, K, gate_rows):
+    test_step_on_tensors_beyond_the_caches(M, C, K, gate_rows)
