@@ -754,7 +754,7 @@ size_t resnorm_scratch_bytes(int64_t M, int C) {
   // The blocks without a gate, and where groups of rows are cut: a group of g rows takes at most g / rows + 1 teams, or a block more where a block
   // has four, and there are M / g + 1 groups of more than `rows` rows, so at most M / rows + M / g + g / rows + ... <= 2 M / rows + 2 blocks' worth.
   const int team = team_of(pieces);
-  const Shares s = shares_of(M, 0, team, false);
+  const Shares s = shares_of(M > 0 ? M : 1, 0, team, false);   // (no rows: a size that is never 0 for valid arguments)
   const int64_t blocks = 2 * s.teams + 2;
   return (size_t)blocks * 3 * pieces * 8 * sizeof(float);
 }

@@ -212,3 +212,13 @@ def test_wgrad_workspace_stays_small_for_long_batches():
     for M, ci, co in ((1 << 18, 8192, 32768), (1 << 20, 4096, 8192), (1 << 13, 1 << 20, 2047), (1 << 13, 2047, 1 << 20), (1 << 22, 96, 64)):
         for dtype in (torch.bfloat16, torch.float32):
             assert 0 < B.abl_ckpt_wgrad_scratch_bytes(M, ci, co, dtype) <= 256 << 20
+
+
+def test_workspaces_of_no_rows_have_a_size():
+    """M = 0 is a valid batch: every size is given, and none is that of invalid arguments."""
+    import torch
+    for C in (1, 64, 513, 1111, 8193, 16384):
+        assert 0 < B.abl_resnorm_scratch_bytes(0, C) <= B.abl_resnorm_scratch_bytes(1, C)
+        assert B.abl_ckpt_bytes(0, C, 4) == B.abl_ckpt_bytes(0, C, 8) == 128
+        for dtype in (torch.bfloat16, torch.float32):
+            assert B.abl_ckpt_wgrad_scratch_bytes(0, C, C, dtype) > 0
