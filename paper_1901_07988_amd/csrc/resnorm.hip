@@ -25,7 +25,9 @@ __device__ inline int left(int C, uint32_t c) { return C - (int)c; }
 
 // ---- a team's rows in memory ----
 // A team has consecutive rows, and accesses go through buffer descriptors of them: a lane beyond the row's end has an offset beyond
-// the descriptor, and a tensor that is not there has a descriptor of no bytes; both read zero and store nothing.  Without branches
+// the descriptor, and a tensor that is not there has a descriptor of no bytes; both read zero and store nothing.  (An access is out of
+// range where its own offset is not below the descriptor's bytes less the scalar offset.  So that this difference is never
+// negative, what may be absent takes no row's offset where it is.)  Without branches
 // around them the compiler can count the accesses on their way, so waiting for the next row's loads does not wait for
 // this row's stores, and from row to row only three scalar offsets change.  (A store takes the sum of its offsets in a vector register:
 // with the row's in the instruction's scalar operand the compiler lets the next instruction overwrite the store's data, and wrong
@@ -83,8 +85,8 @@ __device__ inline void shift_down(Raw<float>& r, uint32_t by) {
   r.a = f32x4_any4{w[0], w[1], w[2], w[3]}, r.b = f32x4_any4{w[4], w[5], w[6], w[7]};
 }
 
-// Rows of T from `first` on.
-template <typename T, Form FORM>
+// Rows of T from `first` on.  MAYBE: may be absent.
+template <typename T, Form FORM, bool MAYBE = false>
 struct TeamRows {
   const T* p;
   int C;
@@ -98,11 +100,13 @@ struct TeamRows {
     if constexpr (FORM == kShort) {
       return p != nullptr ? load_raw(p + (int64_t)k * C + l.q * 8, left(C, l.q * 8)) : Raw<T>{};
     } else {
-      const uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
+      uint32_t row = k * (uint32_t)C * (uint32_t)sizeof(T);
+      if constexpr (MAYBE) row = p != nullptr ? row : 0;
       if constexpr (std::is_same_v<T, float>) {
         Raw<float> r;
         r.a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row, kAux));
-        r.b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row + 16, kAux));
+        r.b = __builtin_bit_cast(f32x4_any4, MAYBE ? __builtin_amdgcn_raw_buffer_load_b128(d, l.at + 16, row, kAux)
+                                                   : __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row + 16, kAux));
         return r;
       } else {
         return Raw<bf16_t>{__builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(d, l.at, row, kAux))};
@@ -154,21 +158,23 @@ struct StoreLane {   // byte offsets in a row of a lane's codes (over K) and sca
     own = in && (piece & 3u) == 0 ? piece >> 2 : kNowhere;
   }
 };
-template <int K>
+template <int K, bool MAYBE = false>
 struct StoreRows {
   __amdgpu_buffer_rsrc_t codes, scales;
   uint32_t pieces;
+  bool there;
   __device__ inline StoreRows(const unsigned char* store, int64_t M, int n, int64_t first, int64_t rows)
       : codes(descriptor(store != nullptr ? store + first * n * K : nullptr, rows * n * K)),
         scales(descriptor(store != nullptr ? store + M * n * K + (first * n >> 2) : nullptr, rows * n >> 2)),
-        pieces((uint32_t)n) {}
+        pieces((uint32_t)n), there(!MAYBE || store != nullptr) {}
   static __device__ inline uint32_t at(const StoreLane& l) { return l.q < kNowhere / 8 ? l.q * K : kNowhere; }
   __device__ inline void load(uint32_t k, const StoreLane& l, Codes<K>& c, uint32_t& byte) const {
+    const uint32_t of = there ? k * pieces * K : 0, of_scale = there ? k * (pieces >> 2) : 0;
     if constexpr (K == 8)
-      c.w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at(l), k * pieces * 8, 0));
+      c.w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at(l), of, 0));
     else
-      c.w = __builtin_amdgcn_raw_buffer_load_b32(codes, at(l), k * pieces * 4, 0);
-    byte = __builtin_amdgcn_raw_buffer_load_b8(scales, l.scale, k * (pieces >> 2), 0);
+      c.w = __builtin_amdgcn_raw_buffer_load_b32(codes, at(l), of, 0);
+    byte = __builtin_amdgcn_raw_buffer_load_b8(scales, l.scale, of_scale, 0);
   }
   __device__ inline void keep(uint32_t k, const StoreLane& l, const float (&v)[8]) const {
     const uint32_t byte = scale_byte<K>(v);
@@ -305,7 +311,8 @@ __global__ __launch_bounds__(kBlock<TEAM>, NV >= 2 ? 2 : 4) void resnorm_fwd_ker
   if (first >= a.M) return;   // (a whole wave; blocks of larger teams are as many as teams)
   const uint32_t rows = (uint32_t)(first + a.rows < a.M ? a.rows : a.M - first);
   using In = TeamRows<T, FORM>;
-  const In from_r(a.r, first, rows, a.C), from_b(a.b, first, rows, a.C), to_r(a.r_out, first, rows, a.C), to_n(a.n, first, rows, a.C);
+  const TeamRows<T, FORM, true> from_b(a.b, first, rows, a.C);
+  const In from_r(a.r, first, rows, a.C), to_r(a.r_out, first, rows, a.C), to_n(a.n, first, rows, a.C);
   const StoreRows<K == 0 ? 8 : K> keep_b(K != 0 ? a.ckpt_b : nullptr, a.M, a.pieces, first, rows);
   const StoreRows<K == 0 ? 8 : K> keep_n(K != 0 ? a.ckpt_n : nullptr, a.M, a.pieces, first, rows);
   const auto lane = lanes<T, FORM, TEAM>(t, a.C, a.pieces, std::make_integer_sequence<int, NV>{});
@@ -491,8 +498,10 @@ __global__ __launch_bounds__(kBlock<TEAM>, NV == 1 ? 4 : 2) void resnorm_bwd_ker
   const int64_t first = row;
   const uint32_t rows = row < end ? (uint32_t)(end - row) : 0;
   using In = TeamRows<T, FORM>;
-  const In from_dn(a.dn, first, rows, a.C), from_dr(a.dr_out, first, rows, a.C), to_r(a.dr, first, rows, a.C), to_b(a.db, first, rows, a.C);
-  const StoreRows<K> kept_n(a.ckpt_n, a.M, a.pieces, first, rows), kept_b(a.ckpt_b, a.M, a.pieces, first, rows);
+  const TeamRows<T, FORM, true> from_dr(a.dr_out, first, rows, a.C);
+  const In from_dn(a.dn, first, rows, a.C), to_r(a.dr, first, rows, a.C), to_b(a.db, first, rows, a.C);
+  const StoreRows<K> kept_n(a.ckpt_n, a.M, a.pieces, first, rows);
+  const StoreRows<K, true> kept_b(a.ckpt_b, a.M, a.pieces, first, rows);
   const auto lane = lanes<T, FORM, TEAM>(t, a.C, a.pieces, std::make_integer_sequence<int, NV>{});
   RowIn<T, K, NV> in;
   auto fetch = [&](uint32_t k) __attribute__((always_inline)) {

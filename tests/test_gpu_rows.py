@@ -575,3 +575,99 @@ def test_binding_refuses_wrong_tensors():
         B.abl_ckpt_pack(x.half(), 8, s)
     with pytest.raises(B.AblError):
         B.abl_ckpt_pack(x, 5, torch.zeros(10000, dtype=torch.uint8, device="cuda"))
+
+
+# ---- what is not there, where a team has several rows --------------------------------------------------
+SEVERAL = [(17000, 5), (17000, 40), (9000, 104), (4500, 1000), (3000, 1111), (2500, 1800), (2500, 2100), (2200, 4096), (1100, 4104), (1100, 8190), (1100, 8200),
+           (9000, 4096)]   # M, C: every kind of team, whole and ragged rows, each team with two rows or more; the last beyond the caches
+
+
+def same(a, b, what):
+    assert a.keys() == b.keys(), what
+    for k in a:
+        assert torch.equal(a[k].view(torch.uint8), b[k].view(torch.uint8)), (what, k)
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C", SEVERAL)
+def test_step_forward_without_a_branch_or_its_sum(M, C, dtype, K):
+    """No b is a b of zeros, no r_out changes nothing else, and the rows of a team are as rows by themselves: bit for bit."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(C)
+    r, b = (torch.randn(M, C, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    w, gate = ((torch.randn(n, C, generator=gen, device="cuda") * 0.3 + 1).to(dtype) for n in (1, 3))
+
+    def call(r, b, gate, rows, post, k, want_r=True):
+        m = len(r)
+        keep = dict(n=torch.full_like(r, 7.0))
+        if want_r:
+            keep["r"] = torch.full_like(r, 7.0)
+        if k:
+            keep |= dict(sn=store(m, C, k), rn=tensor(m))
+            if post or gate is not None:
+                keep["sb"] = store(m, C, k)
+            if post:
+                keep["rb"] = tensor(m)
+        B.abl_resnorm_forward(r, b, gate, rows, w[0] if post else None, w[0], keep.get("r"), keep["n"], k, keep.get("sb"), keep.get("rb"),
+                              keep.get("sn"), keep.get("rn"), 0.75, 0.5)
+        return keep
+
+    for k in (0, K):
+        none = call(r, None, None, 0, False, k)
+        same(none, call(r, torch.zeros_like(b), None, 0, False, k), "no b")
+        for with_b in (False, True):
+            whole = call(r, b, gate, -(-M // 3), True, k) if with_b else none
+            part = call(r, b, gate, -(-M // 3), True, k, want_r=False) if with_b else call(r, None, None, 0, False, k, want_r=False)
+            same({n: v for n, v in whole.items() if n != "r"}, part, "no r_out")
+        for first in (0, M - 120):   # (120 rows: a row a team)
+            one = call(r[first: first + 120], None, None, 0, False, k)
+            for n in ("n", "r") + (("rn",) if k else ()):
+                assert torch.equal(none[n][first: first + 120], one[n]), n
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C", SEVERAL)
+def test_step_backward_without_a_stream_a_branch_or_an_output(M, C, dtype, K):
+    """No dr_out is one of zeros; without gate and norm db is dr where alpha is beta; without b, db or dr the others stay: bit for bit."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(C + 1)
+    dn, dr_out, z, y = (torch.randn(M, C, generator=gen, device="cuda").to(dtype) for _ in range(4))
+    rn, rb = (torch.exp(torch.randn(M, generator=gen, device="cuda") * 0.3) for _ in range(2))
+    w, gate = ((torch.randn(n, C, generator=gen, device="cuda") * 0.3 + 1).to(dtype) for n in (1, 3))
+    sn, sb = store(M, C, K), store(M, C, K)
+    B.abl_ckpt_pack(z, K, sn)
+    B.abl_ckpt_pack(y, K, sb)
+    ws = torch.empty(B.abl_resnorm_scratch_bytes(M, C), dtype=torch.uint8, device="cuda")
+
+    def call(dn, dr_out, full, has_b=True, drop=(), rows=slice(None), stores=None):
+        m = len(dn)
+        kn, kb = stores or (sn, sb)
+        out = dict(dr=torch.full_like(dn, 7.0), db=torch.full_like(dn, 7.0), dw_pre=tensor(C))
+        if full:
+            out |= dict(dgate=tensor(3, C), dw_post=tensor(C))
+        for k in drop if has_b else ("db",) + drop:
+            del out[k]
+        B.abl_resnorm_backward(dn, dr_out, gate if full else None, -(-m // 3) if full else 0, w[0] if full else None, w[0], K, kb if full else None,
+                               rb[rows] if full else None, kn, rn[rows], ws, out.get("dr"), out.get("db"), out.get("dgate"), out.get("dw_post"),
+                               out["dw_pre"], 0.5, 0.5, 0, has_b)
+        return out
+
+    without = lambda d, *names: {k: v for k, v in d.items() if k not in names}  # noqa: E731
+    for full in (False, True):
+        with_dr = call(dn, dr_out, full)
+        same(call(dn, None, full), call(dn, torch.zeros_like(dn), full), "no dr_out")
+        same(without(with_dr, "db"), call(dn, dr_out, full, drop=("db",)), "no db")
+        same(without(with_dr, "dr"), call(dn, dr_out, full, drop=("dr",)), "no dr")
+        if not full:
+            assert torch.equal(with_dr["dr"], with_dr["db"])
+            for d in (dr_out, None):
+                same(without(call(dn, d, False), "db"), call(dn, d, False, has_b=False), "no b")
+            same(without(call(dn, None, False), "db", "dr"), call(dn, None, False, has_b=False, drop=("dr",)), "no b, no dr")
+    for first in (0, M - 60):   # rows by themselves
+        part = slice(first, first + 60)
+        one = store(60, C, K)
+        B.abl_ckpt_pack(z[part], K, one)
+        for d, e in ((dr_out, dr_out[part]), (None, None)):
+            assert torch.equal(call(dn, d, False)["dr"][part], call(dn[part], e, False, rows=part, stores=(one, None))["dr"])
