@@ -259,6 +259,10 @@ __global__ __launch_bounds__(512, (kPerUnit<BI, NP, RAGGED> * 2)) void store_wgr
   const bool ends = m1 == a.M;
   const int64_t last = rows == 0 ? 0 : ends ? (rows - 1) * a.ldy + a.Cout : rows * a.ldy + (RAGGED ? 8 : 0);
   const auto dy = descriptor((const T*)a.dy + m0 * a.ldy, last * (int64_t)sizeof(T));
+  // Steps beyond the last one are asked for too.  An access is out of range, and reads zero, where its own offset is not below the descriptor's
+  // bytes less the scalar offset, so that one stays within the bytes.
+  const uint32_t c_end = (uint32_t)rows * (uint32_t)a.blocks * (4u * K), s_end = (uint32_t)rows * (uint32_t)a.blocks, y_end = (uint32_t)(last * (int64_t)sizeof(T));
+  auto within = [](uint32_t at, uint32_t end) __attribute__((always_inline)) { return at < end ? at : end; };
   const uint32_t s_at = block < a.blocks ? (uint32_t)xr * (uint32_t)a.blocks + (uint32_t)block : kNowhere;
   const uint32_t c_at = block < a.blocks ? s_at * (4u * K) + (uint32_t)(xq & 3) * K : kNowhere;
   uint32_t y_at[PY];
@@ -280,7 +284,7 @@ __global__ __launch_bounds__(512, (kPerUnit<BI, NP, RAGGED> * 2)) void store_wgr
     Raw<T> r[PY];
   };
   auto fetch_x = [&](int step, XCodes& t) __attribute__((always_inline)) {
-    const uint32_t at = (uint32_t)step * c_step;
+    const uint32_t at = within((uint32_t)step * c_step, c_end);
     if constexpr (K * XP == 16) {
       const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, c_at, at, 0));
       t.c[0].w = u32x2{w[0], w[1]}, t.c[1].w = u32x2{w[2], w[3]};
@@ -293,10 +297,10 @@ __global__ __launch_bounds__(512, (kPerUnit<BI, NP, RAGGED> * 2)) void store_wgr
     } else {
       t.c[0].w = __builtin_amdgcn_raw_buffer_load_b32(codes, c_at, at, 0);
     }
-    t.s = __builtin_amdgcn_raw_buffer_load_b8(scales, s_at, (uint32_t)step * s_step, 0);
+    t.s = __builtin_amdgcn_raw_buffer_load_b8(scales, s_at, within((uint32_t)step * s_step, s_end), 0);
   };
   auto fetch_y = [&](int step, YPieces& t) __attribute__((always_inline)) {
-    const uint32_t at = (uint32_t)step * y_step;
+    const uint32_t at = within((uint32_t)step * y_step, y_end);
     const int left = rows - step * BK;
 #pragma unroll
     for (int p = 0; p < PY; ++p) {
@@ -304,7 +308,7 @@ __global__ __launch_bounds__(512, (kPerUnit<BI, NP, RAGGED> * 2)) void store_wgr
       if constexpr (RAGGED) of = y_row[p] < left ? of : kNowhere;
       if constexpr (std::is_same_v<T, float>) {
         t.r[p].a = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at, 0));
-        t.r[p].b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at + 16, 0));
+        t.r[p].b = __builtin_bit_cast(f32x4_any4, __builtin_amdgcn_raw_buffer_load_b128(dy, of + 16, at, 0));
       } else {
         t.r[p].a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(dy, of, at, 0));
       }

@@ -671,3 +671,26 @@ def test_step_backward_without_a_stream_a_branch_or_an_output(M, C, dtype, K):
         B.abl_ckpt_pack(z[part], K, one)
         for d, e in ((dr_out, dr_out[part]), (None, None)):
             assert torch.equal(call(dn, d, False)["dr"][part], call(dn[part], e, False, rows=part, stores=(one, None))["dr"])
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Cin,Cout", [(64, 64), (130, 260), (100, 133), (300, 520)])
+@pytest.mark.parametrize("M", [1, 31, 33, 65, 95, 161, 449])
+def test_weight_gradient_takes_nothing_from_behind_its_rows(M, Cin, Cout, dtype, K):
+    """Steps of 32 rows are asked for beyond the last: NaN lies there, behind dy and behind the store.  Small integers: the result is exact."""
+    rng = np.random.default_rng(M + Cin)
+    x = rng.integers(-4, 5, (M, Cin)).astype(float)
+    x[:, ::32] = 4                                     # every block has a scale that its values are multiples of
+    x[:, Cin - 1] = 4
+    raw = R.pack(x, K)
+    x = R.unpack(raw, M, Cin, K)
+    y = rng.integers(-8, 9, (M, Cout)).astype(float)
+    big = torch.full((M + 300, Cout), float("nan"), dtype=dtype, device="cuda")
+    big[:M] = dev(y, dtype)
+    behind = torch.full((raw.size + (1 << 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    behind[: raw.size] = torch.from_numpy(raw).cuda()
+    ws = torch.full((B.abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
+    dW = tensor(Cin, Cout)
+    B.abl_ckpt_wgrad(behind, K, None, big[:M], ws, dW)
+    np.testing.assert_array_equal(f64(dW), x.T @ y)
