@@ -278,7 +278,7 @@ __device__ inline float normalize(float (&v)[NV][8], const FwdArgs& a, TeamSum<T
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = __builtin_fmaf(v[i][j], v[i][j], s);
   const double x = __builtin_fma(sum(s), a.inv_c, (double)a.eps);
-  const float root = __builtin_amdgcn_rsqf((float)x);
+  const float root = (float)__builtin_amdgcn_rsq(x);   // (that of 32 bits takes numbers below the least normal one for zero)
   const double e = __builtin_fma(-x * root, root, 1.0);
   const float more = finite((float)x) ? (float)(0.5 * root * e) : 0.0f;   // (an infinite or NaN sum: zero or NaN)
 #pragma unroll

@@ -694,3 +694,20 @@ def test_weight_gradient_takes_nothing_from_behind_its_rows(M, Cin, Cout, dtype,
     dW = tensor(Cin, Cout)
     B.abl_ckpt_wgrad(behind, K, None, big[:M], ws, dW)
     np.testing.assert_array_equal(f64(dW), x.T @ y)
+
+
+@pytest.mark.parametrize("C", [40, 1111, 4096, 8200])
+@pytest.mark.parametrize("center", [False, True])
+def test_step_with_an_eps_below_the_least_normal_number(C, center):
+    """Rows of zeros, of values whose squares vanish beside eps, and of values beside which eps vanishes.  (Ends: results to 2^-16 of them, as above;
+    the subnormal eps itself is what its 32 bits hold.)"""
+    eps = float(np.float32(1e-40))
+    sign = np.where(np.arange(C) % 2 == 0, 1.0, -1.0)
+    sign[-1] = 0.0 if C % 2 else sign[-1]              # (so that a row's sum is zero)
+    x = np.stack([0 * sign, 2.0 ** -84 * sign, 2.0 ** -50 * sign, sign])
+    r, w = dev(x, torch.float32), torch.ones(C, device="cuda")
+    n, rn = tensor(4, C), tensor(4)
+    B.abl_resnorm_forward(r, None, None, 0, None, w, None, n, 8, None, None, store(4, C, 8), rn, eps=eps, flags=B.ABL_NORM_CENTER if center else 0)
+    want, rstd = R.norm(x, eps, center)
+    np.testing.assert_allclose(f64(rn), rstd, rtol=2.0 ** -16)
+    np.testing.assert_allclose(f64(n), want, rtol=2.0 ** -16, atol=0)
