@@ -45,7 +45,8 @@ def random_parameters(layers, C, F, samples, seed):
 
 
 class TokenNet:
-    """The network on `tokens` rows of bf16 with K-bit stores.  Rows come in `samples` equal runs, each with a row of every gate."""
+    """The network on `tokens` rows of bf16 with K-bit stores.  Rows come in `samples` runs of ceil(tokens / samples), the last one shorter, each
+    with a row of every gate; where fewer runs hold all tokens, the gates' last rows are not used and their gradients are zero."""
 
     def __init__(self, parameters, w_last, tokens, K, act=B.ABL_ACT_SILU, alpha=1.0, beta=1.0):
         self.master, self.w_last32 = parameters, w_last
@@ -53,6 +54,7 @@ class TokenNet:
         self.M, self.C, self.F, self.K, self.act = tokens, C, F2 // 2, K, act
         samples = parameters[0]["gate"].shape[0]
         self.gate_rows, self.alpha, self.beta = -(-tokens // samples), alpha, beta
+        self.runs = -(-tokens // self.gate_rows)
 
         def tensor(*shape, dtype=torch.bfloat16):
             return torch.empty(shape, dtype=dtype, device="cuda")
@@ -72,7 +74,7 @@ class TokenNet:
         self.r, self.n, self.b = tensor(tokens, C), tensor(tokens, C), tensor(tokens, C)
         self.gu, self.h = tensor(tokens, 2 * self.F), tensor(tokens, self.F)
         self.h_store = store(self.F, 8)
-        self.grads = [{k: torch.empty_like(p[k]) for k in PARAMETERS} for p in parameters]
+        self.grads = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
         self.g_last = torch.empty_like(w_last)
         self.velocity = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
         self.scratch = tensor(max(B.abl_resnorm_scratch_bytes(tokens, C),
@@ -96,7 +98,7 @@ class TokenNet:
             unit, out, keep = self.units[i], self.outputs[i], self.norms[i + 1]
             B.abl_glu_forward(self.gu[:, : self.F], self.gu[:, self.F:], self.h, self.act, self.K, unit["g"], unit["u"])
             torch.mm(self.h, p["W2"], out=self.b)
-            B.abl_resnorm_forward(self.r, self.b, p["gate"], self.gate_rows, p["w_post"], self._w_pre(i + 1), self.r, self.n,
+            B.abl_resnorm_forward(self.r, self.b, p["gate"][: self.runs], self.gate_rows, p["w_post"], self._w_pre(i + 1), self.r, self.n,
                                   ckpt_b=out["store"], rstd_b=out["rstd"], ckpt_n=keep["store"], rstd_n=keep["rstd"],
                                   alpha=self.alpha, beta=self.beta, **how)
         return self.n
@@ -110,9 +112,9 @@ class TokenNet:
         for i in reversed(range(len(self.half))):
             p, g, out, keep = self.half[i], self.grads[i], self.outputs[i], self.norms[i + 1]
             dr_new = dr if dr is not None else torch.empty_like(self.r)
-            B.abl_resnorm_backward(dn, dr, p["gate"], self.gate_rows, p["w_post"], self._w_pre(i + 1), self.K, out["store"], out["rstd"],
-                                   keep["store"], keep["rstd"], self.scratch, dr_new, db, g["gate"], g["w_post"], self._grad_pre(i + 1),
-                                   self.alpha, self.beta)
+            B.abl_resnorm_backward(dn, dr, p["gate"][: self.runs], self.gate_rows, p["w_post"], self._w_pre(i + 1), self.K, out["store"],
+                                   out["rstd"], keep["store"], keep["rstd"], self.scratch, dr_new, db, g["gate"][: self.runs], g["w_post"],
+                                   self._grad_pre(i + 1), self.alpha, self.beta)
             dr = dr_new
             torch.mm(db, p["W2"].t(), out=dh)
             unit = self.units[i]

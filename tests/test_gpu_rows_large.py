@@ -360,3 +360,26 @@ def test_gated_unit_on_tensors_of_more_than_4_gb():
 ])
 def test_step_at_the_widths_where_teams_change(M, C, K, gate_rows):
     test_step_on_tensors_beyond_the_caches(M, C, K, gate_rows)
+
+
+@pytest.mark.parametrize("tokens,samples", [(10, 6), (9, 4), (130, 64), (3, 5)])
+def test_network_of_more_gate_rows_than_runs_of_tokens(tokens, samples):
+    """Rows of the gates that no token takes: their gradients are zero, whatever lay in the memory, and an update leaves them as they are."""
+    C, F = 64, 96
+    used = -(-tokens // -(-tokens // samples))
+    assert used < samples
+    dirt = [torch.full((samples, C), float("nan"), device="cuda") for _ in range(64)]    # (what freed memory may hold)
+    del dirt
+    net = T.TokenNet(*T.random_parameters(2, C, F, samples, seed=3), tokens, 8)
+    exact = T.ExactNet(*T.random_parameters(2, C, F, samples, seed=3), tokens)
+    x, dn = T.batch(tokens, C, 1), T.batch(tokens, C, 2)
+    for n in (net, exact):
+        n.forward(x)
+        n.backward(dn)
+    before = [p["gate"].clone() for p in net.master]
+    for g, e in zip(net.grads, exact.grads):
+        assert bool((g["gate"][used:] == 0).all()) and bool((e["gate"][used:] == 0).all())
+        assert bool((g["gate"][:used] != 0).any(1).all())
+    net.update(0.1)
+    for p, b in zip(net.master, before):
+        assert torch.equal(p["gate"][used:], b[used:]) and not torch.equal(p["gate"][:used], b[:used])
