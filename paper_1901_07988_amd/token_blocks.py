@@ -29,6 +29,7 @@ from . import binding as B
 
 EPS = 1e-5
 PARAMETERS = ("W1", "W2", "gate", "w_post", "w_pre")
+VECTORS = PARAMETERS[2:]
 
 
 def random_parameters(layers, C, F, samples, seed):
@@ -75,7 +76,8 @@ class TokenNet:
         self.gu, self.h = tensor(tokens, 2 * self.F), tensor(tokens, self.F)
         self.h_store = store(self.F, 8)
         self.grads = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
-        self.g_last = torch.empty_like(w_last)
+        self.g_last = torch.zeros_like(w_last)
+        self.earlier = []    # of a batch in several parts: the vectors' gradients of all parts but the last, per block
         self.velocity = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
         self.scratch = tensor(max(B.abl_resnorm_scratch_bytes(tokens, C),
                                   B.abl_ckpt_wgrad_scratch_bytes(tokens, C, 2 * self.F, torch.bfloat16),
@@ -105,7 +107,16 @@ class TokenNet:
 
     def backward(self, dn, accumulate=False):
         """dn: the loss gradient of forward's output.  Leaves every gradient in `grads` and `g_last`, returns the input's.
-        accumulate: the products' gradients are added to what is there (batches in several parts)."""
+        accumulate: this is a further part of the last call's batch.  The products' gradients (W1, W2) are added to what is there; the others
+        are this part's, those of the parts before wait in `earlier`, and `update` takes the sums."""
+        if not accumulate:
+            self.earlier = []
+        elif self.earlier:
+            for e, g in zip(self.earlier, self._vectors()):
+                for k in e:
+                    e[k] += g[k]
+        else:
+            self.earlier = [{k: g[k].clone() for k in g} for g in self._vectors()]
         flags = B.ABL_ACCUM_DW if accumulate else 0
         dr, db, dn = None, torch.empty_like(self.b), dn.clone()
         dgu, dh = torch.empty_like(self.gu), torch.empty_like(self.h)
@@ -127,14 +138,18 @@ class TokenNet:
                                dr, None, None, None, self._grad_pre(0), has_b=False)
         return dr
 
+    def _vectors(self):
+        return [{k: g[k] for k in VECTORS} for g in self.grads]
+
     def _grad_pre(self, i):
         return self.grads[i]["w_pre"] if i < len(self.grads) else self.g_last
 
     def update(self, lr, momentum=0.9, weight_decay=0.0):
         """SGD on the fp32 parameters, and their bf16 copies."""
-        for p, g, v, h in zip(self.master, self.grads, self.velocity, self.half):
+        for i, (p, g, v, h) in enumerate(zip(self.master, self.grads, self.velocity, self.half)):
             for k in PARAMETERS:
-                B.abl_sgd_momentum(p[k].view(-1), g[k].view(-1), v[k].view(-1), lr, momentum, weight_decay)
+                d = g[k] + self.earlier[i][k] if self.earlier and k in VECTORS else g[k]
+                B.abl_sgd_momentum(p[k].view(-1), d.view(-1), v[k].view(-1), lr, momentum, weight_decay)
                 h[k].copy_(p[k])
 
 

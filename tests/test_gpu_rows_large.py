@@ -383,3 +383,28 @@ def test_network_of_more_gate_rows_than_runs_of_tokens(tokens, samples):
     net.update(0.1)
     for p, b in zip(net.master, before):
         assert torch.equal(p["gate"][used:], b[used:]) and not torch.equal(p["gate"][:used], b[:used])
+
+
+@pytest.mark.parametrize("parts", [2, 3])
+def test_network_updates_with_the_sum_of_a_batch_in_parts(parts):
+    """Against the parts' own gradients, added here: sums of two or three numbers in fp32, and W1 and W2 in the kernel's order."""
+    tokens, C, F, K, lr = 70, 64, 96, 8, 0.5
+    fresh = lambda: T.TokenNet(*T.random_parameters(2, C, F, 3, seed=4), tokens, K)  # noqa: E731
+    net, sums, size = fresh(), None, None
+    before = [{k: v.clone() for k, v in p.items()} for p in net.master]
+    for i in range(parts):
+        x, dn = T.batch(tokens, C, 10 + i), T.batch(tokens, C, 20 + i)
+        alone = fresh()
+        for n in (net, alone):
+            n.forward(x)
+        net.backward(dn, accumulate=i > 0)
+        alone.backward(dn)
+        g = [{k: v.double() for k, v in d.items()} for d in alone.grads]
+        sums = g if sums is None else [{k: a[k] + b[k] for k in a} for a, b in zip(sums, g)]
+        size = [{k: v.abs() for k, v in d.items()} for d in g] if size is None else [{k: a[k] + b[k].abs() for k in a} for a, b in zip(size, g)]
+    net.update(lr)
+    for p, b, s, m in zip(net.master, before, sums, size):
+        for k in T.PARAMETERS:
+            within(p[k], b[k].double() - lr * s[k], (2 * parts + 4) * U * (b[k].abs() + lr * m[k]), k)
+    net.backward(dn)                                   # a new batch takes nothing of the old one
+    assert not net.earlier
