@@ -77,8 +77,9 @@ class TokenNet:
         self.h_store = store(self.F, 8)
         self.grads = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
         self.g_last = torch.zeros_like(w_last)
-        self.earlier = []    # of a batch in several parts: the vectors' gradients of all parts but the last, per block
+        self.earlier = []    # of a batch in several parts: the vectors' gradients of all parts but the last, per block; w_last's
         self.velocity = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
+        self.v_last = torch.zeros_like(w_last)
         self.scratch = tensor(max(B.abl_resnorm_scratch_bytes(tokens, C),
                                   B.abl_ckpt_wgrad_scratch_bytes(tokens, C, 2 * self.F, torch.bfloat16),
                                   B.abl_ckpt_wgrad_scratch_bytes(tokens, self.F, C, torch.bfloat16)), dtype=torch.uint8)
@@ -139,7 +140,7 @@ class TokenNet:
         return dr
 
     def _vectors(self):
-        return [{k: g[k] for k in VECTORS} for g in self.grads]
+        return [{k: g[k] for k in VECTORS} for g in self.grads] + [{"w_last": self.g_last}]
 
     def _grad_pre(self, i):
         return self.grads[i]["w_pre"] if i < len(self.grads) else self.g_last
@@ -151,6 +152,9 @@ class TokenNet:
                 d = g[k] + self.earlier[i][k] if self.earlier and k in VECTORS else g[k]
                 B.abl_sgd_momentum(p[k].view(-1), d.view(-1), v[k].view(-1), lr, momentum, weight_decay)
                 h[k].copy_(p[k])
+        d = self.g_last + self.earlier[-1]["w_last"] if self.earlier else self.g_last
+        B.abl_sgd_momentum(self.w_last32, d, self.v_last, lr, momentum, weight_decay)
+        self.w_last.copy_(self.w_last32)
 
 
 class ExactNet:
@@ -161,6 +165,7 @@ class ExactNet:
         self.M = tokens
         self.gate_rows = -(-tokens // parameters[0]["gate"].shape[0])
         self.velocity = [{k: torch.zeros_like(p[k]) for k in PARAMETERS} for p in parameters]
+        self.v_last = torch.zeros_like(w_last)
 
     @staticmethod
     def _norm(x):
@@ -188,6 +193,7 @@ class ExactNet:
         for p, g, v in zip(self.master, self.grads, self.velocity):
             for k in PARAMETERS:
                 B.abl_sgd_momentum(p[k].view(-1), g[k].contiguous().view(-1), v[k].view(-1), lr, momentum, weight_decay)
+        B.abl_sgd_momentum(self.w_last32, self.g_last.contiguous(), self.v_last, lr, momentum, weight_decay)
 
 
 def batch(tokens, C, seed):

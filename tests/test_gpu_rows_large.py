@@ -408,3 +408,22 @@ def test_network_updates_with_the_sum_of_a_batch_in_parts(parts):
             within(p[k], b[k].double() - lr * s[k], (2 * parts + 4) * U * (b[k].abs() + lr * m[k]), k)
     net.backward(dn)                                   # a new batch takes nothing of the old one
     assert not net.earlier
+
+
+@pytest.mark.parametrize("parts", [1, 2])
+def test_network_updates_the_last_norms_weight(parts):
+    tokens, C, F, lr = 70, 64, 96, 0.5
+    fresh = lambda: T.random_parameters(2, C, F, 3, seed=4)  # noqa: E731
+    net, exact = T.TokenNet(*fresh(), tokens, 8), T.ExactNet(*fresh(), tokens)
+    before, total = net.w_last32.clone(), 0.0
+    for i in range(parts):
+        net.forward(T.batch(tokens, C, 10 + i))
+        net.backward(T.batch(tokens, C, 20 + i), accumulate=i > 0)
+        total = total + net.g_last.double()
+    net.update(lr)
+    within(net.w_last32, before.double() - lr * total, 8 * U * (before.abs() + lr * total.abs() + 1), "w_last")
+    assert torch.equal(net.w_last, net.w_last32.bfloat16())
+    exact.forward(T.batch(tokens, C, 10))
+    exact.backward(T.batch(tokens, C, 20))
+    exact.update(lr)
+    within(exact.w_last32, before.double() - lr * exact.g_last.double(), 8 * U * (before.abs() + lr * exact.g_last.abs()), "w_last, exact")
