@@ -53,6 +53,13 @@ bool address(void*& p, PyObject* o, at::ScalarType type, int64_t n, const char* 
   p = t->data_ptr();
   return true;
 }
+// A contiguous [M, C]; None as above.
+bool matrix_address(void*& p, PyObject* o, at::ScalarType type, int64_t M, int64_t C, const char* what) {
+  if (!address(p, o, type, M * C, what)) return false;
+  if (o == Py_None) return true;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return (t.dim() == 2 && t.size(0) == M && t.size(1) == C) || fail(what, "of another shape than it has to be");
+}
 // A tensor of bytes that holds the K-bit store of [M, C].
 bool store(void*& p, PyObject* o, int64_t M, int64_t C, long K, const char* what) {
   p = nullptr;
@@ -125,7 +132,11 @@ PyObject* ckpt_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return code(abl_ckpt_unpack(stream(), dtype_of(x.type), s, x.M, (int32_t)x.C, (int)K, x.p, x.ld));
 }
 
-int64_t groups_of(int64_t M, long rows) { return rows > 0 && M > 0 ? (M - 1) / rows + 1 : 0; }
+// A row for each group of `rows` rows.  (Where `rows` is below one, the library says so; a gate for no rows is not looked at.)
+bool gate_address(void*& p, PyObject* o, at::ScalarType type, const Matrix& of, long rows, const char* what) {
+  if (rows < 1 || of.M == 0) return address(p, o, type, 0, what);
+  return matrix_address(p, o, type, (of.M - 1) / rows + 1, of.C, what);
+}
 
 // (r, b, gate, gate_rows, w_post, w_pre, r_out, n, K, ckpt_b, rstd_b, ckpt_n, rstd_n, alpha, beta, eps, flags)
 PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -136,10 +147,10 @@ PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!count(n, 17) || !matrix(r, a[0], "r") || !channels(r, "r") || !whole(rows, a[3]) || !whole(K, a[8]) || !number(s.alpha, a[13]) ||
       !number(s.beta, a[14]) || !number(s.eps, a[15]) || !whole(flags, a[16]))
     return nullptr;
-  const int64_t E = r.M * r.C;
-  if (!address(rp, a[0], r.type, E, "r") || !address(b, a[1], r.type, E, "b") ||
-      !address(gate, a[2], r.type, groups_of(r.M, rows) * r.C, "gate") || !address(w_post, a[4], r.type, r.C, "w_post") ||
-      !address(w_pre, a[5], r.type, r.C, "w_pre") || !address(r_out, a[6], r.type, E, "r_out") || !address(out, a[7], r.type, E, "n") ||
+  if (!matrix_address(rp, a[0], r.type, r.M, r.C, "r") || !matrix_address(b, a[1], r.type, r.M, r.C, "b") ||
+      !gate_address(gate, a[2], r.type, r, rows, "gate") || !address(w_post, a[4], r.type, r.C, "w_post") ||
+      !address(w_pre, a[5], r.type, r.C, "w_pre") || !matrix_address(r_out, a[6], r.type, r.M, r.C, "r_out") ||
+      !matrix_address(out, a[7], r.type, r.M, r.C, "n") ||
       !store(sb, a[9], r.M, r.C, K, "ckpt_b") || !address(rb, a[10], kF32, r.M, "rstd_b") || !store(sn, a[11], r.M, r.C, K, "ckpt_n") ||
       !address(rn, a[12], kF32, r.M, "rstd_n"))
     return nullptr;
@@ -158,12 +169,12 @@ PyObject* resnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !number(s.beta, a[18]) || !whole(flags, a[19]))
     return nullptr;
   const int has_b = PyObject_IsTrue(a[20]);
-  const int64_t E = d.M * d.C, G = groups_of(d.M, rows);
-  if (has_b < 0 || !address(dn, a[0], d.type, E, "dn") || !address(dr_out, a[1], d.type, E, "dr_out") ||
-      !address(gate, a[2], d.type, G * d.C, "gate") || !address(w_post, a[4], d.type, d.C, "w_post") ||
+  if (has_b < 0 || !matrix_address(dn, a[0], d.type, d.M, d.C, "dn") || !matrix_address(dr_out, a[1], d.type, d.M, d.C, "dr_out") ||
+      !gate_address(gate, a[2], d.type, d, rows, "gate") || !address(w_post, a[4], d.type, d.C, "w_post") ||
       !address(w_pre, a[5], d.type, d.C, "w_pre") || !store(sb, a[7], d.M, d.C, K, "ckpt_b") || !address(rb, a[8], kF32, d.M, "rstd_b") ||
       !store(sn, a[9], d.M, d.C, K, "ckpt_n") || !address(rn, a[10], kF32, d.M, "rstd_n") || !workspace(ws, bytes, a[11]) ||
-      !address(dr, a[12], d.type, E, "dr") || !address(db, a[13], d.type, E, "db") || !address(dgate, a[14], kF32, G * d.C, "dgate") ||
+      !matrix_address(dr, a[12], d.type, d.M, d.C, "dr") || !matrix_address(db, a[13], d.type, d.M, d.C, "db") ||
+      !gate_address(dgate, a[14], kF32, d, rows, "dgate") ||
       !address(dw_post, a[15], kF32, d.C, "dw_post") || !address(dw_pre, a[16], kF32, d.C, "dw_pre"))
     return nullptr;
   s.M = d.M, s.gate_rows = rows, s.C = (int32_t)d.C, s.dtype = dtype_of(d.type), s.K = (int32_t)K, s.flags = (uint32_t)flags, s.eps = 0.0f;

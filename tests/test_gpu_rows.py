@@ -711,3 +711,37 @@ def test_step_with_an_eps_below_the_least_normal_number(C, center):
     want, rstd = R.norm(x, eps, center)
     np.testing.assert_allclose(f64(rn), rstd, rtol=2.0 ** -16)
     np.testing.assert_allclose(f64(n), want, rtol=2.0 ** -16, atol=0)
+
+
+def test_binding_refuses_step_tensors_of_another_shape():
+    """Enough elements are not enough: a transposed branch, a longer batch, a gate of other groups."""
+    M, C, K, rows = 40, 64, 8, 10
+    f = dict(device="cuda")
+    good = dict(r=torch.randn(M, C, **f), b=torch.randn(M, C, **f), gate=torch.randn(4, C, **f), w=torch.ones(C, **f), r_out=tensor(M, C), n=tensor(M, C),
+                dn=torch.randn(M, C, **f), dr_out=torch.randn(M, C, **f), dr=tensor(M, C), db=tensor(M, C), dgate=tensor(4, C))
+    sb, sn, rb, rn, wp, wq = store(M, C, K), store(M, C, K), tensor(M), tensor(M), tensor(C), tensor(C)
+    ws = torch.empty(B.abl_resnorm_scratch_bytes(M, C), dtype=torch.uint8, **f)
+
+    def both(**kw):
+        t = {**good, **kw}
+        B.abl_resnorm_forward(t["r"], t["b"], t["gate"], rows, t["w"], t["w"], t["r_out"], t["n"], K, sb, rb, sn, rn)
+        B.abl_resnorm_backward(t["dn"], t["dr_out"], t["gate"], rows, t["w"], t["w"], K, sb, rb, sn, rn, ws, t["dr"], t["db"], t["dgate"], wp, wq)
+
+    both()
+    for k, t in good.items():
+        if k in ("gate", "dgate"):
+            others = [t.new_zeros(5, C), t.new_zeros(3, C), t.new_zeros(2, 2 * C), t.flatten()]
+        elif k == "w":
+            others = [t.new_ones(C - 1), t.bfloat16()]
+        elif k in ("r", "dn"):                                         # (they say how many rows there are: the others do not fit)
+            others = [t.new_zeros(C, M), t.new_zeros(M + 1, C), t.new_zeros(2, M, C), t.flatten()]
+        else:
+            others = [t.new_zeros(C, M), t.new_zeros(M + 1, C), t.new_zeros(M, C + 1), t.flatten(), t.new_zeros(1, M, C)]
+        for other in others:
+            with pytest.raises(AssertionError):
+                both(**{k: other})
+    # no rows: the gate and its gradient have none that count
+    none, keep = torch.empty(0, C, **f), store(1, C, K)
+    B.abl_resnorm_forward(none, none, good["gate"], rows, good["w"], good["w"], none, none, K, keep, rb, keep, rn)
+    B.abl_resnorm_backward(none, none, good["gate"], rows, good["w"], good["w"], K, keep, rb, keep, rn, ws, none, none, good["dgate"], wp, wq)
+    assert bool((wp == 0).all()) and bool((wq == 0).all())
