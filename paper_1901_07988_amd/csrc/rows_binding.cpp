@@ -35,6 +35,13 @@ bool whole(long& v, PyObject* o) {
   v = PyLong_AsLong(o);
   return v != -1 || PyErr_Occurred() == nullptr;
 }
+// A number that the library takes as 32 bits.
+bool small(int& v, PyObject* o, const char* what) {
+  long w;
+  if (!whole(w, o)) return false;
+  v = (int)w;
+  return v == w || fail(what, "out of range");
+}
 bool number(float& v, PyObject* o) {
   const double d = PyFloat_AsDouble(o);
   v = (float)d;
@@ -61,13 +68,13 @@ bool matrix_address(void*& p, PyObject* o, at::ScalarType type, int64_t M, int64
   return (t.dim() == 2 && t.size(0) == M && t.size(1) == C) || fail(what, "of another shape than it has to be");
 }
 // A tensor of bytes that holds the K-bit store of [M, C].
-bool store(void*& p, PyObject* o, int64_t M, int64_t C, long K, const char* what) {
+bool store(void*& p, PyObject* o, int64_t M, int64_t C, int K, const char* what) {
   p = nullptr;
   if (o == Py_None) return true;
   const at::Tensor* t = tensor(o, what);
   if (t == nullptr) return false;
   if (t->element_size() != 1 || !t->is_contiguous()) return fail(what, "contiguous bytes");
-  const int64_t used = M * ((C + 31) / 32) * (4 * K + 1);
+  const int64_t used = M * ((C + 31) / 32) * (4 * (int64_t)K + 1);
   if (t->numel() < (used + 127) / 128 * 128) return fail(what, "too few bytes");
   p = t->data_ptr();
   return true;
@@ -117,19 +124,19 @@ PyObject* code(int e) { return PyLong_FromLong(e); }
 // (x, K, ckpt)
 PyObject* ckpt_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix x;
-  long K;
+  int K;
   void* s;
-  if (!count(n, 3) || !matrix(x, a[0], "x") || !channels(x, "x") || !whole(K, a[1]) || !store(s, a[2], x.M, x.C, K, "ckpt")) return nullptr;
-  return code(abl_ckpt_pack(stream(), dtype_of(x.type), x.p, x.ld, x.M, (int32_t)x.C, (int)K, s));
+  if (!count(n, 3) || !matrix(x, a[0], "x") || !channels(x, "x") || !small(K, a[1], "K") || !store(s, a[2], x.M, x.C, K, "ckpt")) return nullptr;
+  return code(abl_ckpt_pack(stream(), dtype_of(x.type), x.p, x.ld, x.M, (int32_t)x.C, K, s));
 }
 
 // (ckpt, K, x)
 PyObject* ckpt_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix x;
-  long K;
+  int K;
   void* s;
-  if (!count(n, 3) || !matrix(x, a[2], "x") || !channels(x, "x") || !whole(K, a[1]) || !store(s, a[0], x.M, x.C, K, "ckpt")) return nullptr;
-  return code(abl_ckpt_unpack(stream(), dtype_of(x.type), s, x.M, (int32_t)x.C, (int)K, x.p, x.ld));
+  if (!count(n, 3) || !matrix(x, a[2], "x") || !channels(x, "x") || !small(K, a[1], "K") || !store(s, a[0], x.M, x.C, K, "ckpt")) return nullptr;
+  return code(abl_ckpt_unpack(stream(), dtype_of(x.type), s, x.M, (int32_t)x.C, K, x.p, x.ld));
 }
 
 // A row for each group of `rows` rows.  (Where `rows` is below one, the library says so; a gate for no rows is not looked at.)
@@ -142,10 +149,11 @@ bool gate_address(void*& p, PyObject* o, at::ScalarType type, const Matrix& of, 
 PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix r;
   abl_resnorm s;
-  long rows, K, flags;
+  long rows;
+  int K, flags;
   void *b, *gate, *w_post, *w_pre, *r_out, *out, *sb, *rb, *sn, *rn, *rp;
-  if (!count(n, 17) || !matrix(r, a[0], "r") || !channels(r, "r") || !whole(rows, a[3]) || !whole(K, a[8]) || !number(s.alpha, a[13]) ||
-      !number(s.beta, a[14]) || !number(s.eps, a[15]) || !whole(flags, a[16]))
+  if (!count(n, 17) || !matrix(r, a[0], "r") || !channels(r, "r") || !whole(rows, a[3]) || !small(K, a[8], "K") || !number(s.alpha, a[13]) ||
+      !number(s.beta, a[14]) || !number(s.eps, a[15]) || !small(flags, a[16], "flags"))
     return nullptr;
   if (!matrix_address(rp, a[0], r.type, r.M, r.C, "r") || !matrix_address(b, a[1], r.type, r.M, r.C, "b") ||
       !gate_address(gate, a[2], r.type, r, rows, "gate") || !address(w_post, a[4], r.type, r.C, "w_post") ||
@@ -154,7 +162,7 @@ PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !store(sb, a[9], r.M, r.C, K, "ckpt_b") || !address(rb, a[10], kF32, r.M, "rstd_b") || !store(sn, a[11], r.M, r.C, K, "ckpt_n") ||
       !address(rn, a[12], kF32, r.M, "rstd_n"))
     return nullptr;
-  s.M = r.M, s.gate_rows = rows, s.C = (int32_t)r.C, s.dtype = dtype_of(r.type), s.K = (int32_t)K, s.flags = (uint32_t)flags;
+  s.M = r.M, s.gate_rows = rows, s.C = (int32_t)r.C, s.dtype = dtype_of(r.type), s.K = K, s.flags = (uint32_t)flags;
   return code(abl_resnorm_forward(stream(), &s, rp, b, gate, w_post, w_pre, r_out, out, sb, (float*)rb, sn, (float*)rn));
 }
 
@@ -162,11 +170,12 @@ PyObject* resnorm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* resnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix d;
   abl_resnorm s;
-  long rows, K, flags;
+  long rows;
+  int K, flags;
   size_t bytes;
   void *dn, *dr_out, *gate, *w_post, *w_pre, *sb, *rb, *sn, *rn, *ws, *dr, *db, *dgate, *dw_post, *dw_pre;
-  if (!count(n, 21) || !matrix(d, a[0], "dn") || !channels(d, "dn") || !whole(rows, a[3]) || !whole(K, a[6]) || !number(s.alpha, a[17]) ||
-      !number(s.beta, a[18]) || !whole(flags, a[19]))
+  if (!count(n, 21) || !matrix(d, a[0], "dn") || !channels(d, "dn") || !whole(rows, a[3]) || !small(K, a[6], "K") || !number(s.alpha, a[17]) ||
+      !number(s.beta, a[18]) || !small(flags, a[19], "flags"))
     return nullptr;
   const int has_b = PyObject_IsTrue(a[20]);
   if (has_b < 0 || !matrix_address(dn, a[0], d.type, d.M, d.C, "dn") || !matrix_address(dr_out, a[1], d.type, d.M, d.C, "dr_out") ||
@@ -177,7 +186,7 @@ PyObject* resnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !gate_address(dgate, a[14], kF32, d, rows, "dgate") ||
       !address(dw_post, a[15], kF32, d.C, "dw_post") || !address(dw_pre, a[16], kF32, d.C, "dw_pre"))
     return nullptr;
-  s.M = d.M, s.gate_rows = rows, s.C = (int32_t)d.C, s.dtype = dtype_of(d.type), s.K = (int32_t)K, s.flags = (uint32_t)flags, s.eps = 0.0f;
+  s.M = d.M, s.gate_rows = rows, s.C = (int32_t)d.C, s.dtype = dtype_of(d.type), s.K = K, s.flags = (uint32_t)flags, s.eps = 0.0f;
   return code(abl_resnorm_backward(stream(), &s, has_b, dn, dr_out, gate, w_post, w_pre, sb, (float*)rb, sn, (float*)rn, ws, bytes, dr, db,
                                    (float*)dgate, (float*)dw_post, (float*)dw_pre));
 }
@@ -185,34 +194,34 @@ PyObject* resnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // (g, u, h, act, K, ckpt_g, ckpt_u)
 PyObject* glu_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix g, u, h;
-  long act, K;
+  int act, K;
   void *sg, *su;
   if (!count(n, 7) || !matrix(g, a[0], "g") || !channels(g, "g") || !matrix_like(u, g, a[1], "u") || !matrix_like(h, g, a[2], "h") ||
-      !whole(act, a[3]) || !whole(K, a[4]) || !store(sg, a[5], g.M, g.C, K, "ckpt_g") || !store(su, a[6], g.M, g.C, K, "ckpt_u"))
+      !small(act, a[3], "act") || !small(K, a[4], "K") || !store(sg, a[5], g.M, g.C, K, "ckpt_g") || !store(su, a[6], g.M, g.C, K, "ckpt_u"))
     return nullptr;
-  return code(abl_glu_forward(stream(), dtype_of(g.type), (int)act, g.p, g.ld, u.p, u.ld, g.M, (int32_t)g.C, (int)K, h.p, h.ld, sg, su));
+  return code(abl_glu_forward(stream(), dtype_of(g.type), act, g.p, g.ld, u.p, u.ld, g.M, (int32_t)g.C, K, h.p, h.ld, sg, su));
 }
 
 // (dh, ckpt_g, ckpt_u, K, dg, du, act, ckpt_h)
 PyObject* glu_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix d, g, u;
-  long act, K;
+  int act, K;
   void *sg, *su, *sh;
-  if (!count(n, 8) || !matrix(d, a[0], "dh") || !channels(d, "dh") || !whole(K, a[3]) || !store(sg, a[1], d.M, d.C, K, "ckpt_g") ||
-      !store(su, a[2], d.M, d.C, K, "ckpt_u") || !matrix_like(g, d, a[4], "dg") || !matrix_like(u, d, a[5], "du") || !whole(act, a[6]) ||
+  if (!count(n, 8) || !matrix(d, a[0], "dh") || !channels(d, "dh") || !small(K, a[3], "K") || !store(sg, a[1], d.M, d.C, K, "ckpt_g") ||
+      !store(su, a[2], d.M, d.C, K, "ckpt_u") || !matrix_like(g, d, a[4], "dg") || !matrix_like(u, d, a[5], "du") || !small(act, a[6], "act") ||
       !store(sh, a[7], d.M, d.C, 8, "ckpt_h"))
     return nullptr;
-  return code(abl_glu_backward(stream(), dtype_of(d.type), (int)act, d.p, d.ld, sg, su, d.M, (int32_t)d.C, (int)K, g.p, g.ld, u.p, u.ld, sh));
+  return code(abl_glu_backward(stream(), dtype_of(d.type), act, d.p, d.ld, sg, su, d.M, (int32_t)d.C, K, g.p, g.ld, u.p, u.ld, sh));
 }
 
 // (ckpt, K, scale, dy, scratch, dW, flags)
 PyObject* ckpt_wgrad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix dy, w;
-  long K, flags;
+  int K, flags;
   size_t bytes;
   void *s, *scale, *ws, *dW;
-  if (!count(n, 7) || !whole(K, a[1]) || !matrix(dy, a[3], "dy") || !channels(dy, "dy") || !matrix(w, a[5], "dW") || !channels(w, "dW") ||
-      !whole(flags, a[6]))
+  if (!count(n, 7) || !small(K, a[1], "K") || !matrix(dy, a[3], "dy") || !channels(dy, "dy") || !matrix(w, a[5], "dW") || !channels(w, "dW") ||
+      !small(flags, a[6], "flags"))
     return nullptr;
   if (w.C != dy.C || w.M > INT32_MAX) {
     fail("dW", "as many columns as dy");
@@ -221,7 +230,7 @@ PyObject* ckpt_wgrad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!address(dW, a[5], kF32, w.M * w.C, "dW") || !store(s, a[0], dy.M, w.M, K, "ckpt") || !address(scale, a[2], dy.type, w.M, "scale") ||
       !workspace(ws, bytes, a[4]))
     return nullptr;
-  return code(abl_ckpt_wgrad(stream(), dtype_of(dy.type), (uint32_t)flags, s, dy.M, (int32_t)w.M, (int)K, scale, dy.p, dy.ld, (int32_t)dy.C, ws,
+  return code(abl_ckpt_wgrad(stream(), dtype_of(dy.type), (uint32_t)flags, s, dy.M, (int32_t)w.M, K, scale, dy.p, dy.ld, (int32_t)dy.C, ws,
                              bytes, (float*)dW));
 }
 

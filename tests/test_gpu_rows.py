@@ -745,3 +745,18 @@ def test_binding_refuses_step_tensors_of_another_shape():
     B.abl_resnorm_forward(none, none, good["gate"], rows, good["w"], good["w"], none, none, K, keep, rb, keep, rn)
     B.abl_resnorm_backward(none, none, good["gate"], rows, good["w"], good["w"], K, keep, rb, keep, rn, ws, none, none, good["dgate"], wp, wq)
     assert bool((wp == 0).all()) and bool((wq == 0).all())
+
+
+@pytest.mark.parametrize("far", [1 << 32, -(1 << 32), 1 << 40])
+def test_binding_refuses_numbers_beyond_32_bits(far):
+    """Not their low bits: K = 2^32 is not a call that keeps nothing, act = 2^32 is not the first unit, flags = 2^32 are not none."""
+    M, C = 4, 64
+    x, w, wp, wq, rn = torch.randn(M, C, device="cuda"), torch.ones(C, device="cuda"), tensor(C), tensor(C), tensor(M)
+    s = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    for call in (lambda: B.abl_ckpt_pack(x, far + 8, s), lambda: B.abl_ckpt_unpack(s, far + 8, x), lambda: B.abl_glu_forward(x, x, x, far),
+                 lambda: B.abl_glu_forward(x, x, x, 0, far), lambda: B.abl_glu_backward(x, s, s, 8, x, x, far),
+                 lambda: B.abl_resnorm_forward(x, None, None, 0, None, w, x, x, flags=far), lambda: B.abl_resnorm_forward(x, None, None, 0, None, w, x, x, far),
+                 lambda: B.abl_resnorm_backward(x, None, None, 0, None, w, 8, None, None, s, rn, s, x, x, None, None, wq, flags=far),
+                 lambda: B.abl_ckpt_wgrad(s, 8, None, x, s, torch.empty(C, C, device="cuda"), far)):
+        with pytest.raises(AssertionError):
+            call()
