@@ -47,11 +47,27 @@ class abl_resnorm(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
-if not (os.path.exists(LIB_PATH) and os.path.exists(os.path.join(_HERE, "_rows.so"))):
-    raise ImportError("libabl.so (and _rows.so) is not built: run `python -m paper_1901_07988_amd.build` "
+if not os.path.exists(LIB_PATH):
+    raise ImportError("libabl.so is not built: run `python -m paper_1901_07988_amd.build` "
                       "(there is no CPU fallback)")
 lib = ctypes.CDLL(LIB_PATH)
-from . import _rows  # noqa: E402  (links libabl.so)
+
+
+class _NoRows:
+    """In the place of _rows.so where it cannot be loaded: the operators on rows say so when they are called, the others do without it."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError("_rows.so, which the operators on rows of channels need, is not built or does not fit this torch: run "
+                          "`python -m paper_1901_07988_amd.build` (there is no other path): %s" % self._why)
+
+
+try:
+    from . import _rows  # (links libabl.so)
+except ImportError as e:
+    _rows = _NoRows(e)
 
 _vp, _sz, _i32, _i64, _u32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
 _shp = ctypes.POINTER(abl_shape)

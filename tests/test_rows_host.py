@@ -222,3 +222,32 @@ def test_workspaces_of_no_rows_have_a_size():
         assert B.abl_ckpt_bytes(0, C, 4) == B.abl_ckpt_bytes(0, C, 8) == 128
         for dtype in (torch.bfloat16, torch.float32):
             assert B.abl_ckpt_wgrad_scratch_bytes(0, C, C, dtype) > 0
+
+
+def test_the_other_operators_do_without_the_compiled_marshalling(tmp_path):
+    """_rows.so absent, or built against another torch: everything else is there, and the operators on rows say what is missing."""
+    import os
+    import shutil
+    import subprocess
+    import sys
+    package = os.path.dirname(B.__file__)
+    for bad in (None, b"not a library"):
+        there = tmp_path / ("none" if bad is None else "bad")
+        shutil.copytree(package, there / "paper_1901_07988_amd", ignore=shutil.ignore_patterns("_rows.so", "csrc", "__pycache__"))
+        if bad is not None:
+            (there / "paper_1901_07988_amd" / "_rows.so").write_bytes(bad)
+        run = subprocess.run([sys.executable, "-c", """
+from paper_1901_07988_amd import binding as B, runtime
+import os
+assert os.getcwd() in os.path.realpath(B.__file__)
+assert B.abl_packed_bytes((1, 1, 1, 3, 4, 1, 1, 1, 0), 4) == 128
+assert B.abl_ckpt_bytes(4, 64, 8) == 384
+for call in (lambda: B.abl_ckpt_pack(None, 8, None), lambda: B.abl_glu_forward(None, None, None, 0)):
+    try:
+        call()
+    except ImportError as e:
+        assert "_rows.so" in str(e)
+    else:
+        raise SystemExit("no error")
+"""], cwd=there, capture_output=True, text=True, timeout=300, env={**os.environ, "PYTHONPATH": str(there)})
+        assert run.returncode == 0, run.stderr
