@@ -427,3 +427,49 @@ def test_network_updates_the_last_norms_weight(parts):
     exact.backward(T.batch(tokens, C, 20))
     exact.update(lr)
     within(exact.w_last32, before.double() - lr * exact.g_last.double(), 8 * U * (before.abs() + lr * exact.g_last.abs()), "w_last, exact")
+
+
+@pytest.mark.parametrize("K", [4, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,C,gate_rows", [
+    (17000, 5, 0), (17000, 5, 700), (17001, 40, 3), (17001, 40, 1), (5000, 104, 5000), (9001, 500, 450), (4500, 1000, 2), (3000, 1111, 1), (3001, 1111, 1300),
+    (40000, 1280, 2000), (70000, 1500, 0), (2500, 1800, 2500), (2500, 2100, 7), (8192, 4096, 2048), (8191, 4096, 33), (8191, 4096, 31), (9000, 4104, 9000),
+    (4096, 8192, 1), (1100, 8190, 500), (1100, 8200, 0), (1101, 8200, 2), (700, 16381, 100)])
+def test_sums_over_the_rows_of_a_step_are_exact_for_whole_numbers(M, C, gate_rows, dtype, K):
+    """Stores of whole numbers, gradients of whole numbers, weights and gates of powers of two: no sum is rounded, in whatever order, so that a row or
+    a share that is missing, doubled or in another group is seen.  dw_pre with no dr_out; dw_post and dgate with no dn, where D is dr_out."""
+    gen = generator(M + C)
+    top = 127 if K == 8 else 6
+
+    def whole(lo, hi, *shape):
+        return torch.randint(lo, hi + 1, shape, generator=gen, device="cuda").float()
+
+    def kept():
+        x = whole(-4, 4, M, C)
+        x[:, ::32] = top                     # (the scale of every block is 1)
+        s, v = stored(x, K)
+        assert torch.equal(v.float(), x)
+        return s, v
+
+    (sn, z), (sb, y) = kept(), kept()
+    one = torch.ones(M, device="cuda")
+    G = -(-M // gate_rows) if gate_rows else 0
+    w_post, w_pre = (torch.exp2(whole(-1, 1, C)).to(dtype) for _ in range(2))
+    gate = torch.exp2(whole(-1, 1, G, C)).to(dtype) if G else None
+    ws = torch.full((B.abl_resnorm_scratch_bytes(M, C),), 0xFF, dtype=torch.uint8, device="cuda")
+    group = torch.arange(M, device="cuda") // gate_rows if G else None
+    for dn, dr_out in ((whole(-2, 2, M, C), None), (torch.zeros(M, C, device="cuda"), whole(-2, 2, M, C))):
+        dwp, dwq = torch.full((C,), 7.0, device="cuda"), torch.full((C,), 7.0, device="cuda")
+        dgate = torch.full((G, C), 7.0, device="cuda") if G else None
+        dr, db = torch.empty(M, C, dtype=dtype, device="cuda"), torch.empty(M, C, dtype=dtype, device="cuda")
+        B.abl_resnorm_backward(dn.to(dtype), None if dr_out is None else dr_out.to(dtype), gate, gate_rows, w_post, w_pre, K, sb, one, sn, one, ws, dr, db,
+                               dgate, dwp, dwq, 1.0, 0.5)
+        assert torch.equal(dwq.double(), (dn.double() * z).sum(0)), "dw_pre"
+        if dr_out is None:
+            continue
+        assert torch.equal(dr.float(), dr_out)
+        e = 0.5 * dr_out.double() * y
+        assert torch.equal(dwp.double(), (e * gate.double()[group] if G else e).sum(0)), "dw_post"
+        if G:
+            want = torch.zeros(G, C, dtype=torch.float64, device="cuda").index_add_(0, group, e * w_post.double())
+            assert torch.equal(dgate.double(), want), "dgate"

@@ -251,3 +251,42 @@ for call in (lambda: B.abl_ckpt_pack(None, 8, None), lambda: B.abl_glu_forward(N
         raise SystemExit("no error")
 """], cwd=there, capture_output=True, text=True, timeout=300, env={**os.environ, "PYTHONPATH": str(there)})
         assert run.returncode == 0, run.stderr
+
+
+def shares(M, C, gate_rows):
+    """How the backward of the residual step cuts M rows: (rows of a team, teams of a group or 0, blocks that write sums of their own)."""
+    pieces = R.blocks_of(C) * 4
+    team = next((t for t in (64, 128, 192, 256) if pieces <= t), 512)
+    most, block = 128 * 1024 // team, 4 if team == 64 else 1
+    rows = -(-M // most)
+    if gate_rows and gate_rows <= rows:
+        rows, per_group = -(-rows // gate_rows) * gate_rows, 0
+        teams = -(-M // rows)
+    elif gate_rows:
+        group = min(gate_rows, M)
+        per_group = -(-(-(-group // rows)) // block) * block
+        rows = -(-group // per_group)
+        teams = -(-M // group) * per_group
+    else:
+        per_group, teams = 0, -(-M // rows)
+    return rows, per_group, -(-teams // block)
+
+
+def test_resnorm_workspace_holds_the_sums_of_every_cut():
+    """Three planes of a block's sums for every way to cut the rows: no gate, groups below, at and beyond a team's rows, one group of all."""
+    rng = np.random.default_rng(0)
+    cuts = set()
+    for C in (1, 40, 512, 513, 1000, 1111, 1536, 1537, 2048, 2100, 4096, 4104, 8192, 8193, 16384):
+        for M in [1, 2, 7, 300, 2047, 2048, 2049, 5000, 16384, 70000, 100001, 1 << 22] + [int(2 ** rng.uniform(0, 22)) for _ in range(40)]:
+            if M * R.blocks_of(C) >= 1 << 29:      # (refused)
+                continue
+            have = B.abl_resnorm_scratch_bytes(M, C)
+            rows = shares(M, C, 0)[0]
+            for g in {0, 1, 2, 3, rows - 1, rows, rows + 1, 2 * rows, 2 * rows + 1, M // 3, M // 2, M - 1, M, M + 1, 1 << 40} | {
+                    int(2 ** rng.uniform(0, 22)) for _ in range(4)}:
+                if g < 0:
+                    continue
+                team_rows, per_group, blocks = shares(M, C, g)
+                cuts.add((g > 0, per_group > 1, team_rows > 1))
+                assert blocks * 3 * R.blocks_of(C) * 32 * 4 <= have, (M, C, g)
+    assert len(cuts) >= 6, cuts
