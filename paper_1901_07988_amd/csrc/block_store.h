@@ -234,6 +234,13 @@ __device__ inline void keep_piece(unsigned char* codes, unsigned char* scales, I
   if ((threadIdx.x & 3u) == 0) scales[piece >> 2] = (unsigned char)byte;
 }
 
+// The zeros behind the scales, up to a multiple of 128 bytes: by the threads of one block, 128 or more.
+__device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
+  const int64_t used = pieces * K + (pieces >> 2);
+  const int64_t all = (used + 127) / 128 * 128;
+  if (used + threadIdx.x < all) store[used + threadIdx.x] = 0;
+}
+
 // ---- sums ----
 // Sum over the 64 lanes, the same for all of them; of the four rows of 16 in S.
 template <typename S = float>
@@ -266,8 +273,8 @@ int launch_glu_backward(hipStream_t st, int dtype, int act, Rows dh, const void*
 int launch_resnorm_forward(hipStream_t st, const abl_resnorm& s, const void* r, const void* b, const void* gate, const void* w_post,
                            const void* w_pre, void* r_out, void* n, void* ckpt_b, float* rstd_b, void* ckpt_n, float* rstd_n);
 size_t resnorm_scratch_bytes(int64_t M, int C);
-int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, bool has_b, const void* dn, const void* dr_out, const void* gate,
-                            const void* w_post, const void* w_pre, const void* ckpt_b, const float* rstd_b, const void* ckpt_n,
+int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, const void* dn, const void* dr_out, const void* gate, const void* w_post,
+                            const void* w_pre, const void* ckpt_b, const float* rstd_b, const void* ckpt_n,
                             const float* rstd_n, void* scratch, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre);
 size_t store_wgrad_scratch_bytes(int64_t M, int Cin, int Cout, int dtype);
 int launch_store_wgrad(hipStream_t st, int dtype, uint32_t flags, const void* ckpt, int64_t M, int Cin, int K, const void* scale,

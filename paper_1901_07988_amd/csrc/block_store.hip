@@ -49,17 +49,9 @@ __device__ inline Place place_of(const Pieces& g) {
   return p;
 }
 
-// The zeros behind the scales, up to a multiple of 128 bytes.
-__device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
-  if (blockIdx.x != 0) return;
-  const int64_t used = pieces * K + (pieces >> 2);
-  const int64_t all = (used + 127) / 128 * 128;
-  if (used + threadIdx.x < all) store[used + threadIdx.x] = 0;
-}
-
 template <typename T, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void pack_kernel(Pieces g, const T* __restrict__ x, int64_t ldx, unsigned char* __restrict__ store) {
-  zero_tail(store, g.total, K);
+  if (blockIdx.x == 0) zero_tail(store, g.total, K);
   const Place p = place_of(g);
   if (p.piece >= g.total) return;
   float v[8];
@@ -92,7 +84,7 @@ __device__ inline void gate(float g, float& s, float& dq) {
 template <typename T, int ACT, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void glu_fwd_kernel(Pieces pc, const T* g, int64_t ldg, const T* u, int64_t ldu, T* h, int64_t ldh,
                                                            unsigned char* __restrict__ store_g, unsigned char* __restrict__ store_u) {
-  if constexpr (K != 0) {
+  if (K != 0 && blockIdx.x == 0) {
     zero_tail(store_g, pc.total, K);
     zero_tail(store_u, pc.total, K);
   }
@@ -118,7 +110,7 @@ template <typename T, int ACT, int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void glu_bwd_kernel(Pieces pc, const T* dh, int64_t lddh, const unsigned char* __restrict__ store_g,
                                                            const unsigned char* __restrict__ store_u, T* dg, int64_t lddg, T* du, int64_t lddu,
                                                            unsigned char* __restrict__ store_h) {
-  if (store_h != nullptr) zero_tail(store_h, pc.total, 8);
+  if (store_h != nullptr && blockIdx.x == 0) zero_tail(store_h, pc.total, 8);
   const Place p = place_of(pc);
   if (p.piece >= pc.total) return;
   float d[8], a[8], b[8], o[8];

@@ -247,12 +247,6 @@ struct FwdArgs {
   double inv_c;
 };
 
-__device__ inline void zero_tail(unsigned char* store, int64_t pieces, int K) {
-  const int64_t used = pieces * K + (pieces >> 2);
-  const int64_t all = (used + 127) / 128 * 128;
-  for (int64_t i = used + threadIdx.x; i < all; i += blockDim.x) store[i] = 0;
-}
-
 // v <- N(v); returns 1 / sqrt(mean square + eps).  Channels that do not exist hold zeros and stay zero.
 // A normalized value should be off by its own rounding only: the rounding of the factor, common to a row, would shift all values that lie near the
 // middle of two codes to one side.  So the sums over waves, the mean and a Newton step on the instruction's root are in 64 bits, and the
@@ -768,9 +762,9 @@ size_t resnorm_scratch_bytes(int64_t M, int C) {
   return (size_t)blocks * 3 * pieces * 8 * sizeof(float);
 }
 
-int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, bool has_b, const void* dn, const void* dr_out, const void* gate,
-                            const void* w_post, const void* w_pre, const void* ckpt_b, const float* rstd_b, const void* ckpt_n,
-                            const float* rstd_n, void* scratch, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre) {
+int launch_resnorm_backward(hipStream_t st, const abl_resnorm& s, const void* dn, const void* dr_out, const void* gate, const void* w_post,
+                            const void* w_pre, const void* ckpt_b, const float* rstd_b, const void* ckpt_n, const float* rstd_n,
+                            void* scratch, void* dr, void* db, float* dgate, float* dw_post, float* dw_pre) {
   const int64_t groups = gate != nullptr && s.M > 0 ? (s.M - 1) / s.gate_rows + 1 : 0;
   if (s.M == 0) {
     for (float* p : {dw_pre, dw_post})

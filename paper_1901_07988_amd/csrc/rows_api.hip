@@ -102,7 +102,7 @@ int abl_resnorm_backward(void* stream, const abl_resnorm* step, int has_b, const
     if (w_post != nullptr && bad(rstd_b, 4)) return ABL_ERR_ARG;
     if (scratch_bytes < resnorm_scratch_bytes(step->M, step->C)) return ABL_ERR_SCRATCH;
   }
-  return launch_resnorm_backward((hipStream_t)stream, *step, has_b != 0, dn, dr_out, gate, w_post, w_pre,
+  return launch_resnorm_backward((hipStream_t)stream, *step, dn, dr_out, gate, w_post, w_pre,
                                  w_post != nullptr || gate != nullptr ? ckpt_b : nullptr, rstd_b, ckpt_n, rstd_n, scratch, dr, db,
                                  dgate, dw_post, dw_pre);
 }
