@@ -7,11 +7,13 @@
 //   db = rstd_b (v - y mean(v y)),   v = e gate w_post
 //
 // Both are bound by memory: an element of bf16 costs 8 bytes and its two stores (10.1 at K = 8).  8192 x 4096 bf16 with a gate for
-// 2048 rows, K = 8 (338 MB): forward 54 us (6.2 TB/s, as a copy; 64 after passes whose output the caches still have to write),
-// backward 60 with the second launch (5.6); calls of a few rows are the launch: 8 rows 3.9 us.  A team of threads holds a row in
-// registers, so that every tensor is read once; the sums over a row go through the waves' registers and, between waves, LDS.  In
-// the backward a team takes consecutive rows and keeps its share of the sums over rows in registers as well; the teams' sums are
-// added in a fixed order by a second launch.
+// 2048 rows, K = 8 (338 MB): forward 55 us (6.2 TB/s, as a copy; 66 after passes whose output the caches still have to write),
+// backward 60 with the second launch (5.6); calls of a few rows are the launch: 8 rows 3.9 us.  That is the width
+// whose pieces are as many as a team's threads: 8192 x 2560 takes 45 and 54 us (4.7 and 3.9 TB/s), 4096 x 5120 46 and 56 (4.6 and
+// 3.7), 2048 x 12288, with four pieces a thread, 57 and 78 (4.5 and 3.2).  A team of threads holds a row in registers, so that every
+// tensor is read once; the sums over a row go through the waves' registers and, between waves, LDS.  In the backward a team takes
+// consecutive rows and keeps its share of the sums over rows in registers as well; the teams' sums are added in a fixed order by a
+// second launch.
 
 #include <utility>
 
@@ -37,7 +39,10 @@ __device__ inline int left(int C, uint32_t c) { return C - (int)c; }
 // channels and shifts them down, so that nothing beyond the row is read, and stores four, two and one of them, as many as there are.
 // Rows of fewer than eight channels (kShort) are taken in parts (load_raw, store_piece).
 // kStream: whole pieces past the caches (kStreamBytes).  8192 x 4096 bf16, K = 8, which moves 338 MB: forward 70 -> 57 us,
-// backward 79 -> 66 (both with 1024 threads a unit).
+// backward 79 -> 66 (both with 1024 threads a unit).  Only for teams of 256 threads and more: with it narrower rows of bf16 take
+// 0.99 to 1.02 of the time forward and 0.95 to 0.98 backward (131072 x 512 140 and 137 us instead of 139 and 144), 200000 x 128 fp32
+// 124 and 183 us instead of 123 and 202, but 30000 x 1536 fp32 195 and 196 instead of 181 and 184.  Ragged rows are stored in parts, which past the caches would be
+// parts of lines; they were not timed so.
 enum Form { kWhole, kRagged, kShort, kStream };
 
 // Where a lane's piece of a row lies: byte offsets in the row, kNowhere where there is nothing of the kind.
@@ -392,7 +397,7 @@ struct Shares {
 // and half as many sums for the second launch where it has one: 1024 / 512 threads a unit take 108 / 92 us at 4096 x 8192 bf16
 // with a gate a row, 64.4 / 59.4 at 8192 x 4096 (256: 84), 17.6 / 17.5 at 1500 x 1111 fp32 (with teams of 256);
 // 19.8 / 21 at 16384 x 200.
-constexpr int64_t kBwdThreads = 128 * 1024;
+constexpr int64_t kBwdThreads = 128 * 1024;   // (1500 x 1111: K = 8, a gate a row, means taken out; counted with a team's idle threads)
 // The forward, 2048 / 1024 threads a unit: 53.5 / 55.2 us at 8192 x 4096 bf16 and 9.4 / 10.3 at 1500 x 1112 fp32; rows of more
 // pieces than threads take the smaller launch (48 / 40 us at 1024 x 16384 bf16).
 constexpr int64_t fwd_threads(int pieces_a_thread) { return (pieces_a_thread == 1 ? 512 : 256) * 1024; }
@@ -469,6 +474,9 @@ struct RowIn {
 };
 
 // As in the forward, the next row's elements are asked for before this one's are worked on.
+// The bound of four waves a SIMD, 128 registers, costs a piece a thread some spills to scratch: 2 to 22 registers in teams of 64 threads, 10 to 19 in
+// fp32 teams of 512, up to 6 in fp32 teams of 192 and 256 and in ragged bf16 ones of 512, none elsewhere.  Four pieces a thread spill 5 to 94 of
+// 256 registers here, and 16 to 60 in the forward (fp32, and ragged bf16 with stores).  Not priced.
 template <typename T, int K, Form FORM, int TEAM, int NV>
 __global__ __launch_bounds__(kBlock<TEAM>, NV == 1 ? 4 : 2) void resnorm_bwd_kernel(BwdArgs a) {
   constexpr bool kHold = NV < 4;   // registers for the weights and for the next row; rows of four pieces a thread read the weights again
@@ -687,9 +695,12 @@ __global__ __launch_bounds__(256) void zero_kernel(float* p, int64_t n) {
 }
 
 // Threads of a team for rows of so many pieces: a piece for each up to 512 threads, then two and four (a block of 1024 threads has too few
-// registers for the backward: 4096 x 8192 bf16 took 162 us).  Between 128 and 256 also 192: 1500 x 1111 fp32 11.0 us forward and 17.4 backward,
-// with 256 11.8 and 18.6.  384 and 768 lose to 512 threads with idle ones or two pieces: 8192 x 2560 bf16 50 and 60 us instead of 45 and 54,
-// 4096 x 5120 51 and 66 instead of 46 and 56.
+// registers for the backward: 4096 x 8192 bf16 took 162 us).  Between 128 and 256 also 192, against 256 (13 shapes of 1032 to 1536 channels, both
+// types): forward 0.88 to 1.05 of the time, 0.94 in the mean (1500 x 1111 fp32 10.1 instead of 11.4 us, 4096 x 1500 bf16 14.3 instead
+// of 16.2); backward 0.91 to 1.10, 1.00 in the mean (1500 x 1111 fp32 15.1 instead of 16.1, 4096 x 1280 fp32 28.4 instead of 25.9).
+// 384 and 768 threads, launched by the rules above (330 and 170 blocks for 256 units in the backward), lost to 512 with idle threads or two
+// pieces: 8192 x 2560 bf16 50 and 60 us instead of 45 and 54, 4096 x 5120 51 and 66 instead of 46 and 56; launches of a whole number of
+// blocks a unit were not tried with them.
 int team_of(int pieces) {
   for (int t : {64, 128, 192, 256})
     if (pieces <= t) return t;

@@ -1,8 +1,8 @@
 // Weight gradient of a product from the block store of its input (abl_ckpt_wgrad): dW [Cin][Cout] = (scale * x~)^T dy, a contraction
 // over the M rows.
 //
-// Bound by the matrix cores and the card's power: 8192 x 4096 x 8192 (rows, Cin, Cout) in bf16 takes 415 us at best and 450 in the
-// mean of many (1330 and 1220 TFLOP/s).  The matrix cores are busy in 62 % of the cycles, at 1.75 GHz; a loop of these instructions
+// Bound by the matrix cores and the card's power: 8192 x 4096 x 8192 (rows, Cin, Cout) in bf16 takes 415 to 430 us at best and 450 to
+// 465 in the mean of many, by the card (1330 and 1200 TFLOP/s).  The matrix cores are busy in 62 % of the cycles, at 1.75 GHz; a loop of these instructions
 // reaches 2420 TFLOP/s on zeros and 2050 on normal data.  Without decoding it would take 374, without loads 368, without staging
 // 294, with a quarter of the matrix instructions 292: the two halves of a step overlap, not perfectly.  dy straight from memory to
 // LDS, past the registers, measured the same.  4096 x 4096 x 4096: 114 us (1210 TFLOP/s); fp32 at 8192 x 1024 x 4096, three
