@@ -406,6 +406,49 @@ int abl_ckpt_wgrad(void* stream, int dtype, uint32_t flags, const void* ckpt, in
                    const void* scale, const void* dy, int64_t lddy, int32_t Cout, void* scratch,
                    size_t scratch_bytes, float* dW);
 
+/* ---- losses over a vocabulary, behind the last block ------------------------------------------
+ * Rows h [M][C] against a table W [V][C] (one row per token of the vocabulary), with the method's economy: the logits
+ *     s = h W^T,  z = scale s
+ * are made a tile at a time and never kept; what waits for the backward pass are a row's log-sums (for distillation also its T logits at
+ * the teacher's tokens), and the backward pass makes the logits again.  With L = log sum_v exp z_v, Lt = log sum_v exp(z_v / temperature):
+ *     CE = (1 - smoothing) (L - z_label) + smoothing (L - mean_v z_v)
+ *     KD = temperature^2 sum_k p_k (log p_k - z_{id_k} / temperature + Lt),   p = softmax of the teacher's logits / temperature over the row's T entries
+ *     abl_xent:     loss = CE + z_weight L^2
+ *     abl_distill:  loss = label_weight CE + z_weight L^2 + teacher_weight KD
+ * A label below zero is none; an entry with an id below zero or a logit of minus infinity is absent; an id may come twice in a row (its
+ * probabilities add up).  A row without a label has no CE, one without entries no KD, and a row with neither does not count: its
+ * loss, log-sums and gradient are zero and its h is not looked at (it may hold anything).  Rows that do not count cost nothing in the products.
+ * A label or id of V or more makes the row's loss NaN, and the gradients NaN.
+ * bf16 operands go into the matrix cores as they are, fp32 ones as three bf16 parts (24 bits; ABL_MATH_BF16: rounded to one).  Logits, sums and
+ * losses are fp32.  The gradient of the logits enters its two products in bf16 where dtype and dw_dtype are bf16, in two bf16 parts
+ * for dW where that is fp32 (ABL_MATH_BF16: one), in three where dtype is fp32.  Sums are taken in a fixed order. */
+typedef struct abl_head {
+  int64_t M;                 /* rows */
+  int32_t C, V, T;           /* channels, tokens of the vocabulary, the teacher's entries of a row (0 for abl_xent) */
+  int32_t dtype, dw_dtype;   /* of h, W and dh; of dW: dtype or ABL_F32 (not looked at by the forward calls) */
+  uint32_t flags;            /* ABL_MATH_BF16; backward: ABL_ACCUM_DW (dW += instead of =) */
+  float scale, smoothing, z_weight;                 /* smoothing in [0, 1) */
+  float temperature, label_weight, teacher_weight;  /* of abl_distill (not looked at by abl_xent); temperature > 0 */
+} abl_head;
+/* M <= 2^25, C <= 2^16, V <= 2^26, M V <= 2^44, T <= 1024 (abl_distill: 1 <= T), or ABL_ERR_SHAPE.  The size depends on M, C, V, T, dtype, dw_dtype
+ * and flags; 0 on invalid arguments, never 0 otherwise. */
+size_t abl_head_scratch_bytes(const abl_head* head, int backward);
+/* labels [M]; loss, lse [M] out.  M = 0: nothing is done. */
+int abl_xent_forward(void* stream, const abl_head* head, const void* h, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                     void* scratch, size_t scratch_bytes, float* loss, float* lse);
+/* lse as the forward wrote it, dloss [M]: the gradient of every row's loss.  dh [M][C] of dtype, dW [V][C] contiguous, of dw_dtype; one of them may be
+ * NULL (not wanted).  dh may alias h (same ld).  M = 0: dW = 0. */
+int abl_xent_backward(void* stream, const abl_head* head, const void* h, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                      const float* lse, const float* dloss, void* scratch, size_t scratch_bytes, void* dh, int64_t lddh, void* dW);
+/* labels [M] or NULL (none); top_ids, top_logits [M][T]; out: loss, lse, lse_t [M], z_top [M][T] (z at the entries, zero where one is absent).
+ * lse may be NULL where labels are and z_weight is zero. */
+int abl_distill_forward(void* stream, const abl_head* head, const void* h, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                        const int64_t* top_ids, const float* top_logits, void* scratch, size_t scratch_bytes, float* loss, float* lse,
+                        float* lse_t, float* z_top);
+int abl_distill_backward(void* stream, const abl_head* head, const void* h, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                         const int64_t* top_ids, const float* top_logits, const float* lse, const float* lse_t, const float* z_top,
+                         const float* dloss, void* scratch, size_t scratch_bytes, void* dh, int64_t lddh, void* dW);
+
 /* ---- parameter update -----------------------------------------------------------
  * SGD with momentum and weight decay, the update rule of the paper's experiments
  * (Sec. 4: momentum 0.9, weight decay 2e-4 on CIFAR and 1e-4 on ImageNet), applied to

@@ -47,6 +47,13 @@ class abl_resnorm(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
+class abl_head(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("C", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("dw_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("smoothing", ctypes.c_float),
+                ("z_weight", ctypes.c_float), ("temperature", ctypes.c_float), ("label_weight", ctypes.c_float),
+                ("teacher_weight", ctypes.c_float)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError("libabl.so is not built: run `python -m paper_1901_07988_amd.build` "
                       "(there is no CPU fallback)")
@@ -129,6 +136,11 @@ _SIGS = {
     "abl_ckpt_wgrad_scratch_bytes": (_sz, [_i64, _i32, _i32, ctypes.c_int]),
     "abl_ckpt_wgrad": (ctypes.c_int, [_vp, ctypes.c_int, _u32, _vp, _i64, _i32, ctypes.c_int, _vp, _vp, _i64, _i32, _vp,
                                       _sz, _vp]),
+    "abl_head_scratch_bytes": (_sz, [ctypes.POINTER(abl_head), ctypes.c_int]),
+    "abl_xent_forward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_head), _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
+    "abl_xent_backward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_head), _vp, _i64, _vp, _i64] + [_vp] * 4 + [_sz, _vp, _i64, _vp]),
+    "abl_distill_forward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_head), _vp, _i64, _vp, _i64] + [_vp] * 4 + [_sz] + [_vp] * 4),
+    "abl_distill_backward": (ctypes.c_int, [_vp, ctypes.POINTER(abl_head), _vp, _i64, _vp, _i64] + [_vp] * 8 + [_sz, _vp, _i64, _vp]),
     "abl_sgd_momentum": (ctypes.c_int, [_vp, _i64, ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp, _vp, _vp]),
     "abl_hbm_probe": (ctypes.c_int, [_vp, ctypes.c_int, _vp, _vp, _sz]),
     "abl_mfma_probe_out_bytes": (_sz, []),
@@ -450,6 +462,38 @@ def abl_ckpt_wgrad_scratch_bytes(M, Cin, Cout, dtype):
 def abl_ckpt_wgrad(ckpt, K, scale, dy, scratch, dW, flags=0):
     """dW [Cin, Cout] fp32 = (scale * x~)^T dy from the store of x [M, Cin]; dy [M, Cout], rows contiguous."""
     _check(_rows.ckpt_wgrad(ckpt, K, scale, dy, scratch, dW, flags), "abl_ckpt_wgrad")
+
+
+# ---- losses over a vocabulary ---------------------------------------------------------------------
+def abl_head_scratch_bytes(M, C, V, dtype, T=0, dw_dtype=None, backward=False, flags=0):
+    """dtype, dw_dtype (None: the same): torch dtypes of h, W, dh and of dW; T: the teacher's entries of a row (0: abl_xent_*)."""
+    d = _DTYPES.get(dtype, -1)
+    p = abl_head(M=M, C=C, V=V, T=T, dtype=d, dw_dtype=d if dw_dtype is None else _DTYPES.get(dw_dtype, -1), flags=flags, scale=1.0, temperature=1.0)
+    return lib.abl_head_scratch_bytes(ctypes.byref(p), 1 if backward else 0)
+
+
+def abl_xent_forward(h, W, labels, scratch, loss, lse, scale=1.0, smoothing=0.0, z_weight=0.0, flags=0):
+    """h [M, C], W [V, C] (rows contiguous, any distance between them); labels [M] int64, below zero: the row does not count; loss, lse [M] fp32."""
+    _check(_rows.xent_forward(h, W, labels, scratch, loss, lse, scale, smoothing, z_weight, flags), "abl_xent_forward")
+
+
+def abl_xent_backward(h, W, labels, lse, dloss, scratch, dh, dW, scale=1.0, smoothing=0.0, z_weight=0.0, flags=0):
+    """dloss [M] fp32; dh [M, C] as h (rows contiguous), dW [V, C] of h's type or fp32; one of them may be None."""
+    _check(_rows.xent_backward(h, W, labels, lse, dloss, scratch, dh, dW, scale, smoothing, z_weight, flags), "abl_xent_backward")
+
+
+def abl_distill_forward(h, W, labels, top_ids, top_logits, scratch, loss, lse, lse_t, z_top, scale=1.0, temperature=1.0, teacher_weight=1.0,
+                        label_weight=0.0, smoothing=0.0, z_weight=0.0, flags=0):
+    """labels [M] int64 or None; top_ids [M, T] int64, top_logits [M, T] fp32: the teacher's; loss, lse, lse_t [M], z_top [M, T] fp32."""
+    _check(_rows.distill_forward(h, W, labels, top_ids, top_logits, scratch, loss, lse, lse_t, z_top, scale, temperature, teacher_weight,
+                                 label_weight, smoothing, z_weight, flags), "abl_distill_forward")
+
+
+def abl_distill_backward(h, W, labels, top_ids, top_logits, lse, lse_t, z_top, dloss, scratch, dh, dW, scale=1.0, temperature=1.0,
+                         teacher_weight=1.0, label_weight=0.0, smoothing=0.0, z_weight=0.0, flags=0):
+    """lse, lse_t, z_top as the forward wrote them; the others as in abl_xent_backward."""
+    _check(_rows.distill_backward(h, W, labels, top_ids, top_logits, lse, lse_t, z_top, dloss, scratch, dh, dW, scale, temperature,
+                                  teacher_weight, label_weight, smoothing, z_weight, flags), "abl_distill_backward")
 
 
 def abl_sgd_momentum(w, grad, v, lr, momentum, weight_decay):

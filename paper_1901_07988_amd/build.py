@@ -35,6 +35,8 @@ UNITS = {
     "resnorm.hip": [],
     "store_wgrad.hip": [],
     "rows_api.hip": [],
+    "head_loss.hip": [],
+    "head_api.hip": [],
     "abl_api.hip": [],
     "abl_noalloc.hip": [],
     "probe_kernels.hip": [],

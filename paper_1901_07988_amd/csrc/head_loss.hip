@@ -1,0 +1,960 @@
+// Losses over a vocabulary (abl_xent_*, abl_distill_*): rows h [M][C] against a table W [V][C] without the logits z = scale h W^T in memory.
+//
+//   forward    a tile of logits at a time: its rows' maximum m and sum_v exp(z - m) (and at the teacher's temperature, and sum_v z) go to memory,
+//              16 bytes for a row of a tile; a second launch joins the tiles and writes the losses
+//   backward   the logits again, a piece of the vocabulary at a time: a row's gradient
+//                  d_v = a exp(z_v - L) + at exp(z_v / tau - Lt) + a0 + ay [v = label] - at sum_k p_k [v = id_k]
+//              goes to a workspace that holds the piece, and dh += d W, dW = d^T h are products from there
+//
+// Rows that count are taken together first: a list of them, made by one block, and copies of their h, filled up with zero rows and
+// channels to what the tiles need.  So the products see no masks, ragged ends or strange strides on that side, and rows
+// that do not count (prompts, padding) cost nothing.  fp32 operands are copied as three bf16 parts whose sum they are; a product of such operands is six
+// products of parts, one after the other in the same sums, the small ones first.
+
+#include "head.h"
+
+namespace abl {
+namespace {
+
+constexpr int kRowTile = 256;        // copies of rows are filled up to a multiple of it
+constexpr int kChannelTile = 64;     // channels of a step of the products
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ inline float log_of(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
+__device__ inline float nan_value() { return __uint_as_float(0x7FC00000u); }
+
+// ---- which rows count -----------------------------------------------------------------------------------
+enum { kLabel = 1, kTeacher = 2, kBad = 4 };   // of a row
+
+__device__ inline bool entry_there(int64_t id, float t) { return id >= 0 && !(t == -__builtin_inff()); }
+
+// Of a row with a teacher, by a wave.
+__device__ inline int row_flags(int64_t row, const int64_t* labels, const int64_t* ids, const float* logits, int T, int V) {
+  const int lane = threadIdx.x & 63;
+  int f = 0;
+  if (labels != nullptr) {
+    const int64_t y = labels[row];
+    f = y < 0 ? 0 : y < V ? kLabel : kLabel | kBad;
+  }
+  if (ids != nullptr) {
+    int any = 0;
+    for (int k = lane; k < T; k += 64) {
+      const int64_t id = ids[row * T + k];
+      if (entry_there(id, logits[row * T + k])) any |= id < V ? kTeacher : kTeacher | kBad;
+    }
+    f |= __any(any & kTeacher) ? kTeacher : 0;
+    f |= __any(any & kBad) ? kBad : 0;
+  }
+  return f;
+}
+
+__global__ __launch_bounds__(256) void head_flags_kernel(int64_t M, const int64_t* __restrict__ labels, const int64_t* __restrict__ ids,
+                                                         const float* __restrict__ logits, int T, int V, unsigned char* __restrict__ flags) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= M) return;
+  const int f = row_flags(row, labels, ids, logits, T, V);
+  if ((threadIdx.x & 63) == 0) flags[row] = (unsigned char)f;
+}
+
+// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, and their number: one block.
+__global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_t* __restrict__ labels, const unsigned char* __restrict__ flags,
+                                                         int* __restrict__ rows, int* __restrict__ count) {
+  __shared__ int sums[17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int base = 0;
+  for (int64_t m0 = 0; m0 < M; m0 += 4096) {
+    const int64_t m = m0 + threadIdx.x * 4;
+    int on = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (m + e < M && (flags != nullptr ? (flags[m + e] & (kLabel | kTeacher)) != 0 : labels[m + e] >= 0)) on |= 1 << e;
+    const int n = __popc(on);
+    int s = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int t = __shfl_up(s, d);
+      if (lane >= d) s += t;
+    }
+    if (lane == 63) sums[wave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int total = 0;
+      for (int w = 0; w < 16; ++w) {
+        const int v = sums[w];
+        sums[w] = total;
+        total += v;
+      }
+      sums[16] = total;
+    }
+    __syncthreads();
+    int at = base + sums[wave] + s - n;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (on >> e & 1) rows[at++] = (int)(m + e);
+    base += sums[16];
+    __syncthreads();
+  }
+  const int end = (base + kRowTile - 1) / kRowTile * kRowTile;
+  for (int i = base + threadIdx.x; i < end; i += 1024) rows[i] = -1;
+  if (threadIdx.x == 0) *count = base;
+}
+
+// ---- copies of rows in bf16 parts -----------------------------------------------------------------------
+// fp32 as three bf16 parts whose sum it is: the nearest, the nearest to what is left, and the rest, which then fits (products of parts that are left out are
+// below 2^-25 of the whole).  A value that is not finite is its first part, one that would round to infinity is cut off there.
+__device__ inline void three_parts(float v, uint32_t& h, uint32_t& m, uint32_t& l) {   // each in the upper half of its word
+  h = two_bf16(0.0f, v);
+  const bool fine = finite(v);
+  if (fine && !finite(__uint_as_float(h))) h = __float_as_uint(v) & 0xFFFF0000u;
+  const float r = fine ? v - __uint_as_float(h) : 0.0f;
+  m = two_bf16(0.0f, r);
+  l = __float_as_uint(r - __uint_as_float(m));
+}
+
+// A row of C elements (nullptr: zeros) to its place in P planes, `plane` bytes apart, with zeros up to Cp channels: by a wave.
+template <typename T, int P>
+__device__ inline void copy_row(const T* from, int C, int Cp, char* to, int64_t plane) {
+  for (int c = (threadIdx.x & 63) * 8; c < Cp; c += 512) {
+    float v[8] = {};
+    if (from != nullptr) load_piece(from + c, C - c, v);
+    if constexpr (P == 1) {
+      *reinterpret_cast<u32x4*>(to + 2 * c) = u32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
+    } else {
+      uint32_t h[8], m[8], l[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) three_parts(v[e], h[e], m[e], l[e]);
+      u32x4 a, b, d;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {   // the upper halves of two words
+        a[e] = __builtin_amdgcn_perm(h[2 * e + 1], h[2 * e], 0x07060302u);
+        b[e] = __builtin_amdgcn_perm(m[2 * e + 1], m[2 * e], 0x07060302u);
+        d[e] = __builtin_amdgcn_perm(l[2 * e + 1], l[2 * e], 0x07060302u);
+      }
+      *reinterpret_cast<u32x4*>(to + 2 * c) = a;
+      *reinterpret_cast<u32x4*>(to + plane + 2 * c) = b;
+      *reinterpret_cast<u32x4*>(to + 2 * plane + 2 * c) = d;
+    }
+  }
+}
+
+// Rows 0..n-1 of a tensor, and zero rows up to n_to.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void head_copy_kernel(const T* __restrict__ from, int64_t ld, int64_t n, int64_t n_to, int C, int Cp,
+                                                        char* __restrict__ to, int64_t plane) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row < n_to) copy_row<T, P>(row < n ? from + row * ld : nullptr, C, Cp, to + row * (2 * (int64_t)Cp), plane);
+}
+
+// What the backward pass knows of a row that counts (the formula above; all times the row's dloss and the logits' scale).  At temperature one a
+// holds at too.
+struct RowGrad {
+  float L, a, Lt, at, a0, ay;
+  int label, unused;
+};
+
+struct Gather {
+  int64_t M, slots;   // rows; places for those that count
+  int C, Cp, T, V;
+  const int* rows;
+  const int* count;
+  const unsigned char* flags;   // nullptr: by the labels
+  const int64_t* labels;
+  char* to;                     // planes of the rows that count
+  int64_t plane, ldh;
+  // forward: of the rows that do not count, written as zeros
+  float *loss, *lse, *lse_t, *z_top;
+  // backward
+  void* dh;
+  int64_t lddh;
+  RowGrad* grad;
+  const float *in_lse, *in_lse_t, *dloss;
+  float scale, smoothing, z_weight, tau, label_weight, teacher_weight;
+};
+
+// The rows that count to their places, with their coefficients (backward), then - blocks of their own - zeros for the rows that do not.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __restrict__ h) {
+  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int count = *g.count;
+  if (n < g.slots) {
+    if (n >= (count + kRowTile - 1) / kRowTile * kRowTile) return;
+    const int64_t row = n < count ? g.rows[n] : -1;
+    copy_row<T, P>(row >= 0 ? h + row * g.ldh : nullptr, g.C, g.Cp, g.to + n * (2 * (int64_t)g.Cp), g.plane);
+    if (g.grad != nullptr && lane == 0) {
+      RowGrad r{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1, 0};
+      if (row >= 0) {
+        const int64_t y = g.labels != nullptr ? g.labels[row] : -1;
+        const int f = g.flags != nullptr ? g.flags[row] : y < g.V ? kLabel : kLabel | kBad;
+        const float w = g.dloss[row] * g.scale, l = f & kLabel ? w * g.label_weight : 0.0f;
+        r.L = g.in_lse != nullptr ? g.in_lse[row] : g.tau == 1.0f ? g.in_lse_t[row] : 0.0f;
+        r.a = __builtin_fmaf(2.0f * g.z_weight * w, r.L, l);
+        r.Lt = g.in_lse_t != nullptr ? g.in_lse_t[row] : 0.0f;
+        r.at = f & kTeacher ? w * g.teacher_weight * g.tau : 0.0f;
+        if (g.tau == 1.0f) r.a += r.at;   // (one exponential for both)
+        r.a0 = -l * g.smoothing / (float)g.V;
+        r.ay = -l * (1.0f - g.smoothing);
+        r.label = f & kLabel && y < g.V ? (int)y : -1;
+        if (f & kBad) r.a0 = nan_value();
+      }
+      g.grad[n] = r;
+    }
+    return;
+  }
+  const int64_t row = n - g.slots;
+  if (row >= g.M) return;
+  if (g.flags != nullptr ? (g.flags[row] & (kLabel | kTeacher)) != 0 : g.labels[row] >= 0) return;
+  if (g.loss != nullptr && lane == 0) {
+    g.loss[row] = 0.0f;
+    if (g.lse != nullptr) g.lse[row] = 0.0f;
+    if (g.lse_t != nullptr) g.lse_t[row] = 0.0f;
+  }
+  if (g.z_top != nullptr)
+    for (int k = lane; k < g.T; k += 64) g.z_top[row * g.T + k] = 0.0f;
+  if (g.dh != nullptr) {
+    const float zero[8] = {};
+    for (int c = lane * 8; c < g.C; c += 512) store_piece((T*)g.dh + row * g.lddh + c, g.C - c, zero);
+  }
+}
+
+// ---- the products ---------------------------------------------------------------------------------------
+// out [x][y] = sum_k X Y, x rows and y columns, both operands bf16 in planes of parts.  An operand lies either with k along its rows ([x][k]) or
+// outermost ([k][x]).
+struct Operand {
+  const char* p;        // first element of the first plane
+  int64_t plane;        // bytes from plane to plane
+  int64_t pitch;        // bytes from row to row
+  int64_t bytes;        // from p on, of a plane: reads beyond give zero
+  int along;            // elements that exist along a row (the others read as zero): a multiple of 8
+};
+struct Partial {        // of a row of a tile of logits: maximum, sum of exp(z - max), of exp((z - max) / tau), of z
+  float top, sum, sum_t, z;
+};
+struct Product {
+  Operand x, y;
+  int nx, ny, k;            // sizes as the host knows them
+  const int* count;         // rows that count: instead of nx, or (count_k) of k
+  int count_k;
+  int parts;                // pairs of planes, in the order of their products: 4 bits each plane, x first
+  uint64_t pairs;
+  // logits
+  float scale, inv_tau;
+  int y0;                   // token of the first column
+  Partial* partial;         // [tile of columns][partial_ld]
+  int64_t partial_ld;
+  const int* row_label;     // the label of a row that counts
+  float* z_label;
+  const RowGrad* grad;
+  char* d;                  // planes of the gradient of the logits
+  int64_t d_plane, d_pitch;
+  int d_parts;
+  // sums
+  void* out;
+  int64_t ld;
+  int out_f32, accumulate;
+  const int* map;           // row of out for each x (nullptr: x itself)
+  const float* add;         // [x][add_ld], added (nullptr: nothing)
+  int64_t add_ld;
+};
+enum { kEpiPartial, kEpiGrad, kEpiSum };
+
+// A 16-byte piece of a staged tile.  k along the rows: rows of 64 k's are 8 pieces, the c-th of row r at place c xor (r / 2) % 8: the 16
+// rows of a fragment's read take all banks once.  k outermost: rows (one k) of B channels; the even pieces come first, the c-th of each kind at place
+// c xor a key of the row, the odd ones further by half of a row's pieces and in other places of it: half a wave's transposing read, 16 pieces of
+// the eight rows 0..3 and 8..11 (or 4..7 and 12..15), takes all banks once.
+__device__ inline int key_of(int k) { return (k & 3) | ((k >> 1) & 4); }
+template <int B, bool OUTER>
+__device__ inline int staged_piece(int row, int q) {
+  if constexpr (OUTER) {
+    constexpr int kHalf = B / 16;
+    return row * (B * 2) + (q & 1) * B + (((q >> 1) ^ key_of(row) ^ ((q & 1) * (kHalf - 4))) * 16);
+  } else {
+    return row * 128 + ((q ^ ((row >> 1) & 7)) * 16);
+  }
+}
+
+// Each lane's 16 bytes at `at` go to LDS, one lane's behind the other's from `to` on (zeros where they lie beyond the descriptor).
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t from, char* to, uint32_t at) {
+#ifdef __HIP_DEVICE_COMPILE__   // (the host's pass does not know this size)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+#endif
+}
+
+// Where a thread's 16-byte loads of a tile come from: the loads go to LDS in the order of the threads, so the places' order is undone here.
+template <int B, bool OUTER, int THREADS>
+struct Source {
+  static constexpr int kLoads = B * 8 / THREADS;
+  uint32_t at[kLoads];
+  int first[kLoads];   // element along the row
+  __device__ inline void init(int64_t pitch) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int place = n * THREADS + (int)threadIdx.x;
+      int row, q;
+      if constexpr (OUTER) {
+        constexpr int kHalf = B / 16;
+        row = place / (2 * kHalf);
+        const int in = place % (2 * kHalf), odd = in / kHalf;
+        q = 2 * ((in % kHalf) ^ key_of(row) ^ (odd * (kHalf - 4))) + odd;
+      } else {
+        row = place / 8;
+        q = (place % 8) ^ ((row >> 1) & 7);
+      }
+      at[n] = (uint32_t)row * (uint32_t)pitch + (uint32_t)q * 16u;
+      first[n] = q * 8;
+    }
+  }
+  // origin: byte of the tile's first element; left: elements along the row from there on.
+  __device__ inline void load(const Operand& o, int64_t origin, int plane, int left, char* lds) const {
+    const int64_t bytes = o.bytes - origin;
+    const auto from = descriptor(o.p + plane * o.plane + origin, bytes < 0 ? 0 : bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n)
+      load_to_lds(from, lds + (n * THREADS + wave * 64) * 16, first[n] < left ? at[n] : kNowhere);
+  }
+};
+
+// The k-step `ks` (32 of a tile's 64) of the 16 rows or columns from w on.
+template <int B, bool OUTER>
+__device__ inline bf16x8_t fragment_of(const char* tile, int w, int ks) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (OUTER) {
+    const char* p = tile + staged_piece<B, true>(ks * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), w / 8 + ((lane >> 1) & 1)) + (lane & 1) * 8;
+    return transposed(p, p + 4 * (B * 2));
+  } else {
+    return piece(tile + staged_piece<B, false>(w + (lane & 15), ks * 4 + (lane >> 4)));
+  }
+}
+
+__device__ inline float lanes16_max(float v) {   // over the four lanes 16 apart
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float lanes16_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// Joins the sums of two sets of logits.
+__device__ inline Partial join(const Partial& a, const Partial& b, float inv_tau) {
+  Partial r;
+  r.top = fmaxf(a.top, b.top);
+  const float ref = r.top == -__builtin_inff() ? 0.0f : r.top;
+  const float da = a.top - ref, db = b.top - ref;
+  r.sum = a.sum * exp_of(da) + b.sum * exp_of(db);
+  r.sum_t = a.sum_t * exp_of(da * inv_tau) + b.sum_t * exp_of(db * inv_tau);
+  r.z = a.z + b.z;
+  return r;
+}
+
+template <int BX, int BY, int WX, int WY, bool XO, bool YO, int EPI>
+__global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
+  constexpr int kThreads = WX * WY * 64, FX = BX / WX / 16, FY = BY / WY / 16;
+  constexpr int kXBytes = BX * 128, kStage = (BX + BY) * 128;
+  extern __shared__ __align__(16) char lds[];   // [2][kStage]
+  const int count = a.count != nullptr ? *a.count : 0;
+  const int nx = a.count != nullptr && !a.count_k ? count : a.nx, nk = a.count != nullptr && a.count_k ? count : a.k;
+  // Blocks 8 apart share an XCD and its L2.  Each XCD takes consecutive items, in bands of eight tiles of rows.
+  constexpr int kBand = 8;
+  const int tiles_x = (nx + BX - 1) / BX, tiles_y = (a.ny + BY - 1) / BY, items = tiles_x * tiles_y;
+  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = items >> 3, more = items & 7;
+  if (slot >= per + (xcd < more ? 1 : 0)) return;
+  const int item = xcd * per + (xcd < more ? xcd : more) + slot;
+  const int band = item / (kBand * tiles_y), rest = item - band * kBand * tiles_y;
+  const int high = tiles_x - band * kBand < kBand ? tiles_x - band * kBand : kBand;
+  const int x0 = (band * kBand + rest % high) * BX, tile_y = rest / high, y0 = tile_y * BY;
+  const int steps_k = (nk + 63) / 64, steps = steps_k * a.parts;
+
+  Source<BX, XO, kThreads> sx;
+  Source<BY, YO, kThreads> sy;
+  sx.init(a.x.pitch);
+  sy.init(a.y.pitch);
+  int load_k = 0, load_part = 0;
+  auto load = [&](char* to) __attribute__((always_inline)) {
+    const int pair = (int)(a.pairs >> (8 * load_part));
+    const int k0 = load_k * 64;
+    const int64_t ox = XO ? k0 * a.x.pitch + x0 * 2 : x0 * a.x.pitch + k0 * 2, oy = YO ? k0 * a.y.pitch + y0 * 2 : y0 * a.y.pitch + k0 * 2;
+    sx.load(a.x, ox, pair & 15, a.x.along - (XO ? x0 : k0), to);
+    sy.load(a.y, oy, (pair >> 4) & 15, a.y.along - (YO ? y0 : k0), to + kXBytes);
+    if (++load_k == steps_k) load_k = 0, ++load_part;
+  };
+
+  floatx4 acc[FX][FY];
+#pragma unroll
+  for (int i = 0; i < FX; ++i)
+#pragma unroll
+    for (int j = 0; j < FY; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wx = wave / WY * (FX * 16), wy = wave % WY * (FY * 16);
+
+  if (steps > 0) load(lds);
+  for (int s = 0; s < steps; ++s) {
+    char* now = lds + (s & 1) * kStage;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (s + 1 < steps) load(lds + ((s + 1) & 1) * kStage);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8_t x[FX], y[FY];
+#pragma unroll
+      for (int i = 0; i < FX; ++i) x[i] = fragment_of<BX, XO>(now, wx + 16 * i, ks);
+#pragma unroll
+      for (int j = 0; j < FY; ++j) y[j] = fragment_of<BY, YO>(now + kXBytes, wy + 16 * j, ks);
+#pragma unroll
+      for (int j = 0; j < FY; ++j)
+#pragma unroll
+        for (int i = 0; i < FX; ++i) acc[i][j] = mfma32(y[j], x[i], acc[i][j]);
+    }
+  }
+
+  // lane: row lane % 16 of a 16 x 16 tile, columns 4 (lane / 16) + 0..3
+  if constexpr (EPI == kEpiPartial) {
+    __syncthreads();
+    Partial* joined = reinterpret_cast<Partial*>(lds);   // [WY][BX]
+#pragma unroll
+    for (int i = 0; i < FX; ++i) {
+      const int x = wx + 16 * i + (lane & 15);
+      const bool there = x0 + x < nx;
+      const int label = a.row_label != nullptr && there ? a.row_label[x0 + x] - a.y0 : -1;
+      float top = -__builtin_inff(), all = 0.0f;
+#pragma unroll
+      for (int j = 0; j < FY; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int col = y0 + wy + 16 * j + (lane >> 4) * 4 + e;
+          const float z = acc[i][j][e] * a.scale;
+          if (col == label) a.z_label[x0 + x] = z;
+          acc[i][j][e] = col < a.ny ? z : -__builtin_inff();
+          all += col < a.ny ? z : 0.0f;
+          top = fmaxf(top, acc[i][j][e]);
+        }
+      top = lanes16_max(top);
+      const float ref = top == -__builtin_inff() ? 0.0f : top;
+      float sum = 0.0f, sum_t = 0.0f;
+#pragma unroll
+      for (int j = 0; j < FY; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = acc[i][j][e] - ref;
+          sum += exp_of(z);
+          if (a.inv_tau != 1.0f) sum_t += exp_of(z * a.inv_tau);
+        }
+      sum = lanes16_sum(sum), sum_t = lanes16_sum(sum_t), all = lanes16_sum(all);
+      if (lane < 16) joined[wave % WY * BX + x] = Partial{top, sum, sum_t, all};
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < BX; x += kThreads) {
+      if (x0 + x >= nx) break;
+      Partial p = joined[x];
+#pragma unroll
+      for (int w = 1; w < WY; ++w) p = join(p, joined[w * BX + x], a.inv_tau);
+      a.partial[(int64_t)tile_y * a.partial_ld + x0 + x] = p;
+    }
+  } else if constexpr (EPI == kEpiGrad) {
+#pragma unroll
+    for (int i = 0; i < FX; ++i) {
+      const int x = x0 + wx + 16 * i + (lane & 15);
+      const RowGrad g = a.grad[x];   // (the rows up to a whole tile are there)
+      const int label = g.label - a.y0;
+#pragma unroll
+      for (int j = 0; j < FY; ++j) {
+        const int col = y0 + wy + 16 * j + (lane >> 4) * 4;
+        float d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = acc[i][j][e] * a.scale;
+          float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
+          if (a.inv_tau != 1.0f) v = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)), v);
+          if (g.label >= 0 && col + e == label) v += g.ay;
+          d[e] = x < nx && col + e < a.ny ? v : 0.0f;
+        }
+        char* to = a.d + x * a.d_pitch + col * 2;
+        if (a.d_parts == 3) {
+          uint32_t p[3][4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) three_parts(d[e], p[0][e], p[1][e], p[2][e]);
+#pragma unroll
+          for (int n = 0; n < 3; ++n)
+            *reinterpret_cast<u32x2*>(to + n * a.d_plane) =
+                u32x2{__builtin_amdgcn_perm(p[n][1], p[n][0], 0x07060302u), __builtin_amdgcn_perm(p[n][3], p[n][2], 0x07060302u)};
+        } else {
+          const u32x2 w{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
+          *reinterpret_cast<u32x2*>(to) = w;
+          if (a.d_parts == 2)
+            *reinterpret_cast<u32x2*>(to + a.d_plane) = u32x2{two_bf16(d[0] - low_bf16(w[0]), d[1] - high_bf16(w[0])),
+                                                              two_bf16(d[2] - low_bf16(w[1]), d[3] - high_bf16(w[1]))};
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < FX; ++i) {
+      const int x = x0 + wx + 16 * i + (lane & 15);
+      if (x >= nx) continue;
+      const int64_t row = a.map != nullptr ? a.map[x] : x;
+#pragma unroll
+      for (int j = 0; j < FY; ++j) {
+        const int col = y0 + wy + 16 * j + (lane >> 4) * 4;
+        if (col >= a.ny) continue;
+        f32x4_any4 v = acc[i][j];
+        const int n = a.ny - col;
+        const float* add = a.add != nullptr ? a.add + x * a.add_ld + col : nullptr;
+        if (a.out_f32) {
+          float* to = (float*)a.out + row * a.ld + col;
+          if (n >= 4) {
+            if (add != nullptr) v += *reinterpret_cast<const f32x4_any4*>(add);
+            if (a.accumulate) v += *reinterpret_cast<const f32x4_any4*>(to);
+            *reinterpret_cast<f32x4_any4*>(to) = v;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (e < n) to[e] = v[e] + (add != nullptr ? add[e] : 0.0f) + (a.accumulate ? to[e] : 0.0f);
+          }
+        } else {
+          bf16_t* to = (bf16_t*)a.out + row * a.ld + col;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < n) v[e] += (add != nullptr ? add[e] : 0.0f) + (a.accumulate ? (float)to[e] : 0.0f);
+          if (n >= 4) {
+            *reinterpret_cast<u32x2_any2*>(to) = u32x2_any2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (e < n) to[e] = (bf16_t)v[e];
+          }
+        }
+      }
+    }
+  }
+}
+
+// ---- the teacher's entries ------------------------------------------------------------------------------
+// z at a row's entries: four waves a row, each takes its entries one after the other.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
+template <typename T>
+__global__ __launch_bounds__(256) void head_entries_kernel(const T* __restrict__ h, int64_t ldh, const T* __restrict__ W, int64_t ldw, int C, int V,
+                                                           const int64_t* __restrict__ ids, const float* __restrict__ logits, int entries,
+                                                           const int* __restrict__ rows, const int* __restrict__ count, float scale,
+                                                           int rounded, float* __restrict__ z_top) {
+  if ((int)blockIdx.x >= *count) return;
+  const int64_t row = rows[blockIdx.x];
+  const int lane = threadIdx.x & 63;
+  for (int k = threadIdx.x >> 6; k < entries; k += 4) {
+    const int64_t at = row * entries + k, id = ids[at];
+    if (!entry_there(id, logits[at]) || id >= V) {
+      if (lane == 0) z_top[at] = id >= V ? nan_value() : 0.0f;
+      continue;
+    }
+    float s = 0.0f;
+    for (int c = lane * 8; c < C; c += 512) {
+      float a[8], b[8];
+      load_piece(h + row * ldh + c, C - c, a);
+      load_piece(W + id * ldw + c, C - c, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        s = rounded ? __builtin_fmaf((float)(bf16_t)a[e], (float)(bf16_t)b[e], s) : __builtin_fmaf(a[e], b[e], s);
+    }
+    s = wave_sum(s);
+    if (lane == 0) z_top[at] = s * scale;
+  }
+}
+
+__device__ inline float wave_max(float v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// Maximum and sum of a row's softmax over its entries at temperature tau, by a wave: p_k = exp(t_k / tau - top) / sum.
+__device__ inline void teacher_sums(const int64_t* ids, const float* logits, int T, float inv_tau, float& top, float& sum) {
+  const int lane = threadIdx.x & 63;
+  top = -__builtin_inff();
+  for (int k = lane; k < T; k += 64)
+    if (entry_there(ids[k], logits[k])) top = fmaxf(top, logits[k] * inv_tau);
+  top = wave_max(top);
+  sum = 0.0f;
+  for (int k = lane; k < T; k += 64)
+    if (entry_there(ids[k], logits[k])) sum += exp_of(logits[k] * inv_tau - top);
+  sum = wave_sum(sum);
+}
+
+// The tiles' sums of each row, joined, and its loss: 16 rows a block, a wave each at the end.
+struct Loss {
+  const Partial* partial;
+  int64_t partial_ld;
+  int tiles;
+  const Partial* before;   // of the pieces of the vocabulary before this one (nullptr: none)
+  Partial* after;          // where more pieces follow (nullptr: this is the last one)
+  const int *rows, *count;
+  const unsigned char* flags;
+  const int64_t *labels, *ids;
+  const float *logits, *z_label;
+  int T, V;
+  float smoothing, z_weight, tau, label_weight, teacher_weight;
+  float *loss, *lse, *lse_t;
+  const float* z_top;
+};
+__global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
+  __shared__ Partial joined[64][17];
+  const int n0 = blockIdx.x * 16, count = *a.count;
+  if (n0 >= count) return;
+  const float inv_tau = 1.0f / a.tau;
+  {
+    const int r = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const Partial none{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+    Partial p = none;
+    if (n0 + r < count) {
+      if (group == 0 && a.before != nullptr) p = a.before[n0 + r];
+      for (int t = group; t < a.tiles; t += 64) p = join(p, a.partial[t * a.partial_ld + n0 + r], inv_tau);
+    }
+    joined[group][r] = p;
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 6, lane = threadIdx.x & 63, n = n0 + r;
+  if (n >= count) return;
+  Partial p = joined[lane][r];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const Partial o{__shfl_xor(p.top, d), __shfl_xor(p.sum, d), __shfl_xor(p.sum_t, d), __shfl_xor(p.z, d)};
+    p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (the same for both lanes)
+  }
+  if (a.after != nullptr) {
+    if (lane == 0) a.after[n] = p;
+    return;
+  }
+  const int64_t row = a.rows[n];
+  const int64_t y = a.labels != nullptr ? a.labels[row] : -1;
+  const int f = a.flags != nullptr ? a.flags[row] : y < a.V ? kLabel : kLabel | kBad;
+  const float ln = log_of(p.sum), L = p.top + ln;
+  const float ln_t = a.tau != 1.0f ? log_of(p.sum_t) : ln, top_t = p.top * inv_tau;
+  float loss = a.z_weight != 0.0f ? a.z_weight * L * L : 0.0f;
+  if (f & kLabel) {   // (differences to the maximum first: L and z are large where the loss is small)
+    float ce = ln + (p.top - a.z_label[n]);
+    if (a.smoothing != 0.0f) ce = (1.0f - a.smoothing) * ce + a.smoothing * (ln + (p.top - p.z / (float)a.V));
+    loss += a.label_weight * ce;
+  }
+  if (f & kTeacher) {
+    const int64_t* ids = a.ids + row * a.T;
+    const float *t = a.logits + row * a.T, *z = a.z_top + row * a.T;
+    float top, sum, kd = 0.0f;
+    teacher_sums(ids, t, a.T, inv_tau, top, sum);
+    const float norm = 1.0f / sum, ln_sum = log_of(sum);
+    for (int k = lane; k < a.T; k += 64)
+      if (entry_there(ids[k], t[k])) {
+        const float u = t[k] * inv_tau - top, q = exp_of(u) * norm;
+        if (q != 0.0f) kd += q * ((u - ln_sum) + (p.top - z[k]) * inv_tau);   // (NaN goes in)
+      }
+    loss += a.teacher_weight * a.tau * a.tau * (wave_sum(kd) + ln_t);
+  }
+  if (f & kBad) loss = nan_value();
+  if (lane == 0) {
+    a.loss[row] = loss;
+    if (a.lse != nullptr) a.lse[row] = L;
+    if (a.lse_t != nullptr) a.lse_t[row] = top_t + ln_t;
+  }
+}
+
+// The gradient of the logits at a row's entries, over what the product wrote there: from the row's z_top, before any rounding; of entries with the
+// same id the first one takes the sum of their probabilities.  A wave a row.
+struct Entries {
+  const int *rows, *count;
+  const int64_t* ids;
+  const float *logits, *z_top;
+  const RowGrad* grad;
+  int T, v0, v1;   // tokens of this piece
+  float inv_tau;
+  char* d;
+  int64_t d_plane, d_pitch;
+  int d_parts;
+};
+__global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
+  const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (n >= *a.count) return;
+  const int64_t row = a.rows[n];
+  const int64_t* ids = a.ids + row * a.T;
+  const float* t = a.logits + row * a.T;
+  float top, sum;
+  teacher_sums(ids, t, a.T, a.inv_tau, top, sum);
+  if (sum == 0.0f) return;   // (no entries)
+  const RowGrad g = a.grad[n];
+  const float norm = 1.0f / sum;
+  for (int k = lane; k < a.T; k += 64) {
+    const int64_t id = ids[k];
+    if (id < a.v0 || id >= a.v1 || !entry_there(id, t[k])) continue;
+    bool first = true;
+    for (int i = 0; i < k; ++i) first = first && !(ids[i] == id && entry_there(id, t[i]));
+    if (!first) continue;
+    float p = 0.0f;
+    for (int i = k; i < a.T; ++i)
+      if (ids[i] == id && entry_there(id, t[i])) p += exp_of(t[i] * a.inv_tau - top) * norm;
+    const float z = a.z_top[row * a.T + k];
+    float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
+    v = __builtin_fmaf(g.at, (a.inv_tau != 1.0f ? exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)) : 0.0f) - p, v);
+    if (id == g.label) v += g.ay;
+    uint16_t* to = reinterpret_cast<uint16_t*>(a.d + n * a.d_pitch + (id - a.v0) * 2);
+    if (a.d_parts == 3) {
+      uint32_t h, m, l;
+      three_parts(v, h, m, l);
+      *to = (uint16_t)(h >> 16);
+      *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)(m >> 16);
+      *(uint16_t*)((char*)to + 2 * a.d_plane) = (uint16_t)(l >> 16);
+    } else {
+      const uint32_t w = two_bf16(v, 0.0f);
+      *to = (uint16_t)w;
+      if (a.d_parts == 2) *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)two_bf16(v - low_bf16(w), 0.0f);
+    }
+  }
+}
+
+// The labels of the rows that count, for the products' tiles.
+__global__ __launch_bounds__(256) void head_labels_kernel(const int* __restrict__ rows, const int* __restrict__ count, const int64_t* __restrict__ labels,
+                                                          int V, int* __restrict__ row_label) {
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= *count) return;
+  const int64_t y = labels[rows[n]];
+  row_label[n] = y >= 0 && y < V ? (int)y : -1;
+}
+
+__global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
+// ---- how a call is cut ----------------------------------------------------------------------------------
+inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+
+constexpr int kTile = 128;
+constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)256 << 20;
+
+struct Plan {
+  int parts, d_parts;       // bf16 parts of h and W; of the gradient of the logits
+  int64_t Mp, Cp;           // rows and channels of the copies
+  int64_t piece, table;     // tokens of a piece; of a piece's copied part of the table (0: in place)
+  int pieces;
+  // places in the workspace
+  size_t count, rows, flags, labels, z_label, h, W, partial, carry, grad, d, acc, bytes;
+};
+
+// copied: whether the table's rows have to be copied; `most`: what a call may need at most, whatever the table's alignment.
+Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
+  Plan q{};
+  const bool one = (p.flags & ABL_MATH_BF16) != 0;
+  q.parts = p.dtype == ABL_F32 && !one ? 3 : 1;
+  q.d_parts = q.parts == 3 ? 3 : p.dtype == ABL_BF16 && p.dw_dtype == ABL_F32 && !one ? 2 : 1;
+  q.Mp = up(p.M > 0 ? p.M : 1, kRowTile), q.Cp = up(p.C, kChannelTile);
+  const int64_t all = up(p.V, 256);
+  auto within = [&](int64_t budget, int64_t bytes) {   // of a token
+    const int64_t n = budget / bytes / 256 * 256;
+    return n < 256 ? 256 : n < all ? n : all;
+  };
+  int64_t piece = backward ? within(kGradBytes, q.Mp * 2 * q.d_parts) : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
+  if (piece > 1 << 20) piece = 1 << 20;
+  const int64_t table = within(kTableBytes, q.Cp * 2 * q.parts);
+  const int64_t widest = piece;
+  if (copied && table < piece) piece = table;
+  q.pieces = (int)((p.V + piece - 1) / piece);
+  q.piece = up((p.V + q.pieces - 1) / q.pieces, 256);
+  q.pieces = (int)((p.V + q.piece - 1) / q.piece);
+  const int64_t held = most ? widest : q.piece;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  q.count = take(16);
+  q.rows = take(q.Mp * 4);
+  q.flags = take(p.T != 0 ? p.M : 0);
+  q.labels = take(backward ? 0 : q.Mp * 4);
+  q.z_label = take(backward ? 0 : q.Mp * 4);
+  q.grad = take(backward ? q.Mp * sizeof(RowGrad) : 0);
+  q.h = take(q.Mp * q.Cp * 2 * q.parts);
+  q.table = copied || most ? (table < held ? table : held) : 0;
+  q.W = take(q.table * q.Cp * 2 * q.parts);
+  q.partial = take(backward ? 0 : held / kTile * q.Mp * sizeof(Partial));
+  const bool several = q.pieces > 1 || (most && table < p.V);
+  q.carry = take(!backward && several ? q.Mp * sizeof(Partial) : 0);
+  q.d = take(backward ? q.Mp * held * 2 * q.d_parts : 0);
+  q.acc = take(backward && several ? q.Mp * p.C * 4 : 0);
+  q.bytes = at;
+  return q;
+}
+
+constexpr uint64_t kPairs1 = 0x00, kPairs2 = 0x0001;                 // (x plane in the low four bits; the first product in the low byte)
+constexpr uint64_t kPairs6 = 0x000110110220ull;                      // (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
+
+template <int BX, int BY, int WX, int WY, bool XO, bool YO, int EPI>
+int launch_tiles(hipStream_t st, const Product& a) {
+  auto kern = head_product_kernel<BX, BY, WX, WY, XO, YO, EPI>;
+  constexpr int kBytes = 2 * (BX + BY) * 128;
+  if (kBytes > 64 * 1024)
+    if (int e = allow_full_lds((const void*)kern)) return e;
+  const int64_t tiles = (int64_t)((a.nx + BX - 1) / BX) * ((a.ny + BY - 1) / BY);
+  kern<<<(unsigned)up(tiles, 8), WX * WY * 64, kBytes, st>>>(a);
+  return hip_status();
+}
+
+template <typename T, int P>
+int copy_table(hipStream_t st, const HeadCall& c, const Plan& q, int64_t v0, int64_t n, int64_t n_to, char* to) {
+  head_copy_kernel<T, P><<<(unsigned)((n_to + 3) / 4), 256, 0, st>>>((const T*)c.W.p + v0 * c.W.ld, c.W.ld, n, n_to, c.p.C, (int)q.Cp, to,
+                                                                    q.table * q.Cp * 2);
+  return hip_status();
+}
+template <typename T, int P>
+int gather(hipStream_t st, const Gather& g, const void* h, bool zeros) {
+  head_gather_kernel<T, P><<<(unsigned)((g.slots + (zeros ? g.M : 0) + 3) / 4), 256, 0, st>>>(g, (const T*)h);
+  return hip_status();
+}
+
+// The table's rows from v0 on as an operand: in place, or copied into the workspace.
+struct Call {
+  const HeadCall& c;
+  const Plan& q;
+  hipStream_t st;
+  char* ws;
+  bool copied;
+
+  int prepare(bool backward, Operand& h) const {
+    const abl_head& p = c.p;
+    int* rows = (int*)(ws + q.rows);
+    int* count = (int*)(ws + q.count);
+    unsigned char* flags = p.T != 0 ? (unsigned char*)(ws + q.flags) : nullptr;
+    if (flags != nullptr) head_flags_kernel<<<(unsigned)((p.M + 3) / 4), 256, 0, st>>>(p.M, c.labels, c.ids, c.logits, p.T, p.V, flags);
+    head_rows_kernel<<<1, 1024, 0, st>>>(p.M, c.labels, flags, rows, count);
+    Gather g{};
+    g.M = p.M, g.slots = q.Mp, g.C = p.C, g.Cp = (int)q.Cp, g.T = p.T, g.V = p.V, g.rows = rows, g.count = count, g.flags = flags;
+    g.labels = c.labels, g.to = ws + q.h, g.plane = q.Mp * q.Cp * 2, g.ldh = c.h.ld;
+    g.loss = c.loss, g.lse = c.lse, g.lse_t = c.lse_t, g.z_top = c.z_top, g.dh = c.dh.p, g.lddh = c.dh.ld;
+    g.grad = backward ? (RowGrad*)(ws + q.grad) : nullptr;
+    g.in_lse = c.in_lse, g.in_lse_t = c.in_lse_t, g.dloss = c.dloss;
+    g.scale = p.scale, g.smoothing = p.smoothing, g.z_weight = p.z_weight, g.tau = p.temperature, g.label_weight = p.label_weight;
+    g.teacher_weight = p.teacher_weight;
+    if (int e = hip_status()) return e;
+    h = {g.to, g.plane, q.Cp * 2, q.Mp * q.Cp * 2, (int)q.Cp};
+    if (p.dtype == ABL_BF16) return gather<bf16_t, 1>(st, g, c.h.p, true);
+    return q.parts == 3 ? gather<float, 3>(st, g, c.h.p, true) : gather<float, 1>(st, g, c.h.p, true);
+  }
+
+  int table(int64_t v0, int64_t n, Operand& w) const {
+    if (!copied) {
+      w = {(const char*)c.W.p + v0 * c.W.ld * 2, 0, c.W.ld * 2, ((n - 1) * c.W.ld + c.p.C) * 2, c.p.C};
+      return ABL_OK;
+    }
+    char* to = ws + q.W;
+    w = {to, q.table * q.Cp * 2, q.Cp * 2, q.table * q.Cp * 2, (int)q.Cp};
+    const int64_t n_to = up(n, 256);
+    if (c.p.dtype == ABL_BF16) return copy_table<bf16_t, 1>(st, c, q, v0, n, n_to, to);
+    return q.parts == 3 ? copy_table<float, 3>(st, c, q, v0, n, n_to, to) : copy_table<float, 1>(st, c, q, v0, n, n_to, to);
+  }
+};
+
+// Whether the products can read the table where it is: bf16, 16-byte pieces within rows that lie close enough for 31-bit offsets.
+bool in_place(const HeadCall& c) {
+  return c.p.dtype == ABL_BF16 && c.p.C % 8 == 0 && c.W.ld % 8 == 0 && c.W.ld < 1 << 21 && (reinterpret_cast<uintptr_t>(c.W.p) & 15u) == 0;
+}
+
+}  // namespace
+
+size_t head_scratch_bytes(const abl_head& p, bool backward) { return plan_of(p, backward, false, true).bytes; }
+
+int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
+  const abl_head& p = c.p;
+  const bool copied = !in_place(c);
+  const Plan q = plan_of(p, false, copied, false);
+  const Call call{c, q, st, (char*)scratch, copied};
+  char* ws = call.ws;
+  const int* rows = (const int*)(ws + q.rows);
+  const int* count = (const int*)(ws + q.count);
+  const unsigned char* flags = p.T != 0 ? (const unsigned char*)(ws + q.flags) : nullptr;
+  Product a{};
+  if (int e = call.prepare(false, a.x)) return e;
+  if (c.labels != nullptr) head_labels_kernel<<<(unsigned)(q.Mp / 256), 256, 0, st>>>(rows, count, c.labels, p.V, (int*)(ws + q.labels));
+  if (c.ids != nullptr) {
+    if (p.dtype == ABL_F32)
+      head_entries_kernel<float><<<(unsigned)p.M, 256, 0, st>>>((const float*)c.h.p, c.h.ld, (const float*)c.W.p, c.W.ld, p.C, p.V, c.ids, c.logits,
+                                                               p.T, rows, count, p.scale, q.parts == 1, c.z_top);
+    else
+      head_entries_kernel<bf16_t><<<(unsigned)p.M, 256, 0, st>>>((const bf16_t*)c.h.p, c.h.ld, (const bf16_t*)c.W.p, c.W.ld, p.C, p.V, c.ids,
+                                                                c.logits, p.T, rows, count, p.scale, 0, c.z_top);
+  }
+  if (int e = hip_status()) return e;
+  Partial* carry = (Partial*)(ws + q.carry);
+  for (int i = 0; i < q.pieces; ++i) {
+    const int64_t v0 = i * q.piece, n = v0 + q.piece < p.V ? q.piece : p.V - v0;
+    if (int e = call.table(v0, n, a.y)) return e;
+    a.nx = (int)p.M, a.ny = (int)n, a.k = (int)q.Cp, a.count = count, a.count_k = 0;
+    a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
+    a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0;
+    a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp;
+    a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
+    if (int e = launch_tiles<kTile, kTile, 2, 2, false, false, kEpiPartial>(st, a)) return e;
+    Loss l{};
+    l.partial = a.partial, l.partial_ld = q.Mp, l.tiles = (int)((n + kTile - 1) / kTile), l.before = i > 0 ? carry : nullptr;
+    l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags, l.labels = c.labels, l.ids = c.ids;
+    l.logits = c.logits, l.z_label = a.z_label, l.T = p.T, l.V = p.V, l.smoothing = p.smoothing, l.z_weight = p.z_weight, l.tau = p.temperature;
+    l.label_weight = p.label_weight, l.teacher_weight = p.teacher_weight, l.loss = c.loss, l.lse = c.lse, l.lse_t = c.lse_t, l.z_top = c.z_top;
+    head_loss_kernel<<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
+    if (int e = hip_status()) return e;
+  }
+  return ABL_OK;
+}
+
+int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
+  const abl_head& p = c.p;
+  const bool accumulate = (p.flags & ABL_ACCUM_DW) != 0;
+  if (p.M == 0) {
+    if (c.dW == nullptr || accumulate) return ABL_OK;
+    const int64_t n = (int64_t)p.V * p.C * (size_of(p.dw_dtype) / 2);
+    head_zero_kernel<<<(unsigned)(n < 1 << 20 ? (n + 255) / 256 : 4096), 256, 0, st>>>((uint16_t*)c.dW, n);
+    return hip_status();
+  }
+  const bool copied = !in_place(c);
+  const Plan q = plan_of(p, true, copied, false);
+  const Call call{c, q, st, (char*)scratch, copied};
+  char* ws = call.ws;
+  const int* rows = (const int*)(ws + q.rows);
+  const int* count = (const int*)(ws + q.count);
+  Operand h, w;
+  if (int e = call.prepare(true, h)) return e;
+  for (int i = 0; i < q.pieces; ++i) {
+    const int64_t v0 = i * q.piece, n = v0 + q.piece < p.V ? q.piece : p.V - v0;
+    if (int e = call.table(v0, n, w)) return e;
+    const Operand d{ws + q.d, q.Mp * q.piece * 2, q.piece * 2, q.Mp * q.piece * 2, (int)q.piece};
+    {
+      Product a{};
+      a.x = h, a.y = w, a.nx = (int)p.M, a.ny = (int)n, a.k = (int)q.Cp, a.count = count;
+      a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
+      a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0, a.grad = (const RowGrad*)(ws + q.grad);
+      a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch, a.d_parts = q.d_parts;
+      if (int e = launch_tiles<kTile, kTile, 2, 2, false, false, kEpiGrad>(st, a)) return e;
+    }
+    if (c.ids != nullptr) {
+      Entries a{};
+      a.rows = rows, a.count = count, a.ids = c.ids, a.logits = c.logits, a.z_top = c.in_z_top, a.grad = (const RowGrad*)(ws + q.grad), a.T = p.T;
+      a.v0 = (int)v0, a.v1 = (int)(v0 + n), a.inv_tau = 1.0f / p.temperature, a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch;
+      a.d_parts = q.d_parts;
+      head_entry_grad_kernel<<<(unsigned)((p.M + 3) / 4), 256, 0, st>>>(a);
+      if (int e = hip_status()) return e;
+    }
+    if (c.dh.p != nullptr) {
+      Product a{};
+      const bool last = i + 1 == q.pieces;
+      float* acc = (float*)(ws + q.acc);
+      a.x = d, a.y = w, a.nx = (int)p.M, a.ny = p.C, a.k = (int)up(n, 64), a.count = count;
+      a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
+      a.out = last ? c.dh.p : acc, a.ld = last ? c.dh.ld : p.C, a.out_f32 = !last || p.dtype == ABL_F32, a.map = last ? rows : nullptr;
+      a.add = i > 0 ? acc : nullptr, a.add_ld = p.C;
+      if (int e = launch_tiles<kTile, kTile, 2, 2, false, true, kEpiSum>(st, a)) return e;
+    }
+    if (c.dW != nullptr) {
+      Product a{};
+      a.x = d, a.y = h, a.nx = (int)n, a.ny = p.C, a.k = (int)p.M, a.count = count, a.count_k = 1;
+      a.parts = q.parts == 3 ? 6 : q.d_parts, a.pairs = q.parts == 3 ? kPairs6 : q.d_parts == 2 ? kPairs2 : kPairs1;
+      a.out = (char*)c.dW + v0 * p.C * size_of(p.dw_dtype), a.ld = p.C, a.out_f32 = p.dw_dtype == ABL_F32, a.accumulate = accumulate;
+      if (int e = launch_tiles<kTile, kTile, 2, 2, true, true, kEpiSum>(st, a)) return e;
+    }
+  }
+  return ABL_OK;
+}
+
+}  // namespace abl

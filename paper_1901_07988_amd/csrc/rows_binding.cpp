@@ -234,6 +234,115 @@ PyObject* ckpt_wgrad(PyObject*, PyObject* const* a, Py_ssize_t n) {
                              bytes, (float*)dW));
 }
 
+// ---- losses over a vocabulary ----
+// (h, W, labels, ids, logits): sizes and addresses; ids, logits are not there for the calls without a teacher.
+bool whole_numbers(void*& p, PyObject* o, int64_t n, const char* what) {
+  if (!address(p, o, at::kLong, n, what)) return false;
+  return o == Py_None || THPVariable_Unpack(o).numel() == n || fail(what, "of another size than it has to be");
+}
+bool row_numbers(void*& p, PyObject* o, int64_t n, const char* what) {
+  if (!address(p, o, kF32, n, what)) return false;
+  return o == Py_None || THPVariable_Unpack(o).numel() == n || fail(what, "of another size than it has to be");
+}
+struct HeadArgs {
+  abl_head p;
+  Matrix h, W;
+  void *labels, *ids = nullptr, *logits = nullptr;
+};
+bool head_operands(HeadArgs& g, PyObject* h, PyObject* W, PyObject* labels) {
+  if (!matrix(g.h, h, "h") || !channels(g.h, "h") || !matrix(g.W, W, "W")) return false;
+  if (g.W.type != g.h.type) return fail("W", "of another type than it has to be");
+  if (g.W.C != g.h.C) return fail("W", "as many channels as h");
+  if (g.W.M > INT32_MAX) return fail("W", "too many rows");
+  g.p = abl_head{};
+  g.p.M = g.h.M, g.p.C = (int32_t)g.h.C, g.p.V = (int32_t)g.W.M, g.p.dtype = g.p.dw_dtype = dtype_of(g.h.type);
+  return whole_numbers(g.labels, labels, g.h.M, "labels");
+}
+bool teacher_operands(HeadArgs& g, PyObject* ids, PyObject* logits) {
+  const at::Tensor* t = tensor(ids, "top_ids");
+  if (t == nullptr) return false;
+  if (t->dim() != 2 || t->size(0) != g.h.M || t->size(1) > INT32_MAX) return fail("top_ids", "a row of entries for each row of h");
+  g.p.T = (int32_t)t->size(1);
+  return whole_numbers(g.ids, ids, g.h.M * t->size(1), "top_ids") && matrix_address(g.logits, logits, kF32, g.h.M, t->size(1), "top_logits");
+}
+bool head_flags(HeadArgs& g, PyObject* o) {
+  int flags;
+  if (!small(flags, o, "flags")) return false;
+  g.p.flags = (uint32_t)flags;
+  return true;
+}
+// dh [M, C] (rows contiguous) and dW [V, C], either None.
+bool head_gradients(HeadArgs& g, PyObject* dh, PyObject* dW, Matrix& d, void*& w) {
+  d.p = nullptr, d.ld = g.h.C, w = nullptr;
+  if (dh != Py_None && !matrix_like(d, g.h, dh, "dh")) return false;
+  if (dW == Py_None) return true;
+  const at::Tensor* t = tensor(dW, "dW");
+  if (t == nullptr) return false;
+  if (t->scalar_type() != kF32 && t->scalar_type() != g.h.type) return fail("dW", "of another type than it has to be");
+  g.p.dw_dtype = dtype_of(t->scalar_type());
+  return matrix_address(w, dW, t->scalar_type(), g.W.M, g.W.C, "dW");
+}
+
+// (h, W, labels, scratch, loss, lse, scale, smoothing, z_weight, flags)
+PyObject* xent_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HeadArgs g;
+  size_t bytes;
+  void *ws, *loss, *lse;
+  if (!count(n, 10) || !head_operands(g, a[0], a[1], a[2]) || !workspace(ws, bytes, a[3]) || !row_numbers(loss, a[4], g.h.M, "loss") ||
+      !row_numbers(lse, a[5], g.h.M, "lse") || !number(g.p.scale, a[6]) || !number(g.p.smoothing, a[7]) || !number(g.p.z_weight, a[8]) ||
+      !head_flags(g, a[9]))
+    return nullptr;
+  return code(abl_xent_forward(stream(), &g.p, g.h.p, g.h.ld, g.W.p, g.W.ld, (const int64_t*)g.labels, ws, bytes, (float*)loss, (float*)lse));
+}
+
+// (h, W, labels, lse, dloss, scratch, dh, dW, scale, smoothing, z_weight, flags)
+PyObject* xent_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HeadArgs g;
+  Matrix dh;
+  size_t bytes;
+  void *ws, *lse, *dloss, *dW;
+  if (!count(n, 12) || !head_operands(g, a[0], a[1], a[2]) || !row_numbers(lse, a[3], g.h.M, "lse") ||
+      !row_numbers(dloss, a[4], g.h.M, "dloss") || !workspace(ws, bytes, a[5]) || !head_gradients(g, a[6], a[7], dh, dW) ||
+      !number(g.p.scale, a[8]) || !number(g.p.smoothing, a[9]) || !number(g.p.z_weight, a[10]) || !head_flags(g, a[11]))
+    return nullptr;
+  return code(abl_xent_backward(stream(), &g.p, g.h.p, g.h.ld, g.W.p, g.W.ld, (const int64_t*)g.labels, (const float*)lse, (const float*)dloss, ws,
+                                bytes, dh.p, dh.ld, dW));
+}
+
+bool distill_numbers(HeadArgs& g, PyObject* const* a) {   // scale, temperature, teacher_weight, label_weight, smoothing, z_weight, flags
+  return number(g.p.scale, a[0]) && number(g.p.temperature, a[1]) && number(g.p.teacher_weight, a[2]) && number(g.p.label_weight, a[3]) &&
+         number(g.p.smoothing, a[4]) && number(g.p.z_weight, a[5]) && head_flags(g, a[6]);
+}
+
+// (h, W, labels, top_ids, top_logits, scratch, loss, lse, lse_t, z_top, 7 numbers)
+PyObject* distill_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HeadArgs g;
+  size_t bytes;
+  void *ws, *loss, *lse, *lse_t, *z_top;
+  if (!count(n, 17) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !workspace(ws, bytes, a[5]) ||
+      !row_numbers(loss, a[6], g.h.M, "loss") || !row_numbers(lse, a[7], g.h.M, "lse") || !row_numbers(lse_t, a[8], g.h.M, "lse_t") ||
+      !matrix_address(z_top, a[9], kF32, g.h.M, g.p.T, "z_top") || !distill_numbers(g, a + 10))
+    return nullptr;
+  return code(abl_distill_forward(stream(), &g.p, g.h.p, g.h.ld, g.W.p, g.W.ld, (const int64_t*)g.labels, (const int64_t*)g.ids,
+                                  (const float*)g.logits, ws, bytes, (float*)loss, (float*)lse, (float*)lse_t, (float*)z_top));
+}
+
+// (h, W, labels, top_ids, top_logits, lse, lse_t, z_top, dloss, scratch, dh, dW, 7 numbers)
+PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HeadArgs g;
+  Matrix dh;
+  size_t bytes;
+  void *ws, *lse, *lse_t, *z_top, *dloss, *dW;
+  if (!count(n, 19) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !row_numbers(lse, a[5], g.h.M, "lse") ||
+      !row_numbers(lse_t, a[6], g.h.M, "lse_t") || !matrix_address(z_top, a[7], kF32, g.h.M, g.p.T, "z_top") ||
+      !row_numbers(dloss, a[8], g.h.M, "dloss") || !workspace(ws, bytes, a[9]) || !head_gradients(g, a[10], a[11], dh, dW) ||
+      !distill_numbers(g, a + 12))
+    return nullptr;
+  return code(abl_distill_backward(stream(), &g.p, g.h.p, g.h.ld, g.W.p, g.W.ld, (const int64_t*)g.labels, (const int64_t*)g.ids,
+                                   (const float*)g.logits, (const float*)lse, (const float*)lse_t, (const float*)z_top, (const float*)dloss, ws,
+                                   bytes, dh.p, dh.ld, dW));
+}
+
 // No C++ exception may pass into the interpreter.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -249,7 +358,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 
 #define ABL_METHOD(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ABL_METHOD(ckpt_pack),   ABL_METHOD(ckpt_unpack),  ABL_METHOD(resnorm_forward), ABL_METHOD(resnorm_backward),
-                          ABL_METHOD(glu_forward), ABL_METHOD(glu_backward), ABL_METHOD(ckpt_wgrad),      {nullptr, nullptr, 0, nullptr}};
+                          ABL_METHOD(glu_forward), ABL_METHOD(glu_backward), ABL_METHOD(ckpt_wgrad),      ABL_METHOD(xent_forward),
+                          ABL_METHOD(xent_backward), ABL_METHOD(distill_forward), ABL_METHOD(distill_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,443 @@
+"""Losses over a vocabulary on the GPU, against the definition in 64 bits (tests/head_reference.py) with bounds that count the roundings."""
+import math
+
+import pytest
+import torch
+
+from tests import head_reference as R
+from paper_1901_07988_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
+
+
+def scratch_for(M, C, V, type, T=0, dw=None, backward=False, flags=0):
+    n = B.abl_head_scratch_bytes(M, C, V, type, T=T, dw_dtype=dw, backward=backward, flags=flags)
+    assert n > 0
+    s = torch.empty(n + 64, dtype=torch.uint8, device="cuda")
+    s.fill_(0xFF)                 # (NaN, wherever it is read before it is written)
+    return s[:n]
+
+
+class Case:
+    """Inputs on the CPU, a call's results on the GPU, and what they are compared with."""
+
+    def __init__(self, M, C, V, type, T=0, ignored=0.3, seed=1, pitch=(0, 0), offset=0, size=1.0, labels=True, device="cuda", **settings):
+        gen = torch.Generator().manual_seed(seed)
+        self.M, self.C, self.V, self.T, self.type = M, C, V, T, type
+        if T:
+            settings.setdefault("teacher_weight", 1.0)
+        self.n, self.settings = R.Settings(**settings), settings
+        self.full_h = torch.randn(M, C + pitch[0], generator=gen).mul_(size * 2).to(type)
+        self.full_W = (torch.randn(V, C + pitch[1], generator=gen) * C ** -0.5).to(type)
+        self.h, self.W = self.full_h[:, offset: offset + C], self.full_W[:, offset: offset + C]
+        on = torch.rand(M, generator=gen) >= ignored
+        if ignored < 1:
+            on[0] = True
+        y = torch.randint(0, V, (M,), generator=gen)
+        self.labels = torch.where(on, y, -100) if labels else None
+        self.ids = self.t = None
+        if T:
+            self.t = torch.randn(M, T, generator=gen) * 3
+            self.ids = torch.randint(0, V, (M, T), generator=gen)
+            self.ids[torch.rand(M, T, generator=gen) < 0.2] = -1
+            self.t[torch.rand(M, T, generator=gen) < 0.1] = -INF
+            if labels:
+                self.ids[::5, 0] = y[::5]                # the label is one of them
+            self.ids[1::7] = -1                          # rows without a teacher, some of them with a label
+            self.ids[~on & (torch.arange(M) % 2 == 0)] = -1
+            if T > 2:
+                self.ids[::3, T - 1] = self.ids[::3, 0]      # the same id twice
+        self.device = device
+
+    def place(self):
+        d = self.device
+        fh, fW = self.full_h.to(d), self.full_W.to(d)
+        o = self.h.storage_offset()
+        self.dh_in, self.dW_in = fh[:, o: o + self.C], fW[:, o: o + self.C]
+        self.gl = None if self.labels is None else self.labels.to(d)
+        if self.T:
+            self.gi, self.gt = self.ids.to(d), self.t.to(d)
+
+    def options(self, flags=0):
+        s = dict(self.settings, flags=flags)
+        if not self.T:
+            s.pop("label_weight", None), s.pop("teacher_weight", None), s.pop("temperature", None)
+        else:
+            s.setdefault("label_weight", 1.0)
+        return s
+
+    def forward(self, flags=0, scratch=None):
+        self.place()
+        d = self.device
+        out = {k: torch.full((self.M,), 7.0, device=d) for k in ("loss", "lse")}
+        if scratch is None:
+            scratch = scratch_for(self.M, self.C, self.V, self.type, self.T, flags=flags)
+        if self.T:
+            out |= dict(lse_t=torch.full((self.M,), 7.0, device=d), z_top=torch.full((self.M, self.T), 7.0, device=d))
+            B.abl_distill_forward(self.dh_in, self.dW_in, self.gl, self.gi, self.gt, scratch, out["loss"], out["lse"], out["lse_t"], out["z_top"],
+                                  **self.options(flags))
+        else:
+            B.abl_xent_forward(self.dh_in, self.dW_in, self.gl, scratch, out["loss"], out["lse"], **self.options(flags))
+        self.out = out
+        return out
+
+    def backward(self, dw=None, flags=0, dh=None, dW=None, want=(True, True), seed=5, scratch=None):
+        d = self.device
+        dw = dw or self.type
+        self.dloss = torch.randn(self.M, generator=torch.Generator().manual_seed(seed))
+        if dh is None and want[0]:
+            dh = torch.full((self.M, self.C), 7.0, dtype=self.type, device=d)
+        if dW is None and want[1]:
+            dW = torch.full((self.V, self.C), 7.0, dtype=dw, device=d)
+        if scratch is None:
+            scratch = scratch_for(self.M, self.C, self.V, self.type, self.T, dw, True, flags)
+        g = self.dloss.to(d)
+        o = self.out
+        if self.T:
+            B.abl_distill_backward(self.dh_in, self.dW_in, self.gl, self.gi, self.gt, o["lse"], o["lse_t"], o["z_top"], g, scratch, dh, dW,
+                                   **self.options(flags))
+        else:
+            B.abl_xent_backward(self.dh_in, self.dW_in, self.gl, o["lse"], g, scratch, dh, dW, **self.options(flags))
+        return dh, dW
+
+    def check_forward(self):
+        got = self.forward()
+        want = R.forward(self.h, self.W, self.labels, self.n, self.ids, self.t)
+        for k in got:
+            R.assert_within(got[k], want[k], want["bound"][k], k)
+        return want
+
+    def reference(self, dw=None, one_part=False):
+        return R.backward(self.h, self.W, self.labels, self.out["lse"].cpu(), self.dloss, self.n, self.type, dw or self.type, one_part, self.ids, self.t,
+                          self.out["lse_t"].cpu() if self.T else None)
+
+    def check(self, dw=None):
+        self.check_forward()
+        dh, dW = self.backward(dw)
+        want = self.reference(dw)
+        R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+        R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+
+
+SIZES = [(1, 1, 1), (1, 64, 2), (3, 7, 5), (2, 8, 130), (17, 72, 300), (61, 1000, 1013), (130, 33, 257), (257, 64, 129), (300, 520, 515)]
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M,C,V", SIZES)
+def test_cross_entropy(M, C, V, type):
+    Case(M, C, V, type).check()
+
+
+@pytest.mark.parametrize("type,dw", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("smoothing,z_weight,scale", [(0.1, 0.0, 1.0), (0.0, 0.01, 0.5), (0.3, 1e-3, -1.7), (0.0, 0.0, 0.0)])
+def test_cross_entropy_options(type, dw, smoothing, z_weight, scale):
+    Case(150, 200, 333, type, smoothing=smoothing, z_weight=z_weight, scale=scale).check(dw)
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M,C,V,T", [(1, 1, 1, 1), (3, 7, 5, 2), (40, 64, 200, 5), (130, 100, 257, 64), (70, 130, 520, 65), (33, 72, 300, 200)])
+def test_distillation(M, C, V, T, type):
+    Case(M, C, V, type, T=T).check()
+
+
+@pytest.mark.parametrize("type,dw", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("tau,labels,kw", [(1.0, False, {}), (2.0, False, dict(z_weight=1e-3)), (3.0, True, dict(label_weight=0.5, smoothing=0.1)),
+                                           (0.5, True, dict(label_weight=0.0)), (1.0, True, dict(teacher_weight=0.3, scale=0.7, z_weight=0.01))])
+def test_distillation_options(type, dw, tau, labels, kw):
+    Case(90, 136, 410, type, T=9, labels=labels, temperature=tau, **kw).check(dw)
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("pitch,offset", [((8, 8), 0), ((8, 16), 8), ((5, 3), 0), ((9, 9), 1), ((0, 1), 0), ((64, 0), 0)])
+def test_slices_of_wider_tensors(type, pitch, offset):
+    c = Case(70, 96, 210, type, pitch=pitch, offset=min(offset, min(pitch)))
+    c.check_forward()
+    wide = torch.full((70, 96 + 13), 7.0, dtype=type, device="cuda")
+    dh, dW = c.backward(dh=wide[:, 5:101])
+    want = c.reference()
+    R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+    assert bool((wide[:, :5] == 7).all()) and bool((wide[:, 101:] == 7).all())     # what lies beside it is left as it was
+    # channels beyond the slice may hold anything
+    if pitch[0] and pitch[1]:
+        before = {k: v.clone() for k, v in c.out.items()}
+        c.full_h[:, c.h.storage_offset() + 96:] = math.nan
+        c.full_W[:, c.W.storage_offset() + 96:] = math.nan
+        c.forward()
+        assert all(torch.equal(before[k], c.out[k]) for k in before)
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("T", [0, 6])
+def test_rows_that_do_not_count(type, T):
+    """Their h may be infinite or NaN, and nothing of it shows; their gradient is zero."""
+    c = Case(200, 80, 140, type, T=T, ignored=0.6)
+    off = c.labels < 0
+    if T:
+        off &= ~((c.ids >= 0) & (c.t > -INF)).any(1)
+    assert 10 < int(off.sum()) < 190
+    c.full_h[off] = torch.tensor([math.nan, INF, -INF, torch.finfo(type).min])[torch.arange(int(off.sum())) % 4][:, None].to(type)
+    c.check()
+    dh, _ = c.backward()
+    assert bool((dh.cpu()[off] == 0).all()) and bool((c.out["loss"].cpu()[off] == 0).all())
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("T", [0, 3])
+def test_no_row_counts(type, T):
+    c = Case(37, 40, 90, type, T=T, ignored=1.0)
+    if T:
+        c.ids[:] = -1
+    out = c.forward()
+    assert all(bool((v == 0).all()) for v in out.values())
+    dh, dW = c.backward()
+    assert bool((dh == 0).all()) and bool((dW == 0).all())
+    kept = torch.ones(90, 40, dtype=type, device="cuda")
+    c.backward(dW=kept, flags=B.ABL_ACCUM_DW)
+    assert bool((kept == 1).all())
+
+
+def test_no_rows():
+    W, h, y = torch.ones(12, 8, device="cuda"), torch.ones(0, 8, device="cuda"), torch.ones(0, dtype=torch.int64, device="cuda")
+    s, e = torch.empty(4096, dtype=torch.uint8, device="cuda"), torch.empty(0, device="cuda")
+    B.abl_xent_forward(h, W, y, s, e, e)
+    dW = torch.ones(12, 8, device="cuda")
+    B.abl_xent_backward(h, W, y, e, e, s, h, dW, flags=B.ABL_ACCUM_DW)
+    assert bool((dW == 1).all())
+    B.abl_xent_backward(h, W, y, e, e, s, h, dW)
+    assert bool((dW == 0).all())
+
+
+@pytest.mark.parametrize("T", [0, 4])
+def test_ids_beyond_the_vocabulary_are_nan(T):
+    c = Case(20, 32, 50, BF16, T=T, ignored=0.0)
+    good = {k: v.clone() for k, v in c.forward().items()}
+    if T:
+        c.ids[3, 1], c.t[3, 1] = 50, 0.5
+        c.ids[9, 0], c.t[9, 0] = 1 << 40, 0.5
+    else:
+        c.labels[3], c.labels[9] = 50, 1 << 40
+    out = c.forward()
+    bad = torch.zeros(20, dtype=torch.bool)
+    bad[[3, 9]] = True
+    assert bool(out["loss"].cpu()[bad].isnan().all())
+    assert torch.equal(out["loss"].cpu()[~bad], good["loss"].cpu()[~bad])
+    dh, dW = c.backward()
+    assert bool(dh.cpu()[bad].isnan().all()) and not bool(dh.cpu()[~bad].isnan().any()) and bool(dW.isnan().any())
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+def test_values_that_are_not_finite(type):
+    c = Case(20, 32, 50, type, ignored=0.0)
+    c.full_h[4, 3] = math.nan
+    c.full_h[7, 1] = INF
+    out = c.forward()
+    bad = torch.zeros(20, dtype=torch.bool)
+    bad[[4, 7]] = True
+    assert not bool(out["loss"].cpu()[bad].isfinite().any()) and bool(out["loss"].cpu()[~bad].isfinite().all())
+    dh, dW = c.backward()
+    assert not bool(dh.cpu()[bad].isfinite().any()) and bool(dh.cpu()[~bad].isfinite().all()) and bool(dW.isnan().any())
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+def test_extreme_logits(type):
+    """A certain row (loss near zero) and one whose label is all but impossible."""
+    c = Case(16, 64, 100, type, ignored=0.0, size=12.0)
+    c.labels[:8] = (c.h[:8].double() @ c.W.double().t()).argmax(1)
+    c.labels[8:] = (c.h[8:].double() @ c.W.double().t()).argmin(1)
+    c.check()
+
+
+@pytest.mark.parametrize("type,dw", [(F32, F32), (BF16, BF16), (BF16, F32)])
+def test_table_gradient_is_added(type, dw):
+    c = Case(90, 72, 133, type)
+    c.forward()
+    dh, dW = c.backward(dw)
+    start = torch.randn(133, 72, generator=torch.Generator().manual_seed(9)).to(dw)
+    got = start.cuda()
+    c.backward(dw, dW=got, flags=B.ABL_ACCUM_DW)
+    want = c.reference(dw)
+    total = want["dW"] + start.double()
+    R.assert_within(got, total, want["bound"]["dW"] + (R.B16 if dw == BF16 else R.F32) * total.abs(), "dW")
+
+
+@pytest.mark.parametrize("T", [0, 5])
+def test_one_gradient_alone_and_dh_over_h(T):
+    c = Case(77, 104, 190, BF16, T=T)
+    c.forward()
+    dh, dW = c.backward()
+    a, none = c.backward(want=(True, False))
+    none2, b = c.backward(want=(False, True))
+    assert torch.equal(a, dh) and torch.equal(b, dW)
+    c.dh_in = c.dh_in.clone()
+    c.backward(dh=c.dh_in, dW=(w := torch.empty_like(dW)))
+    assert torch.equal(c.dh_in, dh) and torch.equal(w, dW)
+
+
+@pytest.mark.parametrize("T", [0, 5])
+def test_operands_rounded_to_bf16(T):
+    """ABL_MATH_BF16 in fp32: as if h and W had been rounded, and the gradient of the logits."""
+    c = Case(77, 104, 190, F32, T=T)
+    out = {k: v.clone() for k, v in c.forward(flags=B.ABL_MATH_BF16).items()}
+    dh, dW = c.backward(flags=B.ABL_MATH_BF16)
+    r = Case(77, 104, 190, F32, T=T)
+    r.full_h.copy_(r.full_h.bfloat16().float()), r.full_W.copy_(r.full_W.bfloat16().float())
+    want = R.forward(r.h, r.W, r.labels, r.n, r.ids, r.t)
+    names = ("loss", "lse", "lse_t", "z_top") if T else ("loss", "lse")
+    for k in names:
+        R.assert_within(out[k], want[k], want["bound"][k], k)
+    want = R.backward(r.h, r.W, r.labels, out["lse"].cpu(), c.dloss, r.n, F32, F32, True, r.ids, r.t, out["lse_t"].cpu() if T else None)
+    # (dh's product, too, takes one part: bounds of that)
+    lost = R.backward(r.h, r.W, r.labels, out["lse"].cpu(), c.dloss, r.n, BF16, BF16, True, r.ids, r.t, out["lse_t"].cpu() if T else None)
+    R.assert_within(dh, want["dh"], lost["bound"]["dh"], "dh")
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+    # fp32 gradient of a bf16 table in one part
+    c = Case(77, 104, 190, BF16, T=T)
+    c.forward()
+    _, dW = c.backward(F32, flags=B.ABL_MATH_BF16)
+    want = c.reference(F32, one_part=True)
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+
+
+@pytest.mark.parametrize("M,C,V,type,T", [(4100, 64, 40000, BF16, 0), (1100, 2049, 20000, BF16, 3), (4000, 40, 24000, F32, 2), (100, 4000, 6000, F32, 0)])
+def test_pieces_of_the_vocabulary(M, C, V, type, T):
+    """More tokens than a workspace holds at a time: the forward's sums and dh go on from piece to piece.  (Rows and tokens are looked at in part.)"""
+    c = Case(M, C, V, type, T=T, ignored=0.9 if M > 2000 else 0.5)
+    c.check_forward()
+    dh, dW = c.backward()
+    want = c.reference()
+    R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+
+
+@pytest.mark.parametrize("type,T", [(BF16, 0), (BF16, 4), (F32, 4)])
+def test_results_repeat(type, T):
+    c = Case(300, 200, 700, type, T=T)
+    out = {k: v.clone() for k, v in c.forward().items()}
+    dh, dW = c.backward()
+    for _ in range(3):
+        again = c.forward()
+        a, b = c.backward()
+        assert all(torch.equal(out[k], again[k]) for k in out) and torch.equal(a, dh) and torch.equal(b, dW)
+
+
+@pytest.mark.parametrize("T", [0, 4])
+def test_side_stream_and_captured(T):
+    """On a stream of its own and captured: new inputs in place, other rows counting, replays between eager calls."""
+    c = Case(150, 96, 300, BF16, T=T)
+    c.forward()
+    ws, wb = scratch_for(150, 96, 300, BF16, T), scratch_for(150, 96, 300, BF16, T, None, True)
+    g = torch.randn(150, device="cuda")
+    out = {k: torch.empty_like(v) for k, v in c.out.items()}
+    dh, dW = torch.empty(150, 96, dtype=BF16, device="cuda"), torch.empty(300, 96, dtype=BF16, device="cuda")
+
+    def step(out, dh, dW, ws, wb):
+        if T:
+            B.abl_distill_forward(c.dh_in, c.dW_in, c.gl, c.gi, c.gt, ws, out["loss"], out["lse"], out["lse_t"], out["z_top"], **c.options())
+            B.abl_distill_backward(c.dh_in, c.dW_in, c.gl, c.gi, c.gt, out["lse"], out["lse_t"], out["z_top"], g, wb, dh, dW, **c.options())
+        else:
+            B.abl_xent_forward(c.dh_in, c.dW_in, c.gl, ws, out["loss"], out["lse"], **c.options())
+            B.abl_xent_backward(c.dh_in, c.dW_in, c.gl, out["lse"], g, wb, dh, dW, **c.options())
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step(out, dh, dW, ws, wb)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(out, dh, dW, ws, wb)
+    e_ws, e_wb = scratch_for(150, 96, 300, BF16, T), scratch_for(150, 96, 300, BF16, T, None, True)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for i in range(4):
+        c.dh_in.copy_(torch.randn(150, 96, generator=gen, device="cuda"))
+        c.gl.copy_(torch.where(torch.rand(150, generator=gen, device="cuda") < 0.2 * i, -1, torch.randint(0, 300, (150,), generator=gen, device="cuda")))
+        for t in (*out.values(), dh, dW):
+            t.fill_(7)
+        graph.replay()
+        e_out, e_dh, e_dW = {k: torch.empty_like(v) for k, v in out.items()}, torch.empty_like(dh), torch.empty_like(dW)
+        step(e_out, e_dh, e_dW, e_ws, e_wb)
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], e_out[k]) for k in out) and torch.equal(dh, e_dh) and torch.equal(dW, e_dW), i
+
+
+def test_two_calls_at_once():
+    """Two streams, each with a workspace of its own."""
+    a, b = Case(260, 128, 900, BF16, seed=1), Case(260, 128, 900, BF16, seed=2, T=4)
+    want = [(dict(c.forward()), *c.backward()) for c in (a, b)]
+    want = [({k: v.clone() for k, v in w[0].items()}, w[1], w[2]) for w in want]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for c, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                got.append((c.forward(), *c.backward()))
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert all(torch.equal(w[0][k], g[0][k]) for k in w[0]) and torch.equal(w[1], g[1]) and torch.equal(w[2], g[2])
+
+
+def test_the_forward_without_log_sums():
+    """lse is not needed where only the teacher counts."""
+    c = Case(50, 64, 120, BF16, T=6, labels=False, temperature=2.0)
+    out = {k: v.clone() for k, v in c.forward().items()}
+    o = {k: torch.empty_like(v) for k, v in out.items()}
+    B.abl_distill_forward(c.dh_in, c.dW_in, None, c.gi, c.gt, scratch_for(50, 64, 120, BF16, 6), o["loss"], None, o["lse_t"], o["z_top"], **c.options())
+    assert all(torch.equal(o[k], out[k]) for k in ("loss", "lse_t", "z_top"))
+    dh, dW = c.backward()
+    a, b = torch.empty_like(dh), torch.empty_like(dW)
+    B.abl_distill_backward(c.dh_in, c.dW_in, None, c.gi, c.gt, None, o["lse_t"], o["z_top"], c.dloss.cuda(), scratch_for(50, 64, 120, BF16, 6, None, True),
+                           a, b, **c.options())
+    assert torch.equal(a, dh) and torch.equal(b, dW)
+
+
+def test_gradients_are_differences_of_the_losses():
+    """The backward calls against what the forward calls say of moved inputs."""
+    for T in (0, 4):
+        c = Case(24, 40, 70, F32, T=T, **(dict(temperature=2.0, label_weight=0.5) if T else dict(smoothing=0.1, z_weight=0.01)))
+        c.forward()
+        dh, dW = c.backward()
+        w = c.dloss.double()
+        base_h, base_W = c.full_h.clone(), c.full_W.clone()
+        gen = torch.Generator().manual_seed(8)
+        for which, grad in (("full_h", dh), ("full_W", dW)):
+            base = base_h if which == "full_h" else base_W
+            step = torch.randn(base.shape, generator=gen)
+            step /= step.norm()
+            eps = 2.0 ** -5
+            values = []
+            for sign in (1, -1):
+                getattr(c, which).copy_(base + sign * eps * step)
+                values.append(float((w * c.forward()["loss"].cpu().double()).sum()))
+            getattr(c, which).copy_(base)
+            d = (values[0] - values[1]) / (2 * eps)
+            want = float((grad.cpu().double() * step.double()).sum())
+            # a loss of 24 rows of up to 10 in fp32: 24 * 10 * 2^-22 / (2 eps); third derivatives: eps^2 times the gradient's size
+            assert abs(d - want) < 24 * 10 * 2.0 ** -22 / (2 * eps) + 2 * eps ** 2 * float(grad.norm()), (T, which, d, want)
+
+
+def test_wrong_tensors_are_refused():
+    h, W = torch.zeros(4, 8, device="cuda"), torch.zeros(6, 8, device="cuda")
+    y, v = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    s = scratch_for(4, 8, 6, F32)
+    for args in ((h, W.bfloat16(), y, s, v, v), (h, W[:, :7], y, s, v, v), (h, W, y.int(), s, v, v), (h, W, y[:3], s, v, v), (h, W, y, s, v[:3], v),
+                 (h, W, y, s, v, v.double()), (h.t(), W, y, s, v, v), (h[0], W, y, s, v, v), (h, W, y, s.cpu(), v, v)):
+        with pytest.raises(AssertionError):
+            B.abl_xent_forward(*args)
+    with pytest.raises(B.AblError):
+        B.abl_xent_forward(h, W, y, s[:16], v, v)
+    with pytest.raises(B.AblError):
+        B.abl_xent_forward(h, W, None, s, v, v)
+    s = scratch_for(4, 8, 6, F32, backward=True)
+    for dh, dW in ((h, W[:5]), (h[:3], W), (h.bfloat16(), W), (h, W.bfloat16()), (h, W.t())):
+        with pytest.raises(AssertionError):
+            B.abl_xent_backward(h, W, y, v, v, s, dh, dW)
+    ids, t = torch.zeros(4, 3, dtype=torch.int64, device="cuda"), torch.zeros(4, 3, device="cuda")
+    s = scratch_for(4, 8, 6, F32, T=3)
+    for i, l, z in ((ids[:3], t, t), (ids, t[:, :2], t), (ids, t, t[:, :2]), (ids.int(), t, t), (ids, t.double(), t)):
+        with pytest.raises(AssertionError):
+            B.abl_distill_forward(h, W, y, i, l, s, v, v, v, z)
