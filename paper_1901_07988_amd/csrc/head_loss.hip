@@ -11,6 +11,8 @@
 // that do not count (prompts, padding) cost nothing.  fp32 operands are copied as three bf16 parts whose sum they are; a product of such operands is six
 // products of parts, one after the other in the same sums, the small ones first.
 
+#include <utility>
+
 #include "head.h"
 
 namespace abl {
@@ -141,9 +143,9 @@ __device__ inline void copy_row(const T* from, int C, int Cp, char* to, int64_t 
 // Rows 0..n-1 of a tensor, and zero rows up to n_to.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void head_copy_kernel(const T* __restrict__ from, int64_t ld, int64_t n, int64_t n_to, int C, int Cp,
-                                                        char* __restrict__ to, int64_t plane) {
+                                                        char* __restrict__ to, int64_t pitch, int64_t plane) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row < n_to) copy_row<T, P>(row < n ? from + row * ld : nullptr, C, Cp, to + row * (2 * (int64_t)Cp), plane);
+  if (row < n_to) copy_row<T, P>(row < n ? from + row * ld : nullptr, C, Cp, to + row * pitch, plane);
 }
 
 // What the backward pass knows of a row that counts (the formula above; all times the row's dloss and the logits' scale).  At temperature one a
@@ -161,7 +163,7 @@ struct Gather {
   const unsigned char* flags;   // nullptr: by the labels
   const int64_t* labels;
   char* to;                     // planes of the rows that count
-  int64_t plane, ldh;
+  int64_t pitch, plane, ldh;
   // forward: of the rows that do not count, written as zeros
   float *loss, *lse, *lse_t, *z_top;
   // backward
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
   if (n < g.slots) {
     if (n >= (count + kRowTile - 1) / kRowTile * kRowTile) return;
     const int64_t row = n < count ? g.rows[n] : -1;
-    copy_row<T, P>(row >= 0 ? h + row * g.ldh : nullptr, g.C, g.Cp, g.to + n * (2 * (int64_t)g.Cp), g.plane);
+    copy_row<T, P>(row >= 0 ? h + row * g.ldh : nullptr, g.C, g.Cp, g.to + n * g.pitch, g.plane);
     if (g.grad != nullptr && lane == 0) {
       RowGrad r{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1, 0};
       if (row >= 0) {
@@ -224,9 +226,8 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
 struct Operand {
   const char* p;        // first element of the first plane
   int64_t plane;        // bytes from plane to plane
-  int64_t pitch;        // bytes from row to row
-  int64_t bytes;        // from p on, of a plane: reads beyond give zero
-  int along;            // elements that exist along a row (the others read as zero): a multiple of 8
+  int64_t pitch;        // bytes from row to row, less than 2^22
+  int rows, along;      // rows, and elements along a row, that exist (others read as zero); along: a multiple of 8
 };
 struct Partial {        // of a row of a tile of logits: maximum, sum of exp(z - max), of exp((z - max) / tau), of z
   float top, sum, sum_t, z;
@@ -259,73 +260,126 @@ struct Product {
 };
 enum { kEpiPartial, kEpiGrad, kEpiSum };
 
-// A 16-byte piece of a staged tile.  k along the rows: rows of 64 k's are 8 pieces, the c-th of row r at place c xor (r / 2) % 8: the 16
+// A 16-byte piece of a staged tile of 64 k's.  k along the rows: rows of eight pieces, the c-th of row r at place c xor (r / 2) % 8: the 16
 // rows of a fragment's read take all banks once.  k outermost: rows (one k) of B channels; the even pieces come first, the c-th of each kind at place
 // c xor a key of the row, the odd ones further by half of a row's pieces and in other places of it: half a wave's transposing read, 16 pieces of
 // the eight rows 0..3 and 8..11 (or 4..7 and 12..15), takes all banks once.
-__device__ inline int key_of(int k) { return (k & 3) | ((k >> 1) & 4); }
+__device__ inline int key_along(int row) { return (row >> 1) & 7; }
+__device__ inline int key_outer(int k) { return (k & 3) | ((k >> 1) & 4); }
 template <int B, bool OUTER>
 __device__ inline int staged_piece(int row, int q) {
   if constexpr (OUTER) {
     constexpr int kHalf = B / 16;
-    return row * (B * 2) + (q & 1) * B + (((q >> 1) ^ key_of(row) ^ ((q & 1) * (kHalf - 4))) * 16);
+    return row * (B * 2) + (q & 1) * B + (((q >> 1) ^ key_outer(row) ^ ((q & 1) * (kHalf - 4))) * 16);
   } else {
-    return row * 128 + ((q ^ ((row >> 1) & 7)) * 16);
+    return row * 128 + ((q ^ key_along(row)) * 16);
   }
 }
 
-// Each lane's 16 bytes at `at` go to LDS, one lane's behind the other's from `to` on (zeros where they lie beyond the descriptor).
-__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t from, char* to, uint32_t at) {
-#ifdef __HIP_DEVICE_COMPILE__   // (the host's pass does not know this size)
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
-#endif
+// Each lane's 16 bytes at `at` + `step` go to LDS, one lane's behind the other's from byte `to` + TO on (zeros where they lie beyond the descriptor).  In
+// assembly: the compiler takes every later read of LDS for one that needs the data and waits for all loads there.  Nothing comes back in registers.
+template <int TO>
+__device__ inline void load_to_lds(u32x4 from, uint32_t to, uint32_t at, uint32_t step) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(at), "s"(from), "s"(step), "i"(TO) : "scc");
 }
 
-// Where a thread's 16-byte loads of a tile come from: the loads go to LDS in the order of the threads, so the places' order is undone here.
-template <int B, bool OUTER, int THREADS>
+__device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }   // the same in all lanes, in a scalar register
+
+// A thread's share of the tiles of an operand, from step to step.  The loads go to LDS in the order of the threads, so the places' order is undone
+// here; the rows of a thread's loads are a constant apart that no key sees.  MASK: elements beyond `along` may lie in a step (k along the rows).
+template <int B, bool OUTER, bool MASK, int THREADS>
 struct Source {
-  static constexpr int kLoads = B * 8 / THREADS;
-  uint32_t at[kLoads];
-  int first[kLoads];   // element along the row
-  __device__ inline void init(int64_t pitch) {
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int place = n * THREADS + (int)threadIdx.x;
-      int row, q;
-      if constexpr (OUTER) {
-        constexpr int kHalf = B / 16;
-        row = place / (2 * kHalf);
-        const int in = place % (2 * kHalf), odd = in / kHalf;
-        q = 2 * ((in % kHalf) ^ key_of(row) ^ (odd * (kHalf - 4))) + odd;
-      } else {
-        row = place / 8;
-        q = (place % 8) ^ ((row >> 1) & 7);
-      }
-      at[n] = (uint32_t)row * (uint32_t)pitch + (uint32_t)q * 16u;
-      first[n] = q * 8;
+  static constexpr int kLoads = B * 8 / THREADS, kPieces = OUTER ? B / 8 : 8, kRows = THREADS / kPieces;   // rows of a load
+  static_assert(kRows % 16 == 0, "the keys' period");
+  static constexpr int kPlaces = OUTER ? 1 : kLoads;   // (k outermost: the loads' distance goes with the scalar offset, to save registers)
+  uint32_t at[kPlaces];
+  int first;              // element along the row
+  uint64_t base;
+  uint32_t pitch, bytes;  // of the rows that a step may read
+  int k, left;            // k outermost: rows that are left
+  u32x4 from;
+  uint32_t step;
+
+  __device__ inline void init(const Operand& o, int w0) {
+    pitch = (uint32_t)o.pitch;
+    const int row = (int)threadIdx.x / kPieces, in = (int)threadIdx.x % kPieces;
+    int q;
+    if constexpr (OUTER) {
+      constexpr int kHalf = B / 16;
+      const int odd = in / kHalf;
+      q = 2 * ((in % kHalf) ^ key_outer(row) ^ (odd * (kHalf - 4))) + odd;
+    } else {
+      q = in ^ key_along(row);
     }
-  }
-  // origin: byte of the tile's first element; left: elements along the row from there on.
-  __device__ inline void load(const Operand& o, int64_t origin, int plane, int left, char* lds) const {
-    const int64_t bytes = o.bytes - origin;
-    const auto from = descriptor(o.p + plane * o.plane + origin, bytes < 0 ? 0 : bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF);
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    first = q * 8;
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n)
-      load_to_lds(from, lds + (n * THREADS + wave * 64) * 16, first[n] < left ? at[n] : kNowhere);
+    for (int n = 0; n < kPlaces; ++n)
+      at[n] = OUTER && w0 + first >= o.along ? kNowhere : (uint32_t)(row + n * kRows) * pitch + (uint32_t)q * 16u;
+  }
+  // On by a step, or to the first step of a plane, or (not more) zeros from here on.  Without branches: a loop of one block keeps the sums in their registers.
+  // first, more: all bits set, or none.
+  __device__ inline void next(const Operand& o, int w0, int first_step, int plane, int more) {
+    const uint64_t begin = (uint64_t)(o.p + plane * o.plane + (OUTER ? w0 * 2 : w0 * o.pitch)) & 0xFFFFFFFFFFFFull;
+    const uint64_t after = base + (OUTER ? (uint64_t)pitch * 64u : 0u);
+    base = after ^ ((after ^ begin) & (uint64_t)(int64_t)first_step);
+    k = (k + 64) & ~first_step;
+    if constexpr (OUTER) {
+      const int rest = left - 64 > 0 ? left - 64 : 0;
+      left = (rest ^ ((rest ^ o.rows) & first_step)) & more;
+    } else {
+      bytes = (uint32_t)(o.rows - w0 < B ? o.rows - w0 : B) * pitch & (uint32_t)more;
+    }
+    from = u32x4{uniform((uint32_t)base), uniform((uint32_t)(base >> 32)), uniform(OUTER ? (uint32_t)(left < 64 ? left : 64) * pitch : bytes), 0x00027000u};
+    step = OUTER ? 0u : uniform((uint32_t)(2 * k & more));   // (an access is out of range where its own offset is not below the bytes less the scalar one)
+  }
+  // The n-th load of a step.
+  template <int TO>
+  __device__ inline void load(const Operand& o, int n, uint32_t to) const {
+    if constexpr (OUTER) {
+      const uint32_t by = (uint32_t)(n * kRows) * pitch;
+      load_to_lds<TO>(from, to, at[0], uniform(by < from[2] ? by : from[2]));
+    } else {
+      load_to_lds<TO>(from, to, !MASK || first + k < o.along ? at[n] : kNowhere, step);
+    }
   }
 };
 
-// The k-step `ks` (32 of a tile's 64) of the 16 rows or columns from w on.
+// Where a wave's fragments of 16 rows or columns from w on lie in a tile: all addresses are the first one's with bits of the place changed and constants added.
 template <int B, bool OUTER>
-__device__ inline bf16x8_t fragment_of(const char* tile, int w, int ks) {
-  const int lane = threadIdx.x & 63;
-  if constexpr (OUTER) {
-    const char* p = tile + staged_piece<B, true>(ks * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), w / 8 + ((lane >> 1) & 1)) + (lane & 1) * 8;
-    return transposed(p, p + 4 * (B * 2));
-  } else {
-    return piece(tile + staged_piece<B, false>(w + (lane & 15), ks * 4 + (lane >> 4)));
+struct Fragments {
+  uint32_t base;
+  __device__ inline void init(uint32_t tile, int w) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (OUTER)
+      base = tile + staged_piece<B, true>((lane >> 4) * 8 + ((lane & 15) >> 2), w / 8 + ((lane >> 1) & 1)) + (lane & 1) * 8;
+    else
+      base = tile + staged_piece<B, false>(w + (lane & 15), lane >> 4);
   }
+  // (keeps the compiler from holding all addresses in registers)
+  __device__ inline void again() {
+    if constexpr (OUTER) asm volatile("" : "+v"(base));
+  }
+  // The n-th one's 32 k's: the first or second of the tile in place `at`.
+  __device__ inline bf16x8_t get(int n, int half, int at) const {
+    constexpr int kTileBytes = B * 128;
+    if constexpr (OUTER) {
+      lds_short4* p = (lds_short4*)(uintptr_t)((base ^ (n * 16)) + at * kTileBytes + half * (kTileBytes / 2));
+      struct two { short4_t a, b; };
+      return __builtin_bit_cast(bf16x8_t, two{__builtin_amdgcn_ds_read_tr16_b64_v4i16(p), __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 4 * (B * 2) / 8)});
+    } else {
+      typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
+      return *(lds_bf16x8*)(uintptr_t)((base ^ (half * 64)) + at * kTileBytes + n * (16 * 128));
+    }
+  }
+};
+
+template <int N, typename F, int... I>
+__device__ inline void for_each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ inline void for_each(F f) {
+  for_each<N>(f, std::make_integer_sequence<int, N>{});
 }
 
 __device__ inline float lanes16_max(float v) {   // over the four lanes 16 apart
@@ -349,12 +403,14 @@ __device__ inline Partial join(const Partial& a, const Partial& b, float inv_tau
   return r;
 }
 
+// A block has a tile of BX x BY, WX x WY waves a part of it each.  Steps of 64 k's: their operands go from memory straight to one of two places in
+// LDS, a step and a half ahead, and from there to registers half a step ahead, all between matrix instructions.
 template <int BX, int BY, int WX, int WY, bool XO, bool YO, int EPI>
 __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   constexpr int kThreads = WX * WY * 64, FX = BX / WX / 16, FY = BY / WY / 16;
-  constexpr int kXBytes = BX * 128, kStage = (BX + BY) * 128;
-  extern __shared__ __align__(16) char lds[];   // [2][kStage]
-  const int count = a.count != nullptr ? *a.count : 0;
+  constexpr int kXBytes = BX * 128, kYBytes = BY * 128;
+  extern __shared__ __align__(16) char lds[];   // [2][BX][128], [2][BY][128]
+  const int count = a.count != nullptr ? (int)uniform((uint32_t)*a.count) : 0;
   const int nx = a.count != nullptr && !a.count_k ? count : a.nx, nk = a.count != nullptr && a.count_k ? count : a.k;
   // Blocks 8 apart share an XCD and its L2.  Each XCD takes consecutive items, in bands of eight tiles of rows.
   constexpr int kBand = 8;
@@ -367,18 +423,29 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   const int x0 = (band * kBand + rest % high) * BX, tile_y = rest / high, y0 = tile_y * BY;
   const int steps_k = (nk + 63) / 64, steps = steps_k * a.parts;
 
-  Source<BX, XO, kThreads> sx;
-  Source<BY, YO, kThreads> sy;
-  sx.init(a.x.pitch);
-  sy.init(a.y.pitch);
-  int load_k = 0, load_part = 0;
-  auto load = [&](char* to) __attribute__((always_inline)) {
-    const int pair = (int)(a.pairs >> (8 * load_part));
-    const int k0 = load_k * 64;
-    const int64_t ox = XO ? k0 * a.x.pitch + x0 * 2 : x0 * a.x.pitch + k0 * 2, oy = YO ? k0 * a.y.pitch + y0 * 2 : y0 * a.y.pitch + k0 * 2;
-    sx.load(a.x, ox, pair & 15, a.x.along - (XO ? x0 : k0), to);
-    sy.load(a.y, oy, (pair >> 4) & 15, a.y.along - (YO ? y0 : k0), to + kXBytes);
-    if (++load_k == steps_k) load_k = 0, ++load_part;
+  Source<BX, XO, false, kThreads> sx;
+  Source<BY, YO, !YO, kThreads> sy;
+  sx.init(a.x, x0);
+  sy.init(a.y, y0);
+  constexpr int kLoads = sx.kLoads + sy.kLoads;   // of a step
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  int load_k = steps_k - 1, load_part = -1;
+  auto next_load = [&]() __attribute__((always_inline)) {   // (beyond the last step: zeros)
+    ++load_k;
+    const int first = ~((load_k - steps_k) >> 31);
+    load_k &= ~first;
+    load_part -= first;
+    const int pair = (int)(a.pairs >> (8 * load_part)), more = (load_part - a.parts) >> 31;
+    sx.next(a.x, x0, first, pair & 15, more);
+    sy.next(a.y, y0, first, (pair >> 4) & 15, more);
+  };
+  const uint32_t load_to = uniform(lds0 + (threadIdx.x >> 6) * 1024);
+  auto load = [&](auto n, auto to) __attribute__((always_inline)) {   // the n-th load of a step, to place `to`
+    constexpr int kN = n.value, kY = kN - sx.kLoads;
+    if constexpr (kN < sx.kLoads)
+      sx.template load<to.value * kXBytes + kN * kThreads * 16>(a.x, kN, load_to);
+    else
+      sy.template load<2 * kXBytes + to.value * kYBytes + kY * kThreads * 16>(a.y, kY, load_to);
   };
 
   floatx4 acc[FX][FY];
@@ -389,25 +456,68 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wx = wave / WY * (FX * 16), wy = wave % WY * (FY * 16);
 
-  if (steps > 0) load(lds);
-  for (int s = 0; s < steps; ++s) {
-    char* now = lds + (s & 1) * kStage;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (s + 1 < steps) load(lds + ((s + 1) & 1) * kStage);
+  // Fragments: of x, which a wave has more of, each is read for the next half as soon as its products of this one are issued (the last one aside); of y, which
+  // all products take, two sets.
+  bf16x8_t x[FX - 1], x_last[2], y[2][FY];
+  Fragments<BX, XO> fx;
+  Fragments<BY, YO> fy;
+  fx.init(lds0, wx);
+  fy.init(lds0 + 2 * kXBytes, wy);
+  auto loads = [&](int i, auto place) __attribute__((always_inline)) {   // the i-th of FX shares
+    for_each<kLoads>([&](auto n) {
+      if (n.value * FX / kLoads == i) load(n, place);
+    });
+  };
+  // All loads but the last `left` have come, and what was read of LDS, of all waves.  (No fence: it would wait for all loads.)
+  auto arrived = [&](auto left) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(left.value) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto step = [&](auto place_of) __attribute__((always_inline)) {
+    constexpr int place = place_of.value;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8_t x[FX], y[FY];
+    for (int half = 0; half < 2; ++half) {
+      if (half == 1) {
+        arrived(std::integral_constant<int, 0>{});
+        next_load();
+      }
+      const int from = half == 0 ? place : place ^ 1;
+      fx.again();
+      fy.again();
 #pragma unroll
-      for (int i = 0; i < FX; ++i) x[i] = fragment_of<BX, XO>(now, wx + 16 * i, ks);
+      for (int i = 0; i < FX; ++i) {
+        if (half == 1) loads(i, place_of);   // of the step after the next one
+        if (i == 0)
+          x_last[half ^ 1] = fx.get(FX - 1, half ^ 1, from);
+        else
+          x[i - 1] = fx.get(i - 1, half ^ 1, from);
 #pragma unroll
-      for (int j = 0; j < FY; ++j) y[j] = fragment_of<BY, YO>(now + kXBytes, wy + 16 * j, ks);
+        for (int n = i * FY / FX; n < (i + 1) * FY / FX; ++n) y[half ^ 1][n] = fy.get(n, half ^ 1, from);
 #pragma unroll
-      for (int j = 0; j < FY; ++j)
+        for (int j = 0; j < FY; ++j) acc[i][j] = mfma32(y[half][j], i == FX - 1 ? x_last[half] : x[i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);   // (left to itself the compiler puts reads where it then waits for them)
+      }
+    }
+  };
+  if (steps > 0) {
 #pragma unroll
-        for (int i = 0; i < FX; ++i) acc[i][j] = mfma32(y[j], x[i], acc[i][j]);
+    for (int s = 0; s < 2; ++s) {
+      next_load();
+      for_each<kLoads>([&](auto n) { s == 0 ? load(n, std::integral_constant<int, 0>{}) : load(n, std::integral_constant<int, 1>{}); });
+    }
+    arrived(std::integral_constant<int, kLoads>{});
+#pragma unroll
+    for (int n = 0; n < FY; ++n) y[0][n] = fy.get(n, 0, 0);
+#pragma unroll
+    for (int n = 0; n < FX - 1; ++n) x[n] = fx.get(n, 0, 0);
+    x_last[0] = fx.get(FX - 1, 0, 0);
+    for (int s = 0; s < steps; s += 2) {
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});   // (beyond the last step of an odd number: of zeros)
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may come to LDS any more)
 
   // lane: row lane % 16 of a 16 x 16 tile, columns 4 (lane / 16) + 0..3
   if constexpr (EPI == kEpiPartial) {
@@ -531,33 +641,188 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
 }
 
 // ---- the teacher's entries ------------------------------------------------------------------------------
-// z at a row's entries: four waves a row, each takes its entries one after the other.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
+// z at the k-th entry of a row, by a wave.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
+struct EntryLogits {
+  const void *h, *W;
+  int64_t ldh, ldw;
+  int C, V, T, rounded;
+  const int64_t* ids;
+  const float* logits;
+  float scale;
+  float* z_top;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void head_entries_kernel(const T* __restrict__ h, int64_t ldh, const T* __restrict__ W, int64_t ldw, int C, int V,
-                                                           const int64_t* __restrict__ ids, const float* __restrict__ logits, int entries,
-                                                           const int* __restrict__ rows, const int* __restrict__ count, float scale,
-                                                           int rounded, float* __restrict__ z_top) {
-  if ((int)blockIdx.x >= *count) return;
-  const int64_t row = rows[blockIdx.x];
+__device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
   const int lane = threadIdx.x & 63;
-  for (int k = threadIdx.x >> 6; k < entries; k += 4) {
-    const int64_t at = row * entries + k, id = ids[at];
-    if (!entry_there(id, logits[at]) || id >= V) {
-      if (lane == 0) z_top[at] = id >= V ? nan_value() : 0.0f;
-      continue;
-    }
-    float s = 0.0f;
-    for (int c = lane * 8; c < C; c += 512) {
-      float a[8], b[8];
-      load_piece(h + row * ldh + c, C - c, a);
-      load_piece(W + id * ldw + c, C - c, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        s = rounded ? __builtin_fmaf((float)(bf16_t)a[e], (float)(bf16_t)b[e], s) : __builtin_fmaf(a[e], b[e], s);
-    }
-    s = wave_sum(s);
-    if (lane == 0) z_top[at] = s * scale;
+  const int64_t at = row * a.T + k, id = a.ids[at];
+  if (!entry_there(id, a.logits[at]) || id >= a.V) {
+    if (lane == 0) a.z_top[at] = id >= a.V ? nan_value() : 0.0f;
+    return;
   }
+  const T *h = (const T*)a.h + row * a.ldh, *w = (const T*)a.W + id * a.ldw;
+  float s = 0.0f;
+  for (int c = lane * 8; c < a.C; c += 512) {
+    float x[8], y[8];
+    load_piece(h + c, a.C - c, x);
+    load_piece(w + c, a.C - c, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      s = a.rounded ? __builtin_fmaf((float)(bf16_t)x[e], (float)(bf16_t)y[e], s) : __builtin_fmaf(x[e], y[e], s);
+  }
+  s = wave_sum(s);
+  if (lane == 0) a.z_top[at] = s * a.scale;
+}
+// Four waves a row that counts, each takes its entries one after the other.
+template <typename T>
+__global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const int* __restrict__ rows, const int* __restrict__ count) {
+  if ((int)blockIdx.x >= *count) return;
+  for (int k = threadIdx.x >> 6; k < a.T; k += 4) entry_logit<T>(a, rows[blockIdx.x], k);
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------
+// Logits of up to 64 rows: bound by the table, which is read once, straight into registers.  A block takes 16 YT tokens at a time, its four waves a quarter of
+// the channels each, so that a small table, too, is many waves' work; rows come from the caches again and again.  A lane's 32 bytes of a row are
+// its operands of two matrix instructions (bf16) or eight (fp32, exact): which k they stand for does not matter as long as both sides agree.
+struct Thin {
+  const void *h, *W;
+  int64_t ldh, ldw;
+  int M, C, V, groups;    // groups: blocks that share the tokens; blocks behind them take the entries, four each
+  const int64_t* labels;
+  float scale, inv_tau;
+  float* z_label;
+  Partial* partial;       // [groups][partial_ld]
+  int64_t partial_ld;
+  EntryLogits entries;
+};
+template <typename T>
+struct Run {   // 32 bytes of a row
+  static constexpr int kElements = 32 / sizeof(T);
+  u32x4_any2 a, b;
+};
+template <typename T>
+__device__ inline Run<T> load_run(const T* p) {
+  return {*reinterpret_cast<const u32x4_any2*>(p), *reinterpret_cast<const u32x4_any2*>(p + 16 / sizeof(T))};
+}
+template <typename T>
+__device__ inline Run<T> load_run_end(const T* p, int n) {   // n elements exist
+  Run<T> r;
+  if constexpr (std::is_same_v<T, float>) {
+    r.a = u32x4{}, r.b = u32x4{};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e < n) r.a[e] = __float_as_uint(p[e]);
+      if (e + 4 < n) r.b[e] = __float_as_uint(p[e + 4]);
+    }
+  } else {
+    r.a = load_raw(p, n).a, r.b = load_raw(p + 8, n - 8).a;
+  }
+  return r;
+}
+__device__ inline floatx4 multiply(const Run<bf16_t>& y, const Run<bf16_t>& x, floatx4 c) {
+  c = mfma32(__builtin_bit_cast(bf16x8_t, (u32x4)y.a), __builtin_bit_cast(bf16x8_t, (u32x4)x.a), c);
+  return mfma32(__builtin_bit_cast(bf16x8_t, (u32x4)y.b), __builtin_bit_cast(bf16x8_t, (u32x4)x.b), c);
+}
+__device__ inline floatx4 multiply(const Run<float>& y, const Run<float>& x, floatx4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(y.a[e]), __uint_as_float(x.a[e]), c, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(y.b[e]), __uint_as_float(x.b[e]), c, 0, 0, 0);
+  return c;
+}
+
+template <typename T, int XT, int YT>
+__global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
+  constexpr int kRun = Run<T>::kElements, kStep = 4 * kRun;
+  __shared__ floatx4 sums[4][XT * YT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  if ((int)blockIdx.x >= a.groups) {
+    const int n = ((int)blockIdx.x - a.groups) * 4 + wave;
+    if (n < a.M * a.entries.T) entry_logit<T>(a.entries, n / a.entries.T, n % a.entries.T);
+    return;
+  }
+  const int tiles = (a.V + 16 * YT - 1) / (16 * YT), whole = a.C / kStep;
+  const T* h[XT];
+#pragma unroll
+  for (int i = 0; i < XT; ++i) h[i] = (const T*)a.h + (int64_t)(16 * i + r < a.M ? 16 * i + r : a.M - 1) * a.ldh + g * kRun;
+  Partial all{-__builtin_inff(), 0.0f, 0.0f, 0.0f};   // of this lane's row of the tile that its wave sums up
+  for (int tile = blockIdx.x; tile < tiles; tile += a.groups) {
+    const int v0 = tile * (16 * YT);
+    const T* w[YT];
+#pragma unroll
+    for (int j = 0; j < YT; ++j) w[j] = (const T*)a.W + (int64_t)(v0 + 16 * j + r < a.V ? v0 + 16 * j + r : a.V - 1) * a.ldw + g * kRun;
+    floatx4 acc[XT][YT];
+#pragma unroll
+    for (int i = 0; i < XT; ++i)
+#pragma unroll
+      for (int j = 0; j < YT; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto steps = [&](int s, auto n) __attribute__((always_inline)) {   // n steps, all their loads on the way together
+      Run<T> y[n.value][YT], x[n.value][XT];
+#pragma unroll
+      for (int u = 0; u < n.value; ++u) {
+#pragma unroll
+        for (int j = 0; j < YT; ++j) y[u][j] = load_run(w[j] + (int64_t)(s + 4 * u) * kStep);
+#pragma unroll
+        for (int i = 0; i < XT; ++i) x[u][i] = load_run(h[i] + (int64_t)(s + 4 * u) * kStep);
+      }
+#pragma unroll
+      for (int u = 0; u < n.value; ++u)
+#pragma unroll
+        for (int j = 0; j < YT; ++j)
+#pragma unroll
+          for (int i = 0; i < XT; ++i) acc[i][j] = multiply(y[u][j], x[u][i], acc[i][j]);
+    };
+    int s = wave;
+    constexpr int kAhead = XT * YT <= 2 ? 4 : 2;
+    for (; s + 4 * (kAhead - 1) < whole; s += 4 * kAhead) steps(s, std::integral_constant<int, kAhead>{});
+    for (; s < whole; s += 4) steps(s, std::integral_constant<int, 1>{});
+    if (s == whole && whole * kStep < a.C) {   // the ragged end, of one wave
+      const int n = a.C - whole * kStep - g * kRun;
+#pragma unroll
+      for (int j = 0; j < YT; ++j) {
+        const Run<T> y = load_run_end(w[j] + (int64_t)whole * kStep, n);
+#pragma unroll
+        for (int i = 0; i < XT; ++i) acc[i][j] = multiply(y, load_run_end(h[i] + (int64_t)whole * kStep, n), acc[i][j]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < XT; ++i)
+#pragma unroll
+      for (int j = 0; j < YT; ++j) sums[wave][i * YT + j][lane] = acc[i][j];
+    __syncthreads();
+    if (wave < XT) {   // the wave's tile of rows: lane's row lane % 16, tokens 4 (lane / 16) + 0..3 of each tile of tokens
+      const int row = 16 * wave + r;
+      const int64_t label = a.labels != nullptr && row < a.M ? a.labels[row] : -1;
+      float z[YT][4];
+      Partial p{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < YT; ++j) {
+        const int at = wave * YT + j;
+        const floatx4 v = (sums[0][at][lane] + sums[1][at][lane]) + (sums[2][at][lane] + sums[3][at][lane]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int col = v0 + 16 * j + 4 * g + e;
+          z[j][e] = v[e] * a.scale;
+          if (col == label) a.z_label[row] = z[j][e];
+          p.z += col < a.V ? z[j][e] : 0.0f;
+          z[j][e] = col < a.V ? z[j][e] : -__builtin_inff();
+          p.top = fmaxf(p.top, z[j][e]);
+        }
+      }
+      p.top = lanes16_max(p.top);
+      const float ref = p.top == -__builtin_inff() ? 0.0f : p.top;
+#pragma unroll
+      for (int j = 0; j < YT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p.sum += exp_of(z[j][e] - ref);
+          if (a.inv_tau != 1.0f) p.sum_t += exp_of((z[j][e] - ref) * a.inv_tau);
+        }
+      p.sum = lanes16_sum(p.sum), p.sum_t = lanes16_sum(p.sum_t), p.z = lanes16_sum(p.z);
+      all = join(all, p, a.inv_tau);
+    }
+    __syncthreads();
+  }
+  if (wave < XT && g == 0 && 16 * wave + r < a.M) a.partial[(int64_t)blockIdx.x * a.partial_ld + 16 * wave + r] = all;
 }
 
 __device__ inline float wave_max(float v) {
@@ -579,8 +844,10 @@ __device__ inline void teacher_sums(const int64_t* ids, const float* logits, int
   sum = wave_sum(sum);
 }
 
-// The tiles' sums of each row, joined, and its loss: 16 rows a block, a wave each at the end.
+// The tiles' sums of each row, joined, and its loss: 16 rows a block, a wave each at the end.  Without a list of rows (rows = nullptr) all M of them are
+// there, and those that do not count get zeros here.
 struct Loss {
+  int M;
   const Partial* partial;
   int64_t partial_ld;
   int tiles;
@@ -597,7 +864,7 @@ struct Loss {
 };
 __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
   __shared__ Partial joined[64][17];
-  const int n0 = blockIdx.x * 16, count = *a.count;
+  const int n0 = blockIdx.x * 16, count = a.rows != nullptr ? *a.count : a.M;
   if (n0 >= count) return;
   const float inv_tau = 1.0f / a.tau;
   {
@@ -623,9 +890,16 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
     if (lane == 0) a.after[n] = p;
     return;
   }
-  const int64_t row = a.rows[n];
-  const int64_t y = a.labels != nullptr ? a.labels[row] : -1;
-  const int f = a.flags != nullptr ? a.flags[row] : y < a.V ? kLabel : kLabel | kBad;
+  const int64_t row = a.rows != nullptr ? a.rows[n] : n;
+  const int f = a.flags != nullptr ? a.flags[row] : row_flags(row, a.labels, a.ids, a.logits, a.T, a.V);
+  if ((f & (kLabel | kTeacher)) == 0) {
+    if (lane == 0) {
+      a.loss[row] = 0.0f;
+      if (a.lse != nullptr) a.lse[row] = 0.0f;
+      if (a.lse_t != nullptr) a.lse_t[row] = 0.0f;
+    }
+    return;   // (its entries are absent: z_top has zeros there)
+  }
   const float ln = log_of(p.sum), L = p.top + ln;
   const float ln_t = a.tau != 1.0f ? log_of(p.sum_t) : ln, top_t = p.top * inv_tau;
   float loss = a.z_weight != 0.0f ? a.z_weight * L * L : 0.0f;
@@ -724,11 +998,14 @@ __global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) 
 inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int kTile = 128;
+constexpr int kThinRows = 64, kThinGroups = 1024;
+constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
 constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)256 << 20;
 
 struct Plan {
   int parts, d_parts;       // bf16 parts of h and W; of the gradient of the logits
   int64_t Mp, Cp;           // rows and channels of the copies
+  int64_t c_pitch, d_pitch; // bytes from row to row of the copies, of the gradient of the logits
   int64_t piece, table;     // tokens of a piece; of a piece's copied part of the table (0: in place)
   int pieces;
   // places in the workspace
@@ -768,13 +1045,15 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   q.labels = take(backward ? 0 : q.Mp * 4);
   q.z_label = take(backward ? 0 : q.Mp * 4);
   q.grad = take(backward ? q.Mp * sizeof(RowGrad) : 0);
-  q.h = take(q.Mp * q.Cp * 2 * q.parts);
+  q.c_pitch = q.Cp * 2 + kPad, q.d_pitch = q.piece * 2 + kPad;
+  q.h = take(q.Mp * q.c_pitch * q.parts);
   q.table = copied || most ? (table < held ? table : held) : 0;
-  q.W = take(q.table * q.Cp * 2 * q.parts);
-  q.partial = take(backward ? 0 : held / kTile * q.Mp * sizeof(Partial));
+  q.W = take(q.table * q.c_pitch * q.parts);
+  const int64_t sums = held / kTile > kThinGroups ? held / kTile : kThinGroups;
+  q.partial = take(backward ? 0 : (p.M <= kThinRows ? sums : held / kTile) * q.Mp * sizeof(Partial));
   const bool several = q.pieces > 1 || (most && table < p.V);
   q.carry = take(!backward && several ? q.Mp * sizeof(Partial) : 0);
-  q.d = take(backward ? q.Mp * held * 2 * q.d_parts : 0);
+  q.d = take(backward ? q.Mp * (held * 2 + kPad) * q.d_parts : 0);
   q.acc = take(backward && several ? q.Mp * p.C * 4 : 0);
   q.bytes = at;
   return q;
@@ -794,10 +1073,16 @@ int launch_tiles(hipStream_t st, const Product& a) {
   return hip_status();
 }
 
+template <bool XO, bool YO, int EPI>
+int launch_product(hipStream_t st, const Product& a) {
+  const int64_t large = (int64_t)((a.nx + 255) / 256) * ((a.ny + 255) / 256);
+  return large >= 200 ? launch_tiles<256, 256, 2, 4, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 2, XO, YO, EPI>(st, a);
+}
+
 template <typename T, int P>
 int copy_table(hipStream_t st, const HeadCall& c, const Plan& q, int64_t v0, int64_t n, int64_t n_to, char* to) {
   head_copy_kernel<T, P><<<(unsigned)((n_to + 3) / 4), 256, 0, st>>>((const T*)c.W.p + v0 * c.W.ld, c.W.ld, n, n_to, c.p.C, (int)q.Cp, to,
-                                                                    q.table * q.Cp * 2);
+                                                                    q.c_pitch, q.table * q.c_pitch);
   return hip_status();
 }
 template <typename T, int P>
@@ -823,25 +1108,25 @@ struct Call {
     head_rows_kernel<<<1, 1024, 0, st>>>(p.M, c.labels, flags, rows, count);
     Gather g{};
     g.M = p.M, g.slots = q.Mp, g.C = p.C, g.Cp = (int)q.Cp, g.T = p.T, g.V = p.V, g.rows = rows, g.count = count, g.flags = flags;
-    g.labels = c.labels, g.to = ws + q.h, g.plane = q.Mp * q.Cp * 2, g.ldh = c.h.ld;
+    g.labels = c.labels, g.to = ws + q.h, g.pitch = q.c_pitch, g.plane = q.Mp * q.c_pitch, g.ldh = c.h.ld;
     g.loss = c.loss, g.lse = c.lse, g.lse_t = c.lse_t, g.z_top = c.z_top, g.dh = c.dh.p, g.lddh = c.dh.ld;
     g.grad = backward ? (RowGrad*)(ws + q.grad) : nullptr;
     g.in_lse = c.in_lse, g.in_lse_t = c.in_lse_t, g.dloss = c.dloss;
     g.scale = p.scale, g.smoothing = p.smoothing, g.z_weight = p.z_weight, g.tau = p.temperature, g.label_weight = p.label_weight;
     g.teacher_weight = p.teacher_weight;
     if (int e = hip_status()) return e;
-    h = {g.to, g.plane, q.Cp * 2, q.Mp * q.Cp * 2, (int)q.Cp};
+    h = {g.to, g.plane, q.c_pitch, (int)q.Mp, (int)q.Cp};
     if (p.dtype == ABL_BF16) return gather<bf16_t, 1>(st, g, c.h.p, true);
     return q.parts == 3 ? gather<float, 3>(st, g, c.h.p, true) : gather<float, 1>(st, g, c.h.p, true);
   }
 
   int table(int64_t v0, int64_t n, Operand& w) const {
     if (!copied) {
-      w = {(const char*)c.W.p + v0 * c.W.ld * 2, 0, c.W.ld * 2, ((n - 1) * c.W.ld + c.p.C) * 2, c.p.C};
+      w = {(const char*)c.W.p + v0 * c.W.ld * 2, 0, c.W.ld * 2, (int)n, c.p.C};
       return ABL_OK;
     }
     char* to = ws + q.W;
-    w = {to, q.table * q.Cp * 2, q.Cp * 2, q.table * q.Cp * 2, (int)q.Cp};
+    w = {to, q.table * q.c_pitch, q.c_pitch, (int)q.table, (int)q.Cp};
     const int64_t n_to = up(n, 256);
     if (c.p.dtype == ABL_BF16) return copy_table<bf16_t, 1>(st, c, q, v0, n, n_to, to);
     return q.parts == 3 ? copy_table<float, 3>(st, c, q, v0, n, n_to, to) : copy_table<float, 1>(st, c, q, v0, n, n_to, to);
@@ -857,8 +1142,50 @@ bool in_place(const HeadCall& c) {
 
 size_t head_scratch_bytes(const abl_head& p, bool backward) { return plan_of(p, backward, false, true).bytes; }
 
+namespace {
+
+EntryLogits entry_logits(const HeadCall& c, const Plan& q) {
+  return {c.h.p, c.W.p, c.h.ld, c.W.ld, c.p.C, c.p.V, c.p.T, c.p.dtype == ABL_F32 && q.parts == 1, c.ids, c.logits, c.p.scale, c.z_top};
+}
+
+Loss loss_of(const HeadCall& c, const Plan& q, char* ws) {
+  const abl_head& p = c.p;
+  Loss l{};
+  l.M = (int)p.M, l.partial = (const Partial*)(ws + q.partial), l.partial_ld = q.Mp, l.labels = c.labels, l.ids = c.ids;
+  l.logits = c.logits, l.z_label = (const float*)(ws + q.z_label), l.T = p.T, l.V = p.V, l.smoothing = p.smoothing, l.z_weight = p.z_weight;
+  l.tau = p.temperature, l.label_weight = p.label_weight, l.teacher_weight = p.teacher_weight, l.loss = c.loss, l.lse = c.lse, l.lse_t = c.lse_t;
+  l.z_top = c.z_top;
+  return l;
+}
+
+// Few rows: two launches.
+template <typename T, int XT, int YT>
+int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
+  const abl_head& p = c.p;
+  const int tiles = (p.V + 16 * YT - 1) / (16 * YT);
+  Thin a{c.h.p, c.W.p, c.h.ld, c.W.ld, (int)p.M, p.C, p.V, tiles < kThinGroups ? tiles : kThinGroups, c.labels, p.scale, 1.0f / p.temperature,
+         (float*)(ws + q.z_label), (Partial*)(ws + q.partial), q.Mp, entry_logits(c, q)};
+  const int64_t entries = (p.M * p.T + 3) / 4;
+  head_thin_kernel<T, XT, YT><<<(unsigned)(a.groups + entries), 256, 0, st>>>(a);
+  Loss l = loss_of(c, q, ws);
+  l.tiles = a.groups;
+  head_loss_kernel<<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
+  return hip_status();
+}
+template <typename T>
+int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
+  if (c.p.M <= 16) return launch_thin<T, 1, 2>(st, c, q, ws);
+  return c.p.M <= 32 ? launch_thin<T, 2, 2>(st, c, q, ws) : launch_thin<T, 4, 2>(st, c, q, ws);
+}
+
+}  // namespace
+
 int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
   const abl_head& p = c.p;
+  if (p.M <= kThinRows && !(p.dtype == ABL_F32 && (p.flags & ABL_MATH_BF16))) {
+    const Plan q = plan_of(p, false, false, false);
+    return p.dtype == ABL_F32 ? launch_thin<float>(st, c, q, (char*)scratch) : launch_thin<bf16_t>(st, c, q, (char*)scratch);
+  }
   const bool copied = !in_place(c);
   const Plan q = plan_of(p, false, copied, false);
   const Call call{c, q, st, (char*)scratch, copied};
@@ -870,12 +1197,11 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
   if (int e = call.prepare(false, a.x)) return e;
   if (c.labels != nullptr) head_labels_kernel<<<(unsigned)(q.Mp / 256), 256, 0, st>>>(rows, count, c.labels, p.V, (int*)(ws + q.labels));
   if (c.ids != nullptr) {
+    const EntryLogits e = entry_logits(c, q);
     if (p.dtype == ABL_F32)
-      head_entries_kernel<float><<<(unsigned)p.M, 256, 0, st>>>((const float*)c.h.p, c.h.ld, (const float*)c.W.p, c.W.ld, p.C, p.V, c.ids, c.logits,
-                                                               p.T, rows, count, p.scale, q.parts == 1, c.z_top);
+      head_entries_kernel<float><<<(unsigned)p.M, 256, 0, st>>>(e, rows, count);
     else
-      head_entries_kernel<bf16_t><<<(unsigned)p.M, 256, 0, st>>>((const bf16_t*)c.h.p, c.h.ld, (const bf16_t*)c.W.p, c.W.ld, p.C, p.V, c.ids,
-                                                                c.logits, p.T, rows, count, p.scale, 0, c.z_top);
+      head_entries_kernel<bf16_t><<<(unsigned)p.M, 256, 0, st>>>(e, rows, count);
   }
   if (int e = hip_status()) return e;
   Partial* carry = (Partial*)(ws + q.carry);
@@ -887,12 +1213,11 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
     a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0;
     a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp;
     a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
-    if (int e = launch_tiles<kTile, kTile, 2, 2, false, false, kEpiPartial>(st, a)) return e;
-    Loss l{};
-    l.partial = a.partial, l.partial_ld = q.Mp, l.tiles = (int)((n + kTile - 1) / kTile), l.before = i > 0 ? carry : nullptr;
-    l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags, l.labels = c.labels, l.ids = c.ids;
-    l.logits = c.logits, l.z_label = a.z_label, l.T = p.T, l.V = p.V, l.smoothing = p.smoothing, l.z_weight = p.z_weight, l.tau = p.temperature;
-    l.label_weight = p.label_weight, l.teacher_weight = p.teacher_weight, l.loss = c.loss, l.lse = c.lse, l.lse_t = c.lse_t, l.z_top = c.z_top;
+    const bool large = (int64_t)((a.nx + 255) / 256) * ((a.ny + 255) / 256) >= 200;
+    if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
+    Loss l = loss_of(c, q, ws);
+    l.tiles = (int)((n + (large ? 256 : kTile) - 1) / (large ? 256 : kTile));
+    l.before = i > 0 ? carry : nullptr, l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags;
     head_loss_kernel<<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
     if (int e = hip_status()) return e;
   }
@@ -919,14 +1244,14 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
   for (int i = 0; i < q.pieces; ++i) {
     const int64_t v0 = i * q.piece, n = v0 + q.piece < p.V ? q.piece : p.V - v0;
     if (int e = call.table(v0, n, w)) return e;
-    const Operand d{ws + q.d, q.Mp * q.piece * 2, q.piece * 2, q.Mp * q.piece * 2, (int)q.piece};
+    const Operand d{ws + q.d, q.Mp * q.d_pitch, q.d_pitch, (int)q.Mp, (int)q.piece};
     {
       Product a{};
       a.x = h, a.y = w, a.nx = (int)p.M, a.ny = (int)n, a.k = (int)q.Cp, a.count = count;
       a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
       a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0, a.grad = (const RowGrad*)(ws + q.grad);
       a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch, a.d_parts = q.d_parts;
-      if (int e = launch_tiles<kTile, kTile, 2, 2, false, false, kEpiGrad>(st, a)) return e;
+      if (int e = launch_product<false, false, kEpiGrad>(st, a)) return e;
     }
     if (c.ids != nullptr) {
       Entries a{};
@@ -944,14 +1269,14 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
       a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
       a.out = last ? c.dh.p : acc, a.ld = last ? c.dh.ld : p.C, a.out_f32 = !last || p.dtype == ABL_F32, a.map = last ? rows : nullptr;
       a.add = i > 0 ? acc : nullptr, a.add_ld = p.C;
-      if (int e = launch_tiles<kTile, kTile, 2, 2, false, true, kEpiSum>(st, a)) return e;
+      if (int e = launch_product<false, true, kEpiSum>(st, a)) return e;
     }
     if (c.dW != nullptr) {
       Product a{};
       a.x = d, a.y = h, a.nx = (int)n, a.ny = p.C, a.k = (int)p.M, a.count = count, a.count_k = 1;
       a.parts = q.parts == 3 ? 6 : q.d_parts, a.pairs = q.parts == 3 ? kPairs6 : q.d_parts == 2 ? kPairs2 : kPairs1;
       a.out = (char*)c.dW + v0 * p.C * size_of(p.dw_dtype), a.ld = p.C, a.out_f32 = p.dw_dtype == ABL_F32, a.accumulate = accumulate;
-      if (int e = launch_tiles<kTile, kTile, 2, 2, true, true, kEpiSum>(st, a)) return e;
+      if (int e = launch_product<true, true, kEpiSum>(st, a)) return e;
     }
   }
   return ABL_OK;

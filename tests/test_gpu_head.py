@@ -121,7 +121,8 @@ class Case:
         R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
 
 
-SIZES = [(1, 1, 1), (1, 64, 2), (3, 7, 5), (2, 8, 130), (17, 72, 300), (61, 1000, 1013), (130, 33, 257), (257, 64, 129), (300, 520, 515)]
+SIZES = [(1, 1, 1), (1, 64, 2), (3, 7, 5), (2, 8, 130), (17, 72, 300), (61, 1000, 1013), (130, 33, 257), (257, 64, 129), (300, 520, 515),
+         (16, 200, 40000), (33, 129, 100), (64, 640, 2100), (65, 96, 333)]
 
 
 @pytest.mark.parametrize("type", [F32, BF16])
