@@ -232,6 +232,9 @@ struct Operand {
 struct Partial {        // of a row of a tile of logits: maximum, sum of exp(z - max), of exp((z - max) / tau), of z
   float top, sum, sum_t, z;
 };
+struct Split {            // at most so many shares; compute units' blocks; ns of a step, of the rest of a tile, of the second launch; elements a ns of its slabs
+  int most, units, step, fixed, second, bytes;
+};
 struct Product {
   Operand x, y;
   int nx, ny, k;            // sizes as the host knows them
@@ -244,7 +247,9 @@ struct Product {
   int y0;                   // token of the first column
   Partial* partial;         // [tile of columns][partial_ld]
   int64_t partial_ld;
+  int sum_z;                // whether the sum of z is wanted
   const int* row_label;     // the label of a row that counts
+  const int64_t* labels;    // few rows: of each row, as they are given
   float* z_label;
   const RowGrad* grad;
   char* d;                  // planes of the gradient of the logits
@@ -257,7 +262,22 @@ struct Product {
   const int* map;           // row of out for each x (nullptr: x itself)
   const float* add;         // [x][add_ld], added (nullptr: nothing)
   int64_t add_ld;
+  // sums whose k's are cut into shares of blocks of their own: where there are several, each leaves its sums in a slab [nx][ny] and a second launch adds them
+  Split split;
+  float* slabs;
 };
+
+// The number of shares with the least time, in ns by the estimates of Split: the same for the product and what adds its slabs.
+__host__ __device__ inline int shares_of(const Split& s, int64_t tiles, int steps, int64_t size) {
+  if (s.most <= 1 || tiles >= 4 * s.units) return 1;
+  int best = 1;
+  int64_t least = 0;
+  for (int n = 1; n <= s.most && (n == 1 || steps >= 2 * n); ++n) {
+    const int64_t time = (tiles * n + s.units - 1) / s.units * ((steps + n - 1) / n * (int64_t)s.step + s.fixed) + (n > 1 ? s.second + n * (size / s.bytes) : 0);
+    if (n == 1 || time < least) best = n, least = time;
+  }
+  return best;
+}
 enum { kEpiPartial, kEpiGrad, kEpiSum };
 
 // A 16-byte piece of a staged tile of 64 k's.  k along the rows: rows of eight pieces, the c-th of row r at place c xor (r / 2) % 8: the 16
@@ -329,8 +349,17 @@ struct Source {
     } else {
       bytes = (uint32_t)(o.rows - w0 < B ? o.rows - w0 : B) * pitch & (uint32_t)more;
     }
+    describe(more);
+  }
+  __device__ inline void describe(int more) {
     from = u32x4{uniform((uint32_t)base), uniform((uint32_t)(base >> 32)), uniform(OUTER ? (uint32_t)(left < 64 ? left : 64) * pitch : bytes), 0x00027000u};
     step = OUTER ? 0u : uniform((uint32_t)(2 * k & more));   // (an access is out of range where its own offset is not below the bytes less the scalar one)
+  }
+  // On by so many steps of a plane, from its first one.
+  __device__ inline void skip(int steps) {
+    k = 64 * steps;
+    if constexpr (OUTER) base += (uint64_t)pitch * (uint64_t)k, left = left > k ? left - k : 0;
+    describe(-1);
   }
   // The n-th load of a step.
   template <int TO>
@@ -403,39 +432,42 @@ __device__ inline Partial join(const Partial& a, const Partial& b, float inv_tau
   return r;
 }
 
-// A block has a tile of BX x BY, WX x WY waves a part of it each.  Steps of 64 k's: their operands go from memory straight to one of two places in
-// LDS, a step and a half ahead, and from there to registers half a step ahead, all between matrix instructions.
-template <int BX, int BY, int WX, int WY, bool XO, bool YO, int EPI>
+// A block has a tile of BX x BY, WX x WY waves a part of it each.  Steps of 64 k's: their operands go from memory straight to one of PLACES in
+// LDS, PLACES - 1/2 steps ahead, and from there to registers half a step ahead, all between matrix instructions.  FEW: x may be a user's rows as they are.
+template <int BX, int BY, int WX, int WY, int PLACES, bool XO, bool YO, int EPI, bool FEW>
 __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   constexpr int kThreads = WX * WY * 64, FX = BX / WX / 16, FY = BY / WY / 16;
   constexpr int kXBytes = BX * 128, kYBytes = BY * 128;
-  extern __shared__ __align__(16) char lds[];   // [2][BX][128], [2][BY][128]
+  extern __shared__ __align__(16) char lds[];   // [PLACES][BX][128], [PLACES][BY][128]
   const int count = a.count != nullptr ? (int)uniform((uint32_t)*a.count) : 0;
   const int nx = a.count != nullptr && !a.count_k ? count : a.nx, nk = a.count != nullptr && a.count_k ? count : a.k;
   // Blocks 8 apart share an XCD and its L2.  Each XCD takes consecutive items, in bands of eight tiles of rows.
   constexpr int kBand = 8;
-  const int tiles_x = (nx + BX - 1) / BX, tiles_y = (a.ny + BY - 1) / BY, items = tiles_x * tiles_y;
+  const int tiles_x = (nx + BX - 1) / BX, tiles_y = (a.ny + BY - 1) / BY, tiles = tiles_x * tiles_y;
+  const int steps_k = (nk + 63) / 64, all_steps = steps_k * a.parts;
+  const int shares = EPI == kEpiSum ? shares_of(a.split, tiles, all_steps, (int64_t)nx * a.ny) : 1, items = tiles * shares;
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = items >> 3, more = items & 7;
   if (slot >= per + (xcd < more ? 1 : 0)) return;
-  const int item = xcd * per + (xcd < more ? xcd : more) + slot;
-  const int band = item / (kBand * tiles_y), rest = item - band * kBand * tiles_y;
+  const int item = xcd * per + (xcd < more ? xcd : more) + slot, share = item / tiles, tile = item - share * tiles;
+  const int band = tile / (kBand * tiles_y), rest = tile - band * kBand * tiles_y;
   const int high = tiles_x - band * kBand < kBand ? tiles_x - band * kBand : kBand;
   const int x0 = (band * kBand + rest % high) * BX, tile_y = rest / high, y0 = tile_y * BY;
-  const int steps_k = (nk + 63) / 64, steps = steps_k * a.parts;
+  const int each = (all_steps + shares - 1) / shares, begin = share * each, end = begin + each < all_steps ? begin + each : all_steps;
+  const int steps = end > begin ? end - begin : 0;
 
-  Source<BX, XO, false, kThreads> sx;
+  Source<BX, XO, FEW, kThreads> sx;
   Source<BY, YO, !YO, kThreads> sy;
   sx.init(a.x, x0);
   sy.init(a.y, y0);
   constexpr int kLoads = sx.kLoads + sy.kLoads;   // of a step
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  int load_k = steps_k - 1, load_part = -1;
+  int load_part = steps > 0 ? begin / steps_k - 1 : -1, load_k = steps_k - 1, load_s = -1;
   auto next_load = [&]() __attribute__((always_inline)) {   // (beyond the last step: zeros)
-    ++load_k;
+    ++load_k, ++load_s;
     const int first = ~((load_k - steps_k) >> 31);
     load_k &= ~first;
     load_part -= first;
-    const int pair = (int)(a.pairs >> (8 * load_part)), more = (load_part - a.parts) >> 31;
+    const int pair = (int)(a.pairs >> (8 * load_part)), more = (load_s - steps) >> 31;
     sx.next(a.x, x0, first, pair & 15, more);
     sy.next(a.y, y0, first, (pair >> 4) & 15, more);
   };
@@ -445,7 +477,7 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
     if constexpr (kN < sx.kLoads)
       sx.template load<to.value * kXBytes + kN * kThreads * 16>(a.x, kN, load_to);
     else
-      sy.template load<2 * kXBytes + to.value * kYBytes + kY * kThreads * 16>(a.y, kY, load_to);
+      sy.template load<PLACES * kXBytes + to.value * kYBytes + kY * kThreads * 16>(a.y, kY, load_to);
   };
 
   floatx4 acc[FX][FY];
@@ -462,7 +494,7 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   Fragments<BX, XO> fx;
   Fragments<BY, YO> fy;
   fx.init(lds0, wx);
-  fy.init(lds0 + 2 * kXBytes, wy);
+  fy.init(lds0 + PLACES * kXBytes, wy);
   auto loads = [&](int i, auto place) __attribute__((always_inline)) {   // the i-th of FX shares
     for_each<kLoads>([&](auto n) {
       if (n.value * FX / kLoads == i) load(n, place);
@@ -479,15 +511,15 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       if (half == 1) {
-        arrived(std::integral_constant<int, 0>{});
+        arrived(std::integral_constant<int, (PLACES - 2) * kLoads>{});
         next_load();
       }
-      const int from = half == 0 ? place : place ^ 1;
+      const int from = half == 0 ? place : (place + 1) % PLACES;
       fx.again();
       fy.again();
 #pragma unroll
       for (int i = 0; i < FX; ++i) {
-        if (half == 1) loads(i, place_of);   // of the step after the next one
+        if (half == 1) loads(i, place_of);   // of PLACES steps later
         if (i == 0)
           x_last[half ^ 1] = fx.get(FX - 1, half ^ 1, from);
         else
@@ -501,21 +533,23 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
     }
   };
   if (steps > 0) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for_each<PLACES>([&](auto place) {
       next_load();
-      for_each<kLoads>([&](auto n) { s == 0 ? load(n, std::integral_constant<int, 0>{}) : load(n, std::integral_constant<int, 1>{}); });
-    }
-    arrived(std::integral_constant<int, kLoads>{});
+      if (place.value == 0 && begin % steps_k != 0) {   // (a share that begins inside a plane)
+        load_k = begin % steps_k;
+        sx.skip(load_k);
+        sy.skip(load_k);
+      }
+      for_each<kLoads>([&](auto n) { load(n, place); });
+    });
+    arrived(std::integral_constant<int, (PLACES - 1) * kLoads>{});
 #pragma unroll
     for (int n = 0; n < FY; ++n) y[0][n] = fy.get(n, 0, 0);
 #pragma unroll
     for (int n = 0; n < FX - 1; ++n) x[n] = fx.get(n, 0, 0);
     x_last[0] = fx.get(FX - 1, 0, 0);
-    for (int s = 0; s < steps; s += 2) {
-      step(std::integral_constant<int, 0>{});
-      step(std::integral_constant<int, 1>{});   // (beyond the last step of an odd number: of zeros)
-    }
+    for (int s = 0; s < steps; s += PLACES)   // (beyond the last step: of zeros)
+      for_each<PLACES>([&](auto place) { step(place); });
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing may come to LDS any more)
 
@@ -523,23 +557,32 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   if constexpr (EPI == kEpiPartial) {
     __syncthreads();
     Partial* joined = reinterpret_cast<Partial*>(lds);   // [WY][BX]
+    const bool ragged = y0 + BY > a.ny, soft = a.inv_tau != 1.0f;
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
       const int x = wx + 16 * i + (lane & 15);
-      const bool there = x0 + x < nx;
-      const int label = a.row_label != nullptr && there ? a.row_label[x0 + x] - a.y0 : -1;
+      const int col0 = y0 + wy + (lane >> 4) * 4;
+      int label = -1;
+      if constexpr (FEW) {
+        const int64_t l = a.labels != nullptr && x0 + x < nx ? a.labels[x0 + x] : -1;
+        if (l >= 0 && l < a.ny) label = (int)l;
+      } else if (a.row_label != nullptr && x0 + x < nx) {
+        label = a.row_label[x0 + x] - a.y0;
+      }
       float top = -__builtin_inff(), all = 0.0f;
 #pragma unroll
-      for (int j = 0; j < FY; ++j)
+      for (int j = 0; j < FY; ++j) {
+        const int at = label - col0 - 16 * j;
+        acc[i][j] *= a.scale;
+        if ((uint32_t)at < 4u) a.z_label[x0 + x] = at & 2 ? (at & 1 ? acc[i][j][3] : acc[i][j][2]) : (at & 1 ? acc[i][j][1] : acc[i][j][0]);
+        if (a.sum_z) all += (col0 + 16 * j < a.ny ? acc[i][j][0] : 0.0f) + (col0 + 16 * j + 1 < a.ny ? acc[i][j][1] : 0.0f) +
+                            (col0 + 16 * j + 2 < a.ny ? acc[i][j][2] : 0.0f) + (col0 + 16 * j + 3 < a.ny ? acc[i][j][3] : 0.0f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int col = y0 + wy + 16 * j + (lane >> 4) * 4 + e;
-          const float z = acc[i][j][e] * a.scale;
-          if (col == label) a.z_label[x0 + x] = z;
-          acc[i][j][e] = col < a.ny ? z : -__builtin_inff();
-          all += col < a.ny ? z : 0.0f;
+          if (ragged) acc[i][j][e] = col0 + 16 * j + e < a.ny ? acc[i][j][e] : -__builtin_inff();
           top = fmaxf(top, acc[i][j][e]);
         }
+      }
       top = lanes16_max(top);
       const float ref = top == -__builtin_inff() ? 0.0f : top;
       float sum = 0.0f, sum_t = 0.0f;
@@ -547,11 +590,13 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       for (int j = 0; j < FY; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float z = acc[i][j][e] - ref;
-          sum += exp_of(z);
-          if (a.inv_tau != 1.0f) sum_t += exp_of(z * a.inv_tau);
+          const float z = (acc[i][j][e] - ref) * kLog2e;   // (the difference first: it is exact next to the maximum)
+          sum += __builtin_amdgcn_exp2f(z);
+          if (soft) sum_t += __builtin_amdgcn_exp2f(z * a.inv_tau);
         }
-      sum = lanes16_sum(sum), sum_t = lanes16_sum(sum_t), all = lanes16_sum(all);
+      sum = lanes16_sum(sum);
+      if (soft) sum_t = lanes16_sum(sum_t);
+      if (a.sum_z) all = lanes16_sum(all);
       if (lane < 16) joined[wave % WY * BX + x] = Partial{top, sum, sum_t, all};
     }
     __syncthreads();
@@ -563,11 +608,12 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       a.partial[(int64_t)tile_y * a.partial_ld + x0 + x] = p;
     }
   } else if constexpr (EPI == kEpiGrad) {
+    const bool ragged = x0 + BX > nx || y0 + BY > a.ny, soft = a.inv_tau != 1.0f;
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
       const int x = x0 + wx + 16 * i + (lane & 15);
       const RowGrad g = a.grad[x];   // (the rows up to a whole tile are there)
-      const int label = g.label - a.y0;
+      const int label = g.label >= 0 ? g.label - a.y0 : -1;
 #pragma unroll
       for (int j = 0; j < FY; ++j) {
         const int col = y0 + wy + 16 * j + (lane >> 4) * 4;
@@ -575,10 +621,16 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float z = acc[i][j][e] * a.scale;
-          float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
-          if (a.inv_tau != 1.0f) v = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)), v);
-          if (g.label >= 0 && col + e == label) v += g.ay;
-          d[e] = x < nx && col + e < a.ny ? v : 0.0f;
+          d[e] = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
+          if (soft) d[e] = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)), d[e]);
+        }
+        if ((uint32_t)(label - col) < 4u) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] += col + e == label ? g.ay : 0.0f;
+        }
+        if (ragged) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] = x < nx && col + e < a.ny ? d[e] : 0.0f;
         }
         char* to = a.d + x * a.d_pitch + col * 2;
         if (a.d_parts == 3) {
@@ -595,6 +647,25 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
           if (a.d_parts == 2)
             *reinterpret_cast<u32x2*>(to + a.d_plane) = u32x2{two_bf16(d[0] - low_bf16(w[0]), d[1] - high_bf16(w[0])),
                                                               two_bf16(d[2] - low_bf16(w[1]), d[3] - high_bf16(w[1]))};
+        }
+      }
+    }
+  } else if (shares > 1) {
+    float* slab = a.slabs + (int64_t)share * nx * a.ny;
+#pragma unroll
+    for (int i = 0; i < FX; ++i) {
+      const int x = x0 + wx + 16 * i + (lane & 15);
+      if (x >= nx) continue;
+#pragma unroll
+      for (int j = 0; j < FY; ++j) {
+        const int col = y0 + wy + 16 * j + (lane >> 4) * 4;
+        float* to = slab + (int64_t)x * a.ny + col;
+        if (col + 4 <= a.ny) {
+          *reinterpret_cast<f32x4_any4*>(to) = acc[i][j];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (col + e < a.ny) to[e] = acc[i][j][e];
         }
       }
     }
@@ -640,12 +711,59 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   }
 }
 
+// The shares' slabs of a product, added in turn: a wave takes 256 columns of a row.
+__global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by) {
+  const int count = a.count != nullptr ? *a.count : 0;
+  const int nx = a.count != nullptr && !a.count_k ? count : a.nx, nk = a.count != nullptr && a.count_k ? count : a.k;
+  const int64_t tiles = (int64_t)((nx + bx - 1) / bx) * ((a.ny + by - 1) / by), size = (int64_t)nx * a.ny;
+  const int shares = shares_of(a.split, tiles, (nk + 63) / 64 * a.parts, size);
+  if (shares == 1) return;   // (the product wrote the result)
+  const int across = (a.ny + 255) / 256;
+  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), x = n / across;
+  const int col = (int)(n - x * across) * 256 + (threadIdx.x & 63) * 4, left = a.ny - col;
+  if (x >= nx || left <= 0) return;
+  auto four = [&](const float* p) __attribute__((always_inline)) {
+    f32x4_any4 v{};
+    if (left >= 4) {
+      v = *reinterpret_cast<const f32x4_any4*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) v[e] = p[e];
+    }
+    return v;
+  };
+  f32x4_any4 v{}, slab[8];   // (their loads on the way together)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) slab[i] = i < shares ? four(a.slabs + i * size + x * a.ny + col) : f32x4_any4{};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v += slab[i];
+  if (a.add != nullptr) v += four(a.add + x * a.add_ld + col);
+  const int64_t row = a.map != nullptr ? a.map[x] : x;
+  if (a.out_f32) {
+    float* to = (float*)a.out + row * a.ld + col;
+    if (a.accumulate) v += four(to);
+    if (left >= 4) {
+      *reinterpret_cast<f32x4_any4*>(to) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) to[e] = v[e];
+    }
+  } else {
+    bf16_t* to = (bf16_t*)a.out + row * a.ld + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) to[e] = (bf16_t)(a.accumulate ? v[e] + (float)to[e] : v[e]);
+  }
+}
+
 // ---- the teacher's entries ------------------------------------------------------------------------------
 // z at the k-th entry of a row, by a wave.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
 struct EntryLogits {
   const void *h, *W;
   int64_t ldh, ldw;
-  int C, V, T, rounded;
+  int C, V, T, dtype, rounded;
   const int64_t* ids;
   const float* logits;
   float scale;
@@ -686,35 +804,34 @@ __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const 
 struct Thin {
   const void *h, *W;
   int64_t ldh, ldw;
-  int M, C, V, groups;    // groups: blocks that share the tokens; blocks behind them take the entries, four each
+  int M, C, V, groups;    // groups: blocks that share the tokens
   const int64_t* labels;
   float scale, inv_tau;
   float* z_label;
-  Partial* partial;       // [groups][partial_ld]
-  int64_t partial_ld;
-  EntryLogits entries;
+  Partial* partial;       // [groups][M]
 };
 template <typename T>
-struct Run {   // 32 bytes of a row
+struct Run {   // 32 bytes of a row: 16, and 16 of 64 bytes further
   static constexpr int kElements = 32 / sizeof(T);
   u32x4_any2 a, b;
 };
 template <typename T>
 __device__ inline Run<T> load_run(const T* p) {
-  return {*reinterpret_cast<const u32x4_any2*>(p), *reinterpret_cast<const u32x4_any2*>(p + 16 / sizeof(T))};
+  return {*reinterpret_cast<const u32x4_any2*>(p), *reinterpret_cast<const u32x4_any2*>(p + 64 / sizeof(T))};
 }
 template <typename T>
-__device__ inline Run<T> load_run_end(const T* p, int n) {   // n elements exist
+__device__ inline Run<T> load_run_end(const T* p, int n) {   // n elements exist from p on
+  constexpr int kFar = 64 / sizeof(T);
   Run<T> r;
   if constexpr (std::is_same_v<T, float>) {
     r.a = u32x4{}, r.b = u32x4{};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (e < n) r.a[e] = __float_as_uint(p[e]);
-      if (e + 4 < n) r.b[e] = __float_as_uint(p[e + 4]);
+      if (e + kFar < n) r.b[e] = __float_as_uint(p[e + kFar]);
     }
   } else {
-    r.a = load_raw(p, n).a, r.b = load_raw(p + 8, n - 8).a;
+    r.a = load_raw(p, n).a, r.b = load_raw(p + kFar, n - kFar).a;
   }
   return r;
 }
@@ -730,26 +847,21 @@ __device__ inline floatx4 multiply(const Run<float>& y, const Run<float>& x, flo
   return c;
 }
 
-template <typename T, int XT, int YT>
-__global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
+template <typename T, int XT, int YT, int WAVES, int AHEAD>
+__global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
   constexpr int kRun = Run<T>::kElements, kStep = 4 * kRun;
-  __shared__ floatx4 sums[4][XT * YT][64];
+  __shared__ floatx4 sums[WAVES][XT * YT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  if ((int)blockIdx.x >= a.groups) {
-    const int n = ((int)blockIdx.x - a.groups) * 4 + wave;
-    if (n < a.M * a.entries.T) entry_logit<T>(a.entries, n / a.entries.T, n % a.entries.T);
-    return;
-  }
   const int tiles = (a.V + 16 * YT - 1) / (16 * YT), whole = a.C / kStep;
   const T* h[XT];
 #pragma unroll
-  for (int i = 0; i < XT; ++i) h[i] = (const T*)a.h + (int64_t)(16 * i + r < a.M ? 16 * i + r : a.M - 1) * a.ldh + g * kRun;
+  for (int i = 0; i < XT; ++i) h[i] = (const T*)a.h + (int64_t)(16 * i + r < a.M ? 16 * i + r : a.M - 1) * a.ldh + g * (kRun / 2);
   Partial all{-__builtin_inff(), 0.0f, 0.0f, 0.0f};   // of this lane's row of the tile that its wave sums up
   for (int tile = blockIdx.x; tile < tiles; tile += a.groups) {
     const int v0 = tile * (16 * YT);
     const T* w[YT];
 #pragma unroll
-    for (int j = 0; j < YT; ++j) w[j] = (const T*)a.W + (int64_t)(v0 + 16 * j + r < a.V ? v0 + 16 * j + r : a.V - 1) * a.ldw + g * kRun;
+    for (int j = 0; j < YT; ++j) w[j] = (const T*)a.W + (int64_t)(v0 + 16 * j + r < a.V ? v0 + 16 * j + r : a.V - 1) * a.ldw + g * (kRun / 2);
     floatx4 acc[XT][YT];
 #pragma unroll
     for (int i = 0; i < XT; ++i)
@@ -760,9 +872,9 @@ __global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
 #pragma unroll
       for (int u = 0; u < n.value; ++u) {
 #pragma unroll
-        for (int j = 0; j < YT; ++j) y[u][j] = load_run(w[j] + (int64_t)(s + 4 * u) * kStep);
+        for (int j = 0; j < YT; ++j) y[u][j] = load_run(w[j] + (int64_t)(s + WAVES * u) * kStep);
 #pragma unroll
-        for (int i = 0; i < XT; ++i) x[u][i] = load_run(h[i] + (int64_t)(s + 4 * u) * kStep);
+        for (int i = 0; i < XT; ++i) x[u][i] = load_run(h[i] + (int64_t)(s + WAVES * u) * kStep);
       }
 #pragma unroll
       for (int u = 0; u < n.value; ++u)
@@ -772,11 +884,10 @@ __global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
           for (int i = 0; i < XT; ++i) acc[i][j] = multiply(y[u][j], x[u][i], acc[i][j]);
     };
     int s = wave;
-    constexpr int kAhead = XT * YT <= 2 ? 4 : 2;
-    for (; s + 4 * (kAhead - 1) < whole; s += 4 * kAhead) steps(s, std::integral_constant<int, kAhead>{});
-    for (; s < whole; s += 4) steps(s, std::integral_constant<int, 1>{});
-    if (s == whole && whole * kStep < a.C) {   // the ragged end, of one wave
-      const int n = a.C - whole * kStep - g * kRun;
+    for (; s + WAVES * (AHEAD - 1) < whole; s += WAVES * AHEAD) steps(s, std::integral_constant<int, AHEAD>{});
+    for (; s < whole; s += WAVES) steps(s, std::integral_constant<int, 1>{});
+    if (wave == 0 && whole * kStep < a.C) {   // the ragged end
+      const int n = a.C - whole * kStep - g * (kRun / 2);
 #pragma unroll
       for (int j = 0; j < YT; ++j) {
         const Run<T> y = load_run_end(w[j] + (int64_t)whole * kStep, n);
@@ -797,7 +908,9 @@ __global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
 #pragma unroll
       for (int j = 0; j < YT; ++j) {
         const int at = wave * YT + j;
-        const floatx4 v = (sums[0][at][lane] + sums[1][at][lane]) + (sums[2][at][lane] + sums[3][at][lane]);
+        floatx4 v = sums[0][at][lane];
+#pragma unroll
+        for (int n = 1; n < WAVES; ++n) v += sums[n][at][lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int col = v0 + 16 * j + 4 * g + e;
@@ -822,7 +935,7 @@ __global__ __launch_bounds__(256) void head_thin_kernel(Thin a) {
     }
     __syncthreads();
   }
-  if (wave < XT && g == 0 && 16 * wave + r < a.M) a.partial[(int64_t)blockIdx.x * a.partial_ld + 16 * wave + r] = all;
+  if (wave < XT && g == 0 && 16 * wave + r < a.M) a.partial[(int)blockIdx.x * a.M + 16 * wave + r] = all;
 }
 
 __device__ inline float wave_max(float v) {
@@ -844,7 +957,7 @@ __device__ inline void teacher_sums(const int64_t* ids, const float* logits, int
   sum = wave_sum(sum);
 }
 
-// The tiles' sums of each row, joined, and its loss: 16 rows a block, a wave each at the end.  Without a list of rows (rows = nullptr) all M of them are
+// The tiles' sums of each row, joined, and its loss: a block of 1024 threads takes ROWS of them (16, or one where there are few), a wave each at the end.  Without a list of rows (rows = nullptr) all M of them are
 // there, and those that do not count get zeros here.
 struct Loss {
   int M;
@@ -861,31 +974,51 @@ struct Loss {
   float smoothing, z_weight, tau, label_weight, teacher_weight;
   float *loss, *lse, *lse_t;
   const float* z_top;
+  EntryLogits entries;   // few rows, T > 0: made here
 };
-__global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
-  __shared__ Partial joined[64][17];
-  const int n0 = blockIdx.x * 16, count = a.rows != nullptr ? *a.count : a.M;
-  if (n0 >= count) return;
-  const float inv_tau = 1.0f / a.tau;
-  {
-    const int r = threadIdx.x & 15, group = threadIdx.x >> 4;
-    const Partial none{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
-    Partial p = none;
-    if (n0 + r < count) {
-      if (group == 0 && a.before != nullptr) p = a.before[n0 + r];
-      for (int t = group; t < a.tiles; t += 64) p = join(p, a.partial[t * a.partial_ld + n0 + r], inv_tau);
-    }
-    joined[group][r] = p;
-  }
-  __syncthreads();
-  const int r = threadIdx.x >> 6, lane = threadIdx.x & 63, n = n0 + r;
-  if (n >= count) return;
-  Partial p = joined[lane][r];
+__device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the wave's 64 lanes, the same for all
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const Partial o{__shfl_xor(p.top, d), __shfl_xor(p.sum, d), __shfl_xor(p.sum_t, d), __shfl_xor(p.z, d)};
-    p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (the same for both lanes)
+    p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (in the same order in both lanes)
   }
+  return p;
+}
+template <int ROWS>
+__global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
+  constexpr int kGroups = 1024 / ROWS;
+  __shared__ Partial joined[ROWS == 1 ? 16 : 64][ROWS == 1 ? 1 : ROWS + 1];
+  const int n0 = blockIdx.x * ROWS, count = a.rows != nullptr ? *a.count : a.M;
+  if (n0 >= count) return;
+  const float inv_tau = 1.0f / a.tau;
+  if constexpr (ROWS == 1) {
+    for (int k = threadIdx.x >> 6; k < a.entries.T; k += 16) {   // (read below by the wave of the row, behind the barrier)
+      if (a.entries.dtype == ABL_F32)
+        entry_logit<float>(a.entries, n0, k);
+      else
+        entry_logit<bf16_t>(a.entries, n0, k);
+    }
+  }
+  const Partial none{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+  Partial p = none;
+  {
+    const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
+    if (n0 + r < count) {
+      if (group == 0 && a.before != nullptr) p = a.before[n0 + r];
+      for (int t = group; t < a.tiles; t += kGroups) p = join(p, a.partial[t * a.partial_ld + n0 + r], inv_tau);
+    }
+    if constexpr (ROWS == 1) {
+      p = lanes_joined(p, inv_tau);
+      if ((threadIdx.x & 63) == 0) joined[threadIdx.x >> 6][0] = p;
+    } else {
+      joined[group][r] = p;
+    }
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 6, lane = threadIdx.x & 63, n = n0 + r;
+  if (r >= ROWS || n >= count) return;
+  p = lanes_joined(ROWS > 1 ? joined[lane][r] : lane < 16 ? joined[lane][0] : none, inv_tau);
   if (a.after != nullptr) {
     if (lane == 0) a.after[n] = p;
     return;
@@ -997,8 +1130,9 @@ __global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) 
 // ---- how a call is cut ----------------------------------------------------------------------------------
 inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
+constexpr int64_t kSlabBytes = (int64_t)128 << 20;
 constexpr int kTile = 128;
-constexpr int kThinRows = 64, kThinGroups = 1024;
+constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 128;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
 constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)256 << 20;
 
@@ -1009,7 +1143,8 @@ struct Plan {
   int64_t piece, table;     // tokens of a piece; of a piece's copied part of the table (0: in place)
   int pieces;
   // places in the workspace
-  size_t count, rows, flags, labels, z_label, h, W, partial, carry, grad, d, acc, bytes;
+  size_t count, rows, flags, labels, z_label, h, W, partial, carry, grad, d, acc, slabs, bytes;
+  int64_t slab_bytes;
 };
 
 // copied: whether the table's rows have to be copied; `most`: what a call may need at most, whatever the table's alignment.
@@ -1049,12 +1184,20 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   q.h = take(q.Mp * q.c_pitch * q.parts);
   q.table = copied || most ? (table < held ? table : held) : 0;
   q.W = take(q.table * q.c_pitch * q.parts);
-  const int64_t sums = held / kTile > kThinGroups ? held / kTile : kThinGroups;
-  q.partial = take(backward ? 0 : (p.M <= kThinRows ? sums : held / kTile) * q.Mp * sizeof(Partial));
+  int64_t sums = held / kTile * q.Mp;
+  if (p.M <= kThinRows) {
+    const int64_t few = (int64_t)((p.V + kThinTile - 1) / kThinTile > kThinGroups ? (p.V + kThinTile - 1) / kThinTile : kThinGroups) * kThinRows;
+    sums = sums > few ? sums : few;
+  }
+  q.partial = take(backward ? 0 : sums * sizeof(Partial));
   const bool several = q.pieces > 1 || (most && table < p.V);
   q.carry = take(!backward && several ? q.Mp * sizeof(Partial) : 0);
   q.d = take(backward ? q.Mp * (held * 2 + kPad) * q.d_parts : 0);
   q.acc = take(backward && several ? q.Mp * p.C * 4 : 0);
+  // shares' sums: as many slabs as fit, of dh or of a piece of dW
+  const int64_t widest_sum = (q.Mp > held ? q.Mp : held) * p.C * 4;
+  q.slab_bytes = backward ? (8 * widest_sum < kSlabBytes ? 8 * widest_sum : kSlabBytes) : 0;
+  q.slabs = take(q.slab_bytes);
   q.bytes = at;
   return q;
 }
@@ -1062,21 +1205,57 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
 constexpr uint64_t kPairs1 = 0x00, kPairs2 = 0x0001;                 // (x plane in the low four bits; the first product in the low byte)
 constexpr uint64_t kPairs6 = 0x000110110220ull;                      // (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
 
-template <int BX, int BY, int WX, int WY, bool XO, bool YO, int EPI>
+template <int BX, int BY, int WX, int WY, int PLACES, bool XO, bool YO, int EPI, bool FEW = false>
 int launch_tiles(hipStream_t st, const Product& a) {
-  auto kern = head_product_kernel<BX, BY, WX, WY, XO, YO, EPI>;
-  constexpr int kBytes = 2 * (BX + BY) * 128;
+  auto kern = head_product_kernel<BX, BY, WX, WY, PLACES, XO, YO, EPI, FEW>;
+  constexpr int kBytes = PLACES * (BX + BY) * 128;
   if (kBytes > 64 * 1024)
     if (int e = allow_full_lds((const void*)kern)) return e;
   const int64_t tiles = (int64_t)((a.nx + BX - 1) / BX) * ((a.ny + BY - 1) / BY);
-  kern<<<(unsigned)up(tiles, 8), WX * WY * 64, kBytes, st>>>(a);
+  kern<<<(unsigned)up(tiles * (EPI == kEpiSum && a.split.most > 1 ? a.split.most : 1), 8), WX * WY * 64, kBytes, st>>>(a);
+  if (EPI == kEpiSum && a.split.most > 1) {
+    if (int e = hip_status()) return e;
+    head_sum_kernel<<<(unsigned)(((int64_t)a.nx * ((a.ny + 255) / 256) + 3) / 4), 256, 0, st>>>(a, BX, BY);
+  }
   return hip_status();
 }
 
+// Tiles of 256 x 256 or 128 x 128, whichever takes less time for the rows that a call has, in ns a step and beside the steps.
+constexpr Split kLarge{8, 256, 1130, 7000, 4000, 500}, kSmall{8, 256, 370, 4500, 4000, 500};
+struct Choice {
+  bool large;
+  Split split;
+};
+int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
+  const int n = shares_of(s, tiles, steps, size);
+  return (tiles * n + s.units - 1) / s.units * ((steps + n - 1) / n * (int64_t)s.step + s.fixed) + (n > 1 ? s.second + n * (size / s.bytes) : 0);
+}
+// The rows that count, of which there may be fewer, are k (count_k) or nx.
+Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
+  const int64_t size = nx * ny;
+  const int steps = (int)((k + 63) / 64 * parts);
+  const int64_t tl = ((nx + 255) / 256) * ((ny + 255) / 256), ts = ((nx + 127) / 128) * ((ny + 127) / 128);
+  Split l = kLarge, m = kSmall;
+  const int64_t fit = slab_bytes / (size * 4);
+  l.most = m.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
+  const bool large = time_of(l, tl, steps, size) <= time_of(m, ts, steps, size);
+  Split s = large ? l : m;
+  int most = 1;   // shares that any number of rows may want
+  for (int64_t d = 1; d <= 16 && s.most > 1; d *= 2) {
+    const int b = large ? 256 : 128;
+    const int64_t x = count_k ? nx : (nx + d - 1) / d, kk = count_k ? (k + d - 1) / d : k;
+    const int n = shares_of(s, ((x + b - 1) / b) * ((ny + b - 1) / b), (int)((kk + 63) / 64 * parts), x * ny);
+    if (n > most) most = n;
+  }
+  s.most = most;
+  return {large, s};
+}
+// (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
-int launch_product(hipStream_t st, const Product& a) {
-  const int64_t large = (int64_t)((a.nx + 255) / 256) * ((a.ny + 255) / 256);
-  return large >= 200 ? launch_tiles<256, 256, 2, 4, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 2, XO, YO, EPI>(st, a);
+int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
+  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0);
+  a.split = c.split, a.slabs = slabs;
+  return c.large ? launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
 }
 
 template <typename T, int P>
@@ -1133,19 +1312,19 @@ struct Call {
   }
 };
 
-// Whether the products can read the table where it is: bf16, 16-byte pieces within rows that lie close enough for 31-bit offsets.
-bool in_place(const HeadCall& c) {
-  return c.p.dtype == ABL_BF16 && c.p.C % 8 == 0 && c.W.ld % 8 == 0 && c.W.ld < 1 << 21 && (reinterpret_cast<uintptr_t>(c.W.p) & 15u) == 0;
-}
-
 }  // namespace
 
 size_t head_scratch_bytes(const abl_head& p, bool backward) { return plan_of(p, backward, false, true).bytes; }
 
 namespace {
 
+// Whether the products can read the table where it is: bf16, 16-byte pieces within rows that lie close enough for 31-bit offsets.
+bool in_place(const HeadCall& c) {
+  return c.p.dtype == ABL_BF16 && c.p.C % 8 == 0 && c.W.ld % 8 == 0 && c.W.ld < 1 << 21 && (reinterpret_cast<uintptr_t>(c.W.p) & 15u) == 0;
+}
+
 EntryLogits entry_logits(const HeadCall& c, const Plan& q) {
-  return {c.h.p, c.W.p, c.h.ld, c.W.ld, c.p.C, c.p.V, c.p.T, c.p.dtype == ABL_F32 && q.parts == 1, c.ids, c.logits, c.p.scale, c.z_top};
+  return {c.h.p, c.W.p, c.h.ld, c.W.ld, c.p.C, c.p.V, c.p.T, c.p.dtype, c.p.dtype == ABL_F32 && q.parts == 1, c.ids, c.logits, c.p.scale, c.z_top};
 }
 
 Loss loss_of(const HeadCall& c, const Plan& q, char* ws) {
@@ -1159,23 +1338,41 @@ Loss loss_of(const HeadCall& c, const Plan& q, char* ws) {
 }
 
 // Few rows: two launches.
-template <typename T, int XT, int YT>
+template <typename T, int XT, int YT, int WAVES, int AHEAD>
 int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
   const abl_head& p = c.p;
   const int tiles = (p.V + 16 * YT - 1) / (16 * YT);
   Thin a{c.h.p, c.W.p, c.h.ld, c.W.ld, (int)p.M, p.C, p.V, tiles < kThinGroups ? tiles : kThinGroups, c.labels, p.scale, 1.0f / p.temperature,
-         (float*)(ws + q.z_label), (Partial*)(ws + q.partial), q.Mp, entry_logits(c, q)};
-  const int64_t entries = (p.M * p.T + 3) / 4;
-  head_thin_kernel<T, XT, YT><<<(unsigned)(a.groups + entries), 256, 0, st>>>(a);
+         (float*)(ws + q.z_label), (Partial*)(ws + q.partial)};
+  head_thin_kernel<T, XT, YT, WAVES, AHEAD><<<(unsigned)a.groups, WAVES * 64, 0, st>>>(a);
   Loss l = loss_of(c, q, ws);
-  l.tiles = a.groups;
-  head_loss_kernel<<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
+  l.tiles = a.groups, l.partial_ld = p.M, l.entries = entry_logits(c, q);
+  head_loss_kernel<1><<<(unsigned)p.M, 1024, 0, st>>>(l);
+  return hip_status();
+}
+// The same for a table that the products can read where it is, and rows likewise.
+bool thin_in_place(const HeadCall& c) {
+  return in_place(c) && c.h.ld % 8 == 0 && c.h.ld < 1 << 21 && (reinterpret_cast<uintptr_t>(c.h.p) & 15u) == 0;
+}
+int launch_thin_product(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
+  const abl_head& p = c.p;
+  Product a{};
+  a.x = {(const char*)c.h.p, 0, c.h.ld * 2, (int)p.M, p.C}, a.y = {(const char*)c.W.p, 0, c.W.ld * 2, p.V, p.C};
+  a.nx = (int)p.M, a.ny = p.V, a.k = p.C, a.parts = 1, a.pairs = kPairs1, a.scale = p.scale, a.inv_tau = 1.0f / p.temperature;
+  a.partial = (Partial*)(ws + q.partial), a.partial_ld = kThinRows, a.sum_z = p.smoothing != 0.0f, a.labels = c.labels, a.z_label = (float*)(ws + q.z_label);
+  if (int e = p.M <= 32 ? launch_tiles<32, kThinTile, 1, 4, 4, false, false, kEpiPartial, true>(st, a)
+                        : launch_tiles<64, kThinTile, 1, 4, 4, false, false, kEpiPartial, true>(st, a))
+    return e;
+  Loss l = loss_of(c, q, ws);
+  l.tiles = (p.V + kThinTile - 1) / kThinTile, l.partial_ld = kThinRows, l.entries = entry_logits(c, q);
+  head_loss_kernel<1><<<(unsigned)p.M, 1024, 0, st>>>(l);
   return hip_status();
 }
 template <typename T>
 int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
-  if (c.p.M <= 16) return launch_thin<T, 1, 2>(st, c, q, ws);
-  return c.p.M <= 32 ? launch_thin<T, 2, 2>(st, c, q, ws) : launch_thin<T, 4, 2>(st, c, q, ws);
+  if (std::is_same_v<T, bf16_t> && thin_in_place(c)) return launch_thin_product(st, c, q, ws);
+  if (c.p.M <= 16) return launch_thin<T, 1, 1, 8, 4>(st, c, q, ws);
+  return c.p.M <= 32 ? launch_thin<T, 2, 2, 4, 2>(st, c, q, ws) : launch_thin<T, 4, 2, 4, 2>(st, c, q, ws);
 }
 
 }  // namespace
@@ -1211,14 +1408,14 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
     a.nx = (int)p.M, a.ny = (int)n, a.k = (int)q.Cp, a.count = count, a.count_k = 0;
     a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
     a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0;
-    a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp;
+    a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp, a.sum_z = p.smoothing != 0.0f;
     a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
-    const bool large = (int64_t)((a.nx + 255) / 256) * ((a.ny + 255) / 256) >= 200;
+    const bool large = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).large;
     if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
     Loss l = loss_of(c, q, ws);
     l.tiles = (int)((n + (large ? 256 : kTile) - 1) / (large ? 256 : kTile));
     l.before = i > 0 ? carry : nullptr, l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags;
-    head_loss_kernel<<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
+    head_loss_kernel<16><<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
     if (int e = hip_status()) return e;
   }
   return ABL_OK;
@@ -1269,14 +1466,14 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
       a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
       a.out = last ? c.dh.p : acc, a.ld = last ? c.dh.ld : p.C, a.out_f32 = !last || p.dtype == ABL_F32, a.map = last ? rows : nullptr;
       a.add = i > 0 ? acc : nullptr, a.add_ld = p.C;
-      if (int e = launch_product<false, true, kEpiSum>(st, a)) return e;
+      if (int e = launch_product<false, true, kEpiSum>(st, a, (float*)(ws + q.slabs), q.slab_bytes)) return e;
     }
     if (c.dW != nullptr) {
       Product a{};
       a.x = d, a.y = h, a.nx = (int)n, a.ny = p.C, a.k = (int)p.M, a.count = count, a.count_k = 1;
       a.parts = q.parts == 3 ? 6 : q.d_parts, a.pairs = q.parts == 3 ? kPairs6 : q.d_parts == 2 ? kPairs2 : kPairs1;
       a.out = (char*)c.dW + v0 * p.C * size_of(p.dw_dtype), a.ld = p.C, a.out_f32 = p.dw_dtype == ABL_F32, a.accumulate = accumulate;
-      if (int e = launch_product<true, true, kEpiSum>(st, a)) return e;
+      if (int e = launch_product<true, true, kEpiSum>(st, a, (float*)(ws + q.slabs), q.slab_bytes)) return e;
     }
   }
   return ABL_OK;
