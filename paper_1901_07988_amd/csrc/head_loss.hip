@@ -296,11 +296,21 @@ __device__ inline int staged_piece(int row, int q) {
   }
 }
 
-// Each lane's 16 bytes at `at` + `step` go to LDS, one lane's behind the other's from byte `to` + TO on (zeros where they lie beyond the descriptor).  In
-// assembly: the compiler takes every later read of LDS for one that needs the data and waits for all loads there.  Nothing comes back in registers.
+// Two loads: each lane's 16 bytes at `at` + `step` go to LDS, one lane's behind the other's from byte `to` + TO on (zeros where they lie beyond the
+// descriptor).  In assembly: the compiler takes every later read of LDS for one that needs the data and waits for all loads there.  Nothing comes back in
+// registers.  What the compiler would otherwise see to: a load needs five states from a vector instruction's write of a scalar register that it
+// reads, and one from m0's.
+template <int TO, int TO2>
+__device__ inline void load_two(u32x4 from, uint32_t to, uint32_t at, uint32_t at2, uint32_t step, uint32_t step2) {
+  asm volatile(
+      "s_add_u32 m0, %0, %6\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %3, %4 offen lds\n\t"
+      "s_add_u32 m0, %0, %7\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %5 offen lds" ::"s"(to),
+      "v"(at), "v"(at2), "s"(from), "s"(step), "s"(step2), "i"(TO), "i"(TO2)
+      : "scc");
+}
 template <int TO>
-__device__ inline void load_to_lds(u32x4 from, uint32_t to, uint32_t at, uint32_t step) {
-  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(at), "s"(from), "s"(step), "i"(TO) : "scc");
+__device__ inline void load_one(u32x4 from, uint32_t to, uint32_t at, uint32_t step) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(at), "s"(from), "s"(step), "i"(TO) : "scc");
 }
 
 __device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }   // the same in all lanes, in a scalar register
@@ -322,6 +332,7 @@ struct Source {
 
   __device__ inline void init(const Operand& o, int w0) {
     pitch = (uint32_t)o.pitch;
+    base = 0, k = 0, left = 0, bytes = 0;   // (next() combines old and new values by their bits: both have to have one)
     const int row = (int)threadIdx.x / kPieces, in = (int)threadIdx.x % kPieces;
     int q;
     if constexpr (OUTER) {
@@ -361,15 +372,24 @@ struct Source {
     if constexpr (OUTER) base += (uint64_t)pitch * (uint64_t)k, left = left > k ? left - k : 0;
     describe(-1);
   }
-  // The n-th load of a step.
-  template <int TO>
-  __device__ inline void load(const Operand& o, int n, uint32_t to) const {
-    if constexpr (OUTER) {
-      const uint32_t by = (uint32_t)(n * kRows) * pitch;
-      load_to_lds<TO>(from, to, at[0], uniform(by < from[2] ? by : from[2]));
-    } else {
-      load_to_lds<TO>(from, to, !MASK || first + k < o.along ? at[n] : kNowhere, step);
+  // The n-th load of a step, and the one after it where there is one: to byte TO and TO + THREADS * 16.
+  template <int N, int TO>
+  __device__ inline void load(const Operand& o, uint32_t to) const {
+    constexpr int M = N + 1 < kLoads ? N + 1 : N;
+    uint32_t a[2], by[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      if constexpr (OUTER) {
+        a[n] = at[0], by[n] = (uint32_t)((n == 0 ? N : M) * kRows) * pitch;
+        by[n] = uniform(by[n] < from[2] ? by[n] : from[2]);
+      } else {
+        a[n] = !MASK || first + k < o.along ? at[n == 0 ? N : M] : kNowhere, by[n] = step;
+      }
     }
+    if constexpr (M > N)
+      load_two<TO, TO + THREADS * 16>(from, to, a[0], a[1], by[0], by[1]);
+    else
+      load_one<TO>(from, to, a[0], by[0]);
   }
 };
 
@@ -467,17 +487,18 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
     const int first = ~((load_k - steps_k) >> 31);
     load_k &= ~first;
     load_part -= first;
-    const int pair = (int)(a.pairs >> (8 * load_part)), more = (load_s - steps) >> 31;
+    const int pair = (int)(a.pairs >> (8 * load_part & 63)), more = (load_s - steps) >> 31;
     sx.next(a.x, x0, first, pair & 15, more);
     sy.next(a.y, y0, first, (pair >> 4) & 15, more);
   };
   const uint32_t load_to = uniform(lds0 + (threadIdx.x >> 6) * 1024);
-  auto load = [&](auto n, auto to) __attribute__((always_inline)) {   // the n-th load of a step, to place `to`
+  auto load = [&](auto n, auto to) __attribute__((always_inline)) {   // the n-th load of a step, to place `to`; the second of a pair goes with the first
     constexpr int kN = n.value, kY = kN - sx.kLoads;
-    if constexpr (kN < sx.kLoads)
-      sx.template load<to.value * kXBytes + kN * kThreads * 16>(a.x, kN, load_to);
-    else
-      sy.template load<PLACES * kXBytes + to.value * kYBytes + kY * kThreads * 16>(a.y, kY, load_to);
+    if constexpr (kN < sx.kLoads) {
+      if constexpr (kN % 2 == 0) sx.template load<kN, to.value * kXBytes + kN * kThreads * 16>(a.x, load_to);
+    } else if constexpr (kY % 2 == 0) {
+      sy.template load<kY, PLACES * kXBytes + to.value * kYBytes + kY * kThreads * 16>(a.y, load_to);
+    }
   };
 
   floatx4 acc[FX][FY];
@@ -571,18 +592,28 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       }
       float top = -__builtin_inff(), all = 0.0f;
 #pragma unroll
-      for (int j = 0; j < FY; ++j) {
-        const int at = label - col0 - 16 * j;
-        acc[i][j] *= a.scale;
-        if ((uint32_t)at < 4u) a.z_label[x0 + x] = at & 2 ? (at & 1 ? acc[i][j][3] : acc[i][j][2]) : (at & 1 ? acc[i][j][1] : acc[i][j][0]);
-        if (a.sum_z) all += (col0 + 16 * j < a.ny ? acc[i][j][0] : 0.0f) + (col0 + 16 * j + 1 < a.ny ? acc[i][j][1] : 0.0f) +
-                            (col0 + 16 * j + 2 < a.ny ? acc[i][j][2] : 0.0f) + (col0 + 16 * j + 3 < a.ny ? acc[i][j][3] : 0.0f);
+      for (int j = 0; j < FY; ++j) acc[i][j] *= a.scale;
+      if (__any((uint32_t)(label - col0) < 16u * FY)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (ragged) acc[i][j][e] = col0 + 16 * j + e < a.ny ? acc[i][j][e] : -__builtin_inff();
-          top = fmaxf(top, acc[i][j][e]);
+        for (int j = 0; j < FY; ++j) {
+          const int at = label - col0 - 16 * j;
+          if ((uint32_t)at < 4u) a.z_label[x0 + x] = at & 2 ? (at & 1 ? acc[i][j][3] : acc[i][j][2]) : (at & 1 ? acc[i][j][1] : acc[i][j][0]);
         }
       }
+      if (a.sum_z) {
+#pragma unroll
+        for (int j = 0; j < FY; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) all += col0 + 16 * j + e < a.ny ? acc[i][j][e] : 0.0f;
+      }
+      if (ragged) {
+#pragma unroll
+        for (int j = 0; j < FY; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = col0 + 16 * j + e < a.ny ? acc[i][j][e] : -__builtin_inff();
+      }
+#pragma unroll
+      for (int j = 0; j < FY; ++j) top = fmaxf(fmaxf(top, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
       top = lanes16_max(top);
       const float ref = top == -__builtin_inff() ? 0.0f : top;
       float sum = 0.0f, sum_t = 0.0f;
@@ -620,9 +651,9 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
         float d[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float z = acc[i][j][e] * a.scale;
-          d[e] = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
-          if (soft) d[e] = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)), d[e]);
+          const float s = acc[i][j][e];
+          d[e] = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(s, a.scale, -g.L)), g.a0);
+          if (soft) d[e] = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(s * a.scale, a.inv_tau, -g.Lt)), d[e]);
         }
         if ((uint32_t)(label - col) < 4u) {
 #pragma unroll
