@@ -166,6 +166,7 @@ struct Gather {
   int64_t pitch, plane, ldh;
   // forward: of the rows that do not count, written as zeros
   float *loss, *lse, *lse_t, *z_top;
+  int* row_label;               // and the labels of those that do
   // backward
   void* dh;
   int64_t lddh;
@@ -184,6 +185,10 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
     if (n >= (count + kRowTile - 1) / kRowTile * kRowTile) return;
     const int64_t row = n < count ? g.rows[n] : -1;
     copy_row<T, P>(row >= 0 ? h + row * g.ldh : nullptr, g.C, g.Cp, g.to + n * g.pitch, g.plane);
+    if (g.row_label != nullptr && lane == 0) {
+      const int64_t y = row >= 0 ? g.labels[row] : -1;
+      g.row_label[n] = y >= 0 && y < g.V ? (int)y : -1;
+    }
     if (g.grad != nullptr && lane == 0) {
       RowGrad r{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1, 0};
       if (row >= 0) {
@@ -431,13 +436,23 @@ __device__ inline void for_each(F f) {
   for_each<N>(f, std::make_integer_sequence<int, N>{});
 }
 
-__device__ inline float lanes16_max(float v) {   // over the four lanes 16 apart
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+// Over the four lanes 16 apart: rows of 16 lanes, then halves of the wave, change places with those of a copy.
+template <typename F>
+__device__ inline float lanes16(float v, F f) {
+#ifdef __HIP_DEVICE_COMPILE__
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+  return v;
+#endif
+}
+__device__ inline float lanes16_max(float v) {
+  return lanes16(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ inline float lanes16_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  return lanes16(v, [](float a, float b) { return a + b; });
 }
 
 // Joins the sums of two sets of logits.
@@ -810,14 +825,18 @@ __device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
   }
   const T *h = (const T*)a.h + row * a.ldh, *w = (const T*)a.W + id * a.ldw;
   float s = 0.0f;
-  for (int c = lane * 8; c < a.C; c += 512) {
+  auto add = [&](int c, int n) __attribute__((always_inline)) {
     float x[8], y[8];
-    load_piece(h + c, a.C - c, x);
-    load_piece(w + c, a.C - c, y);
+    load_piece(h + c, n, x);
+    load_piece(w + c, n, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       s = a.rounded ? __builtin_fmaf((float)(bf16_t)x[e], (float)(bf16_t)y[e], s) : __builtin_fmaf(x[e], y[e], s);
-  }
+  };
+  const int whole = a.C / 512 * 512;
+#pragma unroll 4
+  for (int c = 0; c < whole; c += 512) add(c + lane * 8, 8);
+  if (whole < a.C) add(whole + lane * 8, a.C - whole - lane * 8);
   s = wave_sum(s);
   if (lane == 0) a.z_top[at] = s * a.scale;
 }
@@ -1106,12 +1125,47 @@ struct Entries {
   int64_t d_plane, d_pitch;
   int d_parts;
 };
+__device__ inline void put_entry_grad(const Entries& a, const RowGrad& g, int n, int id, float z, float p) {
+  float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
+  v = __builtin_fmaf(g.at, (a.inv_tau != 1.0f ? exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)) : 0.0f) - p, v);
+  if (id == g.label) v += g.ay;
+  uint16_t* to = reinterpret_cast<uint16_t*>(a.d + n * a.d_pitch + (id - a.v0) * 2);
+  if (a.d_parts == 3) {
+    uint32_t h, m, l;
+    three_parts(v, h, m, l);
+    *to = (uint16_t)(h >> 16);
+    *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)(m >> 16);
+    *(uint16_t*)((char*)to + 2 * a.d_plane) = (uint16_t)(l >> 16);
+  } else {
+    const uint32_t w = two_bf16(v, 0.0f);
+    *to = (uint16_t)w;
+    if (a.d_parts == 2) *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)two_bf16(v - low_bf16(w), 0.0f);
+  }
+}
 __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (n >= *a.count) return;
   const int64_t row = a.rows[n];
   const int64_t* ids = a.ids + row * a.T;
   const float* t = a.logits + row * a.T;
+  if (a.T <= 64) {   // an entry a lane; tokens fit 32 bits
+    const int64_t wide = lane < a.T ? ids[lane] : -1;
+    const float u = lane < a.T ? t[lane] * a.inv_tau : 0.0f;
+    const bool there = lane < a.T && entry_there(wide, t[lane]);
+    const int id = there && wide < a.v1 ? (int)wide : -1;
+    if (!__any(id >= a.v0)) return;
+    const float top = wave_max(there ? u : -__builtin_inff());
+    const float e = there ? exp_of(u - top) : 0.0f, mine = e / wave_sum(e);
+    bool first = true;
+    float p = 0.0f;
+    for (int i = 0; i < a.T; ++i) {
+      const bool same = __builtin_amdgcn_readlane(id, i) == id;
+      first = first && !(same && i < lane);
+      p += same ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), i)) : 0.0f;
+    }
+    if (first && id >= a.v0) put_entry_grad(a, a.grad[n], n, id, a.z_top[row * a.T + lane], p);
+    return;
+  }
   float top, sum;
   teacher_sums(ids, t, a.T, a.inv_tau, top, sum);
   if (sum == 0.0f) return;   // (no entries)
@@ -1126,32 +1180,8 @@ __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
     float p = 0.0f;
     for (int i = k; i < a.T; ++i)
       if (ids[i] == id && entry_there(id, t[i])) p += exp_of(t[i] * a.inv_tau - top) * norm;
-    const float z = a.z_top[row * a.T + k];
-    float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
-    v = __builtin_fmaf(g.at, (a.inv_tau != 1.0f ? exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)) : 0.0f) - p, v);
-    if (id == g.label) v += g.ay;
-    uint16_t* to = reinterpret_cast<uint16_t*>(a.d + n * a.d_pitch + (id - a.v0) * 2);
-    if (a.d_parts == 3) {
-      uint32_t h, m, l;
-      three_parts(v, h, m, l);
-      *to = (uint16_t)(h >> 16);
-      *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)(m >> 16);
-      *(uint16_t*)((char*)to + 2 * a.d_plane) = (uint16_t)(l >> 16);
-    } else {
-      const uint32_t w = two_bf16(v, 0.0f);
-      *to = (uint16_t)w;
-      if (a.d_parts == 2) *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)two_bf16(v - low_bf16(w), 0.0f);
-    }
+    put_entry_grad(a, g, n, (int)id, a.z_top[row * a.T + k], p);
   }
-}
-
-// The labels of the rows that count, for the products' tiles.
-__global__ __launch_bounds__(256) void head_labels_kernel(const int* __restrict__ rows, const int* __restrict__ count, const int64_t* __restrict__ labels,
-                                                          int V, int* __restrict__ row_label) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= *count) return;
-  const int64_t y = labels[rows[n]];
-  row_label[n] = y >= 0 && y < V ? (int)y : -1;
 }
 
 __global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) {
@@ -1163,7 +1193,7 @@ inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int64_t kSlabBytes = (int64_t)128 << 20;
 constexpr int kTile = 128;
-constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 128;
+constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
 constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)256 << 20;
 
@@ -1236,6 +1266,7 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
 constexpr uint64_t kPairs1 = 0x00, kPairs2 = 0x0001;                 // (x plane in the low four bits; the first product in the low byte)
 constexpr uint64_t kPairs6 = 0x000110110220ull;                      // (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
 
+constexpr int kUnits = 256;   // compute units
 template <int BX, int BY, int WX, int WY, int PLACES, bool XO, bool YO, int EPI, bool FEW = false>
 int launch_tiles(hipStream_t st, const Product& a) {
   auto kern = head_product_kernel<BX, BY, WX, WY, PLACES, XO, YO, EPI, FEW>;
@@ -1251,42 +1282,49 @@ int launch_tiles(hipStream_t st, const Product& a) {
   return hip_status();
 }
 
-// Tiles of 256 x 256 or 128 x 128, whichever takes less time for the rows that a call has, in ns a step and beside the steps.
-constexpr Split kLarge{8, 256, 1130, 7000, 4000, 500}, kSmall{8, 256, 370, 4500, 4000, 500};
-struct Choice {
-  bool large;
+// Tiles of 256 x 256, 256 x 128 or 128 x 128, whichever takes the least time for the rows that a call has.
+struct Tiling {
+  int bx, by;
   Split split;
 };
+constexpr Tiling kTilings[3] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}};
+int64_t tiles_of(const Tiling& t, int64_t nx, int64_t ny) { return (nx + t.bx - 1) / t.bx * ((ny + t.by - 1) / t.by); }
 int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
   const int n = shares_of(s, tiles, steps, size);
   return (tiles * n + s.units - 1) / s.units * ((steps + n - 1) / n * (int64_t)s.step + s.fixed) + (n > 1 ? s.second + n * (size / s.bytes) : 0);
 }
+struct Choice {
+  int tiling;
+  Split split;
+};
 // The rows that count, of which there may be fewer, are k (count_k) or nx.
 Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
-  const int64_t size = nx * ny;
+  const int64_t size = nx * ny, fit = slab_bytes / (size * 4);
   const int steps = (int)((k + 63) / 64 * parts);
-  const int64_t tl = ((nx + 255) / 256) * ((ny + 255) / 256), ts = ((nx + 127) / 128) * ((ny + 127) / 128);
-  Split l = kLarge, m = kSmall;
-  const int64_t fit = slab_bytes / (size * 4);
-  l.most = m.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
-  const bool large = time_of(l, tl, steps, size) <= time_of(m, ts, steps, size);
-  Split s = large ? l : m;
+  Choice c{};
+  int64_t least = 0;
+  for (int i = 0; i < 3; ++i) {
+    Split s = kTilings[i].split;
+    s.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
+    const int64_t time = time_of(s, tiles_of(kTilings[i], nx, ny), steps, size);
+    if (i == 0 || time < least) c = {i, s}, least = time;
+  }
   int most = 1;   // shares that any number of rows may want
-  for (int64_t d = 1; d <= 16 && s.most > 1; d *= 2) {
-    const int b = large ? 256 : 128;
+  for (int64_t d = 1; d <= 16 && c.split.most > 1; d *= 2) {
     const int64_t x = count_k ? nx : (nx + d - 1) / d, kk = count_k ? (k + d - 1) / d : k;
-    const int n = shares_of(s, ((x + b - 1) / b) * ((ny + b - 1) / b), (int)((kk + 63) / 64 * parts), x * ny);
+    const int n = shares_of(c.split, tiles_of(kTilings[c.tiling], x, ny), (int)((kk + 63) / 64 * parts), x * ny);
     if (n > most) most = n;
   }
-  s.most = most;
-  return {large, s};
+  c.split.most = most;
+  return c;
 }
 // (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
 int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
   const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0);
   a.split = c.split, a.slabs = slabs;
-  return c.large ? launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
+  if (c.tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a);
+  return c.tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
 }
 
 template <typename T, int P>
@@ -1320,6 +1358,7 @@ struct Call {
     g.M = p.M, g.slots = q.Mp, g.C = p.C, g.Cp = (int)q.Cp, g.T = p.T, g.V = p.V, g.rows = rows, g.count = count, g.flags = flags;
     g.labels = c.labels, g.to = ws + q.h, g.pitch = q.c_pitch, g.plane = q.Mp * q.c_pitch, g.ldh = c.h.ld;
     g.loss = c.loss, g.lse = c.lse, g.lse_t = c.lse_t, g.z_top = c.z_top, g.dh = c.dh.p, g.lddh = c.dh.ld;
+    g.row_label = !backward && c.labels != nullptr ? (int*)(ws + q.labels) : nullptr;
     g.grad = backward ? (RowGrad*)(ws + q.grad) : nullptr;
     g.in_lse = c.in_lse, g.in_lse_t = c.in_lse_t, g.dloss = c.dloss;
     g.scale = p.scale, g.smoothing = p.smoothing, g.z_weight = p.z_weight, g.tau = p.temperature, g.label_weight = p.label_weight;
@@ -1391,11 +1430,17 @@ int launch_thin_product(hipStream_t st, const HeadCall& c, const Plan& q, char* 
   a.x = {(const char*)c.h.p, 0, c.h.ld * 2, (int)p.M, p.C}, a.y = {(const char*)c.W.p, 0, c.W.ld * 2, p.V, p.C};
   a.nx = (int)p.M, a.ny = p.V, a.k = p.C, a.parts = 1, a.pairs = kPairs1, a.scale = p.scale, a.inv_tau = 1.0f / p.temperature;
   a.partial = (Partial*)(ws + q.partial), a.partial_ld = kThinRows, a.sum_z = p.smoothing != 0.0f, a.labels = c.labels, a.z_label = (float*)(ws + q.z_label);
-  if (int e = p.M <= 32 ? launch_tiles<32, kThinTile, 1, 4, 4, false, false, kEpiPartial, true>(st, a)
-                        : launch_tiles<64, kThinTile, 1, 4, 4, false, false, kEpiPartial, true>(st, a))
-    return e;
+  // Tiles of 64 tokens where those of 128 are two a compute unit or fewer (16 x 2048 x 32768: 37.6 us instead of 39.2; 8 x 1024 x 131072: 57.6 instead of 53.3).
+  const bool narrow = (p.V + 127) / 128 <= 2 * kUnits;
+  const int columns = narrow ? 64 : 128;
+  int e;
+  if (p.M <= 32)
+    e = narrow ? launch_tiles<32, 64, 1, 4, 4, false, false, kEpiPartial, true>(st, a) : launch_tiles<32, 128, 1, 4, 4, false, false, kEpiPartial, true>(st, a);
+  else
+    e = narrow ? launch_tiles<64, 64, 1, 4, 4, false, false, kEpiPartial, true>(st, a) : launch_tiles<64, 128, 1, 4, 4, false, false, kEpiPartial, true>(st, a);
+  if (e != ABL_OK) return e;
   Loss l = loss_of(c, q, ws);
-  l.tiles = (p.V + kThinTile - 1) / kThinTile, l.partial_ld = kThinRows, l.entries = entry_logits(c, q);
+  l.tiles = (p.V + columns - 1) / columns, l.partial_ld = kThinRows, l.entries = entry_logits(c, q);
   head_loss_kernel<1><<<(unsigned)p.M, 1024, 0, st>>>(l);
   return hip_status();
 }
@@ -1423,7 +1468,6 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
   const unsigned char* flags = p.T != 0 ? (const unsigned char*)(ws + q.flags) : nullptr;
   Product a{};
   if (int e = call.prepare(false, a.x)) return e;
-  if (c.labels != nullptr) head_labels_kernel<<<(unsigned)(q.Mp / 256), 256, 0, st>>>(rows, count, c.labels, p.V, (int*)(ws + q.labels));
   if (c.ids != nullptr) {
     const EntryLogits e = entry_logits(c, q);
     if (p.dtype == ABL_F32)
@@ -1441,10 +1485,10 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
     a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0;
     a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp, a.sum_z = p.smoothing != 0.0f;
     a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
-    const bool large = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).large;
+    const int columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
     if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
     Loss l = loss_of(c, q, ws);
-    l.tiles = (int)((n + (large ? 256 : kTile) - 1) / (large ? 256 : kTile));
+    l.tiles = (int)((n + columns - 1) / columns);
     l.before = i > 0 ? carry : nullptr, l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags;
     head_loss_kernel<16><<<(unsigned)((p.M + 15) / 16), 1024, 0, st>>>(l);
     if (int e = hip_status()) return e;
