@@ -114,6 +114,21 @@ __device__ inline void three_parts(float v, uint32_t& h, uint32_t& m, uint32_t& 
   l = __float_as_uint(r - __uint_as_float(m));
 }
 
+// A value in 1 to 3 parts.
+__device__ inline void put_parts(char* to, int64_t plane, int parts, float v) {
+  if (parts == 3) {
+    uint32_t h, m, l;
+    three_parts(v, h, m, l);
+    *(uint16_t*)to = (uint16_t)(h >> 16);
+    *(uint16_t*)(to + plane) = (uint16_t)(m >> 16);
+    *(uint16_t*)(to + 2 * plane) = (uint16_t)(l >> 16);
+  } else {
+    const uint32_t w = two_bf16(v, 0.0f);
+    *(uint16_t*)to = (uint16_t)w;
+    if (parts == 2) *(uint16_t*)(to + plane) = (uint16_t)two_bf16(v - low_bf16(w), 0.0f);
+  }
+}
+
 // A row of C elements (nullptr: zeros) to its place in P planes, `plane` bytes apart, with zeros up to Cp channels: by a wave.
 template <typename T, int P>
 __device__ inline void copy_row(const T* from, int C, int Cp, char* to, int64_t plane) {
@@ -234,8 +249,8 @@ struct Operand {
   int64_t pitch;        // bytes from row to row, less than 2^22
   int rows, along;      // rows, and elements along a row, that exist (others read as zero); along: a multiple of 8
 };
-struct Partial {        // of a row of a tile of logits: maximum, sum of exp(z - max), of exp((z - max) / tau), of z
-  float top, sum, sum_t, z;
+struct Partial {        // of some logits: maximum; sum of exp(z - max), less one (what a certain row's small loss is made of), and of exp((z - max) / tau); sum of z
+  float top, rest, rest_t, z;
 };
 struct Split {            // at most so many shares; compute units' blocks; ns of a step, of the rest of a tile, of the second launch; elements a ns of its slabs
   int most, units, step, fixed, second, bytes;
@@ -267,7 +282,8 @@ struct Product {
   const int* map;           // row of out for each x (nullptr: x itself)
   const float* add;         // [x][add_ld], added (nullptr: nothing)
   int64_t add_ld;
-  // sums whose k's are cut into shares of blocks of their own: where there are several, each leaves its sums in a slab [nx][ny] and a second launch adds them
+  // sums whose k's are cut into shares of blocks of their own: where there are several, or no out, each leaves its sums in a slab [nx][ny] and a second launch
+  // takes them from there
   Split split;
   float* slabs;
 };
@@ -460,11 +476,22 @@ __device__ inline Partial join(const Partial& a, const Partial& b, float inv_tau
   Partial r;
   r.top = fmaxf(a.top, b.top);
   const float ref = r.top == -__builtin_inff() ? 0.0f : r.top;
-  const float da = a.top - ref, db = b.top - ref;
-  r.sum = a.sum * exp_of(da) + b.sum * exp_of(db);
-  r.sum_t = a.sum_t * exp_of(da * inv_tau) + b.sum_t * exp_of(db * inv_tau);
+  const float da = a.top - ref, db = b.top - ref;   // (one of them is zero and its exponential one, or there are none)
+  auto rest = [](float ra, float rb, float wa, float wb) { return __builtin_fmaf(ra, wa, rb * wb) + ((fmaxf(wa, wb) - 1.0f) + fminf(wa, wb)); };
+  r.rest = rest(a.rest, b.rest, exp_of(da), exp_of(db));
+  r.rest_t = inv_tau != 1.0f ? rest(a.rest_t, b.rest_t, exp_of(da * inv_tau), exp_of(db * inv_tau)) : 0.0f;
   r.z = a.z + b.z;
   return r;
+}
+
+__device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the wave's 64 lanes, the same for all
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const Partial o{__shfl_xor(p.top, d), __shfl_xor(p.rest, d), __shfl_xor(p.rest_t, d), __shfl_xor(p.z, d)};
+    p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (in the same order in both lanes)
+  }
+  return p;
 }
 
 // A block has a tile of BX x BY, WX x WY waves a part of it each.  Steps of 64 k's: their operands go from memory straight to one of PLACES in
@@ -631,19 +658,22 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       for (int j = 0; j < FY; ++j) top = fmaxf(fmaxf(top, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
       top = lanes16_max(top);
       const float ref = top == -__builtin_inff() ? 0.0f : top;
-      float sum = 0.0f, sum_t = 0.0f;
+      float sum = 0.0f, sum_t = 0.0f, tops = 0.0f;   // (FEW, which waits for memory anyway: the maximum is counted beside the sum, so that nothing of a small one is lost)
 #pragma unroll
       for (int j = 0; j < FY; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float z = (acc[i][j][e] - ref) * kLog2e;   // (the difference first: it is exact next to the maximum)
-          sum += __builtin_amdgcn_exp2f(z);
-          if (soft) sum_t += __builtin_amdgcn_exp2f(z * a.inv_tau);
+          const bool hit = FEW && acc[i][j][e] == ref;
+          sum += hit ? 0.0f : __builtin_amdgcn_exp2f(z);
+          if (soft) sum_t += hit ? 0.0f : __builtin_amdgcn_exp2f(z * a.inv_tau);
+          if (FEW) tops += hit ? 1.0f : 0.0f;
         }
       sum = lanes16_sum(sum);
       if (soft) sum_t = lanes16_sum(sum_t);
+      if (FEW) tops = lanes16_sum(tops);
       if (a.sum_z) all = lanes16_sum(all);
-      if (lane < 16) joined[wave % WY * BX + x] = Partial{top, sum, sum_t, all};
+      if (lane < 16) joined[wave % WY * BX + x] = Partial{top, sum + (tops - 1.0f), sum_t + (tops - 1.0f), all};
     }
     __syncthreads();
     for (int x = threadIdx.x; x < BX; x += kThreads) {
@@ -696,7 +726,7 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
         }
       }
     }
-  } else if (shares > 1) {
+  } else if (shares > 1 || a.out == nullptr) {
     float* slab = a.slabs + (int64_t)share * nx * a.ny;
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
@@ -804,6 +834,59 @@ __global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by
   }
 }
 
+// ---- few tiles of logits --------------------------------------------------------------------------------
+// Where the logits are few tiles of many k's, their product, too, is cut into shares, and these launches take the place of its epilogues.
+struct Slabs {
+  const float* p;
+  int shares, nx, ny;
+  __device__ inline float at(int x, int col) const {
+    float v = 0.0f;
+    for (int i = 0; i < shares; ++i) v += p[((int64_t)i * nx + x) * ny + col];
+    return v;
+  }
+};
+__device__ inline Slabs slabs_of(const Product& a, int bx, int by) {
+  const int nx = a.count != nullptr ? *a.count : a.nx;
+  const int64_t tiles = (int64_t)((nx + bx - 1) / bx) * ((a.ny + by - 1) / by);
+  return {a.slabs, shares_of(a.split, tiles, (a.k + 63) / 64 * a.parts, (int64_t)nx * a.ny), nx, a.ny};
+}
+// A row's sums: a block each.
+__global__ __launch_bounds__(256) void head_slab_partial_kernel(Product a, int bx, int by) {
+  __shared__ Partial joined[4];
+  const Slabs s = slabs_of(a, bx, by);
+  const int x = blockIdx.x;
+  if (x >= s.nx) return;
+  const int label = a.row_label != nullptr ? a.row_label[x] - a.y0 : -1;
+  Partial p{-__builtin_inff(), -1.0f, -1.0f, 0.0f};
+  for (int col = threadIdx.x; col < s.ny; col += 256) {
+    const float z = s.at(x, col) * a.scale;
+    if (col == label) a.z_label[x] = z;
+    p = join(p, Partial{z, 0.0f, 0.0f, z}, a.inv_tau);
+  }
+  p = lanes_joined(p, a.inv_tau);
+  if ((threadIdx.x & 63) == 0) joined[threadIdx.x >> 6] = p;
+  __syncthreads();
+  if (threadIdx.x == 0) a.partial[x] = join(join(joined[0], joined[1], a.inv_tau), join(joined[2], joined[3], a.inv_tau), a.inv_tau);
+}
+// The gradient of a row's logits, with the zeros behind it that the products take: a block each.
+__global__ __launch_bounds__(256) void head_slab_grad_kernel(Product a, int bx, int by) {
+  const Slabs s = slabs_of(a, bx, by);
+  const int x = blockIdx.x;
+  if (x >= (s.nx + kRowTile - 1) / kRowTile * kRowTile) return;
+  const RowGrad g = a.grad[x];
+  const int label = g.label >= 0 ? g.label - a.y0 : -1;
+  for (int col = threadIdx.x; col < (s.ny + 63) / 64 * 64; col += 256) {
+    float d = 0.0f;
+    if (x < s.nx && col < s.ny) {
+      const float v = s.at(x, col);
+      d = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(v, a.scale, -g.L)), g.a0);
+      if (a.inv_tau != 1.0f) d = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(v * a.scale, a.inv_tau, -g.Lt)), d);
+      if (col == label) d += g.ay;
+    }
+    put_parts(a.d + x * a.d_pitch + col * 2, a.d_plane, a.d_parts, d);
+  }
+}
+
 // ---- the teacher's entries ------------------------------------------------------------------------------
 // z at the k-th entry of a row, by a wave.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
 struct EntryLogits {
@@ -906,7 +989,7 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
   const T* h[XT];
 #pragma unroll
   for (int i = 0; i < XT; ++i) h[i] = (const T*)a.h + (int64_t)(16 * i + r < a.M ? 16 * i + r : a.M - 1) * a.ldh + g * (kRun / 2);
-  Partial all{-__builtin_inff(), 0.0f, 0.0f, 0.0f};   // of this lane's row of the tile that its wave sums up
+  Partial all{-__builtin_inff(), -1.0f, -1.0f, 0.0f};   // of this lane's row of the tile that its wave sums up
   for (int tile = blockIdx.x; tile < tiles; tile += a.groups) {
     const int v0 = tile * (16 * YT);
     const T* w[YT];
@@ -954,7 +1037,7 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
       const int row = 16 * wave + r;
       const int64_t label = a.labels != nullptr && row < a.M ? a.labels[row] : -1;
       float z[YT][4];
-      Partial p{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+      Partial p{-__builtin_inff(), -1.0f, -1.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < YT; ++j) {
         const int at = wave * YT + j;
@@ -972,15 +1055,20 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
         }
       }
       p.top = lanes16_max(p.top);
+      float tops = 0.0f;
+      p.rest = p.rest_t = 0.0f;
       const float ref = p.top == -__builtin_inff() ? 0.0f : p.top;
 #pragma unroll
       for (int j = 0; j < YT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p.sum += exp_of(z[j][e] - ref);
-          if (a.inv_tau != 1.0f) p.sum_t += exp_of((z[j][e] - ref) * a.inv_tau);
+          const bool hit = z[j][e] == ref;
+          p.rest += hit ? 0.0f : exp_of(z[j][e] - ref);
+          if (a.inv_tau != 1.0f) p.rest_t += hit ? 0.0f : exp_of((z[j][e] - ref) * a.inv_tau);
+          tops += hit ? 1.0f : 0.0f;
         }
-      p.sum = lanes16_sum(p.sum), p.sum_t = lanes16_sum(p.sum_t), p.z = lanes16_sum(p.z);
+      tops = lanes16_sum(tops);
+      p.rest = lanes16_sum(p.rest) + (tops - 1.0f), p.rest_t = lanes16_sum(p.rest_t) + (tops - 1.0f), p.z = lanes16_sum(p.z);
       all = join(all, p, a.inv_tau);
     }
     __syncthreads();
@@ -1026,15 +1114,6 @@ struct Loss {
   const float* z_top;
   EntryLogits entries;   // few rows, T > 0: made here
 };
-__device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the wave's 64 lanes, the same for all
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const Partial o{__shfl_xor(p.top, d), __shfl_xor(p.sum, d), __shfl_xor(p.sum_t, d), __shfl_xor(p.z, d)};
-    p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (in the same order in both lanes)
-  }
-  return p;
-}
 template <int ROWS>
 __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
   constexpr int kGroups = 1024 / ROWS;
@@ -1050,7 +1129,7 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
         entry_logit<bf16_t>(a.entries, n0, k);
     }
   }
-  const Partial none{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+  const Partial none{-__builtin_inff(), -1.0f, -1.0f, 0.0f};
   Partial p = none;
   {
     const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
@@ -1083,8 +1162,8 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
     }
     return;   // (its entries are absent: z_top has zeros there)
   }
-  const float ln = log_of(p.sum), L = p.top + ln;
-  const float ln_t = a.tau != 1.0f ? log_of(p.sum_t) : ln, top_t = p.top * inv_tau;
+  const float ln = log1pf(p.rest), L = p.top + ln;
+  const float ln_t = a.tau != 1.0f ? log1pf(p.rest_t) : ln, top_t = p.top * inv_tau;
   float loss = a.z_weight != 0.0f ? a.z_weight * L * L : 0.0f;
   if (f & kLabel) {   // (differences to the maximum first: L and z are large where the loss is small)
     float ce = ln + (p.top - a.z_label[n]);
@@ -1129,18 +1208,7 @@ __device__ inline void put_entry_grad(const Entries& a, const RowGrad& g, int n,
   float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
   v = __builtin_fmaf(g.at, (a.inv_tau != 1.0f ? exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)) : 0.0f) - p, v);
   if (id == g.label) v += g.ay;
-  uint16_t* to = reinterpret_cast<uint16_t*>(a.d + n * a.d_pitch + (id - a.v0) * 2);
-  if (a.d_parts == 3) {
-    uint32_t h, m, l;
-    three_parts(v, h, m, l);
-    *to = (uint16_t)(h >> 16);
-    *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)(m >> 16);
-    *(uint16_t*)((char*)to + 2 * a.d_plane) = (uint16_t)(l >> 16);
-  } else {
-    const uint32_t w = two_bf16(v, 0.0f);
-    *to = (uint16_t)w;
-    if (a.d_parts == 2) *(uint16_t*)((char*)to + a.d_plane) = (uint16_t)two_bf16(v - low_bf16(w), 0.0f);
-  }
+  put_parts(a.d + n * a.d_pitch + (id - a.v0) * 2, a.d_plane, a.d_parts, v);
 }
 __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -1191,7 +1259,7 @@ __global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) 
 // ---- how a call is cut ----------------------------------------------------------------------------------
 inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
-constexpr int64_t kSlabBytes = (int64_t)128 << 20;
+constexpr int64_t kSlabBytes = (int64_t)128 << 20, kFewLogits = (int64_t)16 << 20;
 constexpr int kTile = 128;
 constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
@@ -1255,9 +1323,11 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   q.carry = take(!backward && several ? q.Mp * sizeof(Partial) : 0);
   q.d = take(backward ? q.Mp * (held * 2 + kPad) * q.d_parts : 0);
   q.acc = take(backward && several ? q.Mp * p.C * 4 : 0);
-  // shares' sums: as many slabs as fit, of dh or of a piece of dW
-  const int64_t widest_sum = (q.Mp > held ? q.Mp : held) * p.C * 4;
-  q.slab_bytes = backward ? (8 * widest_sum < kSlabBytes ? 8 * widest_sum : kSlabBytes) : 0;
+  // shares' sums: as many slabs as fit, of dh or of a piece of dW or of the logits (where these are few tiles: more have no use for shares)
+  const int64_t logits = q.Mp * (held < all ? held : all) * 4, few = logits <= kFewLogits ? 8 * logits : 0;
+  const int64_t widest_sum = 8 * (q.Mp > held ? q.Mp : held) * p.C * 4;
+  q.slab_bytes = backward ? (widest_sum > few ? widest_sum : few) : few < 2 * kFewLogits ? few : 2 * kFewLogits;
+  if (q.slab_bytes > kSlabBytes) q.slab_bytes = kSlabBytes;
   q.slabs = take(q.slab_bytes);
   q.bytes = at;
   return q;
@@ -1275,7 +1345,7 @@ int launch_tiles(hipStream_t st, const Product& a) {
     if (int e = allow_full_lds((const void*)kern)) return e;
   const int64_t tiles = (int64_t)((a.nx + BX - 1) / BX) * ((a.ny + BY - 1) / BY);
   kern<<<(unsigned)up(tiles * (EPI == kEpiSum && a.split.most > 1 ? a.split.most : 1), 8), WX * WY * 64, kBytes, st>>>(a);
-  if (EPI == kEpiSum && a.split.most > 1) {
+  if (EPI == kEpiSum && a.split.most > 1 && a.out != nullptr) {
     if (int e = hip_status()) return e;
     head_sum_kernel<<<(unsigned)(((int64_t)a.nx * ((a.ny + 255) / 256) + 3) / 4), 256, 0, st>>>(a, BX, BY);
   }
@@ -1296,6 +1366,7 @@ int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
 struct Choice {
   int tiling;
   Split split;
+  int64_t time;
 };
 // The rows that count, of which there may be fewer, are k (count_k) or nx.
 Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
@@ -1307,7 +1378,7 @@ Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_
     Split s = kTilings[i].split;
     s.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
     const int64_t time = time_of(s, tiles_of(kTilings[i], nx, ny), steps, size);
-    if (i == 0 || time < least) c = {i, s}, least = time;
+    if (i == 0 || time < least) c = {i, s, time}, least = time;
   }
   int most = 1;   // shares that any number of rows may want
   for (int64_t d = 1; d <= 16 && c.split.most > 1; d *= 2) {
@@ -1317,6 +1388,18 @@ Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_
   }
   c.split.most = most;
   return c;
+}
+// Whether few tiles of logits are cut into shares (the launch that takes their slabs costs what one that adds them does).
+bool cut_logits(const Product& a, int64_t slab_bytes, Choice& c) {
+  const Choice whole = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false);
+  c = choice_of(a.nx, a.ny, a.k, a.parts, true, slab_bytes, false);
+  return c.split.most > 1 && c.time + 5000 < whole.time * 3 / 4;
+}
+template <bool XO, bool YO>
+int launch_slabs(hipStream_t st, Product& a, const Choice& c, float* slabs) {
+  a.split = c.split, a.slabs = slabs, a.out = nullptr;
+  if (c.tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, kEpiSum>(st, a);
+  return c.tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, kEpiSum>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, kEpiSum>(st, a);
 }
 // (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
@@ -1485,8 +1568,16 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
     a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0;
     a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp, a.sum_z = p.smoothing != 0.0f;
     a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
-    const int columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
-    if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
+    Choice how;
+    int columns = (int)n;   // of a tile that the loss finds sums of
+    if (cut_logits(a, q.slab_bytes, how)) {
+      const Tiling& t = kTilings[how.tiling];
+      if (int e = launch_slabs<false, false>(st, a, how, (float*)(ws + q.slabs))) return e;
+      head_slab_partial_kernel<<<(unsigned)p.M, 256, 0, st>>>(a, t.bx, t.by);
+    } else {
+      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
+      if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
+    }
     Loss l = loss_of(c, q, ws);
     l.tiles = (int)((n + columns - 1) / columns);
     l.before = i > 0 ? carry : nullptr, l.after = i + 1 < q.pieces ? carry : nullptr, l.rows = rows, l.count = count, l.flags = flags;
@@ -1523,7 +1614,15 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
       a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
       a.scale = p.scale, a.inv_tau = 1.0f / p.temperature, a.y0 = (int)v0, a.grad = (const RowGrad*)(ws + q.grad);
       a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch, a.d_parts = q.d_parts;
-      if (int e = launch_product<false, false, kEpiGrad>(st, a)) return e;
+      Choice how;
+      if (cut_logits(a, q.slab_bytes, how)) {
+        const Tiling& t = kTilings[how.tiling];
+        if (int e = launch_slabs<false, false>(st, a, how, (float*)(ws + q.slabs))) return e;
+        head_slab_grad_kernel<<<(unsigned)q.Mp, 256, 0, st>>>(a, t.bx, t.by);
+        if (int e = hip_status()) return e;
+      } else if (int e = launch_product<false, false, kEpiGrad>(st, a)) {
+        return e;
+      }
     }
     if (c.ids != nullptr) {
       Entries a{};

@@ -230,6 +230,48 @@ def test_ids_beyond_the_vocabulary_are_nan(T):
 
 
 @pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M,C,V,T", [(70, 8200, 100, 0), (200, 4000, 300, 4), (700, 8192, 130, 0), (300, 6001, 257, 3)])
+def test_few_tiles_of_many_channels(M, C, V, T, type):
+    """Logits of few tiles: their product is cut along the channels."""
+    Case(M, C, V, type, T=T, size=0.5, ignored=0.4, **(dict(temperature=2.0, label_weight=0.5) if T else dict(smoothing=0.1))).check()
+
+
+@pytest.mark.parametrize("type,dw", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("M,C,V,T", [(1500, 200, 5003, 0), (1300, 100, 5100, 2)])
+def test_middle_sizes(M, C, V, T, type, dw):
+    Case(M, C, V, type, T=T, ignored=0.15).check(dw)
+
+
+def test_many_channels_and_rows():
+    Case(4096, 4096, 300, BF16, size=0.5, ignored=0.05).check()
+
+
+@pytest.mark.parametrize("type,M,C,V,T", [(BF16, 5, 64, 70001, 0), (BF16, 40, 72, 70000, 3), (F32, 40, 72, 70000, 3), (BF16, 9, 61, 70000, 2)])
+def test_few_rows_of_a_large_vocabulary(type, M, C, V, T):
+    Case(M, C, V, type, T=T).check()
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M", [3, 40])
+def test_small_losses_of_few_rows(type, M):
+    """A row's loss is the logarithm of one and the other tokens' share: where that is small it is not lost next to the one."""
+    c = Case(M, 64, 1000, type, ignored=0.0, size=0.25)
+    c.full_h += 20 * c.full_W[torch.arange(M)]
+    c.full_h.copy_(c.full_h.to(type))
+    c.labels = torch.arange(M)
+    loss = c.forward()["loss"]
+    z = c.h.double() @ c.W.double().t()
+    zy = z[torch.arange(M), torch.arange(M)]
+    share = torch.exp(z - zy[:, None])
+    share[torch.arange(M), torch.arange(M)] = 0
+    share = share.sum(1)
+    assert float(share.min()) < 1e-4
+    # what a share may be off: both logits, the exponent's argument (|z - z_label| < 40, two roundings), the instructions, the sums
+    off = 2 * R.logit_bound(c.h.double(), c.W.double(), c.n).amax(1) + 2 * 40 * R.F32 + 2.0 ** -20 + 100 * R.F32
+    R.assert_within(loss, torch.log1p(share), torch.log1p(share) * off * 1.01, "loss")
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
 def test_values_that_are_not_finite(type):
     c = Case(20, 32, 50, type, ignored=0.0)
     c.full_h[4, 3] = math.nan
