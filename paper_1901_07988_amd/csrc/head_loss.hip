@@ -452,6 +452,15 @@ __device__ inline void for_each(F f) {
   for_each<N>(f, std::make_integer_sequence<int, N>{});
 }
 
+// The second and fourth 16 lanes of a change places with the first and third of b.
+__device__ inline u32x2 lanes16_swap(uint32_t a, uint32_t b) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return u32x2{r[0], r[1]};
+#else
+  return u32x2{a, b};
+#endif
+}
 // Over the four lanes 16 apart: rows of 16 lanes, then halves of the wave, change places with those of a copy.
 template <typename F>
 __device__ inline float lanes16(float v, F f) {
@@ -685,44 +694,61 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
     }
   } else if constexpr (EPI == kEpiGrad) {
     const bool ragged = x0 + BX > nx || y0 + BY > a.ny, soft = a.inv_tau != 1.0f;
+    // Two neighbouring tiles' columns at a time: lanes 16 apart change places, so that each has eight columns of one of them and a row's 64 bytes go to
+    // memory together.
+    auto store = [&](char* row, int j, u32x2 even, u32x2 odd) __attribute__((always_inline)) {
+      const int g = lane >> 4;
+      const u32x2 lo = lanes16_swap(even[0], odd[0]), hi = lanes16_swap(even[1], odd[1]);
+      *reinterpret_cast<u32x4*>(row + (y0 + wy + 16 * (j + (g & 1)) + (g >> 1) * 8) * 2) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+    };
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
       const int x = x0 + wx + 16 * i + (lane & 15);
       const RowGrad g = a.grad[x];   // (the rows up to a whole tile are there)
       const int label = g.label >= 0 ? g.label - a.y0 : -1;
+      char* row = a.d + x * a.d_pitch;
 #pragma unroll
-      for (int j = 0; j < FY; ++j) {
-        const int col = y0 + wy + 16 * j + (lane >> 4) * 4;
-        float d[4];
+      for (int j = 0; j < FY; j += 2) {
+        float d[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float s = acc[i][j][e];
-          d[e] = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(s, a.scale, -g.L)), g.a0);
-          if (soft) d[e] = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(s * a.scale, a.inv_tau, -g.Lt)), d[e]);
+        for (int h = 0; h < 2; ++h) {
+          const int col = y0 + wy + 16 * (j + h) + (lane >> 4) * 4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float s = acc[i][j + h][e];
+            d[h][e] = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(s, a.scale, -g.L)), g.a0);
+            if (soft) d[h][e] = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(s * a.scale, a.inv_tau, -g.Lt)), d[h][e]);
+          }
+          if ((uint32_t)(label - col) < 4u) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[h][e] += col + e == label ? g.ay : 0.0f;
+          }
+          if (ragged) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[h][e] = x < nx && col + e < a.ny ? d[h][e] : 0.0f;
+          }
         }
-        if ((uint32_t)(label - col) < 4u) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) d[e] += col + e == label ? g.ay : 0.0f;
-        }
-        if (ragged) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) d[e] = x < nx && col + e < a.ny ? d[e] : 0.0f;
-        }
-        char* to = a.d + x * a.d_pitch + col * 2;
         if (a.d_parts == 3) {
-          uint32_t p[3][4];
+          uint32_t p[2][3][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) three_parts(d[e], p[0][e], p[1][e], p[2][e]);
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int n = 0; n < 3; ++n)
-            *reinterpret_cast<u32x2*>(to + n * a.d_plane) =
-                u32x2{__builtin_amdgcn_perm(p[n][1], p[n][0], 0x07060302u), __builtin_amdgcn_perm(p[n][3], p[n][2], 0x07060302u)};
+            for (int e = 0; e < 4; ++e) three_parts(d[h][e], p[h][0][e], p[h][1][e], p[h][2][e]);
+          auto upper = [](const uint32_t(&v)[4]) {
+            return u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+          };
+#pragma unroll
+          for (int n = 0; n < 3; ++n) store(row + n * a.d_plane, j, upper(p[0][n]), upper(p[1][n]));
         } else {
-          const u32x2 w{two_bf16(d[0], d[1]), two_bf16(d[2], d[3])};
-          *reinterpret_cast<u32x2*>(to) = w;
-          if (a.d_parts == 2)
-            *reinterpret_cast<u32x2*>(to + a.d_plane) = u32x2{two_bf16(d[0] - low_bf16(w[0]), d[1] - high_bf16(w[0])),
-                                                              two_bf16(d[2] - low_bf16(w[1]), d[3] - high_bf16(w[1]))};
+          u32x2 w[2], r[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            w[h] = u32x2{two_bf16(d[h][0], d[h][1]), two_bf16(d[h][2], d[h][3])};
+            r[h] = u32x2{two_bf16(d[h][0] - low_bf16(w[h][0]), d[h][1] - high_bf16(w[h][0])),
+                         two_bf16(d[h][2] - low_bf16(w[h][1]), d[h][3] - high_bf16(w[h][1]))};
+          }
+          store(row, j, w[0], w[1]);
+          if (a.d_parts == 2) store(row + a.d_plane, j, r[0], r[1]);
         }
       }
     }
@@ -1263,7 +1289,10 @@ constexpr int64_t kSlabBytes = (int64_t)128 << 20, kFewLogits = (int64_t)16 << 2
 constexpr int kTile = 128;
 constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
-constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)256 << 20;
+// Bytes of the workspace's parts.  A piece's gradient of the logits, a part: what stays in the last-level cache (256 MB) beside the piece's rows of the table until the
+// products have read it, or twice that where it is all there is (8192 x 4096 x 65536: 10.2 ms with 128 MB, 10.5 with 256, 10.3 with 512; 3277 x 2048 x
+// 32768, one piece: 1.28 ms, two: 1.35).
+constexpr int64_t kPartialBytes = (int64_t)64 << 20, kTableBytes = (int64_t)64 << 20, kGradBytes = (int64_t)128 << 20;
 
 struct Plan {
   int parts, d_parts;       // bf16 parts of h and W; of the gradient of the logits
@@ -1288,7 +1317,8 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
     const int64_t n = budget / bytes / 256 * 256;
     return n < 256 ? 256 : n < all ? n : all;
   };
-  int64_t piece = backward ? within(kGradBytes, q.Mp * 2 * q.d_parts) : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
+  const int64_t grad_token = q.Mp * 2 * q.d_parts;
+  int64_t piece = backward ? within(all * grad_token <= 2 * kGradBytes * q.d_parts ? 2 * kGradBytes * q.d_parts : kGradBytes * q.d_parts, grad_token) : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
   if (piece > 1 << 20) piece = 1 << 20;
   const int64_t table = within(kTableBytes, q.Cp * 2 * q.parts);
   const int64_t widest = piece;
