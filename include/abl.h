@@ -430,7 +430,7 @@ typedef struct abl_head {
   float scale, smoothing, z_weight;                 /* smoothing in [0, 1) */
   float temperature, label_weight, teacher_weight;  /* of abl_distill (not looked at by abl_xent); temperature > 0 */
 } abl_head;
-/* M <= 2^25, C <= 2^16, V <= 2^26, M V <= 2^44, T <= 1024 (abl_distill: 1 <= T), or ABL_ERR_SHAPE.  The size depends on M, C, V, T, dtype, dw_dtype
+/* M <= 2^23, C <= 2^16, V <= 2^26, M V <= 2^44, T <= 1024 (abl_distill: 1 <= T), or ABL_ERR_SHAPE.  The size depends on M, C, V, T, dtype, dw_dtype
  * and flags; 0 on invalid arguments, never 0 otherwise. */
 size_t abl_head_scratch_bytes(const abl_head* head, int backward);
 /* labels [M]; loss, lse [M] out.  M = 0: nothing is done. */

@@ -23,8 +23,9 @@ int check_head(const abl_head* head, bool backward, bool teacher, abl_head& p) {
   if (!teacher) p.T = 0, p.temperature = 1.0f, p.label_weight = 1.0f, p.teacher_weight = 0.0f;
   if (!finite_number(p.scale) || !(p.smoothing >= 0.0f && p.smoothing < 1.0f) || !finite_number(p.z_weight)) return ABL_ERR_ARG;
   if (!(p.temperature > 0.0f) || !finite_number(p.temperature) || !finite_number(1.0f / p.temperature)) return ABL_ERR_ARG;
+  if (1.0f / p.temperature == 1.0f) p.temperature = 1.0f;
   if (!finite_number(p.label_weight) || !finite_number(p.teacher_weight)) return ABL_ERR_ARG;
-  if (p.M < 0 || p.M > (int64_t)1 << 25 || p.C < 1 || p.C > 1 << 16 || p.V < 1 || p.V > 1 << 26) return ABL_ERR_SHAPE;
+  if (p.M < 0 || p.M > (int64_t)1 << 23 || p.C < 1 || p.C > 1 << 16 || p.V < 1 || p.V > 1 << 26) return ABL_ERR_SHAPE;
   if (p.M * p.V > (int64_t)1 << 44 || p.T > kTopEntries || p.T < (teacher ? 1 : 0)) return ABL_ERR_SHAPE;
   return ABL_OK;
 }

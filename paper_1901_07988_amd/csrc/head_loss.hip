@@ -210,8 +210,9 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
         const int64_t y = g.labels != nullptr ? g.labels[row] : -1;
         const int f = g.flags != nullptr ? g.flags[row] : y < g.V ? kLabel : kLabel | kBad;
         const float w = g.dloss[row] * g.scale, l = f & kLabel ? w * g.label_weight : 0.0f;
-        r.L = g.in_lse != nullptr ? g.in_lse[row] : g.tau == 1.0f ? g.in_lse_t[row] : 0.0f;
-        r.a = __builtin_fmaf(2.0f * g.z_weight * w, r.L, l);
+        // (without a log-sum nothing is multiplied with its exponentials, which must not overflow then)
+        r.L = g.in_lse != nullptr ? g.in_lse[row] : g.tau == 1.0f ? g.in_lse_t[row] : 1e38f;
+        r.a = g.z_weight != 0.0f ? __builtin_fmaf(2.0f * g.z_weight * w, r.L, l) : l;
         r.Lt = g.in_lse_t != nullptr ? g.in_lse_t[row] : 0.0f;
         r.at = f & kTeacher ? w * g.teacher_weight * g.tau : 0.0f;
         if (g.tau == 1.0f) r.a += r.at;   // (one exponential for both)

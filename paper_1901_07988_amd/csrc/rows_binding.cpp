@@ -6,6 +6,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -249,6 +250,13 @@ struct HeadArgs {
   Matrix h, W;
   void *labels, *ids = nullptr, *logits = nullptr;
 };
+// All tensors of a call lie on the device whose stream it goes to.
+bool on_this_device(PyObject* const* a, Py_ssize_t n) {
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (THPVariable_Check(a[i]) && THPVariable_Unpack(a[i]).is_cuda() && THPVariable_Unpack(a[i]).device().index() != c10::hip::current_device())
+      return fail("tensors", "on another device than the current one");
+  return true;
+}
 bool head_operands(HeadArgs& g, PyObject* h, PyObject* W, PyObject* labels) {
   if (!matrix(g.h, h, "h") || !channels(g.h, "h") || !matrix(g.W, W, "W")) return false;
   if (g.W.type != g.h.type) return fail("W", "of another type than it has to be");
@@ -288,7 +296,7 @@ PyObject* xent_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HeadArgs g;
   size_t bytes;
   void *ws, *loss, *lse;
-  if (!count(n, 10) || !head_operands(g, a[0], a[1], a[2]) || !workspace(ws, bytes, a[3]) || !row_numbers(loss, a[4], g.h.M, "loss") ||
+  if (!count(n, 10) || !on_this_device(a, n) || !head_operands(g, a[0], a[1], a[2]) || !workspace(ws, bytes, a[3]) || !row_numbers(loss, a[4], g.h.M, "loss") ||
       !row_numbers(lse, a[5], g.h.M, "lse") || !number(g.p.scale, a[6]) || !number(g.p.smoothing, a[7]) || !number(g.p.z_weight, a[8]) ||
       !head_flags(g, a[9]))
     return nullptr;
@@ -301,7 +309,7 @@ PyObject* xent_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix dh;
   size_t bytes;
   void *ws, *lse, *dloss, *dW;
-  if (!count(n, 12) || !head_operands(g, a[0], a[1], a[2]) || !row_numbers(lse, a[3], g.h.M, "lse") ||
+  if (!count(n, 12) || !on_this_device(a, n) || !head_operands(g, a[0], a[1], a[2]) || !row_numbers(lse, a[3], g.h.M, "lse") ||
       !row_numbers(dloss, a[4], g.h.M, "dloss") || !workspace(ws, bytes, a[5]) || !head_gradients(g, a[6], a[7], dh, dW) ||
       !number(g.p.scale, a[8]) || !number(g.p.smoothing, a[9]) || !number(g.p.z_weight, a[10]) || !head_flags(g, a[11]))
     return nullptr;
@@ -319,7 +327,7 @@ PyObject* distill_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HeadArgs g;
   size_t bytes;
   void *ws, *loss, *lse, *lse_t, *z_top;
-  if (!count(n, 17) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !workspace(ws, bytes, a[5]) ||
+  if (!count(n, 17) || !on_this_device(a, n) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !workspace(ws, bytes, a[5]) ||
       !row_numbers(loss, a[6], g.h.M, "loss") || !row_numbers(lse, a[7], g.h.M, "lse") || !row_numbers(lse_t, a[8], g.h.M, "lse_t") ||
       !matrix_address(z_top, a[9], kF32, g.h.M, g.p.T, "z_top") || !distill_numbers(g, a + 10))
     return nullptr;
@@ -333,7 +341,7 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Matrix dh;
   size_t bytes;
   void *ws, *lse, *lse_t, *z_top, *dloss, *dW;
-  if (!count(n, 19) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !row_numbers(lse, a[5], g.h.M, "lse") ||
+  if (!count(n, 19) || !on_this_device(a, n) || !head_operands(g, a[0], a[1], a[2]) || !teacher_operands(g, a[3], a[4]) || !row_numbers(lse, a[5], g.h.M, "lse") ||
       !row_numbers(lse_t, a[6], g.h.M, "lse_t") || !matrix_address(z_top, a[7], kF32, g.h.M, g.p.T, "z_top") ||
       !row_numbers(dloss, a[8], g.h.M, "dloss") || !workspace(ws, bytes, a[9]) || !head_gradients(g, a[10], a[11], dh, dW) ||
       !distill_numbers(g, a + 12))

@@ -424,9 +424,11 @@ def test_two_calls_at_once():
             assert all(torch.equal(w[0][k], g[0][k]) for k in w[0]) and torch.equal(w[1], g[1]) and torch.equal(w[2], g[2])
 
 
-def test_the_forward_without_log_sums():
-    """lse is not needed where only the teacher counts."""
-    c = Case(50, 64, 120, BF16, T=6, labels=False, temperature=2.0)
+@pytest.mark.parametrize("size,temperature", [(1.0, 2.0), (30.0, 2.0), (30.0, 1.0)])
+def test_the_forward_without_log_sums(size, temperature):
+    """lse is not needed where only the teacher counts, however large the logits are."""
+    c = Case(50, 64, 120, BF16, T=6, labels=False, temperature=temperature, size=size)
+    assert (size > 1) == bool((c.h.float() @ c.W.float().t()).max() > 90)
     out = {k: v.clone() for k, v in c.forward().items()}
     o = {k: torch.empty_like(v) for k, v in out.items()}
     B.abl_distill_forward(c.dh_in, c.dW_in, None, c.gi, c.gt, scratch_for(50, 64, 120, BF16, 6), o["loss"], None, o["lse_t"], o["z_top"], **c.options())

@@ -65,7 +65,7 @@ def test_scratch_sizes():
     assert size(8192, 4096, 65536, bf16, backward=True) < (512 + 192) << 20
     assert size(8192, 4096, 65536, bf16) < (192 + 64) << 20
     assert size(1 << 20, 1024, 1 << 17, bf16, backward=True) > 1 << 32
-    for kw in (dict(M=-1), dict(C=0), dict(V=0), dict(M=(1 << 25) + 1), dict(C=(1 << 16) + 1), dict(V=(1 << 26) + 1), dict(M=1 << 25, V=1 << 20),
+    for kw in (dict(M=-1), dict(C=0), dict(V=0), dict(M=(1 << 23) + 1), dict(C=(1 << 16) + 1), dict(V=(1 << 26) + 1), dict(M=1 << 23, V=1 << 22),
                dict(T=1025), dict(T=-1), dict(dtype=torch.float16), dict(dw_dtype=torch.float16, backward=True),
                dict(dtype=f32, dw_dtype=bf16, backward=True), dict(flags=B.ABL_ACCUM_DW), dict(flags=1)):
         assert size(**{**dict(M=4, C=8, V=16, dtype=bf16), **kw}) == 0, kw
@@ -108,7 +108,7 @@ def test_calls_refuse(name):
                   dict(label_weight=nan), dict(teacher_weight=inf)]
     for head in wrong:
         assert call(name, head) == B.ABL_ERR_ARG, head
-    sizes = [dict(M=-1), dict(M=(1 << 25) + 1), dict(C=0), dict(C=(1 << 16) + 1), dict(V=0), dict(V=(1 << 26) + 1), dict(M=1 << 25, V=1 << 20)]
+    sizes = [dict(M=-1), dict(M=(1 << 23) + 1), dict(C=0), dict(C=(1 << 16) + 1), dict(V=0), dict(V=(1 << 26) + 1), dict(M=1 << 23, V=1 << 22)]
     for head in sizes + ([dict(T=0), dict(T=-1), dict(T=1025)] if teacher else []):
         assert call(name, head) == B.ABL_ERR_SHAPE, head
     may_be_null = {"dh", "dW"} | ({"labels"} if teacher else set())
