@@ -483,21 +483,22 @@ __device__ inline float lanes16_sum(float v) {
 
 // Joins the sums of two sets of logits.
 __device__ inline Partial join(const Partial& a, const Partial& b, float inv_tau) {
+  const bool first = a.top >= b.top;
+  const Partial &big = first ? a : b, &small = first ? b : a;
+  const float d = a.top == b.top ? 0.0f : small.top - big.top;   // (there may be none on both sides)
   Partial r;
   r.top = fmaxf(a.top, b.top);
-  const float ref = r.top == -__builtin_inff() ? 0.0f : r.top;
-  const float da = a.top - ref, db = b.top - ref;   // (one of them is zero and its exponential one, or there are none)
-  auto rest = [](float ra, float rb, float wa, float wb) { return __builtin_fmaf(ra, wa, rb * wb) + ((fmaxf(wa, wb) - 1.0f) + fminf(wa, wb)); };
-  r.rest = rest(a.rest, b.rest, exp_of(da), exp_of(db));
-  r.rest_t = inv_tau != 1.0f ? rest(a.rest_t, b.rest_t, exp_of(da * inv_tau), exp_of(db * inv_tau)) : 0.0f;
+  r.rest = __builtin_fmaf(small.rest + 1.0f, exp_of(d), big.rest);
+  r.rest_t = inv_tau != 1.0f ? __builtin_fmaf(small.rest_t + 1.0f, exp_of(d * inv_tau), big.rest_t) : 0.0f;
   r.z = a.z + b.z;
   return r;
 }
 
-__device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the wave's 64 lanes, the same for all
+template <int LANES = 64>
+__device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the wave's 64 lanes (or each 16 of them), the same for all of these
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
+  for (int d = 1; d < LANES; d *= 2) {
     const Partial o{__shfl_xor(p.top, d), __shfl_xor(p.rest, d), __shfl_xor(p.rest_t, d), __shfl_xor(p.z, d)};
     p = lane & d ? join(o, p, inv_tau) : join(p, o, inv_tau);   // (in the same order in both lanes)
   }
@@ -950,11 +951,50 @@ __device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
   s = wave_sum(s);
   if (lane == 0) a.z_top[at] = s * a.scale;
 }
-// Four waves a row that counts, each takes its entries one after the other.
+// Four waves a row that counts.  A wave takes two entries at a time, their rows of the table on the way together: rows from anywhere in a table that
+// no cache holds.
 template <typename T>
 __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const int* __restrict__ rows, const int* __restrict__ count) {
   if ((int)blockIdx.x >= *count) return;
-  for (int k = threadIdx.x >> 6; k < a.T; k += 4) entry_logit<T>(a, rows[blockIdx.x], k);
+  const int64_t row = rows[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const T* h = (const T*)a.h + row * a.ldh;
+  for (int k0 = 0; k0 < a.T; k0 += 64) {
+    // the tokens of 64 entries, one a lane: -1: absent, V: beyond the vocabulary
+    const int64_t at = row * a.T + k0 + lane, wide = k0 + lane < a.T ? a.ids[at] : -1;
+    const bool there = k0 + lane < a.T && entry_there(wide, a.logits[at]);
+    const int id = !there ? -1 : wide < a.V ? (int)wide : a.V, n = a.T - k0 < 64 ? a.T - k0 : 64;
+    float mine = there ? nan_value() : 0.0f;
+    uint64_t left = __ballot(there && id < a.V) & (0x1111111111111111ull << wave);   // of this wave
+    while (left != 0) {
+      const int i = __builtin_ctzll(left);
+      left &= left - 1;
+      const int j = left != 0 ? __builtin_ctzll(left) : i;
+      left &= left - 1;
+      const T *wi = (const T*)a.W + (int64_t)__builtin_amdgcn_readlane(id, i) * a.ldw, *wj = (const T*)a.W + (int64_t)__builtin_amdgcn_readlane(id, j) * a.ldw;
+      float si = 0.0f, sj = 0.0f;
+      auto add = [&](int c, int m) __attribute__((always_inline)) {
+        float x[8], y[8], z[8];
+        load_piece(wi + c, m, y);
+        load_piece(wj + c, m, z);
+        load_piece(h + c, m, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float u = a.rounded ? (float)(bf16_t)x[e] : x[e];
+          si = __builtin_fmaf(u, a.rounded ? (float)(bf16_t)y[e] : y[e], si);
+          sj = __builtin_fmaf(u, a.rounded ? (float)(bf16_t)z[e] : z[e], sj);
+        }
+      };
+      const int whole = a.C / 512 * 512;
+#pragma unroll 4
+      for (int c = 0; c < whole; c += 512) add(c + lane * 8, 8);
+      if (whole < a.C) add(whole + lane * 8, a.C - whole - lane * 8);
+      si = wave_sum(si), sj = wave_sum(sj);
+      if (lane == i) mine = si * a.scale;
+      if (lane == j) mine = sj * a.scale;
+    }
+    if (lane < n && (lane & 3) == wave) a.z_top[at] = mine;
+  }
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------
@@ -1156,13 +1196,33 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
         entry_logit<bf16_t>(a.entries, n0, k);
     }
   }
+  // What a wave will need of its row, on the way while the sums are joined.
+  const int r = threadIdx.x >> 6, lane = threadIdx.x & 63, n = n0 + r;
+  const bool mine = r < ROWS && n < count;
+  int64_t row = n;
+  int f = 0;
+  float z_label = 0.0f;
+  if (mine && a.after == nullptr) {
+    if (a.rows != nullptr) row = a.rows[n];
+    f = a.flags != nullptr ? a.flags[row] : row_flags(row, a.labels, a.ids, a.logits, a.T, a.V);
+    if (f & kLabel) z_label = a.z_label[n];
+  }
   const Partial none{-__builtin_inff(), -1.0f, -1.0f, 0.0f};
   Partial p = none;
   {
     const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
     if (n0 + r < count) {
       if (group == 0 && a.before != nullptr) p = a.before[n0 + r];
-      for (int t = group; t < a.tiles; t += kGroups) p = join(p, a.partial[t * a.partial_ld + n0 + r], inv_tau);
+      const Partial* from = a.partial + n0 + r;
+      int t = group;
+      for (; t + 3 * kGroups < a.tiles; t += 4 * kGroups) {   // (four loads on the way together)
+        Partial q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = from[(t + i * kGroups) * a.partial_ld];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p = join(p, q[i], inv_tau);
+      }
+      for (; t < a.tiles; t += kGroups) p = join(p, from[t * a.partial_ld], inv_tau);
     }
     if constexpr (ROWS == 1) {
       p = lanes_joined(p, inv_tau);
@@ -1172,15 +1232,15 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
     }
   }
   __syncthreads();
-  const int r = threadIdx.x >> 6, lane = threadIdx.x & 63, n = n0 + r;
-  if (r >= ROWS || n >= count) return;
-  p = lanes_joined(ROWS > 1 ? joined[lane][r] : lane < 16 ? joined[lane][0] : none, inv_tau);
+  if (!mine) return;
+  if constexpr (ROWS == 1)
+    p = lanes_joined<16>(joined[lane & 15][0], inv_tau);
+  else
+    p = lanes_joined(joined[lane][r], inv_tau);
   if (a.after != nullptr) {
     if (lane == 0) a.after[n] = p;
     return;
   }
-  const int64_t row = a.rows != nullptr ? a.rows[n] : n;
-  const int f = a.flags != nullptr ? a.flags[row] : row_flags(row, a.labels, a.ids, a.logits, a.T, a.V);
   if ((f & (kLabel | kTeacher)) == 0) {
     if (lane == 0) {
       a.loss[row] = 0.0f;
@@ -1193,7 +1253,7 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
   const float ln_t = a.tau != 1.0f ? log1pf(p.rest_t) : ln, top_t = p.top * inv_tau;
   float loss = a.z_weight != 0.0f ? a.z_weight * L * L : 0.0f;
   if (f & kLabel) {   // (differences to the maximum first: L and z are large where the loss is small)
-    float ce = ln + (p.top - a.z_label[n]);
+    float ce = ln + (p.top - z_label);
     if (a.smoothing != 0.0f) ce = (1.0f - a.smoothing) * ce + a.smoothing * (ln + (p.top - p.z / (float)a.V));
     loss += a.label_weight * ce;
   }
