@@ -864,13 +864,22 @@ __global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by
 
 // ---- few tiles of logits --------------------------------------------------------------------------------
 // Where the logits are few tiles of many k's, their product, too, is cut into shares, and these launches take the place of its epilogues.
+constexpr int kSlabColumns = 1024;   // of a block: four a thread, 256 apart, all shares' loads on the way together
 struct Slabs {
   const float* p;
   int shares, nx, ny;
-  __device__ inline float at(int x, int col) const {
-    float v = 0.0f;
-    for (int i = 0; i < shares; ++i) v += p[((int64_t)i * nx + x) * ny + col];
-    return v;
+  __device__ inline void get(int x, int col, float (&z)[4]) const {   // (zeros beyond the last column)
+    float v[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = i < shares && col + 256 * e < ny ? p[((int64_t)i * nx + x) * ny + col + 256 * e] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[e] += v[i][e];
+    }
   }
 };
 __device__ inline Slabs slabs_of(const Product& a, int bx, int by) {
@@ -878,40 +887,46 @@ __device__ inline Slabs slabs_of(const Product& a, int bx, int by) {
   const int64_t tiles = (int64_t)((nx + bx - 1) / bx) * ((a.ny + by - 1) / by);
   return {a.slabs, shares_of(a.split, tiles, (a.k + 63) / 64 * a.parts, (int64_t)nx * a.ny), nx, a.ny};
 }
-// A row's sums: a block each.
+// The sums of a row's kSlabColumns logits: a block each.
 __global__ __launch_bounds__(256) void head_slab_partial_kernel(Product a, int bx, int by) {
   __shared__ Partial joined[4];
   const Slabs s = slabs_of(a, bx, by);
-  const int x = blockIdx.x;
+  const int x = blockIdx.x, col = blockIdx.y * kSlabColumns + threadIdx.x;
   if (x >= s.nx) return;
   const int label = a.row_label != nullptr ? a.row_label[x] - a.y0 : -1;
   Partial p{-__builtin_inff(), -1.0f, -1.0f, 0.0f};
-  for (int col = threadIdx.x; col < s.ny; col += 256) {
-    const float z = s.at(x, col) * a.scale;
-    if (col == label) a.z_label[x] = z;
-    p = join(p, Partial{z, 0.0f, 0.0f, z}, a.inv_tau);
+  float z[4];
+  s.get(x, col, z);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (col + 256 * e >= s.ny) continue;
+    z[e] *= a.scale;
+    if (col + 256 * e == label) a.z_label[x] = z[e];
+    p = join(p, Partial{z[e], 0.0f, 0.0f, z[e]}, a.inv_tau);
   }
   p = lanes_joined(p, a.inv_tau);
   if ((threadIdx.x & 63) == 0) joined[threadIdx.x >> 6] = p;
   __syncthreads();
-  if (threadIdx.x == 0) a.partial[x] = join(join(joined[0], joined[1], a.inv_tau), join(joined[2], joined[3], a.inv_tau), a.inv_tau);
+  if (threadIdx.x == 0)
+    a.partial[(int64_t)blockIdx.y * a.partial_ld + x] = join(join(joined[0], joined[1], a.inv_tau), join(joined[2], joined[3], a.inv_tau), a.inv_tau);
 }
-// The gradient of a row's logits, with the zeros behind it that the products take: a block each.
+// The gradient of a row's logits, with the zeros behind it that the products take: likewise.
 __global__ __launch_bounds__(256) void head_slab_grad_kernel(Product a, int bx, int by) {
   const Slabs s = slabs_of(a, bx, by);
-  const int x = blockIdx.x;
+  const int x = blockIdx.x, col = blockIdx.y * kSlabColumns + threadIdx.x;
   if (x >= (s.nx + kRowTile - 1) / kRowTile * kRowTile) return;
   const RowGrad g = a.grad[x];
   const int label = g.label >= 0 ? g.label - a.y0 : -1;
-  for (int col = threadIdx.x; col < (s.ny + 63) / 64 * 64; col += 256) {
-    float d = 0.0f;
-    if (x < s.nx && col < s.ny) {
-      const float v = s.at(x, col);
-      d = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(v, a.scale, -g.L)), g.a0);
-      if (a.inv_tau != 1.0f) d = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(v * a.scale, a.inv_tau, -g.Lt)), d);
-      if (col == label) d += g.ay;
-    }
-    put_parts(a.d + x * a.d_pitch + col * 2, a.d_plane, a.d_parts, d);
+  float z[4] = {};
+  if (x < s.nx) s.get(x, col, z);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int c = col + 256 * e;
+    if (c >= (s.ny + 63) / 64 * 64) continue;
+    float d = __builtin_fmaf(g.a, exp_of(__builtin_fmaf(z[e], a.scale, -g.L)), g.a0);
+    if (a.inv_tau != 1.0f) d = __builtin_fmaf(g.at, exp_of(__builtin_fmaf(z[e] * a.scale, a.inv_tau, -g.Lt)), d);
+    if (c == label) d += g.ay;
+    put_parts(a.d + x * a.d_pitch + c * 2, a.d_plane, a.d_parts, x < s.nx && c < s.ny ? d : 0.0f);
   }
 }
 
@@ -1189,7 +1204,8 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
   if (n0 >= count) return;
   const float inv_tau = 1.0f / a.tau;
   if constexpr (ROWS == 1) {
-    for (int k = threadIdx.x >> 6; k < a.entries.T; k += 16) {   // (read below by the wave of the row, behind the barrier)
+    // (by the last waves first, which have no sums to join where there are few; read below by the wave of the row, behind the barrier)
+    for (int k = 15 - (int)(threadIdx.x >> 6); k < a.entries.T; k += 16) {
       if (a.entries.dtype == ABL_F32)
         entry_logit<float>(a.entries, n0, k);
       else
@@ -1443,12 +1459,12 @@ int launch_tiles(hipStream_t st, const Product& a) {
   return hip_status();
 }
 
-// Tiles of 256 x 256, 256 x 128 or 128 x 128, whichever takes the least time for the rows that a call has.
+// Tiles of 256 x 256, 256 x 128, 128 x 128 or - k along the rows of both operands - 64 x 64, whichever takes the least time for the rows that a call has.
 struct Tiling {
   int bx, by;
   Split split;
 };
-constexpr Tiling kTilings[3] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}};
+constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 256, 350, 4500, 4000, 800}}};
 int64_t tiles_of(const Tiling& t, int64_t nx, int64_t ny) { return (nx + t.bx - 1) / t.bx * ((ny + t.by - 1) / t.by); }
 int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
   const int n = shares_of(s, tiles, steps, size);
@@ -1460,12 +1476,12 @@ struct Choice {
   int64_t time;
 };
 // The rows that count, of which there may be fewer, are k (count_k) or nx.
-Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
+Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k, bool along) {
   const int64_t size = nx * ny, fit = slab_bytes / (size * 4);
   const int steps = (int)((k + 63) / 64 * parts);
   Choice c{};
   int64_t least = 0;
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < (along ? 4 : 3); ++i) {
     Split s = kTilings[i].split;
     s.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
     const int64_t time = time_of(s, tiles_of(kTilings[i], nx, ny), steps, size);
@@ -1482,23 +1498,27 @@ Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_
 }
 // Whether few tiles of logits are cut into shares (the launch that takes their slabs costs what one that adds them does).
 bool cut_logits(const Product& a, int64_t slab_bytes, Choice& c) {
-  const Choice whole = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false);
-  c = choice_of(a.nx, a.ny, a.k, a.parts, true, slab_bytes, false);
+  const Choice whole = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, true);
+  c = choice_of(a.nx, a.ny, a.k, a.parts, true, slab_bytes, false, true);
   return c.split.most > 1 && c.time + 5000 < whole.time * 3 / 4;
 }
-template <bool XO, bool YO>
+template <bool XO, bool YO, int EPI>
+int launch_tiling(hipStream_t st, const Product& a, int tiling) {
+  if constexpr (!XO && !YO)
+    if (tiling == 3) return launch_tiles<64, 64, 2, 2, 4, XO, YO, EPI>(st, a);
+  if (tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a);
+  return tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
+}
 int launch_slabs(hipStream_t st, Product& a, const Choice& c, float* slabs) {
   a.split = c.split, a.slabs = slabs, a.out = nullptr;
-  if (c.tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, kEpiSum>(st, a);
-  return c.tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, kEpiSum>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, kEpiSum>(st, a);
+  return launch_tiling<false, false, kEpiSum>(st, a, c.tiling);
 }
 // (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
 int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
-  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0);
+  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0, !XO && !YO);
   a.split = c.split, a.slabs = slabs;
-  if (c.tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a);
-  return c.tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
+  return launch_tiling<XO, YO, EPI>(st, a, c.tiling);
 }
 
 template <typename T, int P>
@@ -1660,13 +1680,14 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
     a.partial = (Partial*)(ws + q.partial), a.partial_ld = q.Mp, a.sum_z = p.smoothing != 0.0f;
     a.row_label = c.labels != nullptr ? (const int*)(ws + q.labels) : nullptr, a.z_label = (float*)(ws + q.z_label);
     Choice how;
-    int columns = (int)n;   // of a tile that the loss finds sums of
+    int columns;   // of a tile that the loss finds sums of
     if (cut_logits(a, q.slab_bytes, how)) {
       const Tiling& t = kTilings[how.tiling];
-      if (int e = launch_slabs<false, false>(st, a, how, (float*)(ws + q.slabs))) return e;
-      head_slab_partial_kernel<<<(unsigned)p.M, 256, 0, st>>>(a, t.bx, t.by);
+      if (int e = launch_slabs(st, a, how, (float*)(ws + q.slabs))) return e;
+      head_slab_partial_kernel<<<dim3((unsigned)p.M, (unsigned)((n + kSlabColumns - 1) / kSlabColumns)), 256, 0, st>>>(a, t.bx, t.by);
+      columns = kSlabColumns;
     } else {
-      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
+      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, true).tiling].by;
       if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
     }
     Loss l = loss_of(c, q, ws);
@@ -1708,8 +1729,8 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
       Choice how;
       if (cut_logits(a, q.slab_bytes, how)) {
         const Tiling& t = kTilings[how.tiling];
-        if (int e = launch_slabs<false, false>(st, a, how, (float*)(ws + q.slabs))) return e;
-        head_slab_grad_kernel<<<(unsigned)q.Mp, 256, 0, st>>>(a, t.bx, t.by);
+        if (int e = launch_slabs(st, a, how, (float*)(ws + q.slabs))) return e;
+        head_slab_grad_kernel<<<dim3((unsigned)q.Mp, (unsigned)((n + 63 + kSlabColumns - 1) / kSlabColumns)), 256, 0, st>>>(a, t.bx, t.by);
         if (int e = hip_status()) return e;
       } else if (int e = launch_product<false, false, kEpiGrad>(st, a)) {
         return e;
