@@ -305,12 +305,16 @@ enum { kEpiPartial, kEpiGrad, kEpiSum };
 // A 16-byte piece of a staged tile of 64 k's.  k along the rows: rows of eight pieces, the c-th of row r at place c xor (r / 2) % 8: the 16
 // rows of a fragment's read take all banks once.  k outermost: rows (one k) of B channels; the even pieces come first, the c-th of each kind at place
 // c xor a key of the row, the odd ones further by half of a row's pieces and in other places of it: half a wave's transposing read, 16 pieces of
-// the eight rows 0..3 and 8..11 (or 4..7 and 12..15), takes all banks once.
+// the eight rows 0..3 and 8..11 (or 4..7 and 12..15), takes all banks once.  Rows of 64 channels are half of the banks: their pieces stay in order, the c-th at
+// place c xor a key of bits 1 and 3 of the row.
 __device__ inline int key_along(int row) { return (row >> 1) & 7; }
 __device__ inline int key_outer(int k) { return (k & 3) | ((k >> 1) & 4); }
+__device__ inline int key_narrow(int k) { return (k & 2) | ((k >> 1) & 4); }
 template <int B, bool OUTER>
 __device__ inline int staged_piece(int row, int q) {
-  if constexpr (OUTER) {
+  if constexpr (OUTER && B == 64) {
+    return row * 128 + ((q ^ key_narrow(row)) * 16);
+  } else if constexpr (OUTER) {
     constexpr int kHalf = B / 16;
     return row * (B * 2) + (q & 1) * B + (((q >> 1) ^ key_outer(row) ^ ((q & 1) * (kHalf - 4))) * 16);
   } else {
@@ -357,7 +361,9 @@ struct Source {
     base = 0, k = 0, left = 0, bytes = 0;   // (next() combines old and new values by their bits: both have to have one)
     const int row = (int)threadIdx.x / kPieces, in = (int)threadIdx.x % kPieces;
     int q;
-    if constexpr (OUTER) {
+    if constexpr (OUTER && B == 64) {
+      q = in ^ key_narrow(row);
+    } else if constexpr (OUTER) {
       constexpr int kHalf = B / 16;
       const int odd = in / kHalf;
       q = 2 * ((in % kHalf) ^ key_outer(row) ^ (odd * (kHalf - 4))) + odd;
@@ -434,7 +440,7 @@ struct Fragments {
   __device__ inline bf16x8_t get(int n, int half, int at) const {
     constexpr int kTileBytes = B * 128;
     if constexpr (OUTER) {
-      lds_short4* p = (lds_short4*)(uintptr_t)((base ^ (n * 16)) + at * kTileBytes + half * (kTileBytes / 2));
+      lds_short4* p = (lds_short4*)(uintptr_t)((base ^ (n * (B == 64 ? 32 : 16))) + at * kTileBytes + half * (kTileBytes / 2));
       struct two { short4_t a, b; };
       return __builtin_bit_cast(bf16x8_t, two{__builtin_amdgcn_ds_read_tr16_b64_v4i16(p), __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 4 * (B * 2) / 8)});
     } else {
@@ -1459,12 +1465,12 @@ int launch_tiles(hipStream_t st, const Product& a) {
   return hip_status();
 }
 
-// Tiles of 256 x 256, 256 x 128, 128 x 128 or - k along the rows of both operands - 64 x 64, whichever takes the least time for the rows that a call has.
+// Tiles of 256 x 256, 256 x 128, 128 x 128 or 64 x 64, whichever takes the least time for the rows that a call has.
 struct Tiling {
   int bx, by;
   Split split;
 };
-constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 256, 350, 4500, 4000, 800}}};
+constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 512, 500, 4500, 4000, 800}}};
 int64_t tiles_of(const Tiling& t, int64_t nx, int64_t ny) { return (nx + t.bx - 1) / t.bx * ((ny + t.by - 1) / t.by); }
 int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
   const int n = shares_of(s, tiles, steps, size);
@@ -1476,12 +1482,12 @@ struct Choice {
   int64_t time;
 };
 // The rows that count, of which there may be fewer, are k (count_k) or nx.
-Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k, bool along) {
+Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
   const int64_t size = nx * ny, fit = slab_bytes / (size * 4);
   const int steps = (int)((k + 63) / 64 * parts);
   Choice c{};
   int64_t least = 0;
-  for (int i = 0; i < (along ? 4 : 3); ++i) {
+  for (int i = 0; i < 4; ++i) {
     Split s = kTilings[i].split;
     s.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
     const int64_t time = time_of(s, tiles_of(kTilings[i], nx, ny), steps, size);
@@ -1498,14 +1504,13 @@ Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_
 }
 // Whether few tiles of logits are cut into shares (the launch that takes their slabs costs what one that adds them does).
 bool cut_logits(const Product& a, int64_t slab_bytes, Choice& c) {
-  const Choice whole = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, true);
-  c = choice_of(a.nx, a.ny, a.k, a.parts, true, slab_bytes, false, true);
+  const Choice whole = choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false);
+  c = choice_of(a.nx, a.ny, a.k, a.parts, true, slab_bytes, false);
   return c.split.most > 1 && c.time + 5000 < whole.time * 3 / 4;
 }
 template <bool XO, bool YO, int EPI>
 int launch_tiling(hipStream_t st, const Product& a, int tiling) {
-  if constexpr (!XO && !YO)
-    if (tiling == 3) return launch_tiles<64, 64, 2, 2, 4, XO, YO, EPI>(st, a);
+  if (tiling == 3) return launch_tiles<64, 64, 2, 2, 4, XO, YO, EPI>(st, a);
   if (tiling == 0) return launch_tiles<256, 256, 2, 4, 2, XO, YO, EPI>(st, a);
   return tiling == 1 ? launch_tiles<256, 128, 4, 2, 3, XO, YO, EPI>(st, a) : launch_tiles<128, 128, 2, 4, 4, XO, YO, EPI>(st, a);
 }
@@ -1516,7 +1521,7 @@ int launch_slabs(hipStream_t st, Product& a, const Choice& c, float* slabs) {
 // (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
 int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
-  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0, !XO && !YO);
+  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0);
   a.split = c.split, a.slabs = slabs;
   return launch_tiling<XO, YO, EPI>(st, a, c.tiling);
 }
@@ -1687,7 +1692,7 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
       head_slab_partial_kernel<<<dim3((unsigned)p.M, (unsigned)((n + kSlabColumns - 1) / kSlabColumns)), 256, 0, st>>>(a, t.bx, t.by);
       columns = kSlabColumns;
     } else {
-      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, true).tiling].by;
+      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
       if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
     }
     Loss l = loss_of(c, q, ws);
