@@ -129,13 +129,16 @@ __device__ inline void put_parts(char* to, int64_t plane, int parts, float v) {
   }
 }
 
-// A row of C elements (nullptr: zeros) to its place in P planes, `plane` bytes apart, with zeros up to Cp channels: by a wave.
+// A row of C elements (nullptr: zeros) to its place in P planes, `plane` bytes apart, with zeros up to Cp channels: by a wave.  P = 0: as fp32.
 template <typename T, int P>
 __device__ inline void copy_row(const T* from, int C, int Cp, char* to, int64_t plane) {
   for (int c = (threadIdx.x & 63) * 8; c < Cp; c += 512) {
     float v[8] = {};
     if (from != nullptr) load_piece(from + c, C - c, v);
-    if constexpr (P == 1) {
+    if constexpr (P == 0) {
+      *reinterpret_cast<floatx4*>(to + 4 * c) = floatx4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<floatx4*>(to + 4 * c + 16) = floatx4{v[4], v[5], v[6], v[7]};
+    } else if constexpr (P == 1) {
       *reinterpret_cast<u32x4*>(to + 2 * c) = u32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
     } else {
       uint32_t h[8], m[8], l[8];
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
   const int lane = threadIdx.x & 63;
   const int count = *g.count;
   if (n < g.slots) {
-    if (n >= (count + kRowTile - 1) / kRowTile * kRowTile) return;
+    if (n >= ((count > 1 ? count : 1) + kRowTile - 1) / kRowTile * kRowTile) return;
     const int64_t row = n < count ? g.rows[n] : -1;
     copy_row<T, P>(row >= 0 ? h + row * g.ldh : nullptr, g.C, g.Cp, g.to + n * g.pitch, g.plane);
     if (g.row_label != nullptr && lane == 0) {
@@ -1030,6 +1033,11 @@ struct Thin {
   float scale, inv_tau;
   float* z_label;
   Partial* partial;       // [groups][M]
+  // backward: the rows that count, with zero rows up to the tiles', and the gradient of their logits
+  const RowGrad* grad;
+  float* d;
+  int64_t d_ld;
+  int v0;                 // the table's first row, in the vocabulary
 };
 template <typename T>
 struct Run {   // 32 bytes of a row: 16, and 16 of 64 bytes further
@@ -1068,7 +1076,7 @@ __device__ inline floatx4 multiply(const Run<float>& y, const Run<float>& x, flo
   return c;
 }
 
-template <typename T, int XT, int YT, int WAVES, int AHEAD>
+template <typename T, int XT, int YT, int WAVES, int AHEAD, bool GRAD>
 __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
   constexpr int kRun = Run<T>::kElements, kStep = 4 * kRun;
   __shared__ floatx4 sums[WAVES][XT * YT][64];
@@ -1121,7 +1129,27 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
 #pragma unroll
       for (int j = 0; j < YT; ++j) sums[wave][i * YT + j][lane] = acc[i][j];
     __syncthreads();
-    if (wave < XT) {   // the wave's tile of rows: lane's row lane % 16, tokens 4 (lane / 16) + 0..3 of each tile of tokens
+    if (GRAD && wave < XT) {   // (the lanes' rows and tokens: see below)
+      const int row = 16 * wave + r;
+      const RowGrad k = a.grad[row];
+#pragma unroll
+      for (int j = 0; j < YT; ++j) {
+        const int at = wave * YT + j, col = v0 + 16 * j + 4 * g;
+        floatx4 v = sums[0][at][lane], d;
+#pragma unroll
+        for (int n = 1; n < WAVES; ++n) v += sums[n][at][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = v[e] * a.scale;
+          d[e] = __builtin_fmaf(k.a, exp_of(z - k.L), k.a0);
+          if (a.inv_tau != 1.0f) d[e] = __builtin_fmaf(k.at, exp_of(__builtin_fmaf(z, a.inv_tau, -k.Lt)), d[e]);
+          if (k.label >= 0 && col + e == k.label - a.v0) d[e] += k.ay;
+          if (row >= a.M || col + e >= a.V) d[e] = 0.0f;
+        }
+        *reinterpret_cast<floatx4*>(a.d + row * a.d_ld + col) = d;
+      }
+    }
+    if (!GRAD && wave < XT) {   // the wave's tile of rows: lane's row lane % 16, tokens 4 (lane / 16) + 0..3 of each tile of tokens
       const int row = 16 * wave + r;
       const int64_t label = a.labels != nullptr && row < a.M ? a.labels[row] : -1;
       float z[YT][4];
@@ -1161,7 +1189,182 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
     }
     __syncthreads();
   }
-  if (wave < XT && g == 0 && 16 * wave + r < a.M) a.partial[(int)blockIdx.x * a.M + 16 * wave + r] = all;
+  if (!GRAD && wave < XT && g == 0 && 16 * wave + r < a.M) a.partial[(int)blockIdx.x * a.M + 16 * wave + r] = all;
+}
+
+// Both gradients of up to 64 rows, from the gradient of their logits in fp32 and in fp32 throughout (matrix instructions of 16 x 16 x 4): bound by the table, which is
+// read, and its gradient, which is written.  A wave keeps 64 channels of h and of dh in its registers (128: 10 to 30 % slower, fewer waves fit) and goes along a share
+// of the tokens, 16 at a time: four neighbours of the channels are a lane's, in all its loads and stores.  The shares' sums of dh are joined by a launch of their own.
+// 2 x 2688 x 116480 fp32: 829 us with the logits' launch, 4.5 TB/s (three bf16 parts padded to 64 rows: 3437); 64 x 4096 x 65536: 1228 (2993); bf16, 7 x 5632 x 11705:
+// 121 us (156), 8 x 4096 x 131072: 1012 (1059).  With 17 to 64 rows of bf16 the products in bf16 are faster (32 x 2048 x 32768: 138 us, here 186; 64: 137, 324).
+struct ThinGrad {
+  const void *h, *W;          // h: the copy, with zeros up to the tiles' rows and whole 64 channels
+  int64_t ldh, ldw;
+  int M, C, n;                // n: tokens
+  const float* d;             // [rows][d_ld]: zeros behind the tokens up to a multiple of 16
+  int64_t d_ld;
+  int shares, per, more;      // per: tokens of a share, a multiple of 16; more: the slabs hold sums of earlier pieces
+  float* slabs;               // [shares][M][C]; nullptr: no dh
+  void* dW;                   // nullptr: none
+  int out_f32, accumulate;
+};
+// Four elements, n of which exist.
+__device__ inline floatx4 load_four(const float* p, int n) {
+  if (n >= 4) return *reinterpret_cast<const f32x4_any4*>(p);
+  floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < n) v[e] = p[e];
+  return v;
+}
+__device__ inline floatx4 load_four(const bf16_t* p, int n) {
+  if (n >= 4) {
+    const u32x2_any2 w = *reinterpret_cast<const u32x2_any2*>(p);
+    return floatx4{low_bf16(w[0]), high_bf16(w[0]), low_bf16(w[1]), high_bf16(w[1])};
+  }
+  floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < n) v[e] = (float)p[e];
+  return v;
+}
+__device__ inline void store_four(float* p, int n, floatx4 v) {
+  if (n >= 4) {
+    *reinterpret_cast<f32x4_any4*>(p) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+__device__ inline void store_four(bf16_t* p, int n, floatx4 v) {
+  if (n >= 4) {
+    *reinterpret_cast<u32x2_any2*>(p) = u32x2_any2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = (bf16_t)v[e];
+  }
+}
+template <typename T, int XT>
+__global__ __launch_bounds__(256, XT == 4 ? 1 : 2) void head_thin_grad_kernel(ThinGrad a) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int across = (a.C + 63) / 64;
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int share = (int)(id / across), c = (int)(id - (int64_t)share * across) * 64 + 4 * r;
+  if (share >= a.shares) return;
+  const int t0 = share * a.per, t1 = a.n - t0 < a.per ? a.n : t0 + a.per;
+  const T* W = (const T*)a.W + c;
+  floatx4 h[XT][4], dh[XT][4];   // h of row 16 x + 4 k + g; dh of rows 16 x + 4 g + 0..3 and channel c + e
+#pragma unroll
+  for (int x = 0; x < XT; ++x)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[x][k] = load_four((const T*)a.h + (16 * x + 4 * k + g) * a.ldh + c, 4);
+      dh[x][k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  if (a.more && a.slabs != nullptr) {
+#pragma unroll
+    for (int x = 0; x < XT; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = 16 * x + 4 * g + q;
+        const floatx4 v = load_four(a.slabs + ((int64_t)share * a.M + row) * a.C + c, row < a.M ? a.C - c : 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dh[x][e][q] = v[e];
+      }
+  }
+  floatx4 w[4], by_token[XT];
+  float by_row[XT][4];
+  auto load = [&](int t) __attribute__((always_inline)) {
+    if (a.slabs != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int v = t + 4 * g + u < a.n ? t + 4 * g + u : a.n - 1;   // (d is zero behind the last token)
+        w[u] = load_four(W + v * a.ldw, a.C - c);
+      }
+#pragma unroll
+      for (int x = 0; x < XT; ++x) by_token[x] = *reinterpret_cast<const floatx4*>(a.d + (16 * x + r) * a.d_ld + t + 4 * g);
+    }
+    if (a.dW != nullptr) {
+#pragma unroll
+      for (int x = 0; x < XT; ++x)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) by_row[x][k] = a.d[(16 * x + 4 * k + g) * a.d_ld + t + r];
+    }
+  };
+  if (t0 < t1) load(t0);
+  for (int t = t0; t < t1; t += 16) {
+    floatx4 v[4], bt[XT];
+    float br[XT][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = w[u];
+#pragma unroll
+    for (int x = 0; x < XT; ++x) {
+      bt[x] = by_token[x];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) br[x][k] = by_row[x][k];
+    }
+    if (t + 16 < t1) load(t + 16);   // on the way while these are multiplied
+    if (a.slabs != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int x = 0; x < XT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dh[x][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(bt[x][u], v[u][e], dh[x][e], 0, 0, 0);
+    }
+    if (a.dW == nullptr) continue;
+    floatx4 dw[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dw[e] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int x = 0; x < XT; ++x)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dw[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(br[x][k], h[x][k][e], dw[e], 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int token = t + 4 * g + q, n = token < a.n ? a.C - c : 0;
+      floatx4 o{dw[0][q], dw[1][q], dw[2][q], dw[3][q]};
+      auto put = [&](auto* to) __attribute__((always_inline)) {
+        if (a.accumulate) o += load_four(to, n);
+        store_four(to, n, o);
+      };
+      if (a.out_f32)
+        put((float*)a.dW + (int64_t)token * a.C + c);
+      else
+        put((bf16_t*)a.dW + (int64_t)token * a.C + c);
+    }
+  }
+  if (a.slabs == nullptr) return;
+#pragma unroll
+  for (int x = 0; x < XT; ++x)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = 16 * x + 4 * g + q;
+      store_four(a.slabs + ((int64_t)share * a.M + row) * a.C + c, row < a.M ? a.C - c : 0, floatx4{dh[x][0][q], dh[x][1][q], dh[x][2][q], dh[x][3][q]});
+    }
+}
+// dh of a row: the shares' sums, 64 channels a block, a quarter of the shares a wave.
+__global__ __launch_bounds__(256) void head_thin_sum_kernel(ThinGrad a, const int* __restrict__ rows, const int* __restrict__ count, void* dh, int64_t ld, int f32) {
+  __shared__ float joined[4][64];
+  const int x = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 64 + lane;
+  if (x >= *count) return;
+  float v = 0.0f;
+  if (c < a.C)
+#pragma unroll 8
+    for (int i = wave; i < a.shares; i += 4) v += a.slabs[((int64_t)i * a.M + x) * a.C + c];
+  joined[wave][lane] = v;
+  __syncthreads();
+  if (wave != 0 || c >= a.C) return;
+  v = (joined[0][lane] + joined[1][lane]) + (joined[2][lane] + joined[3][lane]);
+  const int64_t at = rows[x] * ld + c;
+  if (f32)
+    ((float*)dh)[at] = v;
+  else
+    ((bf16_t*)dh)[at] = (bf16_t)v;
 }
 
 __device__ inline float wave_max(float v) {
@@ -1317,7 +1520,10 @@ __device__ inline void put_entry_grad(const Entries& a, const RowGrad& g, int n,
   float v = __builtin_fmaf(g.a, exp_of(z - g.L), g.a0);
   v = __builtin_fmaf(g.at, (a.inv_tau != 1.0f ? exp_of(__builtin_fmaf(z, a.inv_tau, -g.Lt)) : 0.0f) - p, v);
   if (id == g.label) v += g.ay;
-  put_parts(a.d + n * a.d_pitch + (id - a.v0) * 2, a.d_plane, a.d_parts, v);
+  if (a.d_parts == 0)   // (fp32)
+    ((float*)(a.d + n * a.d_pitch))[id - a.v0] = v;
+  else
+    put_parts(a.d + n * a.d_pitch + (id - a.v0) * 2, a.d_plane, a.d_parts, v);
 }
 __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -1370,7 +1576,7 @@ inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int64_t kSlabBytes = (int64_t)128 << 20, kFewLogits = (int64_t)16 << 20;
 constexpr int kTile = 128;
-constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64;
+constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64, kThinWaves = 4096, kThinShares = 256;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
 // Bytes of the workspace's parts.  A piece's gradient of the logits, a part: what stays in the last-level cache (256 MB) beside the piece's rows of the table until the
 // products have read it, or twice that where it is all there is (8192 x 4096 x 65536: 10.2 ms with 128 MB, 10.5 with 256, 10.3 with 512; 3277 x 2048 x
@@ -1544,7 +1750,7 @@ struct Call {
   const Plan& q;
   hipStream_t st;
   char* ws;
-  bool copied;
+  bool copied, few = false;   // few: rows as they are, up to kThinRows
 
   int prepare(bool backward, Operand& h) const {
     const abl_head& p = c.p;
@@ -1563,6 +1769,12 @@ struct Call {
     g.scale = p.scale, g.smoothing = p.smoothing, g.z_weight = p.z_weight, g.tau = p.temperature, g.label_weight = p.label_weight;
     g.teacher_weight = p.teacher_weight;
     if (int e = hip_status()) return e;
+    if (few) {
+      g.slots = kThinRows;
+      if (p.dtype == ABL_BF16) return gather<bf16_t, 1>(st, g, c.h.p, true);
+      g.pitch = q.Cp * 4 + kPad;
+      return gather<float, 0>(st, g, c.h.p, true);
+    }
     h = {g.to, g.plane, q.c_pitch, (int)q.Mp, (int)q.Cp};
     if (p.dtype == ABL_BF16) return gather<bf16_t, 1>(st, g, c.h.p, true);
     return q.parts == 3 ? gather<float, 3>(st, g, c.h.p, true) : gather<float, 1>(st, g, c.h.p, true);
@@ -1613,7 +1825,7 @@ int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
   const int tiles = (p.V + 16 * YT - 1) / (16 * YT);
   Thin a{c.h.p, c.W.p, c.h.ld, c.W.ld, (int)p.M, p.C, p.V, tiles < kThinGroups ? tiles : kThinGroups, c.labels, p.scale, 1.0f / p.temperature,
          (float*)(ws + q.z_label), (Partial*)(ws + q.partial)};
-  head_thin_kernel<T, XT, YT, WAVES, AHEAD><<<(unsigned)a.groups, WAVES * 64, 0, st>>>(a);
+  head_thin_kernel<T, XT, YT, WAVES, AHEAD, false><<<(unsigned)a.groups, WAVES * 64, 0, st>>>(a);
   Loss l = loss_of(c, q, ws);
   l.tiles = a.groups, l.partial_ld = p.M, l.entries = entry_logits(c, q);
   head_loss_kernel<1><<<(unsigned)p.M, 1024, 0, st>>>(l);
@@ -1704,6 +1916,63 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
   return ABL_OK;
 }
 
+namespace {
+
+void launch_entry_grad(hipStream_t st, const HeadCall& c, const Plan& q, char* ws, int64_t v0, int64_t n, const Operand& d, int d_parts) {
+  const abl_head& p = c.p;
+  Entries a{};
+  a.rows = (const int*)(ws + q.rows), a.count = (const int*)(ws + q.count), a.ids = c.ids, a.logits = c.logits, a.z_top = c.in_z_top;
+  a.grad = (const RowGrad*)(ws + q.grad), a.T = p.T;
+  a.v0 = (int)v0, a.v1 = (int)(v0 + n), a.inv_tau = 1.0f / p.temperature, a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch;
+  a.d_parts = d_parts;
+  head_entry_grad_kernel<<<(unsigned)((p.M + 3) / 4), 256, 0, st>>>(a);
+}
+
+// Few rows: the gradient of a piece's logits in fp32, then both products of it.
+template <typename T, int XT, int YT, int WAVES, int AHEAD>
+int launch_thin_backward(hipStream_t st, const HeadCall& c, char* ws) {
+  const abl_head& p = c.p;
+  const Plan q = plan_of(p, true, false, false);
+  const Call call{c, q, st, ws, false, true};
+  Operand none;
+  if (int e = call.prepare(true, none)) return e;
+  const int64_t pitch = sizeof(T) == 4 ? q.Cp * 4 + kPad : q.c_pitch, d_ld = q.piece;
+  const int across = (p.C + 63) / 64;
+  ThinGrad a{};
+  a.h = ws + q.h, a.ldh = pitch / (int64_t)sizeof(T), a.ldw = c.W.ld, a.M = (int)p.M, a.C = p.C, a.d = (const float*)(ws + q.d), a.d_ld = d_ld;
+  a.slabs = c.dh.p != nullptr ? (float*)(ws + q.slabs) : nullptr, a.out_f32 = p.dw_dtype == ABL_F32, a.accumulate = (p.flags & ABL_ACCUM_DW) != 0;
+  // Shares: as many as make enough waves (of 16 rows 2048 in all: 140 us instead of 121 for 7 x 5632 x 11705 bf16; 8192: 124).
+  int64_t shares = kThinWaves / XT / across;   // (of 64 rows one wave fits a SIMD: not one more than there are)
+  const int64_t fit = q.slab_bytes / ((int64_t)p.M * p.C * 4), of_tokens = (q.piece + 31) / 32;
+  shares = shares < kThinShares ? shares : kThinShares;
+  shares = shares < fit ? shares : fit;
+  shares = shares < of_tokens ? shares : of_tokens;
+  if (shares < 1) shares = 1;
+  a.per = (int)up((q.piece + shares - 1) / shares, 16);
+  a.shares = (int)((q.piece + a.per - 1) / a.per);
+  for (int i = 0; i < q.pieces; ++i) {
+    const int64_t v0 = i * q.piece, n = v0 + q.piece < p.V ? q.piece : p.V - v0;
+    const int tiles = (int)((n + 16 * YT - 1) / (16 * YT));
+    Thin t{};
+    t.h = a.h, t.W = (const T*)c.W.p + v0 * c.W.ld, t.ldh = a.ldh, t.ldw = c.W.ld, t.M = 16 * XT, t.C = p.C, t.V = (int)n;
+    t.groups = tiles < kThinGroups ? tiles : kThinGroups, t.scale = p.scale, t.inv_tau = 1.0f / p.temperature;
+    t.grad = (const RowGrad*)(ws + q.grad), t.d = (float*)(ws + q.d), t.d_ld = d_ld, t.v0 = (int)v0;
+    head_thin_kernel<T, XT, YT, WAVES, AHEAD, true><<<(unsigned)t.groups, WAVES * 64, 0, st>>>(t);
+    if (c.ids != nullptr) launch_entry_grad(st, c, q, ws, v0, n, Operand{nullptr, 0, d_ld * 4, 0, 0}, 0);
+    a.W = t.W, a.n = (int)n, a.more = i > 0, a.dW = c.dW != nullptr ? (char*)c.dW + v0 * p.C * size_of(p.dw_dtype) : nullptr;
+    head_thin_grad_kernel<T, XT><<<(unsigned)(((int64_t)a.shares * across + 3) / 4), 256, 0, st>>>(a);
+    if (int e = hip_status()) return e;
+  }
+  if (c.dh.p != nullptr)
+    head_thin_sum_kernel<<<dim3((unsigned)p.M, (unsigned)((p.C + 63) / 64)), 256, 0, st>>>(a, (const int*)(ws + q.rows), (const int*)(ws + q.count), c.dh.p, c.dh.ld,
+                                                                                      p.dtype == ABL_F32);
+  return hip_status();
+}
+// (fp32 with ABL_MATH_BF16 rounds its operands: not here.)
+bool thin_backward(const abl_head& p) { return p.dtype == ABL_F32 ? p.M <= kThinRows && !(p.flags & ABL_MATH_BF16) : p.M <= 16; }
+
+}  // namespace
+
 int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
   const abl_head& p = c.p;
   const bool accumulate = (p.flags & ABL_ACCUM_DW) != 0;
@@ -1712,6 +1981,12 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
     const int64_t n = (int64_t)p.V * p.C * (size_of(p.dw_dtype) / 2);
     head_zero_kernel<<<(unsigned)(n < 1 << 20 ? (n + 255) / 256 : 4096), 256, 0, st>>>((uint16_t*)c.dW, n);
     return hip_status();
+  }
+  if (thin_backward(p)) {
+    char* ws = (char*)scratch;
+    if (p.dtype == ABL_BF16) return launch_thin_backward<bf16_t, 1, 1, 8, 4>(st, c, ws);
+    if (p.M <= 16) return launch_thin_backward<float, 1, 1, 8, 4>(st, c, ws);
+    return p.M <= 32 ? launch_thin_backward<float, 2, 2, 4, 2>(st, c, ws) : launch_thin_backward<float, 4, 2, 4, 2>(st, c, ws);
   }
   const bool copied = !in_place(c);
   const Plan q = plan_of(p, true, copied, false);
@@ -1742,11 +2017,7 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
       }
     }
     if (c.ids != nullptr) {
-      Entries a{};
-      a.rows = rows, a.count = count, a.ids = c.ids, a.logits = c.logits, a.z_top = c.in_z_top, a.grad = (const RowGrad*)(ws + q.grad), a.T = p.T;
-      a.v0 = (int)v0, a.v1 = (int)(v0 + n), a.inv_tau = 1.0f / p.temperature, a.d = ws + q.d, a.d_plane = d.plane, a.d_pitch = d.pitch;
-      a.d_parts = q.d_parts;
-      head_entry_grad_kernel<<<(unsigned)((p.M + 3) / 4), 256, 0, st>>>(a);
+      launch_entry_grad(st, c, q, ws, v0, n, d, q.d_parts);
       if (int e = hip_status()) return e;
     }
     if (c.dh.p != nullptr) {

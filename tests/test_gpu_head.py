@@ -251,6 +251,30 @@ def test_few_rows_of_a_large_vocabulary(type, M, C, V, T):
     Case(M, C, V, type, T=T).check()
 
 
+@pytest.mark.parametrize("type,dw", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("M,C,V,T", [(1, 5, 700, 0), (15, 63, 1000, 3), (16, 129, 33, 0), (17, 70, 2500, 5), (31, 257, 600, 0), (49, 100, 1300, 2), (64, 66, 17, 2)])
+def test_gradients_of_few_rows(type, dw, M, C, V, T):
+    how = dict(temperature=2.0, label_weight=0.5, z_weight=1e-3) if T else dict(smoothing=0.1, scale=0.5)
+    c = Case(M, C, V, type, T=T, pitch=(3, 5), offset=1, **how)
+    c.forward()
+    before = torch.randn(V, C, generator=torch.Generator().manual_seed(2)).to(dw)
+    dh, dW = c.backward(dw)
+    only_h, none = c.backward(dw, want=(True, False))
+    nothing, only_W = c.backward(dw, want=(False, True))
+    _, added = c.backward(dw, flags=B.ABL_ACCUM_DW, dW=before.cuda())
+    want = c.reference(dw)
+    R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+    assert torch.equal(only_h, dh) and torch.equal(only_W, dW) and none is None and nothing is None
+    half = torch.finfo(dw).eps / 2
+    R.assert_within(added, want["dW"] + before.double(), want["bound"]["dW"] + half * (want["dW"] + before.double()).abs() * 1.01, "dW")
+
+
+@pytest.mark.parametrize("type,M,C,V,T", [(BF16, 3, 9, 600001, 0), (F32, 20, 5, 530000, 4), (BF16, 16, 24, 1100000, 0)])
+def test_few_rows_of_many_pieces(type, M, C, V, T):
+    Case(M, C, V, type, T=T).check()
+
+
 @pytest.mark.parametrize("type", [F32, BF16])
 @pytest.mark.parametrize("M", [3, 40])
 def test_small_losses_of_few_rows(type, M):
