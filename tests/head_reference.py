@@ -100,8 +100,8 @@ def backward(h, W, labels, lse, dloss, n, type, dw_type, one_part=False, ids=Non
     w = torch.where(counts, w, zero)[:, None]
     d, size = d * w, size * w.abs() + 4 * F32 * (d * w).abs()
     # the gradient of the logits in parts of 8 bits, each rounded
-    parts = 1 if one_part else 3 if type == torch.float32 else 2 if dw_type == torch.float32 else 1
-    lost = {1: B16, 2: B16 ** 2, 3: B16 ** 3}
+    parts = 1 if one_part else 3 if torch.float32 in (type, dw_type) else 1
+    lost = {1: B16, 3: B16 ** 3}
     ed_h = size + lost[1 if type == torch.bfloat16 else parts] * d.abs()
     ed_w = size + lost[parts] * d.abs()
     dh, dW = d @ W, d.t() @ h
