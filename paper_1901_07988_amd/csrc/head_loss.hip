@@ -59,7 +59,8 @@ __global__ __launch_bounds__(256) void head_flags_kernel(int64_t M, const int64_
   if ((threadIdx.x & 63) == 0) flags[row] = (unsigned char)f;
 }
 
-// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, and their number: one block.
+// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, and their number: one block (8192 rows: 6 us; places
+// by atomics would change from call to call, and with them the order of the sums).
 __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_t* __restrict__ labels, const unsigned char* __restrict__ flags,
                                                          int* __restrict__ rows, int* __restrict__ count) {
   __shared__ int sums[17];
@@ -191,7 +192,8 @@ struct Gather {
   float scale, smoothing, z_weight, tau, label_weight, teacher_weight;
 };
 
-// The rows that count to their places, with their coefficients (backward), then - blocks of their own - zeros for the rows that do not.
+// The rows that count to their places, with their coefficients (backward), then - blocks of their own - zeros for the rows that do not.  Bound by memory
+// (8192 x 4096 bf16: 25 us, 5.4 TB/s); a wave a row.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __restrict__ h) {
   const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -512,6 +514,8 @@ __device__ inline Partial lanes_joined(Partial p, float inv_tau) {   // of the w
   return p;
 }
 
+// Bound by the matrix cores: 8192 x 4096 x 65536 logits take 3.3 ms, 1.3 PFLOP/s (the library's plain product of this size 3.26 ms), the matrix cores busy in 60 to
+// 66 % of the cycles at 1.9 GHz; a step of 256 x 256 x 64 takes 1.47 us, a tile 7 to 10 us beside its steps.  LDS reads meet no bank twice (counted).
 // A block has a tile of BX x BY, WX x WY waves a part of it each.  Steps of 64 k's: their operands go from memory straight to one of PLACES in
 // LDS, PLACES - 1/2 steps ahead, and from there to registers half a step ahead, all between matrix instructions.  FEW: x may be a user's rows as they are.
 template <int BX, int BY, int WX, int WY, int PLACES, bool XO, bool YO, int EPI, bool FEW>
@@ -814,7 +818,7 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
   }
 }
 
-// The shares' slabs of a product, added in turn: a wave takes 256 columns of a row.
+// The shares' slabs of a product, added in turn: a wave takes 256 columns of a row.  Bound by memory (2867 x 2048, two slabs and what earlier pieces left: 30 us).
 __global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by) {
   const int count = a.count != nullptr ? *a.count : 0;
   const int nx = a.count != nullptr && !a.count_k ? count : a.nx, nk = a.count != nullptr && a.count_k ? count : a.k;
@@ -862,7 +866,8 @@ __global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by
 }
 
 // ---- few tiles of logits --------------------------------------------------------------------------------
-// Where the logits are few tiles of many k's, their product, too, is cut into shares, and these launches take the place of its epilogues.
+// Where the logits are few tiles of many k's, their product, too, is cut into shares, and these launches take the place of its epilogues.  Taken where the fit says a quarter
+// of the time, and 5 us, at least: closer calls went either way.
 constexpr int kSlabColumns = 1024;   // of a block: four a thread, 256 apart, all shares' loads on the way together
 struct Slabs {
   const float* p;
@@ -966,7 +971,7 @@ __device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
   if (lane == 0) a.z_top[at] = s * a.scale;
 }
 // Four waves a row that counts.  A wave takes two entries at a time, their rows of the table on the way together: rows from anywhere in a table that
-// no cache holds.
+// no cache holds (2867 rows, 32 entries of 4 KB each: 59 us, 6.4 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const int* __restrict__ rows, const int* __restrict__ count) {
   if ((int)blockIdx.x >= *count) return;
@@ -1014,7 +1019,8 @@ __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const 
 // ---- few rows -------------------------------------------------------------------------------------------
 // Logits of up to 64 rows: bound by the table, which is read once, straight into registers.  A block takes 16 YT tokens at a time, its four waves a quarter of
 // the channels each, so that a small table, too, is many waves' work; rows come from the caches again and again.  A lane's 32 bytes of a row are
-// its operands of two matrix instructions (bf16) or eight (fp32, exact): which k they stand for does not matter as long as both sides agree.
+// its operands of two matrix instructions (bf16) or eight (fp32, exact): which k they stand for does not matter as long as both sides agree.  fp32 2 x 2688 x 116480:
+// 240 us with the second launch, 5.2 TB/s; 64 x 4096 x 65536: 450, the fp32 instructions' rate.
 struct Thin {
   const void *h, *W;
   int64_t ldh, ldw;
@@ -1376,8 +1382,9 @@ __device__ inline void teacher_sums(const int64_t* ids, const float* logits, int
   sum = wave_sum(sum);
 }
 
-// The tiles' sums of each row, joined, and its loss: a block of 1024 threads takes ROWS of them (16, or one where there are few), a wave each at the end.  Without a list of rows (rows = nullptr) all M of them are
-// there, and those that do not count get zeros here.
+// The tiles' sums of each row, joined, and its loss: a block of 1024 threads takes ROWS of them (16, or one where there are few), a wave each at the end.
+// Without a list of rows (rows = nullptr) all M of them are there, and those that do not count get zeros here.  16 rows read whole 256 bytes of a tile's sums (8192 rows, 256 tiles: 14 us); for few rows the time is the
+// chain of loads, sums and logarithms of a launch (one row: 4 us), and with a teacher its entries' rows of the table (16 rows of 8: 9 us).
 struct Loss {
   int M;
   const Partial* partial;
@@ -1599,7 +1606,9 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
     return n < 256 ? 256 : n < all ? n : all;
   };
   const int64_t grad_token = q.Mp * 2 * q.d_parts;
-  int64_t piece = backward ? within(all * grad_token <= 2 * kGradBytes * q.d_parts ? 2 * kGradBytes * q.d_parts : kGradBytes * q.d_parts, grad_token) : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
+  const int64_t once = 2 * kGradBytes * q.d_parts;
+  int64_t piece = backward ? within(all * grad_token <= once ? once : once / 2, grad_token)
+                           : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
   if (piece > 1 << 20) piece = 1 << 20;
   const int64_t table = within(kTableBytes, q.Cp * 2 * q.parts);
   const int64_t widest = piece;
@@ -1663,12 +1672,15 @@ int launch_tiles(hipStream_t st, const Product& a) {
   return hip_status();
 }
 
-// Tiles of 256 x 256, 256 x 128, 128 x 128 or 64 x 64, whichever takes the least time for the rows that a call has.
+// Tiles of 256 x 256, 256 x 128, 128 x 128 or 64 x 64, whichever takes the least time for the rows that a call has, by a fit of measured times.  Large tiles read their operands
+// less often, small ones fill the units of a small call: bf16 logits of 2048 x 1024 x 8192 in tiles of 256 x 256 50 us, 128 x 128 71, 64 x 64 95; of 100 x 1024 x 3000
+// 128 x 128 25.1 us, 64 x 64 20.6; gradients of 130 x 2048 x 1000 47 and 37, of 1000 x 2048 x 2000 75 and 80.
 struct Tiling {
   int bx, by;
   Split split;
 };
-constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}}, {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 512, 500, 4500, 4000, 800}}};
+constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}},
+                                {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 512, 500, 4500, 4000, 800}}};
 int64_t tiles_of(const Tiling& t, int64_t nx, int64_t ny) { return (nx + t.bx - 1) / t.bx * ((ny + t.by - 1) / t.by); }
 int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
   const int n = shares_of(s, tiles, steps, size);
