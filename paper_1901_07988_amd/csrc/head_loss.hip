@@ -1020,7 +1020,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const 
 // Logits of up to 64 rows: bound by the table, which is read once, straight into registers.  A block takes 16 YT tokens at a time, its four waves a quarter of
 // the channels each, so that a small table, too, is many waves' work; rows come from the caches again and again.  A lane's 32 bytes of a row are
 // its operands of two matrix instructions (bf16) or eight (fp32, exact): which k they stand for does not matter as long as both sides agree.  fp32 2 x 2688 x 116480:
-// 240 us with the second launch, 5.2 TB/s; 64 x 4096 x 65536: 450, the fp32 instructions' rate.
+// 240 us with the second launch, 5.2 TB/s; 48 x 2048 x 32768: 101 (as 64 rows 118); 64 x 4096 x 65536: 450, the fp32 instructions' rate.
 struct Thin {
   const void *h, *W;
   int64_t ldh, ldw;
@@ -1863,7 +1863,8 @@ template <typename T>
 int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
   if (std::is_same_v<T, bf16_t> && thin_in_place(c)) return launch_thin_product(st, c, q, ws);
   if (c.p.M <= 16) return launch_thin<T, 1, 1, 8, 4>(st, c, q, ws);
-  return c.p.M <= 32 ? launch_thin<T, 2, 2, 4, 2>(st, c, q, ws) : launch_thin<T, 4, 2, 4, 2>(st, c, q, ws);
+  if (c.p.M <= 32) return launch_thin<T, 2, 2, 4, 2>(st, c, q, ws);
+  return c.p.M <= 48 ? launch_thin<T, 3, 2, 4, 2>(st, c, q, ws) : launch_thin<T, 4, 2, 4, 2>(st, c, q, ws);
 }
 
 }  // namespace

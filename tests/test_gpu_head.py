@@ -265,7 +265,8 @@ def test_gradients_of_few_rows(type, dw, M, C, V, T):
     want = c.reference(dw)
     R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
     R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
-    assert torch.equal(only_h, dh) and torch.equal(only_W, dW) and none is None and nothing is None
+    over, _ = c.backward(dw, dh=c.dh_in, want=(True, False))
+    assert torch.equal(only_h, dh) and torch.equal(over, dh) and torch.equal(only_W, dW) and none is None and nothing is None
     half = torch.finfo(dw).eps / 2
     R.assert_within(added, want["dW"] + before.double(), want["bound"]["dW"] + half * (want["dW"] + before.double()).abs() * 1.01, "dW")
 
