@@ -276,6 +276,49 @@ def test_few_rows_of_many_pieces(type, M, C, V, T):
     Case(M, C, V, type, T=T).check()
 
 
+@pytest.mark.parametrize("M", [3, 70])
+def test_a_table_beyond_four_gigabytes(M):
+    """bf16, 561003 x 4096: the reference on the GPU in 64 bits, a piece of the table at a time, with the bounds of head_reference.py."""
+    C, V, step = 4096, 561003, 33000
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    W = torch.empty(V, C, dtype=BF16, device="cuda")
+    for v in range(0, V, step):
+        W[v: v + step] = torch.randn(min(step, V - v), C, generator=gen, device="cuda") * C ** -0.5
+    h = (torch.randn(M, C, generator=gen, device="cuda") * 2).to(BF16)
+    labels = torch.randint(0, V, (M,), generator=gen, device="cuda")
+    labels[0] = V - 1
+    dloss = torch.randn(M, generator=gen, device="cuda")
+    loss, lse = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    dh, dW = torch.empty_like(h), torch.full((V, C), 7.0, dtype=BF16, device="cuda")
+    B.abl_xent_forward(h, W, labels, scratch_for(M, C, V, BF16), loss, lse)
+    B.abl_xent_backward(h, W, labels, lse, dloss, scratch_for(M, C, V, BF16, dw=BF16, backward=True), dh, dW)
+    x, w = h.double(), dloss.double()[:, None]
+    pieces = [(v, min(v + step, V)) for v in range(0, V, step)]
+    z = torch.cat([x @ W[a:b].double().t() for a, b in pieces], 1)
+    ez = (C + 70) * R.F32 * torch.cat([x.abs() @ W[a:b].double().abs().t() for a, b in pieces], 1)
+    L, zy = torch.logsumexp(z, 1), z.gather(1, labels[:, None])[:, 0]
+    eL = ez.amax(1) + (V / 64 + 300) * R.F32 + 4 * R.F32 * L.abs() + 2.0 ** -18 + 2.0 ** -20
+    R.assert_within(lse, L.cpu(), eL.cpu(), "lse")
+    R.assert_within(loss, (L - zy).cpu(), (2 * eL + 8 * R.F32 * (L.abs() + z.abs().amax(1))).cpu(), "loss")
+    off = z - lse.double()[:, None]
+    q = torch.exp(off)
+    d = q.clone()
+    d[torch.arange(M, device="cuda"), labels] -= 1
+    ed = (q * (ez + 2.0 ** -20 + 4 * R.F32 * off.abs()) + 8 * R.F32 * (d.abs() + q) + R.B16 * d.abs()) * w.abs()
+    d = d * w
+    want, bound = torch.zeros_like(x), torch.zeros_like(x)
+    for a, b in pieces:
+        Wd = W[a:b].double()
+        want += d[:, a:b] @ Wd
+        bound += (ed[:, a:b] + (V + 70) * R.F32 * d[:, a:b].abs()) @ Wd.abs()
+    R.assert_within(dh, want.cpu(), (1.01 * (bound + R.B16 * want.abs())).cpu(), "dh")
+    for a, b in (pieces[0], pieces[-1]):
+        want = d[:, a:b].t() @ x
+        bound = (ed[:, a:b] + (M + 70) * R.F32 * d[:, a:b].abs()).t() @ x.abs() + R.B16 * want.abs()
+        R.assert_within(dW[a:b], want.cpu(), (1.01 * bound + 1e-37).cpu(), "dW")
+    assert not bool((dW == 7.0).all(1).any())
+
+
 @pytest.mark.parametrize("type", [F32, BF16])
 @pytest.mark.parametrize("M", [3, 40])
 def test_small_losses_of_few_rows(type, M):
