@@ -1572,7 +1572,9 @@ __global__ __launch_bounds__(256) void head_zero_kernel(uint16_t* p, int64_t n) 
 inline int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int64_t kSlabBytes = (int64_t)128 << 20, kFewLogits = (int64_t)16 << 20;
-constexpr int kTile = 128;
+// Columns of the narrowest tile that leaves its rows' sums of the logits: 64 up to kNarrowRows rows.
+constexpr int kNarrowRows = 1024;
+inline int narrowest(int64_t rows) { return rows <= kNarrowRows ? 64 : 128; }
 constexpr int kThinRows = 64, kThinGroups = 1024, kThinTile = 64, kThinWaves = 4096, kThinShares = 256;
 constexpr int64_t kPad = 128;   // bytes behind a row of a copy: rows a power of two apart meet in few channels of the L2
 // Bytes of the workspace's parts.  A piece's gradient of the logits, a part: what stays in the last-level cache (256 MB) beside the piece's rows of the table until the
@@ -1608,7 +1610,7 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   const int64_t grad_token = q.Mp * 2 * q.d_parts;
   const int64_t once = 2 * kGradBytes * q.d_parts;
   int64_t piece = backward ? within(all * grad_token <= once ? once : once / 2, grad_token)
-                           : within(kPartialBytes, (q.Mp * (int64_t)sizeof(Partial) + kTile - 1) / kTile);
+                           : within(kPartialBytes, q.Mp * (int64_t)sizeof(Partial) / narrowest(q.Mp));
   if (piece > 1 << 20) piece = 1 << 20;
   const int64_t table = within(kTableBytes, q.Cp * 2 * q.parts);
   const int64_t widest = piece;
@@ -1633,7 +1635,7 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   q.h = take(q.Mp * q.c_pitch * q.parts);
   q.table = copied || most ? (table < held ? table : held) : 0;
   q.W = take(q.table * q.c_pitch * q.parts);
-  int64_t sums = held / kTile * q.Mp;
+  int64_t sums = held / narrowest(q.Mp) * q.Mp;
   if (p.M <= kThinRows) {
     const int64_t few = (int64_t)((p.V + kThinTile - 1) / kThinTile > kThinGroups ? (p.V + kThinTile - 1) / kThinTile : kThinGroups) * kThinRows;
     sums = sums > few ? sums : few;
@@ -1681,6 +1683,9 @@ struct Tiling {
 };
 constexpr Tiling kTilings[4] = {{256, 256, {8, 256, 1600, 8000, 4000, 800}}, {256, 128, {8, 256, 950, 6000, 4000, 800}},
                                 {128, 128, {8, 256, 800, 5000, 4000, 800}}, {64, 64, {8, 512, 500, 4500, 4000, 800}}};
+// The first so many of them have columns enough for the room that a workspace has for the sums.
+inline int tilings_for_sums(int64_t rows) { return narrowest(rows) == 64 ? 4 : 3; }
+static_assert(kTilings[0].by >= 128 && kTilings[1].by >= 128 && kTilings[2].by >= 128 && kTilings[3].by >= 64 && kSlabColumns >= 128 && kNarrowRows % kRowTile == 0);
 int64_t tiles_of(const Tiling& t, int64_t nx, int64_t ny) { return (nx + t.bx - 1) / t.bx * ((ny + t.by - 1) / t.by); }
 int64_t time_of(const Split& s, int64_t tiles, int steps, int64_t size) {
   const int n = shares_of(s, tiles, steps, size);
@@ -1692,12 +1697,12 @@ struct Choice {
   int64_t time;
 };
 // The rows that count, of which there may be fewer, are k (count_k) or nx.
-Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k) {
+Choice choice_of(int64_t nx, int64_t ny, int64_t k, int parts, bool sums, int64_t slab_bytes, bool count_k, int tilings = 4) {
   const int64_t size = nx * ny, fit = slab_bytes / (size * 4);
   const int steps = (int)((k + 63) / 64 * parts);
   Choice c{};
   int64_t least = 0;
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < tilings; ++i) {
     Split s = kTilings[i].split;
     s.most = !sums || fit < 2 ? 1 : fit < 8 ? (int)fit : 8;
     const int64_t time = time_of(s, tiles_of(kTilings[i], nx, ny), steps, size);
@@ -1731,7 +1736,7 @@ int launch_slabs(hipStream_t st, Product& a, const Choice& c, float* slabs) {
 // (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
 template <bool XO, bool YO, int EPI>
 int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
-  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0);
+  const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0, EPI == kEpiPartial ? tilings_for_sums(a.nx) : 4);
   a.split = c.split, a.slabs = slabs;
   return launch_tiling<XO, YO, EPI>(st, a, c.tiling);
 }
@@ -1909,7 +1914,7 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
       head_slab_partial_kernel<<<dim3((unsigned)p.M, (unsigned)((n + kSlabColumns - 1) / kSlabColumns)), 256, 0, st>>>(a, t.bx, t.by);
       columns = kSlabColumns;
     } else {
-      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false).tiling].by;
+      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, tilings_for_sums(a.nx)).tiling].by;
       if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
     }
     Loss l = loss_of(c, q, ws);

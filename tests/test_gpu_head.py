@@ -276,6 +276,19 @@ def test_few_rows_of_many_pieces(type, M, C, V, T):
     Case(M, C, V, type, T=T).check()
 
 
+@pytest.mark.parametrize("M,C,V,type,T", [(103, 588, 118445, F32, 11), (70, 64, 100000, BF16, 0), (1000, 64, 20000, BF16, 3), (1100, 40, 20000, F32, 0), (1500, 64, 9000, BF16, 2)])
+def test_sums_of_narrow_tiles(M, C, V, type, T):
+    """Nothing is written behind a workspace, and the sums of a piece's tiles fit before what earlier pieces left."""
+    c = Case(M, C, V, type, T=T)
+    n = [B.abl_head_scratch_bytes(M, C, V, type, T=T, dw_dtype=type if b else None, backward=b) for b in (False, True)]
+    rooms = [torch.full((k + (1 << 22),), 0xAB, dtype=torch.uint8, device="cuda") for k in n]
+    got, want = c.forward(scratch=rooms[0][: n[0]]), R.forward(c.h, c.W, c.labels, c.n, c.ids, c.t)
+    for k in got:
+        R.assert_within(got[k], want[k], want["bound"][k], k)
+    c.backward(scratch=rooms[1][: n[1]])
+    assert all(bool((room[k:] == 0xAB).all()) for room, k in zip(rooms, n))
+
+
 @pytest.mark.parametrize("M", [3, 70])
 def test_a_table_beyond_four_gigabytes(M):
     """bf16, 561003 x 4096: the reference on the GPU in 64 bits, a piece of the table at a time, with the bounds of head_reference.py."""
@@ -434,15 +447,16 @@ def test_results_repeat(type, T):
         assert all(torch.equal(out[k], again[k]) for k in out) and torch.equal(a, dh) and torch.equal(b, dW)
 
 
+@pytest.mark.parametrize("M", [150, 12])
 @pytest.mark.parametrize("T", [0, 4])
-def test_side_stream_and_captured(T):
+def test_side_stream_and_captured(T, M):
     """On a stream of its own and captured: new inputs in place, other rows counting, replays between eager calls."""
-    c = Case(150, 96, 300, BF16, T=T)
+    c = Case(M, 96, 300, BF16, T=T)
     c.forward()
-    ws, wb = scratch_for(150, 96, 300, BF16, T), scratch_for(150, 96, 300, BF16, T, None, True)
-    g = torch.randn(150, device="cuda")
+    ws, wb = scratch_for(M, 96, 300, BF16, T), scratch_for(M, 96, 300, BF16, T, None, True)
+    g = torch.randn(M, device="cuda")
     out = {k: torch.empty_like(v) for k, v in c.out.items()}
-    dh, dW = torch.empty(150, 96, dtype=BF16, device="cuda"), torch.empty(300, 96, dtype=BF16, device="cuda")
+    dh, dW = torch.empty(M, 96, dtype=BF16, device="cuda"), torch.empty(300, 96, dtype=BF16, device="cuda")
 
     def step(out, dh, dW, ws, wb):
         if T:
@@ -461,11 +475,11 @@ def test_side_stream_and_captured(T):
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):
         step(out, dh, dW, ws, wb)
-    e_ws, e_wb = scratch_for(150, 96, 300, BF16, T), scratch_for(150, 96, 300, BF16, T, None, True)
+    e_ws, e_wb = scratch_for(M, 96, 300, BF16, T), scratch_for(M, 96, 300, BF16, T, None, True)
     gen = torch.Generator(device="cuda").manual_seed(3)
     for i in range(4):
-        c.dh_in.copy_(torch.randn(150, 96, generator=gen, device="cuda"))
-        c.gl.copy_(torch.where(torch.rand(150, generator=gen, device="cuda") < 0.2 * i, -1, torch.randint(0, 300, (150,), generator=gen, device="cuda")))
+        c.dh_in.copy_(torch.randn(M, 96, generator=gen, device="cuda"))
+        c.gl.copy_(torch.where(torch.rand(M, generator=gen, device="cuda") < 0.2 * i, -1, torch.randint(0, 300, (M,), generator=gen, device="cuda")))
         for t in (*out.values(), dh, dW):
             t.fill_(7)
         graph.replay()
