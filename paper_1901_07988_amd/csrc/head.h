@@ -21,8 +21,10 @@ struct HeadCall {
   void* dW;
 };
 
-size_t head_scratch_bytes(const abl_head& p, bool backward);
-int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch);
-int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch);
+size_t head_layout_bytes(const abl_head& p, bool backward, bool copied);   // of one call's workspace; copied: whether the table is
+size_t head_scratch_bytes(const abl_head& p, bool backward);               // of any call's
+// (nothing is launched where the call's layout exceeds scratch_bytes)
+int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_bytes);
+int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_bytes);
 
 }  // namespace abl

@@ -46,7 +46,7 @@ int forward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_byt
   if (int e = check_operands(c, scratch, scratch_bytes, false)) return e;
   if (bad(c.loss, 4) || (needs_lse(c) ? bad(c.lse, 4) : off(c.lse, 4))) return ABL_ERR_ARG;
   if (c.p.T != 0 && (bad(c.lse_t, 4) || bad(c.z_top, 4))) return ABL_ERR_ARG;
-  return launch_head_forward(st, c, scratch);
+  return launch_head_forward(st, c, scratch, scratch_bytes);
 }
 
 int backward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_bytes) {
@@ -58,12 +58,19 @@ int backward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_by
     if (bad(c.dloss, 4) || (needs_lse(c) ? bad(c.in_lse, 4) : off(c.in_lse, 4))) return ABL_ERR_ARG;
     if (c.p.T != 0 && (bad(c.in_lse_t, 4) || bad(c.in_z_top, 4))) return ABL_ERR_ARG;
   }
-  return launch_head_backward(st, c, scratch);
+  return launch_head_backward(st, c, scratch, scratch_bytes);
 }
 
 }  // namespace
 
 extern "C" {
+
+// No part of the interface: what a call lays out in its workspace, for the tests of abl_head_scratch_bytes.
+size_t abl_head_layout_bytes(const abl_head* head, int backward, int copied) {
+  abl_head p;
+  if (check_head(head, backward != 0, head != nullptr && head->T != 0, p) != ABL_OK) return 0;
+  return head_layout_bytes(p, backward != 0, copied != 0);
+}
 
 size_t abl_head_scratch_bytes(const abl_head* head, int backward) {
   abl_head p;

@@ -1593,8 +1593,8 @@ struct Plan {
   int64_t slab_bytes;
 };
 
-// copied: whether the table's rows have to be copied; `most`: what a call may need at most, whatever the table's alignment.
-Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
+// copied: whether the table's rows have to be copied.
+Plan plan_of(const abl_head& p, bool backward, bool copied) {
   Plan q{};
   const bool one = (p.flags & ABL_MATH_BF16) != 0;
   q.parts = p.dtype == ABL_F32 && !one ? 3 : 1;
@@ -1613,12 +1613,10 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
                            : within(kPartialBytes, q.Mp * (int64_t)sizeof(Partial) / narrowest(q.Mp));
   if (piece > 1 << 20) piece = 1 << 20;
   const int64_t table = within(kTableBytes, q.Cp * 2 * q.parts);
-  const int64_t widest = piece;
   if (copied && table < piece) piece = table;
   q.pieces = (int)((p.V + piece - 1) / piece);
   q.piece = up((p.V + q.pieces - 1) / q.pieces, 256);
   q.pieces = (int)((p.V + q.piece - 1) / q.piece);
-  const int64_t held = most ? widest : q.piece;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -1633,21 +1631,20 @@ Plan plan_of(const abl_head& p, bool backward, bool copied, bool most) {
   q.grad = take(backward ? q.Mp * sizeof(RowGrad) : 0);
   q.c_pitch = q.Cp * 2 + kPad, q.d_pitch = q.piece * 2 + kPad;
   q.h = take(q.Mp * q.c_pitch * q.parts);
-  q.table = copied || most ? (table < held ? table : held) : 0;
+  q.table = copied ? q.piece : 0;
   q.W = take(q.table * q.c_pitch * q.parts);
-  int64_t sums = held / narrowest(q.Mp) * q.Mp;
+  int64_t sums = q.piece / narrowest(q.Mp) * q.Mp;
   if (p.M <= kThinRows) {
     const int64_t few = (int64_t)((p.V + kThinTile - 1) / kThinTile > kThinGroups ? (p.V + kThinTile - 1) / kThinTile : kThinGroups) * kThinRows;
     sums = sums > few ? sums : few;
   }
   q.partial = take(backward ? 0 : sums * sizeof(Partial));
-  const bool several = q.pieces > 1 || (most && table < p.V);
-  q.carry = take(!backward && several ? q.Mp * sizeof(Partial) : 0);
-  q.d = take(backward ? q.Mp * (held * 2 + kPad) * q.d_parts : 0);
-  q.acc = take(backward && several ? q.Mp * p.C * 4 : 0);
+  q.carry = take(!backward && q.pieces > 1 ? q.Mp * sizeof(Partial) : 0);
+  q.d = take(backward ? q.Mp * q.d_pitch * q.d_parts : 0);
+  q.acc = take(backward && q.pieces > 1 ? q.Mp * p.C * 4 : 0);
   // shares' sums: as many slabs as fit, of dh or of a piece of dW or of the logits (where these are few tiles: more have no use for shares)
-  const int64_t logits = q.Mp * (held < all ? held : all) * 4, few = logits <= kFewLogits ? 8 * logits : 0;
-  const int64_t widest_sum = 8 * (q.Mp > held ? q.Mp : held) * p.C * 4;
+  const int64_t logits = q.Mp * q.piece * 4, few = logits <= kFewLogits ? 8 * logits : 0;
+  const int64_t widest_sum = 8 * (q.Mp > q.piece ? q.Mp : q.piece) * p.C * 4;
   q.slab_bytes = backward ? (widest_sum > few ? widest_sum : few) : few < 2 * kFewLogits ? few : 2 * kFewLogits;
   if (q.slab_bytes > kSlabBytes) q.slab_bytes = kSlabBytes;
   q.slabs = take(q.slab_bytes);
@@ -1804,7 +1801,12 @@ struct Call {
 
 }  // namespace
 
-size_t head_scratch_bytes(const abl_head& p, bool backward) { return plan_of(p, backward, false, true).bytes; }
+size_t head_layout_bytes(const abl_head& p, bool backward, bool copied) { return plan_of(p, backward, copied).bytes; }
+// (whether the table is copied goes by its address and pitch, which are not known here; copied pieces are smaller, but what lies beside them need not be)
+size_t head_scratch_bytes(const abl_head& p, bool backward) {
+  const size_t in_place = plan_of(p, backward, false).bytes, copied = plan_of(p, backward, true).bytes;
+  return in_place > copied ? in_place : copied;
+}
 
 namespace {
 
@@ -1874,14 +1876,16 @@ int launch_thin(hipStream_t st, const HeadCall& c, const Plan& q, char* ws) {
 
 }  // namespace
 
-int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch) {
+int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_bytes) {
   const abl_head& p = c.p;
   if (p.M <= kThinRows && !(p.dtype == ABL_F32 && (p.flags & ABL_MATH_BF16))) {
-    const Plan q = plan_of(p, false, false, false);
+    const Plan q = plan_of(p, false, false);
+    if (q.bytes > scratch_bytes) return ABL_ERR_SCRATCH;
     return p.dtype == ABL_F32 ? launch_thin<float>(st, c, q, (char*)scratch) : launch_thin<bf16_t>(st, c, q, (char*)scratch);
   }
   const bool copied = !in_place(c);
-  const Plan q = plan_of(p, false, copied, false);
+  const Plan q = plan_of(p, false, copied);
+  if (q.bytes > scratch_bytes) return ABL_ERR_SCRATCH;
   const Call call{c, q, st, (char*)scratch, copied};
   char* ws = call.ws;
   const int* rows = (const int*)(ws + q.rows);
@@ -1940,9 +1944,10 @@ void launch_entry_grad(hipStream_t st, const HeadCall& c, const Plan& q, char* w
 
 // Few rows: the gradient of a piece's logits in fp32, then both products of it.
 template <typename T, int XT, int YT, int WAVES, int AHEAD>
-int launch_thin_backward(hipStream_t st, const HeadCall& c, char* ws) {
+int launch_thin_backward(hipStream_t st, const HeadCall& c, char* ws, size_t ws_bytes) {
   const abl_head& p = c.p;
-  const Plan q = plan_of(p, true, false, false);
+  const Plan q = plan_of(p, true, false);
+  if (q.bytes > ws_bytes) return ABL_ERR_SCRATCH;
   const Call call{c, q, st, ws, false, true};
   Operand none;
   if (int e = call.prepare(true, none)) return e;
@@ -1983,7 +1988,7 @@ bool thin_backward(const abl_head& p) { return p.dtype == ABL_F32 ? p.M <= kThin
 
 }  // namespace
 
-int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
+int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch, size_t scratch_bytes) {
   const abl_head& p = c.p;
   const bool accumulate = (p.flags & ABL_ACCUM_DW) != 0;
   if (p.M == 0) {
@@ -1994,12 +1999,13 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch) {
   }
   if (thin_backward(p)) {
     char* ws = (char*)scratch;
-    if (p.dtype == ABL_BF16) return launch_thin_backward<bf16_t, 1, 1, 8, 4>(st, c, ws);
-    if (p.M <= 16) return launch_thin_backward<float, 1, 1, 8, 4>(st, c, ws);
-    return p.M <= 32 ? launch_thin_backward<float, 2, 2, 4, 2>(st, c, ws) : launch_thin_backward<float, 4, 2, 4, 2>(st, c, ws);
+    if (p.dtype == ABL_BF16) return launch_thin_backward<bf16_t, 1, 1, 8, 4>(st, c, ws, scratch_bytes);
+    if (p.M <= 16) return launch_thin_backward<float, 1, 1, 8, 4>(st, c, ws, scratch_bytes);
+    return p.M <= 32 ? launch_thin_backward<float, 2, 2, 4, 2>(st, c, ws, scratch_bytes) : launch_thin_backward<float, 4, 2, 4, 2>(st, c, ws, scratch_bytes);
   }
   const bool copied = !in_place(c);
-  const Plan q = plan_of(p, true, copied, false);
+  const Plan q = plan_of(p, true, copied);
+  if (q.bytes > scratch_bytes) return ABL_ERR_SCRATCH;
   const Call call{c, q, st, (char*)scratch, copied};
   char* ws = call.ws;
   const int* rows = (const int*)(ws + q.rows);

@@ -295,6 +295,21 @@ def test_sums_of_narrow_tiles(M, C, V, type, T):
     c.backward(scratch=rooms[1][: n[1]])   # (both look behind the workspace)
 
 
+@pytest.mark.parametrize("type,M,C,V,T,flags,pitch", [(F32, 70, 4096, 18000, 0, 0, 0), (F32, 150, 4096, 18000, 3, 0, 0),
+                                                      (F32, 20, 4096, 18000, 0, B.ABL_MATH_BF16, 0), (BF16, 100, 4096, 18000, 0, 0, 1)])
+def test_logits_in_shares_of_a_copied_table(type, M, C, V, T, flags, pitch):
+    """Pieces of a copied table whose logits are made in shares, where the whole vocabulary's would not be: nothing is written behind the workspace."""
+    c = Case(M, C, V, type, T=T, pitch=(0, pitch), size=0.25)
+    n = B.abl_head_scratch_bytes(M, C, V, type, T=T, flags=flags)
+    room = torch.full((n + (1 << 25),), 0xAB, dtype=torch.uint8, device="cuda")
+    got = c.forward(flags, scratch=room[:n])     # (looks behind the workspace)
+    if flags:
+        c.full_h.copy_(c.full_h.bfloat16().float()), c.full_W.copy_(c.full_W.bfloat16().float())
+    want = R.forward(c.h, c.W, c.labels, c.n, c.ids, c.t)
+    for k in got:
+        R.assert_within(got[k], want[k], want["bound"][k], k)
+
+
 @pytest.mark.parametrize("M", [3, 70])
 def test_a_table_beyond_four_gigabytes(M):
     """bf16, 561003 x 4096: the reference on the GPU in 64 bits, a piece of the table at a time, with the bounds of head_reference.py."""

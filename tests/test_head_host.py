@@ -1,6 +1,8 @@
 """Losses over a vocabulary, what needs no GPU: the reference against itself (gradients against differences), sizes, and what the C ABI
 refuses before any launch."""
 import ctypes
+import math
+import random
 
 import pytest
 import torch
@@ -71,6 +73,43 @@ def test_scratch_sizes():
         assert size(**{**dict(M=4, C=8, V=16, dtype=bf16), **kw}) == 0, kw
     assert size(4, 8, 16, bf16, flags=B.ABL_ACCUM_DW | B.ABL_MATH_BF16, backward=True) > 0
     assert B.lib.abl_head_scratch_bytes(None, 0) == 0
+
+
+def layouts(p):
+    """(size of a workspace as it is given, sizes of what calls lay out there: the table where it is, copied), forward and backward."""
+    lay = B.lib.abl_head_layout_bytes
+    lay.restype, lay.argtypes = ctypes.c_size_t, [ctypes.POINTER(B.abl_head), ctypes.c_int, ctypes.c_int]
+    r = ctypes.byref(p)
+    return [(B.lib.abl_head_scratch_bytes(r, b), lay(r, b, 0), lay(r, b, 1)) for b in (0, 1)]
+
+
+def test_no_call_lays_out_more_than_its_workspace():
+    """The launchers compare a call's own layout with what they are given (ABL_ERR_SCRATCH); a workspace of the size that is asked for is enough."""
+    rng = random.Random(11)
+
+    def size(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    sizes = [(M, C, V, T, t) for M in (0, 1, 16, 17, 64, 65, 256, 257, 1024, 1025) for C in (1, 64, 65, 4096, 1 << 16) for V in (1, 255, 257, 32000, 1 << 26)
+             for T in (0, 1024) for t in range(4)]
+    sizes += [(1 << 23, 1 << 16, 1 << 21, T, t) for T in (0, 7) for t in range(4)]
+    sizes += [(size(1, 8192) if i % 8 else size(1, 1 << 23), size(1, 8192), size(1, 131072), rng.choice([0, 0, 1, 25]), rng.randrange(4)) for i in range(60000)]
+    types = [(B.ABL_BF16, B.ABL_BF16, 0), (B.ABL_BF16, B.ABL_F32, 0), (B.ABL_F32, B.ABL_F32, 0), (B.ABL_F32, B.ABL_F32, B.ABL_MATH_BF16)]
+    for M, C, V, T, t in sizes:
+        if M * V > 1 << 44:
+            continue
+        d, w, flags = types[t]
+        for given, in_place, copied in layouts(B.abl_head(M=M, C=C, V=V, T=T, dtype=d, dw_dtype=w, flags=flags, scale=1.0, temperature=1.0)):
+            assert given > 0 and 0 < in_place <= given and 0 < copied <= given, (M, C, V, T, d, w, flags)
+
+
+@pytest.mark.parametrize("type,M,C,V,T,need", [(torch.float32, 512, 4096, 32000, 0, 110573824), (torch.float32, 256, 4096, 32768, 0, 91430144),
+                                               (torch.float32, 1024, 4096, 50257, 0, 123695360), (torch.float32, 128, 4096, 32000, 0, 91430144),
+                                               (torch.bfloat16, 100, 8192, 20000, 0, 105684224), (torch.float32, 512, 2882, 15078, 25, 98600000)])
+def test_room_for_logits_in_shares_of_a_copied_table(type, M, C, V, T, need):
+    """A table that is copied a piece at a time, whose logits are few enough to be made in shares, where the whole vocabulary's are not: copies of the rows and of a
+    piece of the table, and eight slabs of its logits, all at once."""
+    assert B.abl_head_scratch_bytes(M, C, V, type, T=T) >= need
 
 
 # ---- refusals -----------------------------------------------------------------------------------------
