@@ -420,8 +420,9 @@ int abl_ckpt_wgrad(void* stream, int dtype, uint32_t flags, const void* ckpt, in
  * loss, log-sums and gradient are zero and its h is not looked at (it may hold anything).  Rows that do not count cost nothing in the products.
  * A label or id of V or more makes the row's loss NaN, and the gradients NaN.
  * bf16 operands go into the matrix cores as they are, fp32 ones as three bf16 parts (24 bits; ABL_MATH_BF16: rounded to one).  Logits, sums and
- * losses are fp32.  The gradient of the logits is rounded to bf16 for its product with bf16 operands, except for a dW in fp32, where it enters in three
- * parts (24 bits; ABL_MATH_BF16: one), as it does for operands in fp32; of up to 16 rows it stays in fp32.  Sums are taken in a fixed order. */
+ * losses are fp32.  The gradient of the logits is rounded to bf16 for its product with bf16 operands (over the largest weight of a row's label, so that rows of one
+ * weight share no rounding of it), except for a dW in fp32, where it enters in three parts (24 bits; ABL_MATH_BF16: one), as it does for operands in fp32; of
+ * up to 16 rows, in fp32 up to 64, it stays in fp32.  Sums are taken in a fixed order. */
 typedef struct abl_head {
   int64_t M;                 /* rows */
   int32_t C, V, T;           /* channels, tokens of the vocabulary, the teacher's entries of a row (0 for abl_xent) */

@@ -26,6 +26,12 @@ __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog
 __device__ inline float log_of(float x) { return __builtin_amdgcn_logf(x) * kLn2; }
 __device__ inline float nan_value() { return __uint_as_float(0x7FC00000u); }
 
+__device__ inline float wave_max(float v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
 // ---- which rows count -----------------------------------------------------------------------------------
 enum { kLabel = 1, kTeacher = 2, kBad = 4 };   // of a row
 
@@ -59,11 +65,22 @@ __global__ __launch_bounds__(256) void head_flags_kernel(int64_t M, const int64_
   if ((threadIdx.x & 63) == 0) flags[row] = (unsigned char)f;
 }
 
-// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, and their number: one block (8192 rows: 6 us; places
+// What the backward pass divides the gradient of the logits by where that is rounded to bf16, and multiplies its products with: the largest weight that a row's
+// label has (without labels: its entries have).  Undivided, the labels' entries of rows of one weight - the mean over a batch - are all but the same
+// number, w (q - 1), and share one rounding of up to 2^-9 of them, which no sum over rows averages out; divided they are q - 1, whose roundings have nothing to do with each
+// other and vanish with q.
+struct UnitOf {
+  const float* dloss;      // nullptr: no unit is wanted
+  float scale, first, second;
+};
+
+// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, their number, and the unit: one block (8192 rows: 6 us; places
 // by atomics would change from call to call, and with them the order of the sums).
 __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_t* __restrict__ labels, const unsigned char* __restrict__ flags,
-                                                         int* __restrict__ rows, int* __restrict__ count) {
+                                                         int* __restrict__ rows, int* __restrict__ count, UnitOf of, float* __restrict__ unit) {
   __shared__ int sums[17];
+  __shared__ float largest[16];
+  float large = 0.0f;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int base = 0;
   for (int64_t m0 = 0; m0 < M; m0 += 4096) {
@@ -94,13 +111,28 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_
     int at = base + sums[wave] + s - n;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (on >> e & 1) rows[at++] = (int)(m + e);
+      if (on >> e & 1) {
+        rows[at++] = (int)(m + e);
+        if (of.dloss != nullptr && finite(of.dloss[m + e])) large = fmaxf(large, fabsf(of.dloss[m + e]));
+      }
     base += sums[16];
     __syncthreads();
   }
   const int end = (base + kRowTile - 1) / kRowTile * kRowTile;
   for (int i = base + threadIdx.x; i < end; i += 1024) rows[i] = -1;
-  if (threadIdx.x == 0) *count = base;
+  if (of.dloss != nullptr) {
+    large = wave_max(large);
+    if (lane == 0) largest[wave] = large;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    *count = base;
+    if (of.dloss != nullptr) {
+      for (int w = 0; w < 16; ++w) large = fmaxf(large, largest[w]);
+      const float u = fabsf(large * of.scale * of.first * of.second);   // (in the order of the weights themselves: a quotient is one exactly)
+      *unit = u >= 1e-30f && u <= 1e30f ? u : 1.0f;
+    }
+  }
 }
 
 // ---- copies of rows in bf16 parts -----------------------------------------------------------------------
@@ -165,7 +197,7 @@ __global__ __launch_bounds__(256) void head_copy_kernel(const T* __restrict__ fr
   if (row < n_to) copy_row<T, P>(row < n ? from + row * ld : nullptr, C, Cp, to + row * pitch, plane);
 }
 
-// What the backward pass knows of a row that counts (the formula above; all times the row's dloss and the logits' scale).  At temperature one a
+// What the backward pass knows of a row that counts (the formula above; all times the row's dloss and the logits' scale, over the unit).  At temperature one a
 // holds at too.
 struct RowGrad {
   float L, a, Lt, at, a0, ay;
@@ -189,6 +221,7 @@ struct Gather {
   int64_t lddh;
   RowGrad* grad;
   const float *in_lse, *in_lse_t, *dloss;
+  const float* unit;            // nullptr: one
   float scale, smoothing, z_weight, tau, label_weight, teacher_weight;
 };
 
@@ -222,6 +255,10 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
         r.a0 = -l * g.smoothing / (float)g.V;
         r.ay = -l * (1.0f - g.smoothing);
         r.label = f & kLabel && y < g.V ? (int)y : -1;
+        if (g.unit != nullptr) {
+          const float u = *g.unit;
+          r.a /= u, r.at /= u, r.a0 /= u, r.ay /= u;
+        }
         if (f & kBad) r.a0 = nan_value();
       }
       g.grad[n] = r;
@@ -284,6 +321,7 @@ struct Product {
   int64_t ld;
   int out_f32, accumulate;
   const int* map;           // row of out for each x (nullptr: x itself)
+  const float* unit;        // what the sums are multiplied with (nullptr: nothing), before accumulate
   const float* add;         // [x][add_ld], added (nullptr: nothing)
   int64_t add_ld;
   // sums whose k's are cut into shares of blocks of their own: where there are several, or no out, each leaves its sums in a slab [nx][ny] and a second launch
@@ -777,6 +815,7 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       }
     }
   } else {
+    const float unit = a.unit != nullptr ? *a.unit : 1.0f;
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
       const int x = x0 + wx + 16 * i + (lane & 15);
@@ -793,18 +832,19 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
           float* to = (float*)a.out + row * a.ld + col;
           if (n >= 4) {
             if (add != nullptr) v += *reinterpret_cast<const f32x4_any4*>(add);
+            v *= unit;
             if (a.accumulate) v += *reinterpret_cast<const f32x4_any4*>(to);
             *reinterpret_cast<f32x4_any4*>(to) = v;
           } else {
 #pragma unroll
             for (int e = 0; e < 3; ++e)
-              if (e < n) to[e] = v[e] + (add != nullptr ? add[e] : 0.0f) + (a.accumulate ? to[e] : 0.0f);
+              if (e < n) to[e] = (v[e] + (add != nullptr ? add[e] : 0.0f)) * unit + (a.accumulate ? to[e] : 0.0f);
           }
         } else {
           bf16_t* to = (bf16_t*)a.out + row * a.ld + col;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (e < n) v[e] += (add != nullptr ? add[e] : 0.0f) + (a.accumulate ? (float)to[e] : 0.0f);
+            if (e < n) v[e] = (v[e] + (add != nullptr ? add[e] : 0.0f)) * unit + (a.accumulate ? (float)to[e] : 0.0f);
           if (n >= 4) {
             *reinterpret_cast<u32x2_any2*>(to) = u32x2_any2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
           } else {
@@ -846,6 +886,7 @@ __global__ __launch_bounds__(256) void head_sum_kernel(Product a, int bx, int by
 #pragma unroll
   for (int i = 0; i < 8; ++i) v += slab[i];
   if (a.add != nullptr) v += four(a.add + x * a.add_ld + col);
+  if (a.unit != nullptr) v *= *a.unit;
   const int64_t row = a.map != nullptr ? a.map[x] : x;
   if (a.out_f32) {
     float* to = (float*)a.out + row * a.ld + col;
@@ -1363,12 +1404,6 @@ __global__ __launch_bounds__(256) void head_thin_sum_kernel(ThinGrad a, const in
     ((bf16_t*)dh)[at] = (bf16_t)v;
 }
 
-__device__ inline float wave_max(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-
 // Maximum and sum of a row's softmax over its entries at temperature tau, by a wave: p_k = exp(t_k / tau - top) / sum.
 __device__ inline void teacher_sums(const int64_t* ids, const float* logits, int T, float inv_tau, float& top, float& sum) {
   const int lane = threadIdx.x & 63;
@@ -1589,7 +1624,7 @@ struct Plan {
   int64_t piece, table;     // tokens of a piece; of a piece's copied part of the table (0: in place)
   int pieces;
   // places in the workspace
-  size_t count, rows, flags, labels, z_label, h, W, partial, carry, grad, d, acc, slabs, bytes;
+  size_t count, unit, rows, flags, labels, z_label, h, W, partial, carry, grad, d, acc, slabs, bytes;
   int64_t slab_bytes;
 };
 
@@ -1624,6 +1659,7 @@ Plan plan_of(const abl_head& p, bool backward, bool copied) {
     return here;
   };
   q.count = take(16);
+  q.unit = q.count + 8;
   q.rows = take(q.Mp * 4);
   q.flags = take(p.T != 0 ? p.M : 0);
   q.labels = take(backward ? 0 : q.Mp * 4);
@@ -1764,14 +1800,18 @@ struct Call {
     int* count = (int*)(ws + q.count);
     unsigned char* flags = p.T != 0 ? (unsigned char*)(ws + q.flags) : nullptr;
     if (flags != nullptr) head_flags_kernel<<<(unsigned)((p.M + 3) / 4), 256, 0, st>>>(p.M, c.labels, c.ids, c.logits, p.T, p.V, flags);
-    head_rows_kernel<<<1, 1024, 0, st>>>(p.M, c.labels, flags, rows, count);
+    // (the gradient of the logits of few rows, and of operands in fp32, is not rounded to bf16)
+    float* unit = (float*)(ws + q.unit);
+    UnitOf of{backward && !few && q.parts == 1 ? c.dloss : nullptr, p.scale, p.teacher_weight, p.temperature};
+    if (c.labels != nullptr && p.label_weight != 0.0f) of.first = p.label_weight, of.second = 1.0f - p.smoothing;
+    head_rows_kernel<<<1, 1024, 0, st>>>(p.M, c.labels, flags, rows, count, of, unit);
     Gather g{};
     g.M = p.M, g.slots = q.Mp, g.C = p.C, g.Cp = (int)q.Cp, g.T = p.T, g.V = p.V, g.rows = rows, g.count = count, g.flags = flags;
     g.labels = c.labels, g.to = ws + q.h, g.pitch = q.c_pitch, g.plane = q.Mp * q.c_pitch, g.ldh = c.h.ld;
     g.loss = c.loss, g.lse = c.lse, g.lse_t = c.lse_t, g.z_top = c.z_top, g.dh = c.dh.p, g.lddh = c.dh.ld;
     g.row_label = !backward && c.labels != nullptr ? (int*)(ws + q.labels) : nullptr;
     g.grad = backward ? (RowGrad*)(ws + q.grad) : nullptr;
-    g.in_lse = c.in_lse, g.in_lse_t = c.in_lse_t, g.dloss = c.dloss;
+    g.in_lse = c.in_lse, g.in_lse_t = c.in_lse_t, g.dloss = c.dloss, g.unit = of.dloss != nullptr ? unit : nullptr;
     g.scale = p.scale, g.smoothing = p.smoothing, g.z_weight = p.z_weight, g.tau = p.temperature, g.label_weight = p.label_weight;
     g.teacher_weight = p.teacher_weight;
     if (int e = hip_status()) return e;
@@ -2010,6 +2050,7 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch, size_
   char* ws = call.ws;
   const int* rows = (const int*)(ws + q.rows);
   const int* count = (const int*)(ws + q.count);
+  const float* unit = q.parts == 1 ? (const float*)(ws + q.unit) : nullptr;
   Operand h, w;
   if (int e = call.prepare(true, h)) return e;
   for (int i = 0; i < q.pieces; ++i) {
@@ -2043,6 +2084,7 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch, size_
       a.x = d, a.y = w, a.nx = (int)p.M, a.ny = p.C, a.k = (int)up(n, 64), a.count = count;
       a.parts = q.parts == 3 ? 6 : 1, a.pairs = q.parts == 3 ? kPairs6 : kPairs1;
       a.out = last ? c.dh.p : acc, a.ld = last ? c.dh.ld : p.C, a.out_f32 = !last || p.dtype == ABL_F32, a.map = last ? rows : nullptr;
+      a.unit = last ? unit : nullptr;
       a.add = i > 0 ? acc : nullptr, a.add_ld = p.C;
       if (int e = launch_product<false, true, kEpiSum>(st, a, (float*)(ws + q.slabs), q.slab_bytes)) return e;
     }
@@ -2051,6 +2093,7 @@ int launch_head_backward(hipStream_t st, const HeadCall& c, void* scratch, size_
       a.x = d, a.y = h, a.nx = (int)n, a.ny = p.C, a.k = (int)p.M, a.count = count, a.count_k = 1;
       a.parts = q.parts == 3 ? 6 : q.d_parts, a.pairs = q.parts == 3 ? kPairs6 : q.d_parts == 3 ? kPairs3 : kPairs1;
       a.out = (char*)c.dW + v0 * p.C * size_of(p.dw_dtype), a.ld = p.C, a.out_f32 = p.dw_dtype == ABL_F32, a.accumulate = accumulate;
+      a.unit = unit;
       if (int e = launch_product<true, true, kEpiSum>(st, a, (float*)(ws + q.slabs), q.slab_bytes)) return e;
     }
   }

@@ -310,6 +310,44 @@ def test_logits_in_shares_of_a_copied_table(type, M, C, V, T, flags, pitch):
         R.assert_within(got[k], want[k], want["bound"][k], k)
 
 
+@pytest.mark.parametrize("M,C,V,smoothing,teacher", [(300, 64, 5003, 0.0, False), (300, 64, 5003, 0.1, False), (2100, 40, 16000, 0.0, False), (70, 4096, 3000, 0.0, False),
+                                                     (300, 64, 5003, 0.0, True)])
+def test_rows_of_one_weight(M, C, V, smoothing, teacher):
+    """A mean over the rows: the labels' entries of the gradient of the logits, w (q - 1) with a small q, do not share the rounding of w to bf16.  Results in fp32, where it
+    would show: operands that are bf16's, ABL_MATH_BF16.  Labels are 16 tokens, whose rows of the table are all that is not zero."""
+    flags = B.ABL_MATH_BF16
+    c = Case(M, C, V, F32, T=1 if teacher else 0, ignored=0.0, size=0.0625, **(dict(temperature=2.0, label_weight=0.0) if teacher else dict(smoothing=smoothing)))
+    c.full_W[16:] = 0
+    c.full_h.copy_(c.full_h.bfloat16().float()), c.full_W.copy_(c.full_W.bfloat16().float())
+    label = torch.randint(0, 16, (M,), generator=torch.Generator().manual_seed(6))
+    if teacher:
+        c.labels, c.ids[:, 0], c.t[:, 0] = None, label, 1.0
+    else:
+        c.labels = label
+    o = c.forward(flags)
+    w = 257 / 256 * 2.0 ** -9       # halfway between two bf16 values
+    g, dh, dW = torch.full((M,), w, device="cuda"), torch.empty(M, C, device="cuda"), torch.empty(V, C, device="cuda")
+    ws = scratch_for(M, C, V, F32, c.T, F32, True, flags)
+    if teacher:
+        B.abl_distill_backward(c.dh_in, c.dW_in, None, c.gi, c.gt, o["lse"], o["lse_t"], o["z_top"], g, ws, dh, dW, **c.options(flags))
+    else:
+        B.abl_xent_backward(c.dh_in, c.dW_in, c.gl, o["lse"], g, ws, dh, dW, **c.options(flags))
+    want = R.backward(c.h, c.W, c.labels, o["lse"].cpu(), g.cpu(), c.n, F32, F32, True, c.ids, c.t, o["lse_t"].cpu() if teacher else None)
+    x, y, at = c.h.double(), c.W.double(), torch.arange(M)
+    q = torch.softmax(x @ y.t() / c.n.tau, 1)
+    assert float(q.max()) < 2.0 ** -10 and float(q.min()) > 0.3 / V
+    w *= c.n.tau if teacher else 1.0
+    # an entry is off by its rounding to bf16 (of q and of the smoothing's 0.1 / V), and by what its logit is: with the log-sum's, the exponent's argument and instruction
+    # below 2^-8 of q here.  A label's, over the unit, is -1 + q / (1 - smoothing) - ..: less than half a step from -1, so that it rounds to this and is off by twice q at most.
+    assert float(2 * R.logit_bound(x, y, c.n).max()) + 2.0 ** -16 < R.B16
+    off = w * R.B16 * (2 * q + smoothing / V)
+    off[at, label] = w * (2 * q[at, label] + 8 * R.F32)
+    d = w * q
+    d[at, label] += w
+    R.assert_within(dh, want["dh"], 1.01 * (off @ y.abs() + (V + 70) * R.F32 * (d @ y.abs())) + 1e-37, "dh")
+    R.assert_within(dW, want["dW"], 1.01 * (off.t() @ x.abs() + (M + 70) * R.F32 * (d.t() @ x.abs())) + 1e-37, "dW")
+
+
 @pytest.mark.parametrize("M", [3, 70])
 def test_a_table_beyond_four_gigabytes(M):
     """bf16, 561003 x 4096: the reference on the GPU in 64 bits, a piece of the table at a time, with the bounds of head_reference.py."""
