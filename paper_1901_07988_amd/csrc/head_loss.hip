@@ -718,20 +718,31 @@ __global__ __launch_bounds__(WX * WY * 64) void head_product_kernel(Product a) {
       for (int j = 0; j < FY; ++j) top = fmaxf(fmaxf(top, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
       top = lanes16_max(top);
       const float ref = top == -__builtin_inff() ? 0.0f : top;
-      float sum = 0.0f, sum_t = 0.0f, tops = 0.0f;   // (FEW, which waits for memory anyway: the maximum is counted beside the sum, so that nothing of a small one is lost)
+      float sum, sum_t, tops;
+      auto add_up = [&](float ref, auto aside) __attribute__((always_inline)) {   // aside: the maximum is counted beside the sum, so that nothing of a small one is lost
+        sum = sum_t = tops = 0.0f;
 #pragma unroll
-      for (int j = 0; j < FY; ++j)
+        for (int j = 0; j < FY; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float z = (acc[i][j][e] - ref) * kLog2e;   // (the difference first: it is exact next to the maximum)
-          const bool hit = FEW && acc[i][j][e] == ref;
-          sum += hit ? 0.0f : __builtin_amdgcn_exp2f(z);
-          if (soft) sum_t += hit ? 0.0f : __builtin_amdgcn_exp2f(z * a.inv_tau);
-          if (FEW) tops += hit ? 1.0f : 0.0f;
-        }
-      sum = lanes16_sum(sum);
-      if (soft) sum_t = lanes16_sum(sum_t);
-      if (FEW) tops = lanes16_sum(tops);
+          for (int e = 0; e < 4; ++e) {
+            const float z = (acc[i][j][e] - ref) * kLog2e;   // (the difference first: it is exact next to the maximum)
+            const bool hit = aside.value && acc[i][j][e] == ref;
+            sum += hit ? 0.0f : __builtin_amdgcn_exp2f(z);
+            if (soft) sum_t += hit ? 0.0f : __builtin_amdgcn_exp2f(z * a.inv_tau);
+            if (aside.value) tops += hit ? 1.0f : 0.0f;
+          }
+        sum = lanes16_sum(sum);
+        if (soft) sum_t = lanes16_sum(sum_t);
+        if (aside.value) tops = lanes16_sum(tops);
+      };
+      // FEW waits for memory anyway.  The others count the maximum aside only where a row is all but certain of it: the sum of the rest, an eighth or more, is off by 2^-17 of
+      // itself otherwise (16 + 2 roundings of up to 2^-24 next to one).
+      add_up(ref, std::integral_constant<bool, FEW>{});
+      if (!FEW && __builtin_expect(__any(sum < 1.125f || (soft && sum_t < 1.125f)), 0)) {
+        float again = ref;
+        asm volatile("" : "+v"(again));   // (else the terms that both ways have in common are kept, and made where none of them is wanted: 2 %)
+        add_up(again, std::true_type{});
+      }
       if (a.sum_z) all = lanes16_sum(all);
       if (lane < 16) joined[wave % WY * BX + x] = Partial{top, sum + (tops - 1.0f), sum_t + (tops - 1.0f), all};
     }

@@ -411,6 +411,35 @@ def test_small_losses_of_few_rows(type, M):
     R.assert_within(loss, torch.log1p(share), torch.log1p(share) * off * 1.01, "loss")
 
 
+@pytest.mark.parametrize("type,M,C,V,tau", [(F32, 70, 64, 1000, 1.0), (BF16, 70, 64, 1000, 1.0), (BF16, 300, 64, 20000, 1.0), (F32, 300, 64, 20000, 1.0), (BF16, 2100, 64, 9000, 1.0),
+                                           (BF16, 4200, 64, 33000, 1.0), (F32, 2100, 64, 9000, 1.0), (BF16, 100, 4000, 300, 1.0), (BF16, 300, 64, 20000, 0.5), (F32, 300, 64, 3000, 0.5)])
+def test_small_losses(type, M, C, V, tau):
+    """As of few rows, in every tile: a sure row's loss keeps its digits, at the teacher's temperature too (tau < 1: its sum is small where that at one is not)."""
+    c = Case(M, C, V, type, T=0 if tau == 1.0 else 1, ignored=0.0, size=0.25, **({} if tau == 1.0 else dict(temperature=tau, label_weight=0.0)))
+    at = torch.arange(M) % V
+    c.full_h += (15 + 10 * torch.rand(M, 1, generator=torch.Generator().manual_seed(2))) * tau * c.full_W[at]
+    c.full_h.copy_(c.full_h.to(type))
+    if tau == 1.0:
+        c.labels = at
+    else:
+        c.labels, c.ids[:, 0], c.t[:, 0] = None, at, 0.0
+    loss = c.forward()["loss"]
+    x, y = c.h.double(), c.W.double()
+    z = x @ y.t() / tau
+    share = torch.exp(z - z[torch.arange(M), at][:, None])
+    share[torch.arange(M), at] = 0
+    reach = float((z.amax(1) - z.amin(1)).max())
+    share = share.sum(1)
+    assert float(share.min()) < 1e-7 < 1e-4 < float(share.max()) and reach < 64
+    # What a share may be off, as a part of itself: both logits; the exponent's argument (|z - z_label| < 64, three roundings); instructions; the sum, V / 64 of its terms one after the
+    # other at most, and where it is an eighth or more 18 roundings of 2^-24 next to one
+    off = 2 * R.logit_bound(x, y, c.n).amax(1) / tau + 3 * 64 * R.F32 + 2.0 ** -20 + (V / 64 + 100 + 18 * 8) * R.F32
+    want = torch.log1p(share) * tau ** 2
+    # (a teacher's loss: p (log p - z / tau + Lt) of the one entry; its z is another product of the same row of the table, a logit's error away, which no share makes smaller)
+    alone = 0.0 if tau == 1.0 else 2 * R.logit_bound(x, y, c.n).gather(1, at[:, None])[:, 0] * tau
+    R.assert_within(loss, want, want * off * 1.01 + alone, "loss")
+
+
 @pytest.mark.parametrize("type", [F32, BF16])
 def test_values_that_are_not_finite(type):
     c = Case(20, 32, 50, type, ignored=0.0)
