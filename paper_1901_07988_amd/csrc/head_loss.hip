@@ -1415,16 +1415,17 @@ __global__ __launch_bounds__(256) void head_thin_sum_kernel(ThinGrad a, const in
     ((bf16_t*)dh)[at] = (bf16_t)v;
 }
 
-// Maximum and sum of a row's softmax over its entries at temperature tau, by a wave: p_k = exp(t_k / tau - top) / sum.
+// Maximum and sum of a row's softmax over its entries at temperature tau, by a wave: p_k = exp((t_k - top) / tau) / sum (the difference first: a t of the type's largest values
+// may not be divided by a small tau).
 __device__ inline void teacher_sums(const int64_t* ids, const float* logits, int T, float inv_tau, float& top, float& sum) {
   const int lane = threadIdx.x & 63;
   top = -__builtin_inff();
   for (int k = lane; k < T; k += 64)
-    if (entry_there(ids[k], logits[k])) top = fmaxf(top, logits[k] * inv_tau);
+    if (entry_there(ids[k], logits[k])) top = fmaxf(top, logits[k]);
   top = wave_max(top);
   sum = 0.0f;
   for (int k = lane; k < T; k += 64)
-    if (entry_there(ids[k], logits[k])) sum += exp_of(logits[k] * inv_tau - top);
+    if (entry_there(ids[k], logits[k])) sum += exp_of((logits[k] - top) * inv_tau);
   sum = wave_sum(sum);
 }
 
@@ -1533,7 +1534,7 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(Loss a) {
     const float norm = 1.0f / sum, ln_sum = log_of(sum);
     for (int k = lane; k < a.T; k += 64)
       if (entry_there(ids[k], t[k])) {
-        const float u = t[k] * inv_tau - top, q = exp_of(u) * norm;
+        const float u = (t[k] - top) * inv_tau, q = exp_of(u) * norm;
         if (q != 0.0f) kd += q * ((u - ln_sum) + (p.top - z[k]) * inv_tau);   // (NaN goes in)
       }
     loss += a.teacher_weight * a.tau * a.tau * (wave_sum(kd) + ln_t);
@@ -1576,12 +1577,12 @@ __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
   const float* t = a.logits + row * a.T;
   if (a.T <= 64) {   // an entry a lane; tokens fit 32 bits
     const int64_t wide = lane < a.T ? ids[lane] : -1;
-    const float u = lane < a.T ? t[lane] * a.inv_tau : 0.0f;
+    const float u = lane < a.T ? t[lane] : 0.0f;
     const bool there = lane < a.T && entry_there(wide, t[lane]);
     const int id = there && wide < a.v1 ? (int)wide : -1;
     if (!__any(id >= a.v0)) return;
     const float top = wave_max(there ? u : -__builtin_inff());
-    const float e = there ? exp_of(u - top) : 0.0f, mine = e / wave_sum(e);
+    const float e = there ? exp_of((u - top) * a.inv_tau) : 0.0f, mine = e / wave_sum(e);
     bool first = true;
     float p = 0.0f;
     for (int i = 0; i < a.T; ++i) {
@@ -1605,7 +1606,7 @@ __global__ __launch_bounds__(256) void head_entry_grad_kernel(Entries a) {
     if (!first) continue;
     float p = 0.0f;
     for (int i = k; i < a.T; ++i)
-      if (ids[i] == id && entry_there(id, t[i])) p += exp_of(t[i] * a.inv_tau - top) * norm;
+      if (ids[i] == id && entry_there(id, t[i])) p += exp_of((t[i] - top) * a.inv_tau) * norm;
     put_entry_grad(a, g, n, (int)id, a.z_top[row * a.T + k], p);
   }
 }

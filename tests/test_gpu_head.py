@@ -610,6 +610,29 @@ def test_the_forward_without_log_sums(size, temperature):
     assert torch.equal(a, dh) and torch.equal(b, dW)
 
 
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M,T,tau", [(9, 5, 0.5), (90, 5, 0.5), (9, 70, 0.25), (90, 70, 0.25), (90, 5, 2.0)])
+def test_teachers_of_the_largest_and_lowest_values(type, M, T, tau):
+    """A teacher's logits of the type's lowest value (a mask's) have no share beside others, equal shares alone; its largest ones take all, equally."""
+    c = Case(M, 32, 150, type, T=T, labels=False, temperature=tau)
+    c.ids, c.t = torch.randint(0, 150, (M, T), generator=torch.Generator().manual_seed(3)), torch.randn(M, T, generator=torch.Generator().manual_seed(4))
+    big = torch.finfo(F32).max
+    c.t[0::4, 1:] = -big                       # one entry and masked ones
+    c.t[1::4] = -big                           # masked ones alone
+    c.t[2::4, :2] = big                        # two that take all
+    plain = c.t.clone()
+    plain[1::4], plain[2::4, :2], plain[2::4, 2:], plain[0::4, 1:] = 0.0, 0.0, -120 * tau, -120 * tau - 5   # the same shares, to exp(-115)
+    want = R.forward(c.h, c.W, None, c.n, c.ids, plain)
+    got = c.forward()
+    for k in got:
+        R.assert_within(got[k], want[k], want["bound"][k], k)
+    dh, dW = c.backward()
+    c.t = plain
+    want = c.reference()
+    R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+    R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+
+
 def test_gradients_are_differences_of_the_losses():
     """The backward calls against what the forward calls say of moved inputs."""
     for T in (0, 4):
