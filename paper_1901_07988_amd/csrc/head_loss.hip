@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void head_copy_kernel(const T* __restrict__ fr
 // holds at too.
 struct RowGrad {
   float L, a, Lt, at, a0, ay;
-  int label, unused;
+  int label, counts;
 };
 
 struct Gather {
@@ -260,6 +260,7 @@ __global__ __launch_bounds__(256) void head_gather_kernel(Gather g, const T* __r
           r.a /= u, r.at /= u, r.a0 /= u, r.ay /= u;
         }
         if (f & kBad) r.a0 = nan_value();
+        r.counts = 1;
       }
       g.grad[n] = r;
     }
@@ -1192,7 +1193,7 @@ __global__ __launch_bounds__(WAVES * 64) void head_thin_kernel(Thin a) {
           d[e] = __builtin_fmaf(k.a, exp_of(z - k.L), k.a0);
           if (a.inv_tau != 1.0f) d[e] = __builtin_fmaf(k.at, exp_of(__builtin_fmaf(z, a.inv_tau, -k.Lt)), d[e]);
           if (k.label >= 0 && col + e == k.label - a.v0) d[e] += k.ay;
-          if (row >= a.M || col + e >= a.V) d[e] = 0.0f;
+          if (!k.counts || col + e >= a.V) d[e] = 0.0f;   // (whatever the table holds)
         }
         *reinterpret_cast<floatx4*>(a.d + row * a.d_ld + col) = d;
       }

@@ -207,6 +207,20 @@ def test_no_row_counts(type, T):
     assert bool((kept == 1).all())
 
 
+@pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("M", [1, 12, 40, 100])
+@pytest.mark.parametrize("T", [0, 3])
+def test_no_row_counts_against_any_table(type, M, T):
+    c = Case(M, 40, 90, type, T=T, ignored=1.0)
+    c.full_W[::3] = torch.tensor([math.nan, INF, -INF])[torch.arange(30) % 3][:, None].to(type)
+    if T:
+        c.ids[:] = -1
+    out = c.forward()
+    assert all(bool((v == 0).all()) for v in out.values())
+    dh, dW = c.backward()
+    assert bool((dh == 0).all()) and bool((dW == 0).all())
+
+
 def test_no_rows():
     W, h, y = torch.ones(12, 8, device="cuda"), torch.ones(0, 8, device="cuda"), torch.ones(0, dtype=torch.int64, device="cuda")
     s, e = torch.empty(4096, dtype=torch.uint8, device="cuda"), torch.empty(0, device="cuda")
