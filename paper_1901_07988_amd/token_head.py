@@ -28,6 +28,7 @@ class VocabularyHead:
 
     def __init__(self, table, tokens, top=0, temperature=1.0, label_weight=1.0, teacher_weight=1.0, smoothing=0.0, z_weight=0.0):
         self.master = table
+        assert top or (temperature, label_weight, teacher_weight) == (1.0, 1.0, 1.0), "labels alone have neither a temperature nor weights"
         V, C = table.shape
         self.M, self.V, self.C, self.T = tokens, V, C, top
         self.how = dict(smoothing=smoothing, z_weight=z_weight)

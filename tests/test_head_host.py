@@ -9,6 +9,7 @@ import torch
 
 from tests import head_reference as R
 from paper_1901_07988_amd import binding as B
+from paper_1901_07988_amd import token_head as H
 
 
 # ---- the reference ------------------------------------------------------------------------------------
@@ -176,3 +177,10 @@ def test_calls_refuse_tensors_of_the_cpu():
     x = torch.zeros(4, 8)
     with pytest.raises(AssertionError):
         B.abl_xent_forward(x, x, torch.zeros(4, dtype=torch.int64), None, None, None)
+
+
+def test_a_head_of_labels_alone_refuses_weights():
+    """They would not be looked at: a loss half as large was asked for and not given."""
+    for how in (dict(label_weight=0.5), dict(temperature=2.0), dict(teacher_weight=0.0)):
+        with pytest.raises(AssertionError):
+            H.VocabularyHead(torch.zeros(4, 8), 2, **how)
