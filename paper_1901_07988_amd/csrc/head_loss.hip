@@ -988,7 +988,7 @@ __global__ __launch_bounds__(256) void head_slab_grad_kernel(Product a, int bx, 
 }
 
 // ---- the teacher's entries ------------------------------------------------------------------------------
-// z at the k-th entry of a row, by a wave.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
+// z at a row's entries.  rounded: operands as bf16 (fp32 with ABL_MATH_BF16).
 struct EntryLogits {
   const void *h, *W;
   int64_t ldh, ldw;
@@ -998,6 +998,7 @@ struct EntryLogits {
   float scale;
   float* z_top;
 };
+// At the k-th one, by a wave: of few rows, whose operands are never rounded.
 template <typename T>
 __device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
   const int lane = threadIdx.x & 63;
@@ -1013,8 +1014,7 @@ __device__ inline void entry_logit(const EntryLogits& a, int64_t row, int k) {
     load_piece(h + c, n, x);
     load_piece(w + c, n, y);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      s = a.rounded ? __builtin_fmaf((float)(bf16_t)x[e], (float)(bf16_t)y[e], s) : __builtin_fmaf(x[e], y[e], s);
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], y[e], s);
   };
   const int whole = a.C / 512 * 512;
 #pragma unroll 4
@@ -1070,8 +1070,8 @@ __global__ __launch_bounds__(256) void head_entries_kernel(EntryLogits a, const 
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------
-// Logits of up to 64 rows: bound by the table, which is read once, straight into registers.  A block takes 16 YT tokens at a time, its four waves a quarter of
-// the channels each, so that a small table, too, is many waves' work; rows come from the caches again and again.  A lane's 32 bytes of a row are
+// Logits of up to 64 rows: bound by the table, which is read once, straight into registers.  A block takes 16 YT tokens at a time, its WAVES waves a share
+// of the channels each (eight up to 16 rows, four beyond), so that a small table, too, is many waves' work; rows come from the caches again and again.  A lane's 32 bytes of a row are
 // its operands of two matrix instructions (bf16) or eight (fp32, exact): which k they stand for does not matter as long as both sides agree.  fp32 2 x 2688 x 116480:
 // 240 us with the second launch, 5.2 TB/s; 48 x 2048 x 32768: 101 (as 64 rows 118); 64 x 4096 x 65536: 450, the fp32 instructions' rate.
 struct Thin {
@@ -1723,6 +1723,9 @@ int launch_tiles(hipStream_t st, const Product& a) {
 // Tiles of 256 x 256, 256 x 128, 128 x 128 or 64 x 64, whichever takes the least time for the rows that a call has, by a fit of measured times.  Large tiles read their operands
 // less often, small ones fill the units of a small call: bf16 logits of 2048 x 1024 x 8192 in tiles of 256 x 256 50 us, 128 x 128 71, 64 x 64 95; of 100 x 1024 x 3000
 // 128 x 128 25.1 us, 64 x 64 20.6; gradients of 130 x 2048 x 1000 47 and 37, of 1000 x 2048 x 2000 75 and 80.
+// The constants come from few of these sizes.  Over 139 others (M 100 to 4000, C 512 to 4096, V 1000 to 50000, both types) a call that goes by them takes as long as one with the
+// best of the four in the median, and in nine of ten at most 1.4 % longer, bf16 gradients 6 % (their three products in one kind of tiles); at worst 15 % forward (100 x 4096 x 50000
+// bf16: 136 us, 128 x 128: 118) and 25 % backward (2000 x 2048 x 1000 bf16: 121 us, 64 x 64: 97).
 struct Tiling {
   int bx, by;
   Split split;
@@ -1779,11 +1782,12 @@ int launch_slabs(hipStream_t st, Product& a, const Choice& c, float* slabs) {
   a.split = c.split, a.slabs = slabs, a.out = nullptr;
   return launch_tiling<false, false, kEpiSum>(st, a, c.tiling);
 }
-// (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count)
+// (slab_bytes: of the workspace for shares' sums; whether shares are worth it, the kernel decides by the rows that count.  columns: of the tiles that it took)
 template <bool XO, bool YO, int EPI>
-int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0) {
+int launch_product(hipStream_t st, Product a, float* slabs = nullptr, int64_t slab_bytes = 0, int* columns = nullptr) {
   const Choice c = choice_of(a.nx, a.ny, a.k, a.parts, EPI == kEpiSum, slab_bytes, a.count_k != 0, EPI == kEpiPartial ? tilings_for_sums(a.nx) : 4);
   a.split = c.split, a.slabs = slabs;
+  if (columns != nullptr) *columns = kTilings[c.tiling].by;
   return launch_tiling<XO, YO, EPI>(st, a, c.tiling);
 }
 
@@ -1970,9 +1974,8 @@ int launch_head_forward(hipStream_t st, const HeadCall& c, void* scratch, size_t
       if (int e = launch_slabs(st, a, how, (float*)(ws + q.slabs))) return e;
       head_slab_partial_kernel<<<dim3((unsigned)p.M, (unsigned)((n + kSlabColumns - 1) / kSlabColumns)), 256, 0, st>>>(a, t.bx, t.by);
       columns = kSlabColumns;
-    } else {
-      columns = kTilings[choice_of(a.nx, a.ny, a.k, a.parts, false, 0, false, tilings_for_sums(a.nx)).tiling].by;
-      if (int e = launch_product<false, false, kEpiPartial>(st, a)) return e;
+    } else if (int e = launch_product<false, false, kEpiPartial>(st, a, nullptr, 0, &columns)) {
+      return e;
     }
     Loss l = loss_of(c, q, ws);
     l.tiles = (int)((n + columns - 1) / columns);

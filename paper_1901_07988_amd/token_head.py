@@ -2,7 +2,7 @@
 """A vocabulary behind the network of gated blocks (token_blocks.py): its last norm's rows against a table of tokens, trained on labels and on a
 teacher's largest logits.
 
-    loss = label_weight CE + teacher_weight KD, the mean over the rows that count        abl_xent_forward, abl_distill_forward
+    loss = label_weight CE + teacher_weight KD, the mean over the rows (all count here)  abl_xent_forward, abl_distill_forward
     dn, dTable                                                                            abl_xent_backward, abl_distill_backward
 
 The logits are never kept: what waits for the backward pass beside the blocks' stores is a row's log-sums and, with a teacher, its logits
