@@ -362,6 +362,41 @@ def test_rows_of_one_weight(M, C, V, smoothing, teacher):
     R.assert_within(dW, want["dW"], 1.01 * (off.t() @ x.abs() + (M + 70) * R.F32 * (d.t() @ x.abs())) + 1e-37, "dW")
 
 
+@pytest.mark.parametrize("dw", [BF16, F32])
+@pytest.mark.parametrize("labels", [True, False])
+def test_weights_of_any_size(dw, labels):
+    """Nothing but zeros, very small and very large ones, one that is infinite beside others, and rows that do not count whose weight is NaN."""
+    c = Case(90, 40, 200, BF16, T=0 if labels else 4, labels=labels, **({} if labels else dict(temperature=2.0)))
+    c.forward()
+    off = c.labels < 0 if labels else ~((c.ids >= 0) & (c.t > -INF)).any(1)
+    on = (~off).nonzero()[:, 0]
+    assert int(off.sum()) > 2 and len(on) > 20
+
+    def gradients(w):
+        dh, dW = torch.empty(90, 40, dtype=BF16, device="cuda"), torch.empty(200, 40, dtype=dw, device="cuda")
+        ws, o = scratch_for(90, 40, 200, BF16, c.T, dw, True), c.out
+        w = torch.where(off, math.nan, w)
+        if labels:
+            B.abl_xent_backward(c.dh_in, c.dW_in, c.gl, o["lse"], w.cuda(), ws, dh, dW, **c.options())
+        else:
+            B.abl_distill_backward(c.dh_in, c.dW_in, None, c.gi, c.gt, o["lse"], o["lse_t"], o["z_top"], w.cuda(), ws, dh, dW, **c.options())
+        c.dloss = torch.where(off, 0.0, w)
+        return dh, dW, c.reference(dw)
+
+    dh, dW, _ = gradients(torch.zeros(90))
+    assert bool((dh == 0).all()) and bool((dW == 0).all())
+    for size in (1e-25, 1e-12, 1.0, 1e12, 1e32):
+        dh, dW, want = gradients(torch.rand(90, generator=torch.Generator().manual_seed(1)) * size)
+        R.assert_within(dh, want["dh"], want["bound"]["dh"], "dh")
+        R.assert_within(dW, want["dW"], want["bound"]["dW"], "dW")
+    w = torch.rand(90, generator=torch.Generator().manual_seed(1))
+    w[on[3]] = INF
+    dh, dW, want = gradients(w)
+    fine = torch.arange(90) != on[3]
+    R.assert_within(dh[fine.cuda()], want["dh"][fine], want["bound"]["dh"][fine], "dh")
+    assert not bool(dh[on[3]].isfinite().any()) and not bool(dW.isfinite().any())
+
+
 @pytest.mark.parametrize("M", [3, 70])
 def test_a_table_beyond_four_gigabytes(M):
     """bf16, 561003 x 4096: the reference on the GPU in 64 bits, a piece of the table at a time, with the bounds of head_reference.py."""
