@@ -74,7 +74,7 @@ struct UnitOf {
   float scale, first, second;
 };
 
-// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, their number, and the unit: one block (8192 rows: 6 us; places
+// The list of the rows that count, in their order, filled up with -1 to a multiple of kRowTile, their number, and the unit: one block (8192 rows: 7 us, 9 with the unit; places
 // by atomics would change from call to call, and with them the order of the sums).
 __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_t* __restrict__ labels, const unsigned char* __restrict__ flags,
                                                          int* __restrict__ rows, int* __restrict__ count, UnitOf of, float* __restrict__ unit) {
@@ -86,6 +86,10 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_
   for (int64_t m0 = 0; m0 < M; m0 += 4096) {
     const int64_t m = m0 + threadIdx.x * 4;
     int on = 0;
+    float w[4] = {};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (of.dloss != nullptr && m + e < M) w[e] = of.dloss[m + e];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (m + e < M && (flags != nullptr ? (flags[m + e] & (kLabel | kTeacher)) != 0 : labels[m + e] >= 0)) on |= 1 << e;
@@ -113,7 +117,7 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(int64_t M, const int64_
     for (int e = 0; e < 4; ++e)
       if (on >> e & 1) {
         rows[at++] = (int)(m + e);
-        if (of.dloss != nullptr && finite(of.dloss[m + e])) large = fmaxf(large, fabsf(of.dloss[m + e]));
+        large = finite(w[e]) ? fmaxf(large, fabsf(w[e])) : large;
       }
     base += sums[16];
     __syncthreads();
